@@ -62,7 +62,10 @@ typedef enum {
   CLEAVE_ELIMIT = -4  /* the request exceeds a fixed limit of the entry point */
 } cleave_status;
 
-typedef enum { CLEAVE_F32 = 0, CLEAVE_BF16 = 1 } cleave_dtype;
+/* CLEAVE_E4M3: 8-bit floating point, 4 exponent bits, 3 of mantissa, no
+ * infinities; operands and rows with scales of the operators around the GEMMs
+ * only, where their comments name it. */
+typedef enum { CLEAVE_F32 = 0, CLEAVE_BF16 = 1, CLEAVE_E4M3 = 2 } cleave_dtype;
 
 /* One sub-GEMM task: 64-byte POD, same bytes on host and device.
  * Ranges are half-open and refer to the logical op(A) . op(B). */
@@ -395,6 +398,74 @@ int cleave_verify_grouped(cleave_plan* plan, int64_t n_members,
                           const float* partials, const float* r, const float* s, double tol,
                           double* lhs, double* rhs, double* scale, int32_t* accept,
                           void* hip_stream);
+
+/* ---- operators around the GEMMs -------------------------------------------
+ * What a layer's step does between its GEMMs, which the paper keeps on the
+ * parameter server (Sec. 4.1): the norm of the residual stream, bias gradients,
+ * and the optimizer over all tensors of a layer at once.  Matrices are row-major, `rows` x
+ * `cols`, with leading dimensions in elements; any size, stride and alignment of the
+ * elements (rows that start on 16-byte boundaries, of whole 16 bytes of the input
+ * type, take a faster path).  All are asynchronous on hip_stream, allocate
+ * nothing, keep nothing between calls and may be captured into a HIP graph.  Sums are
+ * carried in fp32 in an order that depends on the sizes alone: the same call gives
+ * the same bits.  rows = 0 is allowed: nothing is read, sums over rows are zero.
+ *
+ * cleave_rms_norm:  h = x + residual;  i = 1 / sqrt(mean(h^2) + eps);  y = h i w
+ * per row, from the unrounded h.  x, residual (or NULL), sum_out (h, or NULL): dtype
+ * F32 or BF16; weight: cols floats; inv_rms: rows floats (i), or NULL.
+ * y_dtype = dtype: scales must be NULL.  y_dtype = CLEAVE_E4M3: row t of y holds
+ * h i w / s rounded to nearest even, with scales[t] = s = max|h i w| / 448 (a row whose
+ * largest magnitude is below 2^-100 is stored as zeros with s = 0; one that holds a NaN or
+ * an infinity as NaN with s NaN).  sum_out may be x or residual, y too.
+ * CLEAVE_EINVAL: negative rows, no column, a size above 2^31-1, NULL or misaligned
+ * pointer, short leading dimension, negative, infinite or NaN eps, another dtype. */
+int cleave_rms_norm(int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* residual,
+                    int64_t ldr, int dtype, const float* weight, float eps,
+                    void* y, int64_t ldy, int y_dtype, float* scales,
+                    void* sum_out, int64_t lds, float* inv_rms, void* hip_stream);
+
+/* Its gradient, from dy, the stored h (cleave_rms_norm's sum_out, or x without a
+ * residual) and inv_rms:  xhat = h i;  g = dy w;
+ *   dx = i (g - xhat mean(g xhat)) + dsum;   dweight = sum over rows of dy xhat
+ * dx is the gradient of x and of residual alike.  dsum (or NULL): the gradient that reaches h
+ * itself, through the residual stream.  dy, h, dsum, dx: dtype F32 or BF16, dx may be
+ * dy or dsum; dweight: cols floats.  workspace: cleave_rms_norm_workspace(rows, cols)
+ * floats, of this call alone while it runs.  CLEAVE_EINVAL as above. */
+int64_t cleave_rms_norm_workspace(int64_t rows, int64_t cols);
+int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* dy, int64_t lddy,
+                             const void* h, int64_t ldh, const void* dsum, int64_t ldds, int dtype,
+                             const float* weight, const float* inv_rms, void* dx, int64_t lddx,
+                             float* dweight, float* workspace, void* hip_stream);
+
+/* dbias = sum over rows of dy (the gradient of a bias that every row got).
+ * workspace: cleave_bias_grad_workspace(rows, cols) floats, of this call alone while
+ * it runs. */
+int64_t cleave_bias_grad_workspace(int64_t rows, int64_t cols);
+int cleave_bias_grad(int64_t rows, int64_t cols, const void* dy, int64_t lddy, int dtype,
+                     float* dbias, float* workspace, void* hip_stream);
+
+/* AdamW on n_tensors tensors of sizes[k] contiguous elements in one launch per 56
+ * tensors: with c = *grad_scale (device; NULL: 1), per element
+ *   g = c g;  m = beta1 m + (1-beta1) g;  v = beta2 v + (1-beta2) g^2;
+ *   w = w - lr ( (m / (1-beta1^step)) / (sqrt(v / (1-beta2^step)) + eps) + weight_decay w )
+ * in fp32, every operation rounded by itself.  All arrays are host arrays of n_tensors
+ * device pointers, read during the call only: w (fp32) is updated in place, g (g_dtype F32
+ * or BF16) is read, w_bf16 gets the new weight in bf16 (NULL: none).
+ * States, updated in place: with m_scale and v_scale NULL, m and v are fp32.
+ * Otherwise m[k] and v[k] are e4m3 values of m and of sqrt(v), and m_scale[k], v_scale[k] hold
+ * one fp32 scale for every 256 consecutive elements of the tensor (the last one for what
+ * is left): state = value * scale, scale = largest finite magnitude of the 256 / 448, rounded to
+ * nearest even; what is above zero in sqrt(v) becomes at least 2^-9 of the scale; values that are
+ * not finite become NaN; a block below 2^-100 is zeros with scale 0.  All zeros with scales 0
+ * are the states of step 1.
+ * Empty tensors are allowed (their pointers are not looked at).  CLEAVE_EINVAL: NULL or
+ * misaligned pointer, a negative size or one of 2^40 and more, one of the two scale lists alone, step < 1,
+ * beta outside [0, 1), negative eps, NaN, another dtype. */
+int cleave_adamw(int64_t n_tensors, const int64_t* sizes, float* const* w, const void* const* g,
+                 int g_dtype, void* const* m, void* const* v, float* const* m_scale,
+                 float* const* v_scale, void* const* w_bf16, const float* grad_scale, double lr,
+                 double beta1, double beta2, double eps, double weight_decay, int64_t step,
+                 void* hip_stream);
 
 /* ---- cost model and shard assignment (host only) -------------------------
  * Paper Sec. 4.1: a device d receives alpha rows of A (m x n) and beta columns

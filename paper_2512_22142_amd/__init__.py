@@ -5,6 +5,12 @@
     reduce(plan, partials, C)     -> C = fixed-order sum of each tile's partials
     verify(plan, A, B, partials, r, s, tol, accept) -> per-task random-projection check
 
+and what a layer's step does between its GEMMs:
+
+    rms_norm, rms_norm_backward   norm of the residual stream, its gradient
+    bias_grad                     sum of a gradient's rows
+    adamw                         optimizer step over many tensors, states in 32 or 8 bits
+
 All compute happens in libcleave.so (hand-written HIP for gfx950, C ABI in
 include/cleave.h); build it with `python -m paper_2512_22142_amd.build`.
 """
@@ -51,13 +57,26 @@ _BINDING_NAMES = (
     "version",
 )
 
+# The operators around the GEMMs, loaded likewise.
+_OPERATOR_NAMES = (
+    "adamw",
+    "bias_grad",
+    "bias_grad_workspace",
+    "rms_norm",
+    "rms_norm_backward",
+    "rms_norm_workspace",
+)
+
 
 def __getattr__(name):
     if name in _BINDING_NAMES:
         from . import binding
         return getattr(binding, name)
+    if name in _OPERATOR_NAMES:
+        from . import operators
+        return getattr(operators, name)
     raise AttributeError("module %r has no attribute %r" % (__name__, name))
 
 
 def __dir__():
-    return sorted(list(globals()) + list(_BINDING_NAMES))
+    return sorted(list(globals()) + list(_BINDING_NAMES) + list(_OPERATOR_NAMES))

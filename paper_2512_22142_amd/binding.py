@@ -40,6 +40,8 @@ EXPORTS = (
     "cleave_reduce_batched", "cleave_reduce_residual", "cleave_reduce_adam",
     "cleave_shard_cost", "cleave_shard_fits", "cleave_assign", "cleave_reassign", "cleave_execute_assemble",
     "cleave_execute_grouped", "cleave_reduce_grouped", "cleave_execute_noalloc", "cleave_reassign_sets", "cleave_reduce_adam_grouped", "cleave_verify_batched", "cleave_verify_grouped", "cleave_verify_reduce", "cleave_plan_schedule_loads",
+    "cleave_rms_norm", "cleave_rms_norm_workspace", "cleave_rms_norm_backward", "cleave_bias_grad", "cleave_bias_grad_workspace",
+    "cleave_adamw",
 )
 
 
@@ -146,6 +148,9 @@ def _load():
     lib.cleave_verify_grouped.argtypes = [p, i64, p, i64, ctypes.c_int, p, i64, ctypes.c_int, ctypes.c_int,
                                           p, p, p, ctypes.c_double, p, p, p, p, p]
     lib.cleave_verify_grouped.restype = ctypes.c_int
+    for name in ("cleave_rms_norm_workspace", "cleave_bias_grad_workspace"):
+        getattr(lib, name).argtypes = [i64, i64]
+        getattr(lib, name).restype = i64
     lib.cleave_reduce.restype = ctypes.c_int
     lib.cleave_strerror.argtypes = [ctypes.c_int]
     lib.cleave_strerror.restype = ctypes.c_char_p

@@ -12,7 +12,9 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcleave.so")
 NATIVE = os.path.join(HERE, "_native.so")
 
-SOURCES = ["plan.cpp", "scheduler.cpp", "api.cpp", "execute.hip", "execute_direct.hip", "reduce.hip", "verify.hip", "subset.hip"]
+SOURCES = ["plan.cpp", "scheduler.cpp", "api.cpp", "operators.cpp", "execute.hip", "execute_direct.hip", "reduce.hip", "verify.hip",
+           "subset.hip", "norm.hip", "adamw.hip"]
+NATIVE_SOURCES = ["native.cpp", "native_operators.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 COMMON = [
@@ -58,7 +60,7 @@ def _compile_native():
     rocm = os.path.dirname(os.path.dirname(HIPCC))
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-D__HIP_PLATFORM_AMD__",
            "-DUSE_ROCM", '-DCLEAVE_NATIVE_TAG="%s"' % native_tag(), "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
-           os.path.join(CSRC, "native.cpp"), "-o", NATIVE]
+           *(os.path.join(CSRC, s) for s in NATIVE_SOURCES), "-o", NATIVE]
     for d in inc + [os.path.join(rocm, "include")]:
         cmd += ["-isystem", d]
     for d in cpp_extension.library_paths():
@@ -66,7 +68,7 @@ def _compile_native():
     cmd += ["-L" + HERE, "-l:libcleave.so", "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError("g++ failed on native.cpp:\n%s" % (res.stdout + res.stderr))
+        raise RuntimeError("g++ failed on the checks:\n%s" % (res.stdout + res.stderr))
 
 
 def build(verbose=True, extra=None):

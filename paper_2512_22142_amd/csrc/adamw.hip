@@ -1,0 +1,240 @@
+// AdamW over many tensors in one launch (paper Sec. 4.1 and Sec. 6: optimizer
+// updates stay on the parameter server and stream over its weights):
+//   g = c g;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
+//   w = w - lr ( (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps) + wd w )
+// in fp32, every operation rounded by itself (no fused multiply-adds), so that a
+// program of elementary operations gets the same bits.
+//
+// 8-bit states: m and r = sqrt(v) as e4m3 with one fp32 scale per 256 consecutive elements, the
+// largest magnitude over 448.  e4m3 spans 2^-9 to 448, so r covers a range of 2^35 in v within
+// a block to 6 % steps, where v itself would leave it; an r above zero is never rounded to
+// zero, which would leave m over eps alone as the step.  A value that is not finite becomes
+// NaN and leaves its block's scale to the others.  The update of w uses m and v before they are
+// rounded.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "bf16_round.h"
+#include "fp8_round.h"
+#include "operators.h"
+
+namespace cleave {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// A lane's four elements of a block of 256: neighbours (VEC), or 64 apart.
+template <bool VEC>
+__device__ __forceinline__ uint32_t place(int lane, int e) {
+  return VEC ? 4 * lane + e : lane + 64 * e;
+}
+
+template <bool VEC>
+__device__ __forceinline__ f32x4 load_f32(const float* p, int lane, uint32_t n) {
+  if constexpr (VEC) {
+    if (4 * lane + 4u <= n) return *reinterpret_cast<const f32x4*>(p + 4 * lane);
+  }
+  f32x4 x{};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (place<VEC>(lane, e) < n) x[e] = p[place<VEC>(lane, e)];
+  return x;
+}
+template <bool VEC>
+__device__ __forceinline__ f32x4 load_bf16(const uint16_t* p, int lane, uint32_t n) {
+  if constexpr (VEC) {
+    if (4 * lane + 4u <= n) {
+      const u32x2 b = *reinterpret_cast<const u32x2*>(p + 4 * lane);
+      return f32x4{__builtin_bit_cast(float, b[0] << 16), __builtin_bit_cast(float, b[0] & 0xffff0000u),
+                   __builtin_bit_cast(float, b[1] << 16), __builtin_bit_cast(float, b[1] & 0xffff0000u)};
+    }
+  }
+  f32x4 x{};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (place<VEC>(lane, e) < n) x[e] = __builtin_bit_cast(float, static_cast<uint32_t>(p[place<VEC>(lane, e)]) << 16);
+  return x;
+}
+template <bool VEC>
+__device__ __forceinline__ uint32_t load_bytes(const uint8_t* p, int lane, uint32_t n) {
+  if constexpr (VEC) {
+    if (4 * lane + 4u <= n) return *reinterpret_cast<const uint32_t*>(p + 4 * lane);
+  }
+  uint32_t x = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (place<VEC>(lane, e) < n) x |= static_cast<uint32_t>(p[place<VEC>(lane, e)]) << (8 * e);
+  return x;
+}
+template <bool VEC>
+__device__ __forceinline__ void store_f32(float* p, f32x4 x, int lane, uint32_t n) {
+  if constexpr (VEC) {
+    if (4 * lane + 4u <= n) {
+      *reinterpret_cast<f32x4*>(p + 4 * lane) = x;
+      return;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (place<VEC>(lane, e) < n) p[place<VEC>(lane, e)] = x[e];
+}
+template <bool VEC>
+__device__ __forceinline__ void store_bf16(uint16_t* p, f32x4 x, int lane, uint32_t n) {
+  if constexpr (VEC) {
+    if (4 * lane + 4u <= n) {
+      *reinterpret_cast<u32x2*>(p + 4 * lane) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+      return;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (place<VEC>(lane, e) < n) p[place<VEC>(lane, e)] = to_bf16_bits(x[e]);
+}
+template <bool VEC>
+__device__ __forceinline__ void store_bytes(uint8_t* p, uint32_t x, int lane, uint32_t n) {
+  if constexpr (VEC) {
+    if (4 * lane + 4u <= n) {
+      *reinterpret_cast<uint32_t*>(p + 4 * lane) = x;
+      return;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (place<VEC>(lane, e) < n) p[place<VEC>(lane, e)] = static_cast<uint8_t>(x >> (8 * e));
+}
+
+__device__ __forceinline__ f32x4 decode(uint32_t q, float scale) {
+#pragma clang fp contract(off)
+  return f32x4{from_e4m3<0>(q) * scale, from_e4m3<1>(q) * scale, from_e4m3<2>(q) * scale, from_e4m3<3>(q) * scale};
+}
+
+// The largest finite magnitude of a block.
+__device__ __forceinline__ float largest(f32x4 x) {
+  float most = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float a = __builtin_fabsf(x[e]);
+    most = a > most && a < __builtin_inff() ? a : most;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d));
+  return most;
+}
+
+template <bool UP>
+__device__ __forceinline__ uint32_t encode(f32x4 x, float inverse) {
+#pragma clang fp contract(off)
+  float q[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    q[e] = x[e] * inverse;
+    if (UP && x[e] > 0.0f && inverse > 0.0f) q[e] = __builtin_fmaxf(q[e], kE4M3Least);
+    // infinities and NaN: NaN, whatever the instruction makes of what lies beyond 448
+    if (!(__builtin_fabsf(x[e]) < __builtin_inff())) q[e] = __builtin_nanf("");
+  }
+  return pack_e4m3(q[0], q[1], q[2], q[3]);
+}
+
+struct Block {
+  f32x4 w, g, m, v;
+};
+
+template <bool VEC, bool GRAD_BF16, bool STATES_8>
+struct Update {
+  const AdamTensor& t;
+  const AdamWArgs& args;
+  float clip;
+
+  __device__ __forceinline__ uint64_t elements() const { return (static_cast<uint64_t>(t.n_high) << 32) | t.n_low; }
+
+  __device__ __forceinline__ Block load(uint64_t at, int lane, uint32_t n) const {
+    Block b;
+    b.w = load_f32<VEC>(t.w + at, lane, n);
+    if constexpr (GRAD_BF16) b.g = load_bf16<VEC>(static_cast<const uint16_t*>(t.g) + at, lane, n);
+    else b.g = load_f32<VEC>(static_cast<const float*>(t.g) + at, lane, n);
+    if constexpr (STATES_8) {
+      const uint32_t qm = load_bytes<VEC>(static_cast<const uint8_t*>(t.m) + at, lane, n);
+      const uint32_t qv = load_bytes<VEC>(static_cast<const uint8_t*>(t.v) + at, lane, n);
+      b.m = decode(qm, t.m_scale[at / kStateBlock]);
+      b.v = decode(qv, t.v_scale[at / kStateBlock]);
+    } else {
+      b.m = load_f32<VEC>(static_cast<const float*>(t.m) + at, lane, n);
+      b.v = load_f32<VEC>(static_cast<const float*>(t.v) + at, lane, n);
+    }
+    return b;
+  }
+
+  __device__ __forceinline__ void step(Block b, uint64_t at, int lane, uint32_t n) const {
+#pragma clang fp contract(off)
+    f32x4 w1, m1, v1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float g = b.g[e] * clip;
+      const float v0 = STATES_8 ? b.v[e] * b.v[e] : b.v[e];
+      m1[e] = args.beta1 * b.m[e] + args.one_minus_beta1 * g;
+      v1[e] = args.beta2 * v0 + args.one_minus_beta2 * (g * g);
+      const float root = __builtin_sqrtf(v1[e] * args.inv_bias2) + args.eps;
+      w1[e] = b.w[e] - args.lr * ((m1[e] * args.inv_bias1) / root + args.weight_decay * b.w[e]);
+    }
+    store_f32<VEC>(t.w + at, w1, lane, n);
+    if (t.copy) store_bf16<VEC>(t.copy + at, w1, lane, n);
+    if constexpr (STATES_8) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v1[e] = __builtin_sqrtf(v1[e]);
+      const BlockScale sm = block_scale(largest(m1)), sv = block_scale(largest(v1));
+      store_bytes<VEC>(static_cast<uint8_t*>(t.m) + at, encode<false>(m1, sm.inverse), lane, n);
+      store_bytes<VEC>(static_cast<uint8_t*>(t.v) + at, encode<true>(v1, sv.inverse), lane, n);
+      if (lane == 0) {
+        t.m_scale[at / kStateBlock] = sm.scale;
+        t.v_scale[at / kStateBlock] = sv.scale;
+      }
+    } else {
+      store_f32<VEC>(static_cast<float*>(t.m) + at, m1, lane, n);
+      store_f32<VEC>(static_cast<float*>(t.v) + at, v1, lane, n);
+    }
+  }
+
+  // Wave `wave` of the workgroup takes every kWaves-th block of 256 of the chunk.
+  __device__ __forceinline__ void chunk(uint64_t first, int wave, int lane) const {
+    const uint64_t n = elements();
+    const uint64_t end = first + kAdamChunk < n ? first + kAdamChunk : n;
+    for (uint64_t at = first + wave * kStateBlock; at < end; at += kWaves * kStateBlock) {
+      const uint32_t left = end - at < kStateBlock ? static_cast<uint32_t>(end - at) : kStateBlock;
+      step(load(at, lane, left), at, lane, left);
+    }
+  }
+};
+
+template <bool GRAD_BF16, bool STATES_8>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(AdamWArgs args) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // The tensor that chunk blockIdx.x belongs to: as many as end before it.  (A lane looks at one.)
+  const bool before = lane < args.n_tensors && args.chunk_end[lane] <= blockIdx.x;
+  const int k = __popcll(__ballot(before));
+  const AdamTensor& t = args.tensors[k];
+  const uint32_t chunk0 = k > 0 ? args.chunk_end[k - 1] : 0;
+  const uint64_t first = static_cast<uint64_t>(blockIdx.x - chunk0) * kAdamChunk;
+  const float clip = args.grad_scale ? *args.grad_scale : 1.0f;
+  if (t.vec) Update<true, GRAD_BF16, STATES_8>{t, args, clip}.chunk(first, wave, lane);
+  else Update<false, GRAD_BF16, STATES_8>{t, args, clip}.chunk(first, wave, lane);
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const AdamWArgs& args, uint32_t chunks, int grad_dtype, bool states_8bit, hipStream_t stream) {
+  const dim3 g(chunks), b(kThreads);
+  const bool bf16 = grad_dtype == CLEAVE_BF16;
+  if (bf16 && states_8bit) hipLaunchKernelGGL((adamw_kernel<true, true>), g, b, 0, stream, args);
+  else if (bf16) hipLaunchKernelGGL((adamw_kernel<true, false>), g, b, 0, stream, args);
+  else if (states_8bit) hipLaunchKernelGGL((adamw_kernel<false, true>), g, b, 0, stream, args);
+  else hipLaunchKernelGGL((adamw_kernel<false, false>), g, b, 0, stream, args);
+  return hipGetLastError();
+}
+
+}  // namespace cleave

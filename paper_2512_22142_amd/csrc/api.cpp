@@ -352,6 +352,8 @@ const char* direct_kernel_name(cleave::DirectShape shape, int transA, int transB
 
 }  // namespace
 
+int cleave::record_hip_error(hipError_t e) { return hip_fail(e); }
+
 extern "C" int cleave_last_hip_error(void) { return g_last_hip_error; }
 
 extern "C" int cleave_version(void) { return 107; }

@@ -9,6 +9,9 @@
 
 namespace cleave {
 
+// Keeps `e` for cleave_last_hip_error; returns CLEAVE_EHIP.
+int record_hip_error(hipError_t e);
+
 // Most members a grouped launch (one table entry per member) can have.
 constexpr int kMaxGroup = 8;
 

@@ -1,0 +1,252 @@
+"""Norm, its gradient and the bias gradient against fp64, and their refusals."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_22142_amd as cleave
+from oracle import operators as oo
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+U32, U16 = 2.0 ** -24, 2.0 ** -8   # unit roundoffs: 24 and 8 bits of significand
+
+SIZES = [(1, 1), (3, 64), (2, 511), (5, 512), (6, 513), (4, 1001), (2, 2048), (3, 2056), (7, 4096), (2, 5120), (2, 8192),
+         (2, 8200), (1, 12345), (3, 16384), (2, 16392), (1, 20001), (2, 32768), (1, 40000)]
+
+
+def matrix(rows, cols, dtype, seed, pad=0, shift=0, std=1.0):
+    """A rows x cols view on the GPU with a leading dimension of cols + pad, `shift` elements into its buffer."""
+    g = torch.Generator().manual_seed(seed)
+    flat = torch.zeros(rows * (cols + pad) + shift, dtype=dtype, device="cuda")
+    view = flat[shift:].view(rows, cols + pad)[:, :cols]
+    if std is not None:
+        view.copy_((torch.randn(rows, cols, generator=g) * std).to(dtype))
+    return view
+
+
+def f64(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def close(got, want, dtype, slack, what):
+    """Within the output type's rounding and `slack` (an absolute error, per element) of the fp32 arithmetic."""
+    bound = np.abs(want) * (U16 if dtype == BF16 else U32) * 1.01 + slack
+    bad = np.abs(got - want) - bound
+    assert np.all(bad <= 0), (what, float(bad.max()))
+
+
+def run_norm(rows, cols, dtype, out, residual, pad=0, shift=0, eps=1e-5):
+    x = matrix(rows, cols, dtype, 1, pad, shift, 2.0)
+    r = matrix(rows, cols, dtype, 2, pad, shift) if residual else None
+    w = matrix(1, cols, F32, 3)[0].add_(1.0)
+    y = matrix(rows, cols, out, 0, pad, shift, None)
+    s = matrix(rows, cols, dtype, 0, pad, shift, None) if residual else None
+    inv = torch.empty(rows, dtype=F32, device="cuda")
+    scales = torch.empty(rows, dtype=F32, device="cuda") if out == E4M3 else None
+    cleave.rms_norm(x, w, y, residual=r, sum_out=s, inv_rms=inv, scales=scales, eps=eps)
+    want, h, want_inv = oo.rms_norm(f64(x), f64(w), eps, f64(r))
+    # a sum of n squares in any tree: n rounding errors at most, in practice the depth; half of it under the root
+    n_err = (cols / 64 + 16) * U32
+    assert np.allclose(f64(inv), want_inv, rtol=n_err, atol=0)
+    if residual:
+        close(f64(s), h, dtype, 2 * U32 * np.abs(h), "sum")
+    slack = np.abs(want) * (n_err + 4 * U32)
+    if out == E4M3:
+        ws = oo.row_scales(want)
+        assert np.allclose(f64(scales), ws, rtol=n_err + 8 * U32, atol=0)
+        q = f64(y.float())
+        # half a step: 2^-4 of the value, 2^-10 below the normal numbers
+        near = np.abs(want / ws[:, None])
+        assert np.all(np.abs(q - want / ws[:, None]) <= np.maximum(near * 2.0 ** -4, 2.0 ** -10) * 1.001 + near * (n_err + 8 * U32))
+        assert np.abs(q).max(axis=1).min() == 448.0
+    else:
+        close(f64(y), want, dtype, slack, "y")
+
+
+@pytest.mark.parametrize("rows,cols", SIZES)
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (BF16, E4M3), (F32, F32), (F32, E4M3)])
+def test_norm(rows, cols, dtype, out):
+    run_norm(rows, cols, dtype, out, residual=rows % 2 == 1)
+
+
+@pytest.mark.parametrize("pad,shift", [(8, 0), (3, 0), (8, 1), (0, 4), (5, 7)])
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (BF16, E4M3), (F32, F32)])
+def test_norm_strides_and_alignment(pad, shift, dtype, out):
+    run_norm(9, 768, dtype, out, True, pad, shift)
+
+
+def test_norm_sum_in_place():
+    x, r = matrix(5, 1000, BF16, 1), matrix(5, 1000, BF16, 2)
+    w = torch.ones(1000, device="cuda")
+    y, y2, s = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    cleave.rms_norm(x, w, y, residual=r, sum_out=s)
+    cleave.rms_norm(x, w, y2, residual=r, sum_out=r)
+    assert torch.equal(y, y2) and torch.equal(r, s)
+    cleave.rms_norm(x, w, x, residual=s)          # y over x
+
+
+@pytest.mark.parametrize("cols", [64, 100, 4096, 40000])
+def test_norm_rows_of_zeros_and_what_is_not_finite(cols):
+    x = matrix(6, cols, F32, 1)
+    x[1] = 0
+    x[2, cols // 2] = float("nan")
+    x[3, 0] = float("inf")
+    x[4] = 1e-37
+    w = torch.ones(cols, device="cuda")
+    y, q = torch.empty_like(x), torch.empty(x.shape, dtype=E4M3, device="cuda")
+    scales = torch.empty(6, device="cuda")
+    cleave.rms_norm(x, w, y)
+    cleave.rms_norm(x, w, q, scales=scales)
+    q = q.float()
+    assert torch.all(y[1] == 0) and torch.all(q[1] == 0) and scales[1] == 0
+    assert torch.all(y[2].isnan()) and torch.all(q[2].isnan()) and scales[2].isnan()
+    assert y[3, 0].isnan() and torch.all(y[3, 1:] == 0) and scales[3].isnan()
+    assert torch.all(q[4] == 0) and scales[4] == 0      # 1e-37 / sqrt(1e-5): below 2^-100
+    for k in (0, 5):
+        assert torch.all(y[k].isfinite()) and torch.all(q[k].isfinite()) and scales[k] > 0
+
+
+def test_norm_no_rows():
+    w = torch.ones(64, device="cuda")
+    x = torch.empty(0, 64, device="cuda")
+    cleave.rms_norm(x, w, torch.empty_like(x))
+    dw, db = torch.full((64,), 7.0, device="cuda"), torch.full((64,), 7.0, device="cuda")
+    ws = torch.empty(cleave.rms_norm_workspace(0, 64), device="cuda")
+    cleave.rms_norm_backward(x, x, w, torch.empty(0, device="cuda"), torch.empty_like(x), dw, ws)
+    cleave.bias_grad(x, db, torch.empty(cleave.bias_grad_workspace(0, 64), device="cuda"))
+    assert torch.all(dw == 0) and torch.all(db == 0)
+
+
+def run_backward(rows, cols, dtype, dsum, pad=0, shift=0):
+    h = matrix(rows, cols, dtype, 1, pad, shift, 2.0)
+    dy = matrix(rows, cols, dtype, 2, pad, shift)
+    ds = matrix(rows, cols, dtype, 3, pad, shift) if dsum else None
+    w = matrix(1, cols, F32, 4)[0].add_(1.0)
+    inv = torch.rsqrt(h.float().square().mean(dim=1) + 1e-5)
+    dx = matrix(rows, cols, dtype, 0, pad, shift, None)
+    dw = torch.empty(cols, device="cuda")
+    ws = torch.full((cleave.rms_norm_workspace(rows, cols),), float("nan"), device="cuda")
+    cleave.rms_norm_backward(dy, h, w, inv, dx, dw, ws, dsum=ds)
+    want, want_dw = oo.rms_norm_backward(f64(dy), f64(h), f64(w), f64(inv), f64(ds))
+    xhat = f64(h) * f64(inv)[:, None]
+    g = np.abs(f64(dy) * f64(w))
+    n_err = (cols / 64 + 16) * U32
+    slack = f64(inv)[:, None] * (g * 8 * U32 + np.abs(xhat) * (g * np.abs(xhat)).mean(axis=1, keepdims=True) * n_err)
+    close(f64(dx), want, dtype, slack + 4 * U32 * np.abs(want) + (2 * U32 * np.abs(f64(ds)) if dsum else 0), "dx")
+    # a sum over the rows: up to rows / 8 + 64 additions one behind the other
+    assert np.all(np.abs(f64(dw) - want_dw) <= np.abs(f64(dy) * xhat).sum(axis=0) * (rows / 8 + 64) * U32)
+    return dx, dw
+
+
+@pytest.mark.parametrize("rows,cols", SIZES + [(600, 256), (1025, 100), (700, 4096)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_backward(rows, cols, dtype):
+    run_backward(rows, cols, dtype, dsum=cols % 2 == 0)
+
+
+@pytest.mark.parametrize("pad,shift", [(8, 0), (3, 0), (8, 1), (5, 7)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_backward_strides_and_alignment(pad, shift, dtype):
+    run_backward(9, 768, dtype, True, pad, shift)
+
+
+def test_norm_backward_repeats_its_bits_and_writes_over_dy():
+    a, b = run_backward(777, 1000, BF16, True), run_backward(777, 1000, BF16, True)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    dy, h = matrix(33, 256, F32, 1), matrix(33, 256, F32, 2)
+    inv = torch.rsqrt(h.square().mean(dim=1))
+    w, ws = torch.ones(256, device="cuda"), torch.empty(cleave.rms_norm_workspace(33, 256), device="cuda")
+    dx, dw, dw2 = torch.empty_like(dy), torch.empty(256, device="cuda"), torch.empty(256, device="cuda")
+    cleave.rms_norm_backward(dy, h, w, inv, dx, dw, ws)
+    cleave.rms_norm_backward(dy, h, w, inv, dy, dw2, ws)
+    assert torch.equal(dx, dy) and torch.equal(dw, dw2)
+
+
+def test_norm_gradient_against_differences_of_the_kernel():
+    rows, cols, step = 4, 96, 1.0 / 64
+    x, c, d = (matrix(rows, cols, F32, k) for k in (1, 2, 3))
+    w = torch.ones(cols, device="cuda")
+    y, inv, h = torch.empty_like(x), torch.empty(rows, device="cuda"), x.clone()
+    cleave.rms_norm(x, w, y, inv_rms=inv)
+    dx, dw = torch.empty_like(x), torch.empty(cols, device="cuda")
+    cleave.rms_norm_backward(c, h, w, inv, dx, dw, torch.empty(cleave.rms_norm_workspace(rows, cols), device="cuda"))
+
+    def loss(t):
+        cleave.rms_norm(t, w, y)
+        return float((c.double() * y.double()).sum())
+
+    along = (loss(x + step * d) - loss(x - step * d)) / (2 * step)
+    # third order: step^2 / 6 of third derivatives along d (a few times |c| |d|^3 over the row's norm); rounding 1e-6 / step
+    assert abs(along - float((dx.double() * d.double()).sum())) <= step ** 2 * 4 * float((c.norm() * d.norm())) / cols ** 0.5 + 1e-3
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 300), (31, 64), (33, 512), (64, 513), (1000, 96), (3001, 1001), (4096, 2048),
+                                       (20000, 8)])
+@pytest.mark.parametrize("dtype,pad", [(BF16, 0), (BF16, 5), (F32, 0), (F32, 3)])
+def test_bias_grad(rows, cols, dtype, pad):
+    dy = matrix(rows, cols, dtype, 5, pad)
+    db = torch.empty(cols, device="cuda")
+    ws = torch.full((cleave.bias_grad_workspace(rows, cols),), float("nan"), device="cuda")
+    cleave.bias_grad(dy, db, ws)
+    assert np.all(np.abs(f64(db) - f64(dy).sum(axis=0)) <= np.abs(f64(dy)).sum(axis=0) * (rows / 8 + 64) * U32)
+
+
+def test_on_another_stream_and_in_a_graph():
+    x, r = matrix(64, 4096, BF16, 1), matrix(64, 4096, BF16, 2)
+    w = torch.ones(4096, device="cuda")
+    y, dw = torch.empty_like(x), torch.empty(4096, device="cuda")
+    inv, ws = torch.empty(64, device="cuda"), torch.empty(cleave.rms_norm_workspace(64, 4096), device="cuda")
+    dx = torch.empty_like(x)
+
+    def step():
+        cleave.rms_norm(x, w, y, residual=r, inv_rms=inv)
+        cleave.rms_norm_backward(y, x, w, inv, dx, dw, ws)
+
+    step()
+    want = [t.clone() for t in (y, inv, dx, dw)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(want, (y, inv, dx, dw)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for t in (y, inv, dx, dw):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (y, inv, dx, dw)))
+
+
+def test_refusals():
+    x, w = torch.zeros(4, 64, device="cuda"), torch.ones(64, device="cuda")
+    y = torch.empty_like(x)
+    q, s = torch.empty(4, 64, dtype=E4M3, device="cuda"), torch.empty(4, device="cuda")
+    with pytest.raises(ValueError):
+        cleave.rms_norm(x, w[:-1], y)
+    with pytest.raises(ValueError):
+        cleave.rms_norm(x, w, y[:, :-1])
+    with pytest.raises(ValueError):
+        cleave.rms_norm(x, w, q)                        # no scales
+    with pytest.raises(ValueError):
+        cleave.rms_norm(x, w, y, scales=s)              # scales without 8 bits
+    with pytest.raises(ValueError):
+        cleave.rms_norm(x.t(), w, y)
+    with pytest.raises(ValueError):
+        cleave.rms_norm(x.cpu(), w, y)
+    with pytest.raises(ValueError):
+        cleave.rms_norm(x, w, y, residual=x.bfloat16())
+    with pytest.raises(TypeError):
+        cleave.rms_norm(x.half(), w, y)
+    with pytest.raises(cleave.CleaveError):
+        cleave.rms_norm(x, w, y, eps=-1.0)
+    with pytest.raises(cleave.CleaveError):
+        cleave.rms_norm(torch.zeros(1, 64, device="cuda").expand(4, 64), w, y)     # rows of one place
+    with pytest.raises(ValueError):
+        cleave.rms_norm_backward(x, x, w, s, y, torch.empty(64, device="cuda"), torch.empty(3, device="cuda"))
+    with pytest.raises(ValueError):
+        cleave.bias_grad(x, torch.empty(63, device="cuda"), torch.empty(4096, device="cuda"))
