@@ -67,6 +67,15 @@ typedef enum {
  * only, where their comments name it. */
 typedef enum { CLEAVE_F32 = 0, CLEAVE_BF16 = 1, CLEAVE_E4M3 = 2 } cleave_dtype;
 
+/* Activations of cleave_linear: z; max(z, 0); z/2 (1 + tanh(sqrt(2/pi) (z +
+ * 0.044715 z^3))); z / (1 + e^-z). */
+typedef enum {
+  CLEAVE_ACT_NONE = 0,
+  CLEAVE_ACT_RELU = 1,
+  CLEAVE_ACT_GELU_TANH = 2,
+  CLEAVE_ACT_SILU = 3
+} cleave_act;
+
 /* One sub-GEMM task: 64-byte POD, same bytes on host and device.
  * Ranges are half-open and refer to the logical op(A) . op(B). */
 typedef struct {
@@ -443,6 +452,46 @@ int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* dy, int64_t
 int64_t cleave_bias_grad_workspace(int64_t rows, int64_t cols);
 int cleave_bias_grad(int64_t rows, int64_t cols, const void* dy, int64_t lddy, int dtype,
                      float* dbias, float* workspace, void* hip_stream);
+
+/* Matrix product with an epilogue:
+ *   z = op(A) op(B) + bias;   C = act(z) + residual            (act_grad = 0)
+ *   C = (op(A) op(B)) act'(preact) + residual                  (act_grad = 1)
+ * The first is a layer's forward pass; preact (or NULL) gets z for its gradient.  The second is
+ * the gradient of an activation's input, op(A) being the gradient behind the next layer's
+ * weight.  Sums, bias and activation in fp32, z and C rounded once.  residual (or NULL), preact
+ * and C: out_dtype F32 or BF16, M x N with leading dimensions ldr, ldz, ldc; residual may be C.
+ * bias: N floats or NULL.  A, B, transA, transB as for cleave_execute.
+ * dtype CLEAVE_E4M3: A is M x K and B is N x K (transA = 0, transB = 1) of 8-bit values,
+ * row m of A times scale_a[m], row n of B times scale_b[n] (as cleave_rms_norm leaves
+ * them); A, B on 16-byte boundaries, lda and ldb multiples of 16 below 2^22.  Otherwise the scales are NULL.
+ *
+ * plan: one GEMM (not batched), best cleave_plan_linear's, which chooses tiles and splits
+ * of K for M, N, K and dtype; for CLEAVE_E4M3 it must be that (K a multiple of 16; its tasks
+ * and dims count K in pairs of values, and the other calls refuse it).  partials: cleave_linear_workspace(plan)
+ * floats (may be NULL if that is 0), of this call alone while it runs.
+ * Few rows (M <= 64) read B once, as fast as memory gives it.  Bits: a function of the
+ * arguments' values, sizes and alignment.  Asynchronous; the plan's tables are uploaded by the first call or
+ * cleave_plan_upload, after which nothing is allocated.
+ * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, act_grad with a
+ * bias or (unless act is NONE) without preact, a batched plan, partials missing, a plan of another type. */
+typedef struct {
+  const void* A;
+  const void* B;
+  const float* scale_a;
+  const float* scale_b;
+  const float* bias;
+  const void* residual;
+  void* preact;
+  void* C;
+  float* partials;
+  int64_t lda, ldb, ldr, ldz, ldc;
+  int32_t transA, transB;
+  int32_t dtype, out_dtype;
+  int32_t act, act_grad;
+} cleave_linear_args;
+int cleave_plan_linear(int64_t M, int64_t N, int64_t K, int dtype, cleave_plan** out);
+int64_t cleave_linear_workspace(const cleave_plan* plan);
+int cleave_linear(cleave_plan* plan, const cleave_linear_args* args, void* hip_stream);
 
 /* AdamW on n_tensors tensors of sizes[k] contiguous elements in one launch per 56
  * tensors: with c = *grad_scale (device; NULL: 1), per element

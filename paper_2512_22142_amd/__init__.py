@@ -8,6 +8,7 @@
 and what a layer's step does between its GEMMs:
 
     rms_norm, rms_norm_backward   norm of the residual stream, its gradient
+    linear (plan_linear)          product with bias, activation (or its gradient) and residual; 8-bit operands
     bias_grad                     sum of a gradient's rows
     adamw                         optimizer step over many tensors, states in 32 or 8 bits
 
@@ -62,6 +63,8 @@ _OPERATOR_NAMES = (
     "adamw",
     "bias_grad",
     "bias_grad_workspace",
+    "linear",
+    "plan_linear",
     "rms_norm",
     "rms_norm_backward",
     "rms_norm_workspace",

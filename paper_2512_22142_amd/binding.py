@@ -41,7 +41,7 @@ EXPORTS = (
     "cleave_shard_cost", "cleave_shard_fits", "cleave_assign", "cleave_reassign", "cleave_execute_assemble",
     "cleave_execute_grouped", "cleave_reduce_grouped", "cleave_execute_noalloc", "cleave_reassign_sets", "cleave_reduce_adam_grouped", "cleave_verify_batched", "cleave_verify_grouped", "cleave_verify_reduce", "cleave_plan_schedule_loads",
     "cleave_rms_norm", "cleave_rms_norm_workspace", "cleave_rms_norm_backward", "cleave_bias_grad", "cleave_bias_grad_workspace",
-    "cleave_adamw",
+    "cleave_adamw", "cleave_plan_linear", "cleave_linear_workspace", "cleave_linear",
 )
 
 
@@ -148,6 +148,10 @@ def _load():
     lib.cleave_verify_grouped.argtypes = [p, i64, p, i64, ctypes.c_int, p, i64, ctypes.c_int, ctypes.c_int,
                                           p, p, p, ctypes.c_double, p, p, p, p, p]
     lib.cleave_verify_grouped.restype = ctypes.c_int
+    lib.cleave_plan_linear.argtypes = [i64, i64, i64, ctypes.c_int, ctypes.POINTER(p)]
+    lib.cleave_plan_linear.restype = ctypes.c_int
+    lib.cleave_linear_workspace.argtypes = [p]
+    lib.cleave_linear_workspace.restype = i64
     for name in ("cleave_rms_norm_workspace", "cleave_bias_grad_workspace"):
         getattr(lib, name).argtypes = [i64, i64]
         getattr(lib, name).restype = i64
@@ -183,6 +187,9 @@ class Plan:
         self.num_tasks = int(_lib.cleave_plan_num_tasks(self._h))
         self.num_tiles = int(_lib.cleave_plan_num_tiles(self._h))
         self.partial_elems = int(_lib.cleave_plan_partial_elems(self._h))
+        # for operators.linear: its `partials`, and the inner dimension in elements of the operands
+        self.linear_workspace = max(0, int(_lib.cleave_linear_workspace(self._h)))
+        self.linear_K = self.K
 
     @property
     def tasks(self):

@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "libcleave.so")
 NATIVE = os.path.join(HERE, "_native.so")
 
 SOURCES = ["plan.cpp", "scheduler.cpp", "api.cpp", "operators.cpp", "execute.hip", "execute_direct.hip", "reduce.hip", "verify.hip",
-           "subset.hip", "norm.hip", "adamw.hip"]
+           "subset.hip", "linear.hip", "linear_direct.hip", "linear_general.hip",
+           "linear_8bit.hip", "norm.hip", "adamw.hip"]
 NATIVE_SOURCES = ["native.cpp", "native_operators.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -76,7 +77,7 @@ def build(verbose=True, extra=None):
     os.makedirs(OBJ_DIR, exist_ok=True)
     if extra:
         COMMON.extend(extra)
-    with ThreadPoolExecutor(max_workers=4) as pool:
+    with ThreadPoolExecutor(max_workers=6) as pool:
         results = list(pool.map(_compile, SOURCES))
     objs = []
     for src, obj, res in results:

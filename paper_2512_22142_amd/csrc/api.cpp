@@ -164,6 +164,9 @@ int ensure_device_ready(int dev, int* cus) {
   if (g_device_cus[dev] == 0) {
     CLEAVE_HIP(cleave::configure_execute_kernels());
     CLEAVE_HIP(cleave::configure_execute_direct_kernels());
+    CLEAVE_HIP(cleave::configure_linear_general_kernels());
+    CLEAVE_HIP(cleave::configure_linear_direct_kernels());
+    CLEAVE_HIP(cleave::configure_linear_8bit_kernels());
     void* ptr = nullptr;   // `dev` is the current device: its copy of the array
     CLEAVE_HIP(hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch)));
     g_static_scratch[dev] = static_cast<cleave::WorkItem*>(ptr);
@@ -703,9 +706,11 @@ bool cut_small(const cleave_plan* plan, int cus) {
 int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, const void* A,
                  int64_t lda, int transA, const void* B, int64_t ldb, int transB, int dtype,
                  float* partials, const BatchLayout& bl, void* hip_stream,
-                 const AssembleTarget& asm_to = AssembleTarget{}, bool static_scratch = false) {
+                 const AssembleTarget& asm_to = AssembleTarget{}, bool static_scratch = false,
+                 const cleave::LinearArgs* linear = nullptr) {
   if (!plan || !A || !B || (!partials && !asm_to.C)) return CLEAVE_EINVAL;
   if (dtype != CLEAVE_F32 && dtype != CLEAVE_BF16) return CLEAVE_EINVAL;
+  if (plan->pairs && !linear) return CLEAVE_EINVAL;   // a plan of 8-bit operands
   if ((transA != 0 && transA != 1) || (transB != 0 && transB != 1)) return CLEAVE_EINVAL;
   if ((task_ids == nullptr) != (n_ids == 0) || n_ids < 0) return CLEAVE_EINVAL;
   if (lda < (transA ? plan->M : plan->K) || ldb < (transB ? plan->K : plan->N)) return CLEAVE_EINVAL;
@@ -736,7 +741,8 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
   // with the inner dimension across, 3000 x 2504 x 3001 in 4 77 / 54; odd rows, 3001
   // x 2504 x 1024 in 4 37 / 30.
   const int e = 16 / eb;
-  const bool direct = dtype == CLEAVE_BF16 && plan->all_n_mult8 && (transA ? plan->all_m_mult8 : plan->all_k_mult8) &&
+  // (The epilogue's stores take any number of columns, and its kernels read A along K.)
+  const bool direct = dtype == CLEAVE_BF16 && (plan->all_n_mult8 || (linear && transB)) && !(linear && transA) && (transA ? plan->all_m_mult8 : plan->all_k_mult8) &&
                       (!transB || plan->all_k_mult8) &&
                       lda % e == 0 && ldb % e == 0 && aligned(A, 16) && aligned(B, 16) &&
                       // in-tile byte offsets are kept in 32 bits
@@ -755,7 +761,9 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
   cleave::ListShape shapes[cleave::kNumTileClasses] = {plan->shape, plan->shape};   // (the general kernel runs all tasks, or a subset)
   // which of the plan's lists a class runs from (-1: a subset's own list)
   int list_of[cleave::kNumTileClasses] = {task_ids ? -1 : 0, task_ids ? -1 : 1};
-  if (!task_ids && (!direct || cut_small(plan, cus))) {
+  // (8-bit operands multiplied as bf16 have no large shape)
+  const bool no_large = plan->pairs && !(asm_to.C && asm_to.out_dtype == CLEAVE_BF16);
+  if (!task_ids && (!direct || no_large || cut_small(plan, cus))) {
     list_of[cleave::kTileSmall] = cleave::kNumTileClasses;
     d_lists[cleave::kTileLarge] = nullptr;
     counts[cleave::kTileLarge] = 0;
@@ -831,6 +839,7 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
     args.stream_below_k = task_ids ? 0 : streamed_below(plan, asm_to);
     args.c_bf16 = asm_to.out_dtype == CLEAVE_BF16 ? 1 : 0;
     const bool large = c == cleave::kTileLarge;
+    if (plan->pairs && !direct) return launch_failed(hipErrorInvalidValue);   // (cleave_linear has refused what leads here)
     if (direct) {
       // Persistent workgroups, as many as the chip holds at once: each walks
       // the item list with the grid as stride and fetches the head of its next
@@ -843,7 +852,9 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
       args.wg_ranges = (list >= 0 && plan->wg_ranges_grid[list] == grid)
                            ? plan->d_wg_ranges[list] : nullptr;
       if (args.wg_ranges && list == cleave::kNumTileClasses) args.items += counts[c];   // behind the list as laid out
-      const hipError_t he = cleave::launch_execute_direct(args, shape, plan->chunk_tails, grid, stream);
+      const hipError_t he = plan->pairs ? cleave::launch_linear_8bit(args, *linear, shape, plan->chunk_tails, grid, stream)
+                            : linear    ? cleave::launch_linear_direct(args, *linear, shape, plan->chunk_tails, grid, stream)
+                                        : cleave::launch_execute_direct(args, shape, plan->chunk_tails, grid, stream);
       if (he != hipSuccess) return launch_failed(he);
       if (counts[c] > most) plan->last_kernel = direct_kernel_name(shape, transA, transB);
     } else {
@@ -859,7 +870,12 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
         how.tile = cleave::kTileWide4;
       if (how.tile == cleave::kTileNarrow && cleave::runs_lone(dtype, c, counts[c], shapes[c], cus))
         how.tile = cleave::kTileLone;
-      const hipError_t he = cleave::launch_execute(args, dtype, c, how, stream);
+      if (linear)   // (two tiles serve an epilogue)
+        how.tile = how.tile == cleave::kTileLone || how.tile == cleave::kTileQuarter || how.tile == cleave::kTileNarrow
+                       ? cleave::kTileNarrow
+                       : cleave::kTileWide;
+      const hipError_t he = linear ? cleave::launch_linear_general(args, *linear, dtype, c, how, stream)
+                                   : cleave::launch_execute(args, dtype, c, how, stream);
       if (he != hipSuccess) return launch_failed(he);
       if (counts[c] > most) plan->last_kernel = kernel_name(dtype, how, transA, transB);
     }
@@ -1117,6 +1133,136 @@ extern "C" int cleave_reduce_grouped(cleave_plan* plan, const float* partials, i
   const int rc = group_offsets(C_list, plan->batch, out_dtype == CLEAVE_BF16 ? 2 : 4, &bl.c, &C);
   if (rc != CLEAVE_OK) return rc;
   return reduce_impl(plan, partials, const_cast<void*>(C), ldc, out_dtype, bl, hip_stream);
+}
+
+// ---- linear product ------------------------------------------------------------
+
+namespace {
+
+// Splits of K for products whose tiles alone leave CUs idle.  The chunks are whole
+// sixteen bytes of the operands (`e` elements) where K is.
+int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e) {
+  constexpr int64_t kCUs = 256;
+  int64_t want;
+  if (M <= cleave::kFewRows) {
+    const int64_t groups = (N + 16 * e - 1) / (16 * e);
+    want = std::min(3 * kCUs / std::max<int64_t>(groups, 1), K / (32 * e));
+  } else {
+    const int64_t parts = ((M + 63) / 64) * ((N + 63) / 64);
+    want = std::min(kCUs / parts, K / 512);
+  }
+  want = std::min<int64_t>(want, 64);
+  for (int64_t S = want; S > 1; --S) {
+    const int64_t chunk = (K + S - 1) / S;
+    if ((S - 1) * chunk < K && (chunk % e == 0 || K % e != 0)) return S;
+  }
+  return 1;
+}
+
+bool linear_dtype(int dtype) { return dtype == CLEAVE_F32 || dtype == CLEAVE_BF16 || dtype == CLEAVE_E4M3; }
+
+}  // namespace
+
+extern "C" int cleave_plan_linear(int64_t M, int64_t N, int64_t K, int dtype, cleave_plan** out) {
+  if (!linear_dtype(dtype) || !out || M < 1 || N < 1 || K < 1) return CLEAVE_EINVAL;
+  constexpr int64_t kMost = std::numeric_limits<int32_t>::max();
+  if (M > kMost || N > kMost || K > kMost) return CLEAVE_EINVAL;
+  const bool pairs = dtype == CLEAVE_E4M3;
+  if (pairs && K % 16 != 0) return CLEAVE_EINVAL;
+  const int64_t k = pairs ? K / 2 : K;
+  const int64_t tile = M <= cleave::kFewRows ? cleave::kSmallTileRows : cleave::kLargeTileRows;
+  const int rc = cleave_plan_uniform(M, N, k, tile, tile,
+                                     static_cast<int32_t>(linear_splits(M, N, k, dtype == CLEAVE_F32 ? 4 : 8)), 0, out);
+  if (rc == CLEAVE_OK) (*out)->pairs = pairs;
+  return rc;
+}
+
+extern "C" int64_t cleave_linear_workspace(const cleave_plan* plan) {
+  if (!plan || plan->batch > 0) return CLEAVE_EINVAL;
+  return plan->uniform_splits == 1 ? 0 : plan->partial_elems;
+}
+
+extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, void* hip_stream) {
+  if (!plan || !a || plan->batch > 0 || !linear_dtype(a->dtype)) return CLEAVE_EINVAL;
+  const bool e4m3 = a->dtype == CLEAVE_E4M3;
+  if (plan->pairs != e4m3 || !a->A || !a->B || !a->C) return CLEAVE_EINVAL;
+  if ((a->transA != 0 && a->transA != 1) || (a->transB != 0 && a->transB != 1)) return CLEAVE_EINVAL;
+  if (a->out_dtype != CLEAVE_F32 && a->out_dtype != CLEAVE_BF16) return CLEAVE_EINVAL;
+  if (a->act < CLEAVE_ACT_NONE || a->act > CLEAVE_ACT_SILU || (a->act_grad != 0 && a->act_grad != 1)) return CLEAVE_EINVAL;
+  if (a->act_grad && (a->bias || (a->act != CLEAVE_ACT_NONE && !a->preact))) return CLEAVE_EINVAL;
+  if (e4m3 != (a->scale_a != nullptr) || e4m3 != (a->scale_b != nullptr)) return CLEAVE_EINVAL;
+  const int ob = a->out_dtype == CLEAVE_BF16 ? 2 : 4, eb = e4m3 ? 1 : a->dtype == CLEAVE_BF16 ? 2 : 4;
+  const int64_t M = plan->M, N = plan->N, K = e4m3 ? 2 * plan->K : plan->K;
+  if (a->lda < (a->transA ? M : K) || a->ldb < (a->transB ? K : N) || a->ldc < N || (a->residual && a->ldr < N) ||
+      (a->preact && a->ldz < N))
+    return CLEAVE_EINVAL;
+  if (!aligned(a->A, eb) || !aligned(a->B, eb) || !aligned(a->C, ob) || !aligned(a->residual, ob) || !aligned(a->preact, ob) ||
+      !aligned(a->bias, 4) || !aligned(a->scale_a, 4) || !aligned(a->scale_b, 4) || !aligned(a->partials, 4))
+    return CLEAVE_EINVAL;
+  if (e4m3 && (a->transA || !a->transB || !aligned(a->A, 16) || !aligned(a->B, 16) || a->lda % 16 || a->ldb % 16 ||
+               a->lda >= int64_t{1} << 22 || a->ldb >= int64_t{1} << 22))
+    return CLEAVE_EINVAL;
+  const int64_t splits = plan->uniform_splits;
+  const bool joined = splits != 1;
+  if (joined && !a->partials) return CLEAVE_EINVAL;
+
+  cleave::LinearArgs epi{};
+  epi.bias = a->bias;
+  epi.scale_a = a->scale_a;
+  epi.scale_b = a->scale_b;
+  epi.residual = a->residual;
+  epi.preact = a->act_grad && a->act == CLEAVE_ACT_NONE ? nullptr : a->preact;
+  epi.ldr = a->ldr;
+  epi.ldz = a->ldz;
+  epi.act = a->act;
+  epi.grad = a->act_grad;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  int rc = ensure_uploaded(plan);
+  if (rc != CLEAVE_OK) return rc;
+
+  // Few rows: every sixteen bytes along K belong to one chunk, and along N to B's row.
+  const int64_t e = 16 / eb;
+  const bool few_rows = M <= cleave::kFewRows && !a->transA && splits >= 1 && (K + splits - 1) / splits % e == 0 && K % e == 0 &&
+                        a->lda % e == 0 && a->ldb % e == 0 && aligned(a->A, 16) && aligned(a->B, 16) &&
+                        (a->transB || N % e == 0);
+  AssembleTarget to;
+  to.C = joined ? nullptr : a->C;
+  to.ldc = a->ldc;
+  to.out_dtype = a->out_dtype;
+  if (few_rows) {
+    cleave::ExecuteArgs args{};
+    args.A = a->A;
+    args.B = a->B;
+    args.lda = a->lda;
+    args.ldb = a->ldb;
+    args.transB = a->transB;
+    args.partials = a->partials;
+    args.C = a->C;
+    args.ldc = a->ldc;
+    args.c_bf16 = a->out_dtype == CLEAVE_BF16;
+    args.M = M;
+    args.N = N;
+    args.K = K;
+    CLEAVE_HIP(cleave::launch_linear_few_rows(args, epi, a->dtype, static_cast<int>(splits), stream));
+    plan->last_kernel = "linear_few_rows";
+  } else {
+    // (nothing to do behind the sums: the blocks themselves)
+    const bool bare = !e4m3 && (joined || (!epi.bias && !epi.residual && !epi.preact && epi.act == CLEAVE_ACT_NONE));
+    rc = execute_impl(plan, nullptr, 0, a->A, e4m3 ? a->lda / 2 : a->lda, a->transA, a->B, e4m3 ? a->ldb / 2 : a->ldb, a->transB,
+                      e4m3 ? CLEAVE_BF16 : a->dtype, joined ? a->partials : nullptr, BatchLayout{}, hip_stream, to, false,
+                      bare ? nullptr : &epi);
+    if (rc != CLEAVE_OK) return rc;
+  }
+  if (!joined) return CLEAVE_OK;
+  cleave::ReduceArgs args{};
+  args.items = few_rows ? nullptr : plan->d_reduce_items;
+  args.n_items = plan->reduce_runs;
+  args.partials = a->partials;
+  args.C = a->C;
+  args.ldc = a->ldc;
+  CLEAVE_HIP(cleave::launch_linear_join(args, epi, M, N, static_cast<int>(splits), a->out_dtype,
+                                        plan->all_n_mult4 && aligned(a->partials, 16), stream));
+  return CLEAVE_OK;
 }
 
 #ifndef CLEAVE_AGG_ELEMS

@@ -26,6 +26,17 @@ __device__ __forceinline__ float from_e4m3(uint32_t word) {
   return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(word), BYTE);
 }
 
+// Eight e4m3 values of two words as bf16, which holds them exactly.
+__device__ __forceinline__ auto bf16_of_e4m3(uint32_t lo, uint32_t hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
 // 448 / (the largest magnitude) as the scale's reciprocal; both zero below kLeastScaled.
 // NaN stays NaN.
 struct BlockScale {

@@ -66,6 +66,18 @@ struct ExecuteArgs {
   const uint32_t* wg_ranges;
 };
 
+// Epilogue of a linear product (linear_epilogue.h).  preact and residual have the output's type.
+struct LinearArgs {
+  const float* bias;          // N; may be null
+  const float* scale_a;       // M and N, 8-bit operands; else null
+  const float* scale_b;
+  const void* residual;       // may be null
+  void* preact;               // written, or with `grad` read; may be null
+  int64_t ldr, ldz;           // elements
+  int act;
+  int grad;
+};
+
 // Bytes of the Infinity Cache: what is written last, up to that much, is still
 // there when the next launch reads it.
 constexpr int64_t kCacheBytes = int64_t{256} << 20;
@@ -208,10 +220,31 @@ constexpr int direct_workgroups_per_cu(DirectShape shape) {
 // kDirectParts: one workgroup per item or part, whatever `grid`).
 hipError_t launch_execute_direct(const ExecuteArgs& args, DirectShape shape, bool tails, int grid, hipStream_t stream);
 
+// The same into args.C (assemble mode) through an epilogue.  The direct kernel: transA = 0.
+hipError_t launch_linear_direct(const ExecuteArgs& args, const LinearArgs& epi, DirectShape shape, bool tails, int grid,
+                                hipStream_t stream);
+// Operands of e4m3 values, both K-contiguous; K and the strides count pairs of them.  args.C null: partial blocks.
+// What the direct kernel multiplies.  e4m3 by its own instruction (kE4M3) is only as exact as
+// a bf16 output; as bf16 (kE4M3Exact) it has no large shape.
+enum DirectOperands : int { kBf16 = 0, kE4M3 = 1, kE4M3Exact = 2 };
+hipError_t launch_linear_8bit(const ExecuteArgs& args, const LinearArgs& epi, DirectShape shape, bool tails, int grid,
+                              hipStream_t stream);
+hipError_t launch_linear_general(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int tile_class,
+                                 const GeneralLoads& how, hipStream_t stream);
+
+// Few rows (at most kFewRows), transA = 0: B is read once, sixteen bytes at a time.  Into args.C through the epilogue
+// or, with splits > 1, into partials[s][row][column] for launch_linear_join.  The caller has checked that
+// every 16 bytes of a row of A, and of B, belong to one chunk (see few_rows_fit in api.cpp).
+constexpr int64_t kFewRows = 64;
+hipError_t launch_linear_few_rows(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int splits, hipStream_t stream);
+
 // Raises the dynamic-LDS limit of every execute kernel on the current device
 // (needed once per device and process, before the first launch).
 hipError_t configure_execute_kernels();
 hipError_t configure_execute_direct_kernels();
+hipError_t configure_linear_general_kernels();
+hipError_t configure_linear_direct_kernels();
+hipError_t configure_linear_8bit_kernels();
 
 // ---- work-item lists of subset launches ---------------------------------------
 // One entry per re-issued task: which task, and where its work items go.  The
@@ -250,6 +283,11 @@ struct ReduceArgs {
 // Enqueues the aggregation kernel.  `vec` selects the float4 path.
 hipError_t launch_reduce(const ReduceArgs& args, int out_dtype, bool vec, int grid,
                          hipStream_t stream);
+
+// C = epilogue(sum of the partial blocks of each tile, in ascending chunk order).  args.items null: one tile of
+// M x N with `splits` blocks.  `vec`: four elements at a time.
+hipError_t launch_linear_join(const ReduceArgs& args, const LinearArgs& epi, int64_t M, int64_t N, int splits, int out_dtype,
+                              bool vec, hipStream_t stream);
 
 // Aggregation with a residual added: C = sum of partials + R; R has C's
 // element type, leading dimension and batch strides.

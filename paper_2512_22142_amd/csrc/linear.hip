@@ -1,0 +1,333 @@
+// Linear products of few rows -- tokens being served -- and the join of a split
+// inner dimension with the epilogue.
+//
+// Few rows: y = x . W with at most 64 rows of x reads W once and does nothing else that counts, so it is
+// bound by memory.  A wave takes 16 E columns (B stored K x N) or 64 (N x K) and a run of k; no LDS stands
+// between the loads and the matrix instructions:
+//   N x K: lane (n, q) of a group of 4 E k's (E elements in 16 bytes) loads the E k's from E q on of column n, and x's
+//     rows likewise: fragments as they are.
+//   K x N: lane (n, q) loads the E columns from E n on of the rows k = E q .. E q + E - 1, each 16 E columns in one
+//     run of 256 bytes.  Its E x E square holds, for each of its columns c, the E k's of a fragment; bf16 are put
+//     together by v_perm, 4 per fragment, and fragment c belongs to the columns E n + c.
+// The waves of a workgroup split its chunk of k and are joined through LDS in wave order; workgroups that split K leave
+// partial sums for the second kernel.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "fp8_round.h"
+#include "kernels.h"
+#include "linear_epilogue.h"
+
+namespace cleave {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kWaves = 4;
+constexpr int kColumnBlocks = 4;   // of 16 columns, per wave, for B stored N x K
+
+template <int DTYPE>
+struct Type;
+template <>
+struct Type<CLEAVE_F32> {
+  static constexpr int E = 4;
+};
+template <>
+struct Type<CLEAVE_BF16> {
+  static constexpr int E = 8;
+};
+template <>
+struct Type<CLEAVE_E4M3> {
+  static constexpr int E = 16;
+};
+
+// One group of 4 E k's: sixteen bytes of k's in each lane of both operands.
+template <int DTYPE>
+__device__ __forceinline__ f32x4 multiply(u32x4 x, u32x4 w, f32x4 acc) {
+  if constexpr (DTYPE == CLEAVE_BF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, w), acc, 0, 0, 0);
+  } else if constexpr (DTYPE == CLEAVE_E4M3) {
+    // (as bf16, exactly: the 8-bit instruction drops bits, and memory bounds this kernel)
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_e4m3(x[0], x[1]), bf16_of_e4m3(w[0], w[1]), acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_e4m3(x[2], x[3]), bf16_of_e4m3(w[2], w[3]), acc, 0, 0, 0);
+  } else {
+    const f32x4 a = __builtin_bit_cast(f32x4, x), b = __builtin_bit_cast(f32x4, w);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+template <int DTYPE, bool B_K, int RB>
+struct FewRows {
+  static constexpr int E = Type<DTYPE>::E;
+  static constexpr int KG = 4 * E;                          // k's of a group
+  static constexpr int NC = B_K ? kColumnBlocks : E;        // fragments of columns
+  static constexpr int COLS = 16 * NC;                      // columns of a workgroup
+  static constexpr int EB = 16 / E;                         // bytes per element
+  struct Group {
+    u32x4 x[RB], w[NC];
+  };
+};
+
+template <int DTYPE, bool B_K, int RB>
+__global__ __launch_bounds__(64 * kWaves, RB > 1 ? 2 : 3) void few_rows_kernel(ExecuteArgs args, LinearArgs epi, int splits) {
+  typedef FewRows<DTYPE, B_K, RB> F;
+  constexpr int E = F::E, KG = F::KG, NC = F::NC, COLS = F::COLS, EB = F::EB;
+  __shared__ float sums[kWaves][16][COLS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, lq = lane >> 4;
+  const int64_t M = args.M, N = args.N, K = args.K;
+  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * COLS;
+  // this workgroup's chunk of k, this wave's groups of it
+  const int64_t chunk = (K + splits - 1) / splits;
+  const int64_t k0 = blockIdx.y * chunk, k1 = std::min(k0 + chunk, K);
+  const int64_t groups = (k1 - k0 + KG - 1) / KG, per = (groups + kWaves - 1) / kWaves;
+  const int64_t g0 = std::min(wave * per, groups), g1 = std::min(g0 + per, groups);
+
+  const unsigned char* const A = static_cast<const unsigned char*>(args.A);
+  const unsigned char* const B = static_cast<const unsigned char*>(args.B);
+  // rows and columns that are not there repeat the last one: their sums are not stored
+  const unsigned char* xp[RB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) xp[r] = A + (std::min<int64_t>(16 * r + l16, M - 1) * args.lda + E * lq) * EB;
+  const unsigned char* wp[B_K ? NC : 1];
+  if constexpr (B_K) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) wp[c] = B + (std::min<int64_t>(n0 + 16 * c + l16, N - 1) * args.ldb + E * lq) * EB;
+  } else {
+    wp[0] = B + std::min<int64_t>(n0 + E * l16, N - E) * EB;
+  }
+  const auto load = [&](int64_t g, typename F::Group& to) {
+    const int64_t k = k0 + g * KG;          // wave-uniform
+    const bool valid = k + E * lq < k1;     // all E of them: chunks and rows are whole sixteen bytes
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+      to.x[r] = valid ? *reinterpret_cast<const u32x4*>(xp[r] + k * EB) : u32x4{};
+    if constexpr (B_K) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) to.w[c] = valid ? *reinterpret_cast<const u32x4*>(wp[c] + k * EB) : u32x4{};
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        to.w[i] = valid ? *reinterpret_cast<const u32x4*>(wp[0] + (k + E * lq + i) * args.ldb * EB) : u32x4{};
+    }
+  };
+
+  f32x4 acc[RB][NC];
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[r][c] = f32x4{};
+  const auto compute = [&](const typename F::Group& g) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      u32x4 w = g.w[B_K ? c : 0];
+      if constexpr (!B_K) {
+        if constexpr (DTYPE == CLEAVE_BF16) {
+          // column c of the square: the low or high half of word c / 2 of the rows 2p and 2p + 1
+#pragma unroll
+          for (int p = 0; p < 4; ++p)
+            w[p] = __builtin_amdgcn_perm(g.w[2 * p + 1][c / 2], g.w[2 * p][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+        } else {
+#pragma unroll
+          for (int p = 0; p < 4; ++p) w[p] = g.w[p][c];
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < RB; ++r) acc[r][c] = multiply<DTYPE>(g.x[r], w, acc[r][c]);
+      if constexpr (!B_K && RB > 1) __builtin_amdgcn_sched_barrier(0);   // (all fragments at once would spill)
+    }
+  };
+  if constexpr (!B_K && RB > 1 && DTYPE == CLEAVE_BF16) {
+    // (registers for one group: the other waves' loads cover this one's wait)
+    typename F::Group a;
+#pragma unroll 1
+    for (int64_t g = g0; g < g1; ++g) {
+      load(g, a);
+      compute(a);
+    }
+  } else if (g0 < g1) {   // the next group is on its way while one is multiplied
+    typename F::Group a, b;
+    load(g0, a);
+    int64_t g = g0;
+    for (; g + 2 < g1; g += 2) {
+      load(g + 1, b);
+      compute(a);
+      load(g + 2, a);
+      compute(b);
+    }
+    if (g + 1 < g1) {
+      load(g + 1, b);
+      compute(a);
+      compute(b);
+    } else {
+      compute(a);
+    }
+  }
+
+  // Lane (l16, lq) has rows 4 lq + j of columns E l16 + c (K x N) or 16 c + l16 (N x K).
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    if (16 * r >= M) break;
+    if (r > 0) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sums[wave][4 * lq + j][B_K ? 16 * c + l16 : E * l16 + c] = acc[r][c][j];
+    __syncthreads();
+    const int rows = static_cast<int>(std::min<int64_t>(16, M - 16 * r));
+    for (int at = threadIdx.x; at < rows * COLS; at += 64 * kWaves) {
+      const int row = at / COLS, col = at % COLS;
+      if (n0 + col >= N) continue;
+      float sum = sums[0][row][col];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) sum += sums[w][row][col];
+      const int64_t m = 16 * r + row, n = n0 + col;
+      if (splits > 1) {
+        args.partials[(blockIdx.y * M + m) * N + n] = sum;
+      } else if (args.c_bf16) {
+        store_element<true>(args.C, m * args.ldc + n, finish_element<true>(epi, sum, m, n));
+      } else {
+        store_element<false>(args.C, m * args.ldc + n, finish_element<false>(epi, sum, m, n));
+      }
+    }
+  }
+}
+
+template <int DTYPE, bool B_K, int RB>
+hipError_t launch_rows(const ExecuteArgs& args, const LinearArgs& epi, int splits, hipStream_t stream) {
+  constexpr int COLS = FewRows<DTYPE, B_K, RB>::COLS;
+  hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, RB>), dim3(static_cast<uint32_t>((args.N + COLS - 1) / COLS), splits),
+                     dim3(64 * kWaves), 0, stream, args, epi, splits);
+  return hipGetLastError();
+}
+template <int DTYPE, bool B_K>
+hipError_t launch_layout(const ExecuteArgs& args, const LinearArgs& epi, int splits, hipStream_t stream) {
+  if (args.M <= 16) return launch_rows<DTYPE, B_K, 1>(args, epi, splits, stream);
+  if (args.M <= 32) return launch_rows<DTYPE, B_K, 2>(args, epi, splits, stream);
+  return launch_rows<DTYPE, B_K, 4>(args, epi, splits, stream);
+}
+
+// ---- join ------------------------------------------------------------------------
+
+constexpr int kJoinThreads = 256;
+constexpr int kJoinRun = 1024;   // elements of a workgroup where there is no table of runs
+
+// Four neighbouring elements of a row.
+template <bool BF16>
+struct Quad {
+  typedef uint32_t Words2 __attribute__((ext_vector_type(2), aligned(2)));
+  typedef float Floats __attribute__((ext_vector_type(4), aligned(4)));
+  static __device__ __forceinline__ void load(const void* base, int64_t at, float (&v)[4]) {
+    if constexpr (BF16) {
+      const Words2 w = *reinterpret_cast<const Words2*>(static_cast<const uint16_t*>(base) + at);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        v[2 * e] = __builtin_bit_cast(float, w[e] << 16);
+        v[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xffff0000u);
+      }
+    } else {
+      const Floats w = *reinterpret_cast<const Floats*>(static_cast<const float*>(base) + at);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = w[e];
+    }
+  }
+  static __device__ __forceinline__ void store(void* base, int64_t at, const float (&v)[4]) {
+    if constexpr (BF16) {
+      Words2 w;
+      w[0] = pack_bf16(v[0], v[1]);
+      w[1] = pack_bf16(v[2], v[3]);
+      *reinterpret_cast<Words2*>(static_cast<uint16_t*>(base) + at) = w;
+    } else {
+      *reinterpret_cast<Floats*>(static_cast<float*>(base) + at) = Floats{v[0], v[1], v[2], v[3]};
+    }
+  }
+};
+
+template <bool BF16, bool VEC>
+__global__ __launch_bounds__(kJoinThreads) void linear_join_kernel(ReduceArgs args, LinearArgs epi, int64_t M, int64_t N,
+                                                                   int splits) {
+  for (int64_t it = blockIdx.x; it < args.n_items; it += gridDim.x) {
+    uint64_t partial_off, block;
+    int64_t m0, n0;
+    uint32_t col0, n_len, count;
+    int S;
+    if (args.items) {
+      const ReduceItem item = load_record(args.items, it);
+      partial_off = item.partial_off;
+      block = item.block;
+      m0 = item.m0;
+      n0 = item.n0;
+      col0 = item.col0;
+      n_len = item.n_len;
+      count = item.count;
+      S = item.ksplit_cnt;
+    } else {
+      const int64_t first = it * kJoinRun;
+      partial_off = first;
+      block = M * N;
+      m0 = first / N;
+      n0 = 0;
+      col0 = static_cast<uint32_t>(first % N);
+      n_len = static_cast<uint32_t>(N);
+      count = static_cast<uint32_t>(std::min<int64_t>(kJoinRun, M * N - first));
+      S = splits;
+    }
+    const float* p = args.partials + partial_off;
+    constexpr int W = VEC ? 4 : 1;
+    for (uint32_t e = threadIdx.x * W; e < count; e += kJoinThreads * W) {
+      const uint32_t r = (col0 + e) / n_len;
+      const int64_t row = m0 + r, col = n0 + (col0 + e - r * n_len);
+      if constexpr (VEC) {
+        f32x4 sum = *reinterpret_cast<const f32x4*>(p + e);
+#pragma unroll 8
+        for (int s = 1; s < S; ++s) sum = sum + *reinterpret_cast<const f32x4*>(p + s * block + e);
+        float t[4] = {sum[0], sum[1], sum[2], sum[3]}, z[4] = {}, bias[4] = {}, scale_b[4] = {}, residual[4] = {};
+        if (epi.bias) Quad<false>::load(epi.bias, col, bias);
+        if (epi.scale_b) Quad<false>::load(epi.scale_b, col, scale_b);
+        if (epi.grad && epi.preact) Quad<BF16>::load(epi.preact, row * epi.ldz + col, z);
+        if (epi.residual) Quad<BF16>::load(epi.residual, row * epi.ldr + col, residual);
+        finish<4>(epi, t, z, bias, scale_b, epi.scale_a ? epi.scale_a[row] : 0.0f, residual);
+        if (!epi.grad && epi.preact) Quad<BF16>::store(epi.preact, row * epi.ldz + col, z);
+        Quad<BF16>::store(args.C, row * args.ldc + col, t);
+      } else {
+        float sum = p[e];
+#pragma unroll 8
+        for (int s = 1; s < S; ++s) sum += p[s * block + e];
+        store_element<BF16>(args.C, row * args.ldc + col, finish_element<BF16>(epi, sum, row, col));
+      }
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_linear_few_rows(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int splits, hipStream_t stream) {
+  if (dtype == CLEAVE_E4M3) return launch_layout<CLEAVE_E4M3, true>(args, epi, splits, stream);
+  if (dtype == CLEAVE_BF16)
+    return args.transB ? launch_layout<CLEAVE_BF16, true>(args, epi, splits, stream)
+                       : launch_layout<CLEAVE_BF16, false>(args, epi, splits, stream);
+  return args.transB ? launch_layout<CLEAVE_F32, true>(args, epi, splits, stream)
+                     : launch_layout<CLEAVE_F32, false>(args, epi, splits, stream);
+}
+
+hipError_t launch_linear_join(const ReduceArgs& args, const LinearArgs& epi, int64_t M, int64_t N, int splits, int out_dtype,
+                              bool vec, hipStream_t stream) {
+  ReduceArgs a = args;
+  if (!a.items) a.n_items = (M * N + kJoinRun - 1) / kJoinRun;
+  const dim3 g(static_cast<uint32_t>(std::min<int64_t>(a.n_items, int64_t{1} << 20))), b(kJoinThreads);
+  const bool bf16 = out_dtype == CLEAVE_BF16;
+  if (bf16 && vec) hipLaunchKernelGGL((linear_join_kernel<true, true>), g, b, 0, stream, a, epi, M, N, splits);
+  else if (bf16) hipLaunchKernelGGL((linear_join_kernel<true, false>), g, b, 0, stream, a, epi, M, N, splits);
+  else if (vec) hipLaunchKernelGGL((linear_join_kernel<false, true>), g, b, 0, stream, a, epi, M, N, splits);
+  else hipLaunchKernelGGL((linear_join_kernel<false, false>), g, b, 0, stream, a, epi, M, N, splits);
+  return hipGetLastError();
+}
+
+}  // namespace cleave

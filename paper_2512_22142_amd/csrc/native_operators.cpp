@@ -206,7 +206,59 @@ PyObject* py_adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-PyMethodDef kOperatorMethods[] = {{"rms_norm", as_function(py_rms_norm), METH_FASTCALL, nullptr},
+// linear(plan address, M, N, K, workspace, A, B, C, transA, transB, bias, act, act_grad, residual, preact, scale_a,
+//        scale_b, partials, stream)
+PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 19);
+    const int64_t M = integer(a[1]), N = integer(a[2]), K = integer(a[3]), elems = integer(a[4]);
+    const Operand A = operand(a[5], "A"), B = operand(a[6], "B"), C = operand(a[7], "C");
+    cleave_linear_args args{};
+    args.transA = static_cast<int32_t>(integer(a[8]));
+    args.transB = static_cast<int32_t>(integer(a[9]));
+    if (A.type != B.type) raise(PyExc_TypeError, "A and B must have the same dtype");
+    args.dtype = operand_code(A.type);
+    args.out_dtype = dtype_code(C.type);
+    const bool ta = args.transA != 0, tb = args.transB != 0;
+    if (A.rows != (ta ? K : M) || A.cols != (ta ? M : K) || B.rows != (tb ? N : K) || B.cols != (tb ? K : N) || C.rows != M ||
+        C.cols != N) {
+      PyErr_Format(PyExc_ValueError, "shapes (%lld, %lld), (%lld, %lld), (%lld, %lld) do not match the plan",
+                   static_cast<long long>(A.rows), static_cast<long long>(A.cols), static_cast<long long>(B.rows),
+                   static_cast<long long>(B.cols), static_cast<long long>(C.rows), static_cast<long long>(C.cols));
+      throw Raised{};
+    }
+    const Operand residual = like(a[13], "residual", M, N, C.type, true);
+    const Operand preact = like(a[14], "preact", M, N, C.type, true);
+    args.A = A.ptr;
+    args.lda = A.ld;
+    args.B = B.ptr;
+    args.ldb = B.ld;
+    args.C = C.ptr;
+    args.ldc = C.ld;
+    args.bias = floats(a[10], "bias", N, true);
+    args.act = static_cast<int32_t>(integer(a[11]));
+    args.act_grad = static_cast<int32_t>(integer(a[12]));
+    args.residual = residual.ptr;
+    args.ldr = residual.ld;
+    args.preact = preact.ptr;
+    args.ldz = preact.ld;
+    args.scale_a = floats(a[15], "scale_a", M, true);
+    args.scale_b = floats(a[16], "scale_b", N, true);
+    if (args.dtype != CLEAVE_E4M3 && (args.scale_a || args.scale_b)) raise(PyExc_ValueError, "scales belong to operands in float8_e4m3fn");
+    if (args.dtype == CLEAVE_E4M3 && (!args.scale_a || !args.scale_b)) raise(PyExc_ValueError, "operands in float8_e4m3fn need scale_a and scale_b");
+    if (elems > 0) args.partials = floats(a[17], "partials", elems, false, true);
+    cleave_plan* plan = static_cast<cleave_plan*>(address(a[0]));
+    void* stream = stream_of(a[18]);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = cleave_linear(plan, &args, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+  });
+}
+
+PyMethodDef kOperatorMethods[] = {{"linear", as_function(py_linear), METH_FASTCALL, nullptr},
+{"rms_norm", as_function(py_rms_norm), METH_FASTCALL, nullptr},
                                   {"rms_norm_backward", as_function(py_rms_norm_backward), METH_FASTCALL, nullptr},
                                   {"bias_grad", as_function(py_bias_grad), METH_FASTCALL, nullptr},
                                   {"adamw", as_function(py_adamw), METH_FASTCALL, nullptr},
