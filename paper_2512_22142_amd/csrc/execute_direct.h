@@ -89,6 +89,10 @@ struct Shape {
   static constexpr int kLoadsA = kATile / 1024 / NW;   // wave-wide loads per wave and step
   static constexpr int kLoadsB = kBTile / 1024 / NW;
   static constexpr int kLoadsPerStep = kLoadsA + kLoadsB;
+  static constexpr int kImage = WTN > 64 ? 16 * WTN * 4 : kBlockImageBytes;   // a wave's image for the stores
+  static constexpr int kLds = STAGES * kStage + NW * kImage;
+  // Waves per SIMD: what a CU's workgroups come to.
+  static constexpr int kWavesPerSimd = TM * TN == 256 * 256 ? NW / 4 : 2;
   // A tile smaller than the small class's: a workgroup computes one of the
   // PARTS_M x PARTS_N parts of a work item, and only that.
   static constexpr int PARTS_M = TM < kSmallTileRows ? kSmallTileRows / TM : 1;
@@ -170,12 +174,17 @@ struct DirectTile {
   __device__ __forceinline__ void issue(const unsigned char* gbase, uint32_t lds_tile, int wave) const {
     const uint32_t lds = lds_tile + wave * (kLoads * 1024);
     const unsigned char* base = gbase - (kLoads - 1) * 1024;
-    if constexpr (L == 4) {
+    if constexpr (L == 8) {   // (the offset ends at 4095)
+      issue<FIRST, 4>(gbase, lds_tile, wave);
+      issue<FIRST + 4, 4>(gbase, lds_tile, wave);
+    } else if constexpr (L == 4) {
+      constexpr int kAt = FIRST * 1024;
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
                    "global_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
                    "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
                    :
-                   : "s"(lds), "v"(goff[0]), "v"(goff[1]), "v"(goff[2]), "v"(goff[3]), "s"(base)
+                   : "s"(lds + kAt), "v"(goff[FIRST]), "v"(goff[FIRST + 1]), "v"(goff[FIRST + 2]), "v"(goff[FIRST + 3]),
+                     "s"(base + kAt)
                    : "memory", "m0");
     } else if constexpr (L == 2) {
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
@@ -238,7 +247,7 @@ __device__ __forceinline__ void spread_reads() {
 //     1.6e-5 off (bf16: 9e-8).  For bf16 outputs, which are rounded to 2^-9.
 //   kE4M3Exact: the values as bf16 (v_cvt, exact), for fp32 outputs and partial sums.
 template <typename S, bool A_K, bool B_K, bool TAILS, DirectOperands OPS, typename Epi>
-__global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(ExecuteArgs args, Epi epi) {
+__global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void execute_direct_kernel(ExecuteArgs args, Epi epi) {
   constexpr int TM = S::TM, TN = S::TN, MB = S::MB, NB = S::NB, CPR = S::CPR, kSub = S::kSub;
   constexpr int kStage = S::kStage, kATile = S::kATile, STAGES = S::STAGES, LPS = S::kLoadsPerStep;
   constexpr int kRowBytes = CPR * 16;        // K-contiguous tile row
@@ -389,7 +398,7 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   // Store instructions per lane of a full sub-tile.
   const bool bf16_out = args.C && args.c_bf16;
   const int tile_stores = bf16_out ? MB * NB / 2 : MB * NB;
-  unsigned char* const image = smem + STAGES * kStage + wave * kBlockImageBytes;
+  unsigned char* const image = smem + STAGES * kStage + wave * S::kImage;
 
   // This workgroup's items: first, first + stride, ... below it_end.
   int64_t it_first = blockIdx.x, it_end = args.n_items, stride = gridDim.x;
@@ -428,7 +437,8 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   int phase = 0;   // ring stage that holds the current item's step 0
   // Barrier once at most `steps_behind` steps' loads and `stores` stores are
   // outstanding.  (The counts are multiples of four; the counter holds 63.)
-  static_assert(LPS % 4 == 0 && (STAGES - 1) * LPS + MB * NB <= 40, "the wait counts below");
+  // (Beyond 40 the wait below is for more than it needs to be.)
+  static_assert(LPS % 4 == 0 && (Epi::kLinear || (STAGES - 1) * LPS + MB * NB <= 40), "the wait counts below");
   auto wait_behind = [&](int steps_behind, int stores) {
     switch ((steps_behind * LPS + stores) >> 2) {
       case 0: CLEAVE_WAIT_BARRIER(0); break;
@@ -459,7 +469,7 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   f32x4 acc[MB][NB];
   u32x4 fa[kQuarters ? 1 : 2][MB], fb[kQuarters ? 1 : 2][NB];
   constexpr bool kWide = OPS == kE4M3;   // both sub-steps in one instruction
-  i32x8 wide_a[kWide ? MB : 1], wide_b[kWide ? NB : 1];
+  i32x8 wide_a[kWide ? MH : 1], wide_b[kWide ? NB : 1];
 
   // Fragment reads are ordinary (compiler-visible) LDS loads: the compiler
   // tracks their completion, and every address is a lane-constant register
@@ -527,12 +537,14 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   };
   // The same for whole steps of 8-bit values: a lane's 32 bytes are its sixteen of either sub-step (any
   // order of k will do that both operands share).
-  auto read_wide_a = [&](uint32_t stage, auto i0_tag, auto n_tag) {
+  // Rows I0 .. I0 + N - 1 of A into registers 0 .. N - 1.
+  auto read_wide_a = [&](uint32_t stage, auto to_tag, auto i0_tag, auto n_tag) {
 #pragma unroll
-    for (int i = decltype(i0_tag)::value; i < decltype(i0_tag)::value + decltype(n_tag)::value; ++i) {
+    for (int x = 0; x < decltype(n_tag)::value; ++x) {
+      const int i = decltype(i0_tag)::value + x;
       const u32x4 lo = *reinterpret_cast<const u32x4*>(smem + (a_addr[0] + stage) + i * 16 * kRowBytes);
       const u32x4 hi = *reinterpret_cast<const u32x4*>(smem + (a_addr[1] + stage) + i * 16 * kRowBytes);
-      wide_a[i] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      wide_a[decltype(to_tag)::value + x] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   };
   auto read_wide_b = [&](uint32_t stage, auto j0_tag, auto n_tag) {
@@ -543,7 +555,8 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
       wide_b[j] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   };
-  auto mma_wide = [&](auto i0_tag, auto m_tag, auto j0_tag, auto n_tag, auto fresh_tag) {
+  // Rows I0 .. of the sums, whose fragments sit in registers R0 .., times columns J0 .. .
+  auto mma_wide = [&](auto i0_tag, auto r0_tag, auto m_tag, auto j0_tag, auto n_tag, auto fresh_tag) {
     constexpr int I0 = decltype(i0_tag)::value, J0 = decltype(j0_tag)::value, N = decltype(n_tag)::value;
 #pragma unroll
     for (int x = 0; x < decltype(m_tag)::value; ++x)
@@ -552,8 +565,9 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
         const int i = I0 + x, j = J0 + (i & 1 ? N - 1 - y : y);
         f32x4 sum = acc[i][j];
         if constexpr (decltype(fresh_tag)::value) sum = f32x4{};
-        // (e4m3 both, every scale 2^0)
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_b[j], wide_a[i], sum, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+        // (e4m3 both; no scales: the plain instruction)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_b[j], wide_a[decltype(r0_tag)::value + x], sum, 0, 0, 0,
+                                                                    0, 0, 0);
       }
   };
   constexpr int kReadsA = (A_K ? 1 : 2) * MB, kReadsB = (B_K ? 1 : 2) * NB;
@@ -579,7 +593,7 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
     // The fragments that a step begins with.
     auto first_frags = [&](uint32_t stage) {
       if constexpr (kWide) {
-        read_wide_a(stage, int_c<0>{}, int_c<MH>{});
+        read_wide_a(stage, int_c<0>{}, int_c<0>{}, int_c<MH>{});
         read_wide_b(stage, int_c<0>{}, int_c<NH>{});
       } else if constexpr (kQuarters) {
         read_a(stage, int_c<0>{}, int_c<0>{}, int_c<MH>{});
@@ -596,6 +610,8 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
     if (entry != kPrefetched) {
       wait_behind(min(STAGES, steps) - 1, stores_behind);
       first_frags(0u);   // a ring filled from empty starts at stage 0
+    } else if constexpr (Epi::kLinear) {
+      first_frags(phase * kStage);
     }
 
     // One K step; step s sits in ring stage (s + phase) % STAGES.  While the
@@ -615,6 +631,9 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
       const uint32_t oth = ((st + 1) & (STAGES - 1)) * kStage;
       const bool last = s + 1 >= steps;
       const bool go_on = HOW == kAnyStep ? !last || cont : HOW != 1;   // a step follows in the ring
+      // ... whose first fragments are read in this one.  (An epilogue needs their registers: the next
+      // item's are read behind it.)
+      const bool read_on = Epi::kLinear && HOW == kAnyStep ? !last : go_on;
       auto hand_over = [&]() {
         if constexpr (MID) {
           CLEAVE_WAIT_BARRIER((STAGES - 2) * LPS);
@@ -649,28 +668,42 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
       };
       constexpr int_c<0> k0{};
       constexpr int_c<1> k1{};
+      // 8-bit values: the second half of B times one half of A (rows I0 on), each row's registers being
+      // read anew behind its products: with A's second half of this stage, or the first half of the next.
+      [[maybe_unused]] auto rows_then_reads = [&](auto i0_tag, auto j0_tag, uint32_t stage, auto second_tag, bool on) {
+        const auto row = [&](auto x_tag) {
+          constexpr int X = decltype(x_tag)::value;
+          if constexpr (X < MH) {
+            mma_wide(int_c<decltype(i0_tag)::value + X>{}, x_tag, int_c<1>{}, j0_tag, int_c<NH>{}, fresh);
+            if (on) read_wide_a(stage, x_tag, int_c<(decltype(second_tag)::value ? MH : 0) + X>{}, int_c<1>{});
+            __builtin_amdgcn_sched_group_barrier(0x008, NH, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+          }
+        };
+        row(int_c<0>{});
+        row(int_c<1>{});
+        row(int_c<2>{});
+        row(int_c<3>{});
+        static_assert(MH <= 4, "the rows above");
+      };
       if constexpr (kWide) {
-        // Four quarters; the second halves are read while the first is multiplied, and the next step's first
-        // halves take the place of this one's once these are done with.
+        // Four quarters.  A's second half takes the registers of its first, row by row, in the second quarter, the
+        // next step's first half those of the second one in the last: with both halves at hand the large shape spills.
         constexpr int_c<0> lo{};
-        constexpr int_c<MH> a_hi{}, mh{};
+        constexpr int_c<MH> mh{};
         constexpr int_c<NH> b_hi{}, nh{};
         read_wide_b(cur, b_hi, nh);
-        read_wide_a(cur, a_hi, mh);
-        mma_wide(lo, mh, lo, nh, fresh);
-        spread_reads<MH * NH, MB + NB>();
-        mma_wide(lo, mh, b_hi, nh, fresh);
+        mma_wide(lo, lo, mh, lo, nh, fresh);
+        spread_reads<MH * NH, NB>();
+        rows_then_reads(lo, b_hi, cur, std::true_type{}, true);
+        mma_wide(mh, lo, mh, lo, nh, fresh);
         hand_over();
-        if (go_on) read_wide_a(oth, lo, mh);
-        mma_wide(a_hi, mh, lo, nh, fresh);
-        spread_reads<MH * NH, MB>();
         if constexpr (MID && kQuarters) {
           if constexpr (!kPairs) issue_a(c, st, second_half);
           issue_b(c, st, whole);
         }
-        if (go_on) read_wide_b(oth, lo, nh);
-        mma_wide(a_hi, mh, b_hi, nh, fresh);
-        spread_reads<MH * NH, NB>();
+        if (read_on) read_wide_b(oth, lo, nh);
+        rows_then_reads(mh, b_hi, oth, std::false_type{}, read_on);
       } else if constexpr (kQuarters) {
         // Four quarters per sub-step: (first half of A, one half of B), the other
         // half of B, then the second half of A with B's halves the other way
@@ -699,30 +732,30 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
         hand_over();
         // The refill's loads are spread over the rest of the step.
         if constexpr (kPairs) {
-          if (go_on) read_a(oth, k0, lo, mh);
+          if (read_on) read_a(oth, k0, lo, mh);
           mma(k1, a_hi, mh, lo, nh, more);
           spread_reads<MH * NH, kReadsA / 2>();
           if constexpr (MID) issue_b(c, st, whole);
-          if (go_on) read_b(oth, k0, lo, nh);
+          if (read_on) read_b(oth, k0, lo, nh);
           mma(k1, a_hi, mh, b_hi, nh, more);
           spread_reads<MH * NH, kReadsB / 2>();
         } else {
           constexpr int_c<MH / 2> mq{};
           constexpr int_c<MH + MH / 2> a_last{};
           constexpr int_c<NH / 2> nq{};
-          if (go_on) read_a(oth, k0, lo, mq);
+          if (read_on) read_a(oth, k0, lo, mq);
           mma(k1, a_hi, mq, lo, nh, more);
           spread_reads<MH * NH / 2, kReadsA / 4>();
           if constexpr (MID) issue_a(c, st, second_half);
-          if (go_on) read_a(oth, k0, mq, mq);
+          if (read_on) read_a(oth, k0, mq, mq);
           mma(k1, a_last, mq, lo, nh, more);
           spread_reads<MH * NH / 2, kReadsA / 4>();
           if constexpr (MID) issue_b(c, st, first_half);
-          if (go_on) read_b(oth, k0, lo, nq);
+          if (read_on) read_b(oth, k0, lo, nq);
           mma(k1, a_hi, mq, b_hi, nh, more);
           spread_reads<MH * NH / 2, kReadsB / 4>();
           if constexpr (MID) issue_b(c, st, second_half);
-          if (go_on) read_b(oth, k0, nq, nq);
+          if (read_on) read_b(oth, k0, nq, nq);
           mma(k1, a_last, mq, b_hi, nh, more);
           spread_reads<MH * NH / 2, kReadsB / 4>();
         }
@@ -735,7 +768,7 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
         mma(k0, k0, m, k0, n, fresh);
         spread_reads<MB * NB, kReadsA + kReadsB>();
         hand_over();
-        if (go_on) first_frags(oth);
+        if (read_on) first_frags(oth);
         mma(k1, k0, m, k0, n, more);
         spread_reads<MB * NB, kReadsA + kReadsB>();
       }
@@ -792,7 +825,7 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
         }
       }
       if constexpr (Epi::kLinear)
-        store_linear_rows<decltype(bf16_tag)::value, decltype(interior_tag)::value, MB, NB>(
+        store_linear_rows<decltype(bf16_tag)::value, decltype(interior_tag)::value, OPS != kBf16, 1, MB, NB>(
             acc, late_linear_args<sizeof(ExecuteArgs)>(), target, image, wm * S::WTM, wn * S::WTN, lane, m_valid, n_valid,
             m_base, n_base);
       else
@@ -821,7 +854,7 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
 
 template <typename S, bool A_K, bool B_K, bool TAILS, DirectOperands OPS, typename Epi>
 hipError_t launch_one(const ExecuteArgs& args, const Epi& epi, int grid, hipStream_t stream) {
-  constexpr size_t lds = S::STAGES * S::kStage + S::NW * kBlockImageBytes;
+  constexpr size_t lds = S::kLds;
   hipLaunchKernelGGL((execute_direct_kernel<S, A_K, B_K, TAILS, OPS, Epi>), dim3(grid), dim3(S::NT), lds, stream, args, epi);
   return hipGetLastError();
 }
@@ -830,7 +863,7 @@ template <typename S, bool A_K, bool B_K, bool TAILS, DirectOperands OPS, typena
 hipError_t configure_one() {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(execute_direct_kernel<S, A_K, B_K, TAILS, OPS, Epi>),
                              hipFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(S::STAGES * S::kStage + S::NW * kBlockImageBytes));
+                             S::kLds);
 }
 
 // The layouts that there are: all four, with an epilogue those with A K-contiguous, in 8 bits those with B too.
@@ -875,6 +908,10 @@ hipError_t configure_shape() {
 //     items of 16 steps 164 / 237 us).
 using LargeShape = Shape<kLargeTileRows, kLargeTileCols, 2, 4, 64, 2, false>;
 using SmallShape = Shape<kSmallTileRows, kSmallTileCols, 2, 2, 64, 2, false>;
+// 8-bit operands have twice the products per byte, and what bounds them is the LDS: 256 x 256 in eight waves of 128 x 64
+// takes 125 bytes a clock of its 128 (reads and the ring's fill), in four of 128 x 128, one to a SIMD with 512
+// registers, 94.
+using WideShape = Shape<kLargeTileRows, kLargeTileCols, 2, 2, 64, 2, false>;
 using DeepShape = Shape<kSmallTileRows, kSmallTileCols, 2, 2, 64, 4, true>;
 using PartsShape = Shape<64, 64, 2, 2, 64, 4, true>;
 static_assert(kDirectKStep == LargeShape::BK && kDirectKStep == SmallShape::BK &&
@@ -904,7 +941,7 @@ hipError_t launch_with(const ExecuteArgs& args, const Epi& epi, DirectShape shap
   switch (shape) {
     case kDirectLarge:
       if constexpr (OPS == kE4M3Exact) return hipErrorInvalidValue;
-      else return launch_shape<LargeShape, OPS>(args, epi, tails, grid, stream);
+      else return launch_shape<std::conditional_t<OPS == kE4M3, WideShape, LargeShape>, OPS>(args, epi, tails, grid, stream);
     case kDirectSmall: return launch_shape<SmallShape, OPS>(args, epi, tails, grid, stream);
     case kDirectDeep: return launch_shape<DeepShape, OPS>(args, epi, tails, static_cast<int>(args.n_items), stream);
     default: {   // one workgroup per part of an item; the list is padded to whole rounds of the XCDs
@@ -917,7 +954,7 @@ hipError_t launch_with(const ExecuteArgs& args, const Epi& epi, DirectShape shap
 template <DirectOperands OPS, typename Epi>
 hipError_t configure_all() {
   hipError_t e = hipSuccess;
-  if constexpr (OPS != kE4M3Exact) e = configure_shape<LargeShape, OPS, Epi>();
+  if constexpr (OPS != kE4M3Exact) e = configure_shape<std::conditional_t<OPS == kE4M3, WideShape, LargeShape>, OPS, Epi>();
   if (e == hipSuccess) e = configure_shape<SmallShape, OPS, Epi>();
   if (e == hipSuccess) e = configure_shape<DeepShape, OPS, Epi>();
   if (e == hipSuccess) e = configure_shape<PartsShape, OPS, Epi>();

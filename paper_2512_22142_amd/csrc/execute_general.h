@@ -578,8 +578,11 @@ __global__ __launch_bounds__(S::NT, S::WPE) void execute_kernel(ExecuteArgs args
     TileTarget target = tile_target(args, item);
     target.base += (m_off * target.ld + n_off) * (args.C && args.c_bf16 ? 2 : 4);
     if constexpr (Epi::kLinear) {
-      store_linear_tile<MB, NB>(acc, late_linear_args<sizeof(ExecuteArgs)>(), target, args.c_bf16, row0, col0, m_valid, n_valid,
-                                int64_t{item.m_base} + m_off, int64_t{item.n_base} + n_off);
+      CLEAVE_LDS_BARRIER();   // the operands' place is the images' now (and theirs again behind the next item's first barrier)
+      store_linear_tile<MB, NB>(acc, late_linear_args<sizeof(ExecuteArgs)>(), target, args.c_bf16,
+                                smem + (t >> 6) * kTileImageBytes, wm * S::WTM, wn * S::WTN, lane, m_valid, n_valid,
+                                int64_t{item.m_base} + m_off, int64_t{item.n_base} + n_off, m_valid == TM && n_valid == TN);
+      static_assert(S::NT / 64 * kTileImageBytes <= 2 * S::kStage, "an image for each wave");
     } else if constexpr (S::BLK == 16) {
       store_block(acc[0][0], target, args.C && args.c_bf16, wm * S::WTM + 4 * (lane >> 4), col0, m_valid, n_valid);
     } else {

@@ -288,12 +288,18 @@ __global__ __launch_bounds__(kJoinThreads) void linear_join_kernel(ReduceArgs ar
         f32x4 sum = *reinterpret_cast<const f32x4*>(p + e);
 #pragma unroll 8
         for (int s = 1; s < S; ++s) sum = sum + *reinterpret_cast<const f32x4*>(p + s * block + e);
-        float t[4] = {sum[0], sum[1], sum[2], sum[3]}, z[4] = {}, bias[4] = {}, scale_b[4] = {}, residual[4] = {};
+        float t[4] = {sum[0], sum[1], sum[2], sum[3]}, z[4] = {}, bias[4] = {}, scale_b[4] = {};
         if (epi.bias) Quad<false>::load(epi.bias, col, bias);
         if (epi.scale_b) Quad<false>::load(epi.scale_b, col, scale_b);
         if (epi.grad && epi.preact) Quad<BF16>::load(epi.preact, row * epi.ldz + col, z);
-        if (epi.residual) Quad<BF16>::load(epi.residual, row * epi.ldr + col, residual);
-        finish<4>(epi, t, z, bias, scale_b, epi.scale_a ? epi.scale_a[row] : 0.0f, residual);
+        if (epi.scale_a) finish<true>(epi, t, z, bias, scale_b, epi.scale_a[row]);
+        else finish<false>(epi, t, z, bias, scale_b, 0.0f);
+        if (epi.residual) {
+          float residual[4];
+          Quad<BF16>::load(epi.residual, row * epi.ldr + col, residual);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) t[k] += residual[k];
+        }
         if (!epi.grad && epi.preact) Quad<BF16>::store(epi.preact, row * epi.ldz + col, z);
         Quad<BF16>::store(args.C, row * args.ldc + col, t);
       } else {

@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "bf16_round.h"
 #include "kernels.h"
@@ -29,27 +30,18 @@ __device__ __forceinline__ float sigmoid(float x) {
 constexpr float kGelu2 = 1.5957691216057308f;   // 2 sqrt(2 / pi)
 constexpr float kGelu3 = 0.044715f;
 
-__device__ __forceinline__ float act_value(float z, int act) {
-  switch (act) {
-    case CLEAVE_ACT_RELU: return z < 0.0f ? 0.0f : z;   // NaN stays
-    case CLEAVE_ACT_GELU_TANH: return z * sigmoid(kGelu2 * (z + kGelu3 * z * z * z));
-    case CLEAVE_ACT_SILU: return z * sigmoid(z);
-    default: return z;
-  }
+__device__ __forceinline__ float relu(float z) { return z < 0.0f ? 0.0f : z; }   // NaN stays
+__device__ __forceinline__ float gelu(float z) { return z * sigmoid(kGelu2 * z * (1.0f + kGelu3 * z * z)); }
+__device__ __forceinline__ float silu(float z) { return z * sigmoid(z); }
+__device__ __forceinline__ float relu_slope(float z) { return z > 0.0f ? 1.0f : 0.0f; }
+// (where the sigmoid is 0 or 1 it is the slope, also for infinite z)
+__device__ __forceinline__ float gelu_slope(float z) {
+  const float p = sigmoid(kGelu2 * z * (1.0f + kGelu3 * z * z)), q = p * (1.0f - p);
+  return q > 0.0f ? p + z * q * (kGelu2 * (1.0f + 3.0f * kGelu3 * z * z)) : p;
 }
-__device__ __forceinline__ float act_slope(float z, int act) {
-  switch (act) {
-    case CLEAVE_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-    case CLEAVE_ACT_GELU_TANH: {
-      const float p = sigmoid(kGelu2 * (z + kGelu3 * z * z * z)), q = p * (1.0f - p);
-      return q > 0.0f ? p + z * q * (kGelu2 * (1.0f + 3.0f * kGelu3 * z * z)) : p;   // (infinite z: p)
-    }
-    case CLEAVE_ACT_SILU: {
-      const float p = sigmoid(z), q = p * (1.0f - p);
-      return q > 0.0f ? p + z * q : p;
-    }
-    default: return 1.0f;
-  }
+__device__ __forceinline__ float silu_slope(float z) {
+  const float p = sigmoid(z), q = p * (1.0f - p);
+  return q > 0.0f ? p + z * q : p;
 }
 
 // No epilogue: the kernels as cleave_execute and cleave_execute_assemble run them.
@@ -135,52 +127,102 @@ struct Piece {
   }
 };
 
-// The epilogue of N elements of a row.  t: the sums, then what is stored; z: the given z's, then (without
-// `grad`) the new ones.
-template <int N>
+// The epilogue of N elements of a row, but for the residual (SCALED: operands with scales).  t: the sums, then act(z) or the sums times the slope;
+// z: the given z's, or (without `grad`) the new ones.  Branches are uniform and taken once for all N.
+template <bool SCALED, int N>
 __device__ __forceinline__ void finish(const LinearArgs& e, float (&t)[N], float (&z)[N], const float (&bias)[N],
-                                       const float (&scale_b)[N], float scale_a, const float (&residual)[N]) {
-  if (e.scale_a) {
+                                       const float (&scale_b)[N], float scale_a) {
+  if constexpr (SCALED) {
 #pragma unroll
     for (int k = 0; k < N; ++k) t[k] = t[k] * scale_a * scale_b[k];
   }
   if (e.grad) {
+    switch (e.act) {
+      case CLEAVE_ACT_RELU:
 #pragma unroll
-    for (int k = 0; k < N; ++k) t[k] *= act_slope(z[k], e.act);
-  } else {
+        for (int k = 0; k < N; ++k) t[k] *= relu_slope(z[k]);
+        break;
+      case CLEAVE_ACT_GELU_TANH:
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      z[k] = t[k] + bias[k];
-      t[k] = act_value(z[k], e.act);
+        for (int k = 0; k < N; ++k) t[k] *= gelu_slope(z[k]);
+        break;
+      case CLEAVE_ACT_SILU:
+#pragma unroll
+        for (int k = 0; k < N; ++k) t[k] *= silu_slope(z[k]);
+        break;
+      default: break;
     }
+    return;
+  }
+  if (e.bias) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) t[k] += bias[k];
   }
 #pragma unroll
-  for (int k = 0; k < N; ++k) t[k] += residual[k];
+  for (int k = 0; k < N; ++k) z[k] = t[k];
+  switch (e.act) {
+    case CLEAVE_ACT_RELU:
+#pragma unroll
+      for (int k = 0; k < N; ++k) t[k] = relu(z[k]);
+      break;
+    case CLEAVE_ACT_GELU_TANH:
+#pragma unroll
+      for (int k = 0; k < N; ++k) t[k] = gelu(z[k]);
+      break;
+    case CLEAVE_ACT_SILU:
+#pragma unroll
+      for (int k = 0; k < N; ++k) t[k] = silu(z[k]);
+      break;
+    default: break;
+  }
 }
 
-// ---- stores of the direct kernel -------------------------------------------------
+// Byte offset of the 16-byte piece `q` of row `row` in an image of Q pieces to a row: pieces are exchanged so that a
+// write's rows and a read's pieces fall into different banks.
+template <int Q>
+__device__ __forceinline__ int image_piece(int row, int q) {
+  constexpr int R = Q < 16 ? 16 / Q : 1;   // rows in a cycle of the banks
+  return (row * Q + (q ^ ((row / R) & (Q < 16 ? Q - 1 : 15)))) * 16;
+}
+template <int ROWS, int COLS, int N>
+__device__ __forceinline__ void read_image(const unsigned char* image, int row, int piece, float (&v)[N]) {
+#pragma unroll
+  for (int q = 0; q < N / 4; ++q) {
+    const tile_f32x4 part = *reinterpret_cast<const tile_f32x4*>(image + image_piece<COLS / 4>(row, piece + q));
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[4 * q + c] = part[c];
+  }
+}
 
-// store_rows (tile_store.h) with the epilogue: the sums go through the wave's image in fp32, and a
-// lane takes sixteen output bytes' worth of a row from it.  m_base / n_base: the sub-tile's place in the
-// output.  One turn per row of blocks, not unrolled: with all of them in line the code is beyond
-// the instruction cache and its addresses spill.  What a turn reads is fetched during the one before.
-template <bool BF16, bool INTERIOR, int MB, int NB>
-__device__ __forceinline__ void store_linear_rows(const tile_f32x4 (&acc)[MB][NB], const LinearArgs& e, const TileTarget& t,
-                                                  unsigned char* image, int wave_row0, int wave_col0, int lane, int m_valid,
-                                                  int n_valid, int64_t m_base, int64_t n_base) {
+// ---- a wave's part of the output, image by image -----------------------------------
+
+// At the end of a branch that picks accumulators by a number: different text in each keeps the compiler from merging them
+// into one access through a computed address, for which the accumulators would live in memory.
+#define CLEAVE_KEEP_APART(which) asm volatile("; part %0" ::"n"(which) : "memory")
+
+// Walks `count` images, each ROWS x COLS sums that `write(i)` puts into the wave's piece of LDS: a lane takes sixteen output
+// bytes' worth of a row at a time.  The images lie under each other (their columns are the same).
+// LDS executes a wave's accesses in order and no other wave touches the image: no barrier.
+// One turn per image, not unrolled: with all of them in line the code is beyond the instruction
+// cache and its addresses spill.  The vector-memory counter retires loads and stores in order, so a load waits for
+// the stores issued before it: what a turn reads is fetched AHEAD turns before, and nothing else is
+// loaded between stores (the rows' scales come from registers, across lanes).
+//   row0, col0: the first image's place in the sub-tile, of which m_valid x n_valid elements exist.
+//   out: element (0, 0) of the sub-tile, `ld` elements to a row; m_base, n_base: its place in the output.
+template <bool BF16, bool INTERIOR, bool SCALED, int ROWS, int COLS, int AHEAD, typename Write>
+__device__ __forceinline__ void emit_images(const LinearArgs& e, unsigned char* out_base, int64_t ld,
+                                            const unsigned char* image, int count, int row0, int col0, int lane, int m_valid,
+                                            int n_valid, int64_t m_base, int64_t n_base, Write write) {
   typedef Piece<BF16> P;
   constexpr int N = P::N;
   constexpr int EB = BF16 ? 2 : 4;
-  constexpr int Q = NB * 4;                    // 16-byte pieces of an image row
-  constexpr int R = 16 / Q;                    // image rows in a cycle of the banks
-  constexpr int L = NB * 16 / N;               // lanes to a row
+  constexpr int L = COLS / N;                  // lanes to a row
   constexpr int RR = 64 / L;                   // rows per read of the whole wave
-  constexpr int K = 16 / RR;                   // reads of the whole wave per row of blocks
-  static_assert(16 * Q * 16 <= kBlockImageBytes && Q * R == 16 && 16 % RR == 0, "image");
-  const int wrow = lane & 15, wflip = (wrow / R) & (Q - 1);
+  constexpr int K = ROWS / RR;                 // reads of the whole wave per image
+  static_assert(ROWS % RR == 0 && AHEAD >= 1, "image");
   const int rrow = lane / L, rpiece = (lane % L) * (N / 4);
-  int row = wave_row0 + rrow;
-  const int col = wave_col0 + rpiece * 4;
+  int row = row0 + rrow;
+  const int col = col0 + rpiece * 4;
   // columns of this lane's that there are: all N, where every row of the output is whole pieces
   const int cols = INTERIOR ? N : min(N, n_valid - col);
   const auto valid = [&](int r) { return INTERIOR || (r < m_valid && cols > 0); };
@@ -208,79 +250,98 @@ __device__ __forceinline__ void store_linear_rows(const tile_f32x4 (&acc)[MB][NB
     }
   };
   if (e.bias) read_columns(e.bias, bias);
-  if (e.scale_b) read_columns(e.scale_b, scale_b);
+  float scales[2] = {};   // of rows row0 + lane and row0 + 64 + lane
+  if constexpr (SCALED) {
+    read_columns(e.scale_b, scale_b);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) scales[h] = e.scale_a[m_base + min(row0 + 64 * h + lane, m_valid - 1)];
+  }
   const int64_t grow = m_base + row, gcol = n_base + col;
-  unsigned char* out = t.base + (row * t.ld + col) * EB;
-  unsigned char* zp = static_cast<unsigned char*>(e.preact) + (grow * e.ldz + gcol) * EB;
+  unsigned char* out = out_base + (row * ld + col) * EB;
+  unsigned char* zp = static_cast<unsigned char*>(e.preact) + (grow * e.ldz + gcol) * EB;   // this turn's
   const unsigned char* rp = static_cast<const unsigned char*>(e.residual) + (grow * e.ldr + gcol) * EB;
-  const float* sp = e.scale_a + grow;
-  const int64_t out_pitch = t.ld * EB, z_pitch = e.ldz * EB, r_pitch = e.ldr * EB;
+  const int64_t out_pitch = ld * EB, z_pitch = e.ldz * EB, r_pitch = e.ldr * EB;
   const bool reads_z = e.grad && e.preact, writes_z = !e.grad && e.preact;
 
-  typename P::Raw z_next[K], r_next[K];
-  float s_next[K];
-  const auto fetch = [&](int first) {   // rows first + RR k from the pointers as they stand
+  typename P::Raw z_raw[AHEAD + 1][K], r_raw[AHEAD + 1][K];
+  const auto fetch = [&](int ahead, int d) {   // image i + ahead, into place d
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      z_next[k] = r_next[k] = typename P::Raw{};
-      s_next[k] = 0.0f;
-      if (!valid(first + RR * k)) continue;
-      if (reads_z) z_next[k] = read(zp + RR * k * z_pitch);
-      if (e.residual) r_next[k] = read(rp + RR * k * r_pitch);
-      if (e.scale_a) s_next[k] = sp[RR * k];
+      const int r = ROWS * ahead + RR * k;
+      if (!valid(row + r)) continue;
+      if (reads_z) z_raw[d][k] = read(zp + r * z_pitch);
+      if (e.residual) r_raw[d][k] = read(rp + r * r_pitch);
     }
   };
-  fetch(row);
+#pragma unroll
+  for (int d = 0; d <= AHEAD; ++d)
+#pragma unroll
+    for (int k = 0; k < K; ++k) z_raw[d][k] = r_raw[d][k] = typename P::Raw{};
+#pragma unroll
+  for (int d = 0; d < AHEAD; ++d)
+    if (d < count) fetch(d, d);
 #pragma unroll 1
-  for (int i = 0; i < MB; ++i) {
+  for (int i = 0; i < count; ++i) {
     asm volatile("" ::: "memory");
-#pragma unroll
-    for (int ii = 0; ii < MB; ++ii)
-      if (ii == i) {
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-          *reinterpret_cast<tile_f32x4*>(image + (wrow * Q + ((4 * j + (lane >> 4)) ^ wflip)) * 16) = acc[ii][j];
-      }
+    write(i);
     asm volatile("" ::: "memory");
-    typename P::Raw z_raw[K], r_raw[K];
-    float s_now[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      z_raw[k] = z_next[k];
-      r_raw[k] = r_next[k];
-      s_now[k] = s_next[k];
-    }
-    unsigned char* const z_out = zp;
-    zp += 16 * z_pitch;
-    rp += 16 * r_pitch;
-    sp += 16;
-    if (i + 1 < MB) fetch(row + 16);
+    if (i + AHEAD < count) fetch(AHEAD, AHEAD);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int r = rrow + RR * k;
-      float x[N];
-#pragma unroll
-      for (int q = 0; q < N / 4; ++q) {
-        const tile_f32x4 part =
-            *reinterpret_cast<const tile_f32x4*>(image + (r * Q + ((rpiece + q) ^ ((r / R) & (Q - 1)))) * 16);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) x[4 * q + c] = part[c];
+      P y, z;
+      read_image<ROWS, COLS, N>(image, r, rpiece, y.v);
+      float scale_a = 0.0f;
+      if constexpr (SCALED) {
+        const int at = ROWS * i + r;   // (64 rows' worth in a register; an image does not straddle them)
+        scale_a = __shfl(ROWS * i < 64 ? scales[0] : scales[1], at & 63);
       }
-      P z = P::of(z_raw[k]);
-      const P residual = P::of(r_raw[k]);
-      finish<N>(e, x, z.v, bias, scale_b, s_now[k], residual.v);
-      if (valid(row + RR * k)) {
-        if (writes_z) store(z, z_out + RR * k * z_pitch);
-        P y;
+      if (reads_z) z = P::of(z_raw[0][k]);
+      finish<SCALED>(e, y.v, z.v, bias, scale_b, scale_a);
+      if (e.residual) {
+        const P residual = P::of(r_raw[0][k]);
 #pragma unroll
-        for (int c = 0; c < N; ++c) y.v[c] = x[c];
+        for (int c = 0; c < N; ++c) y.v[c] += residual.v[c];
+      }
+      if (valid(row + RR * k)) {
+        if (writes_z) store(z, zp + RR * k * z_pitch);
         store(y, out + RR * k * out_pitch);
       }
     }
     asm volatile("" ::: "memory");
-    row += 16;
-    out += 16 * out_pitch;
+    row += ROWS;
+    out += ROWS * out_pitch;
+    zp += ROWS * z_pitch;
+    rp += ROWS * r_pitch;
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d)
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        z_raw[d][k] = z_raw[d + 1][k];
+        r_raw[d][k] = r_raw[d + 1][k];
+      }
   }
+}
+
+// ---- stores of the direct kernel -------------------------------------------------
+
+// store_rows (tile_store.h) with the epilogue: a row of 16 x 16 blocks is an image.
+template <bool BF16, bool INTERIOR, bool SCALED, int AHEAD, int MB, int NB>
+__device__ __forceinline__ void store_linear_rows(const tile_f32x4 (&acc)[MB][NB], const LinearArgs& e, const TileTarget& t,
+                                                  unsigned char* image, int wave_row0, int wave_col0, int lane, int m_valid,
+                                                  int n_valid, int64_t m_base, int64_t n_base) {
+  const int row = lane & 15, quad = lane >> 4;   // lane's row and which four columns of a block
+  emit_images<BF16, INTERIOR, SCALED, 16, NB * 16, AHEAD>(
+      e, t.base, t.ld, image, MB, wave_row0, wave_col0, lane, m_valid, n_valid, m_base, n_base, [&](int i) {
+#pragma unroll
+        for (int ii = 0; ii < MB; ++ii)
+          if (ii == i) {
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+              *reinterpret_cast<tile_f32x4*>(image + image_piece<NB * 4>(row, 4 * j + quad)) = acc[ii][j];
+            CLEAVE_KEEP_APART(ii);
+          }
+      });
 }
 
 // ---- single elements -------------------------------------------------------------
@@ -303,52 +364,56 @@ __device__ __forceinline__ float finish_element(const LinearArgs& e, float sum, 
   float t[1] = {sum}, z[1] = {0.0f};
   if (e.grad && e.preact) z[0] = load_element<BF16>(e.preact, row * e.ldz + col);
   const float bias[1] = {e.bias ? e.bias[col] : 0.0f}, scale_b[1] = {e.scale_b ? e.scale_b[col] : 0.0f};
-  const float residual[1] = {e.residual ? load_element<BF16>(e.residual, row * e.ldr + col) : 0.0f};
-  finish<1>(e, t, z, bias, scale_b, e.scale_a ? e.scale_a[row] : 0.0f, residual);
+  if (e.scale_a) finish<true>(e, t, z, bias, scale_b, e.scale_a[row]);
+  else finish<false>(e, t, z, bias, scale_b, 0.0f);
+  if (e.residual) t[0] += load_element<BF16>(e.residual, row * e.ldr + col);
   if (!e.grad && e.preact) store_element<BF16>(e.preact, row * e.ldz + col, z[0]);
   return t[0];
 }
 
 // ---- stores of the general kernel ------------------------------------------------
 
-// store_tile with the epilogue, a block of 32 x 32 sums at a time.
-template <bool BF16, int MB, int NB>
+// Bytes of a wave's image there: half a block of 32 x 32 sums (a whole one would spill at four waves to a SIMD).
+constexpr int kTileImageBytes = 16 * 32 * 4;
+
+// store_tile with the epilogue: half a block is an image; `image` is this wave's, no longer read as operands.
+template <bool BF16, bool INTERIOR, int MB, int NB>
 __device__ __forceinline__ void store_linear_tile_as(const tile_f32x16 (&acc)[MB][NB], const LinearArgs& e, const TileTarget& t,
-                                                     int row0, int col0, int m_valid, int n_valid, int64_t m_base,
-                                                     int64_t n_base) {
+                                                     unsigned char* image, int wave_row0, int wave_col0, int lane, int m_valid,
+                                                     int n_valid, int64_t m_base, int64_t n_base) {
+  const int l32 = lane & 31, lh = lane >> 5;   // lane has column l32 and rows 8 q + 4 lh + r
 #pragma unroll 1
-  for (int b = 0; b < MB * NB; ++b) {
-    tile_f32x16 block{};
+  for (int j = 0; j < NB; ++j) {
+    emit_images<BF16, INTERIOR, false, 16, 32, 1>(
+        e, t.base, t.ld, image, 2 * MB, wave_row0, wave_col0 + 32 * j, lane, m_valid, n_valid, m_base, n_base, [&](int i) {
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+          for (int ii = 0; ii < 2 * MB; ++ii)
 #pragma unroll
-      for (int j = 0; j < NB; ++j)
-        if (b == i * NB + j) block = acc[i][j];
-    const int col = col0 + b % NB * 32;
-    if (col >= n_valid) continue;
-#pragma unroll 1
-    for (int q = 0; q < 4; ++q) {
-      float four[4] = {};
+            for (int jj = 0; jj < NB; ++jj)
+              if (ii == i && jj == j) {
 #pragma unroll
-      for (int p = 0; p < 4; ++p)
-        if (p == q) {
+                for (int q = 0; q < 2; ++q)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) four[r] = block[p * 4 + r];
-        }
-      const int row = row0 + b / NB * 32 + q * 8;
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (row + r < m_valid)
-          store_element<BF16>(t.base, (row + r) * t.ld + col, finish_element<BF16>(e, four[r], m_base + row + r, n_base + col));
-    }
+                  for (int r = 0; r < 4; ++r)
+                    *reinterpret_cast<float*>(image + image_piece<8>(8 * q + 4 * lh + r, l32 / 4) + 4 * (l32 % 4)) =
+                        acc[ii / 2][jj][8 * (ii % 2) + 4 * q + r];
+                CLEAVE_KEEP_APART(ii * NB + jj);
+              }
+        });
   }
 }
 template <int MB, int NB>
 __device__ __forceinline__ void store_linear_tile(const tile_f32x16 (&acc)[MB][NB], const LinearArgs& e, const TileTarget& t,
-                                                  bool bf16, int row0, int col0, int m_valid, int n_valid, int64_t m_base,
-                                                  int64_t n_base) {
-  if (bf16) store_linear_tile_as<true, MB, NB>(acc, e, t, row0, col0, m_valid, n_valid, m_base, n_base);
-  else store_linear_tile_as<false, MB, NB>(acc, e, t, row0, col0, m_valid, n_valid, m_base, n_base);
+                                                  bool bf16, unsigned char* image, int wave_row0, int wave_col0, int lane,
+                                                  int m_valid, int n_valid, int64_t m_base, int64_t n_base, bool interior) {
+  const auto as = [&](auto bf16_tag, auto interior_tag) {
+    store_linear_tile_as<decltype(bf16_tag)::value, decltype(interior_tag)::value, MB, NB>(
+        acc, e, t, image, wave_row0, wave_col0, lane, m_valid, n_valid, m_base, n_base);
+  };
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  if (bf16) interior ? as(yes, yes) : as(yes, no);
+  else interior ? as(no, yes) : as(no, no);
 }
 
 }  // namespace cleave
