@@ -872,8 +872,8 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
         how.tile = cleave::kTileLone;
       if (linear)   // (two tiles serve an epilogue)
         how.tile = how.tile == cleave::kTileLone || how.tile == cleave::kTileQuarter || how.tile == cleave::kTileNarrow
-                       ? cleave::kTileNarrow
-                       : cleave::kTileWide;
+                       ? cleave::kTileLone
+                       : cleave::kTileWide4;
       const hipError_t he = linear ? cleave::launch_linear_general(args, *linear, dtype, c, how, stream)
                                    : cleave::launch_execute(args, dtype, c, how, stream);
       if (he != hipSuccess) return launch_failed(he);
@@ -1139,19 +1139,30 @@ extern "C" int cleave_reduce_grouped(cleave_plan* plan, const float* partials, i
 
 namespace {
 
-// Splits of K for products whose tiles alone leave CUs idle.  The chunks are whole
-// sixteen bytes of the operands (`e` elements) where K is.
+// Splits of K for products whose tiles alone leave CUs idle: a second launch joins them (3 to 4 us with the partial sums'
+// way), so only chains of some length are split.  The chunks are whole sixteen bytes of the operands (`e` elements)
+// where K is.
+//   Few rows, us, 1, 2, 4, 8, 16 splits: one row, bf16, K = 4096, N = 512 11.5, 11.1, 9.3, 8.5, 8.3, 2048 10.9, 10.9, 8.6, 8.6,
+// 9.1, 4096 11.7, 12.3, 9.3, 10.0, 10.6, 5120 12.9, 13.0, 13.2, 13.7, 13.7, 8192 13.2, 15.7, 15.1, 16.6, 16.9, 11008 17.6,
+// 19.8, 19.3, 19.9, 19.8: a CU's own loads are the limit of 64 workgroups, so up to 80 split, to one per CU.
+//   Tiles, us, 1, 2, 4, 8 splits: bf16, 64 x 512 x 11008 32.5, 20.6, 13.6, 14.2, 128 x 768 x 3072 11.8, 10.5, 9.1, 12.2, 300 x 512 x
+// 4096 14.8, 12.7, 10.3, 14.4, 64 x 4096 x 4096 16.8, 15.0, 15.3, 19.7, 500 x 1024 x 4096 15.4, 14.3, 15.3, 19.1, 256 x 4096 x 4096
+// 17.5, 21.7, 21.0, 26.0, 64 x 4096 x 1024 6.7, 9.2, 9.8, 15.2; where two splits make one 128 x 128 item per CU, 64 x 11008 x
+// 4096 29.1, 23.2, 24.7, 29.5, 128 x 11008 x 4096 29.3, 24.9, 27.9, 33.3, 256 x 8192 x 4096 29.3, 28.1, 30.9, 39.2; fp32, whose chains
+// are bound by their products, 64 x 4096 x 4096 72, 43, 28, 32, 167 x 1226 x 4793 84, 53, 51, 56.
 int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e) {
   constexpr int64_t kCUs = 256;
-  int64_t want;
+  int64_t want = 1;
   if (M <= cleave::kFewRows) {
-    const int64_t groups = (N + 16 * e - 1) / (16 * e);
-    want = std::min(3 * kCUs / std::max<int64_t>(groups, 1), K / (32 * e));
+    const int64_t groups = (N + 63) / 64;
+    if (groups <= 80) want = std::min<int64_t>({kCUs / groups, K / (32 * e), 16});
   } else {
     const int64_t parts = ((M + 63) / 64) * ((N + 63) / 64);
-    want = std::min(kCUs / parts, K / 512);
+    const int64_t items = ((M + 127) / 128) * ((N + 127) / 128);
+    if (e == 4) want = std::min<int64_t>({kCUs / parts, K / 256, 4});
+    else if (K >= 3000 && parts <= 48) want = 4;
+    else if (K >= 3000 && (parts <= kCUs / 2 || (items > kCUs / 4 && items <= kCUs / 2))) want = 2;
   }
-  want = std::min<int64_t>(want, 64);
   for (int64_t S = want; S > 1; --S) {
     const int64_t chunk = (K + S - 1) / S;
     if ((S - 1) * chunk < K && (chunk % e == 0 || K % e != 0)) return S;
@@ -1220,11 +1231,12 @@ extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, voi
   int rc = ensure_uploaded(plan);
   if (rc != CLEAVE_OK) return rc;
 
-  // Few rows: every sixteen bytes along K belong to one chunk, and along N to B's row.
+  // Few rows: every sixteen bytes along K belong to one chunk, and every four columns of a K x N operand to its rows.
   const int64_t e = 16 / eb;
   const bool few_rows = M <= cleave::kFewRows && !a->transA && splits >= 1 && (K + splits - 1) / splits % e == 0 && K % e == 0 &&
-                        a->lda % e == 0 && a->ldb % e == 0 && aligned(a->A, 16) && aligned(a->B, 16) &&
-                        (a->transB || N % e == 0);
+                        a->lda % e == 0 && aligned(a->A, 16) &&
+                        (a->transB ? a->ldb % e == 0 && aligned(a->B, 16)
+                                   : N % 4 == 0 && a->ldb % 4 == 0 && aligned(a->B, 4 * static_cast<uintptr_t>(eb)));
   AssembleTarget to;
   to.C = joined ? nullptr : a->C;
   to.ldc = a->ldc;

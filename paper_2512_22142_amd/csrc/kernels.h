@@ -235,7 +235,7 @@ hipError_t launch_linear_general(const ExecuteArgs& args, const LinearArgs& epi,
 // Few rows (at most kFewRows), transA = 0: B is read once, sixteen bytes at a time.  Into args.C through the epilogue
 // or, with splits > 1, into partials[s][row][column] for launch_linear_join.  The caller has checked that
 // every 16 bytes of a row of A, and of B, belong to one chunk (see few_rows_fit in api.cpp).
-constexpr int64_t kFewRows = 64;
+constexpr int64_t kFewRows = 16;
 hipError_t launch_linear_few_rows(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int splits, hipStream_t stream);
 
 // Raises the dynamic-LDS limit of every execute kernel on the current device

@@ -1,20 +1,20 @@
 // Linear products of few rows -- tokens being served -- and the join of a split
 // inner dimension with the epilogue.
 //
-// Few rows: y = x . W with at most 64 rows of x reads W once and does nothing else that counts, so it is
-// bound by memory.  A wave takes 16 E columns (B stored K x N) or 64 (N x K) and a run of k; no LDS stands
-// between the loads and the matrix instructions:
-//   N x K: lane (n, q) of a group of 4 E k's (E elements in 16 bytes) loads the E k's from E q on of column n, and x's
-//     rows likewise: fragments as they are.
-//   K x N: lane (n, q) loads the E columns from E n on of the rows k = E q .. E q + E - 1, each 16 E columns in one
-//     run of 256 bytes.  Its E x E square holds, for each of its columns c, the E k's of a fragment; bf16 are put
-//     together by v_perm, 4 per fragment, and fragment c belongs to the columns E n + c.
-// The waves of a workgroup split its chunk of k and are joined through LDS in wave order; workgroups that split K leave
-// partial sums for the second kernel.
+// Few rows: y = x . W with at most 16 rows of x reads W once and does nothing else that counts, so it is
+// bound by memory.  A workgroup has 64 columns, its waves a run of k each; no LDS stands between the loads and the
+// matrix instructions (E: elements in 16 bytes; a group: 4 E k's):
+//   N x K: lane (n, q) loads the E k's from E q on of column n, and x's rows likewise: fragments as they are.
+//   K x N: lane (n, q) loads the columns 4 n .. 4 n + 3 of the rows k = E q .. E q + E - 1, sixteen lanes the 64
+//     columns of a row in one run.  It holds, for each of its four columns, the E k's of a fragment; bf16 are put
+//     together by v_perm, 4 per fragment, and fragment c belongs to the columns 4 n + c.
+// The waves are joined through LDS in wave order.  Sixteen of them leave the output itself, in one launch; where N has too
+// few columns to go round the CUs, four, whose workgroups split K and leave partial sums for a second kernel.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "fp8_round.h"
 #include "kernels.h"
@@ -26,10 +26,10 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kWaves = 4;
-constexpr int kColumnBlocks = 4;   // of 16 columns, per wave, for B stored N x K
+constexpr int kColumns = 64;   // of a workgroup
 
 template <int DTYPE>
 struct Type;
@@ -63,155 +63,118 @@ __device__ __forceinline__ f32x4 multiply(u32x4 x, u32x4 w, f32x4 acc) {
   }
 }
 
-template <int DTYPE, bool B_K, int RB>
-struct FewRows {
+// Sixteen bytes of a K x N operand's row, or the eight that hold four bf16.
+template <int DTYPE>
+using Columns4 = typename std::conditional<DTYPE == CLEAVE_BF16, u32x2, u32x4>::type;
+
+template <int DTYPE, bool B_K>
+struct Group {   // what a lane holds of a group of k's
   static constexpr int E = Type<DTYPE>::E;
-  static constexpr int KG = 4 * E;                          // k's of a group
-  static constexpr int NC = B_K ? kColumnBlocks : E;        // fragments of columns
-  static constexpr int COLS = 16 * NC;                      // columns of a workgroup
-  static constexpr int EB = 16 / E;                         // bytes per element
-  struct Group {
-    u32x4 x[RB], w[NC];
-  };
+  u32x4 x;
+  std::conditional_t<B_K, u32x4, Columns4<DTYPE>> w[B_K ? 4 : E];
 };
 
-template <int DTYPE, bool B_K, int RB>
-__global__ __launch_bounds__(64 * kWaves, RB > 1 ? 2 : 3) void few_rows_kernel(ExecuteArgs args, LinearArgs epi, int splits) {
-  typedef FewRows<DTYPE, B_K, RB> F;
-  constexpr int E = F::E, KG = F::KG, NC = F::NC, COLS = F::COLS, EB = F::EB;
-  __shared__ float sums[kWaves][16][COLS];
+template <int DTYPE, bool B_K, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, LinearArgs epi, int splits) {
+  constexpr int E = Type<DTYPE>::E, KG = 4 * E, EB = 16 / E;
+  __shared__ float sums[WAVES][kFewRows][kColumns];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, lq = lane >> 4;
   const int64_t M = args.M, N = args.N, K = args.K;
-  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * COLS;
+  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kColumns;
   // this workgroup's chunk of k, this wave's groups of it
   const int64_t chunk = (K + splits - 1) / splits;
   const int64_t k0 = blockIdx.y * chunk, k1 = std::min(k0 + chunk, K);
-  const int64_t groups = (k1 - k0 + KG - 1) / KG, per = (groups + kWaves - 1) / kWaves;
+  const int64_t groups = (k1 - k0 + KG - 1) / KG, per = (groups + WAVES - 1) / WAVES;
   const int64_t g0 = std::min(wave * per, groups), g1 = std::min(g0 + per, groups);
 
-  const unsigned char* const A = static_cast<const unsigned char*>(args.A);
-  const unsigned char* const B = static_cast<const unsigned char*>(args.B);
   // rows and columns that are not there repeat the last one: their sums are not stored
-  const unsigned char* xp[RB];
-#pragma unroll
-  for (int r = 0; r < RB; ++r) xp[r] = A + (std::min<int64_t>(16 * r + l16, M - 1) * args.lda + E * lq) * EB;
-  const unsigned char* wp[B_K ? NC : 1];
+  const unsigned char* const B = static_cast<const unsigned char*>(args.B);
+  const unsigned char* const xp =
+      static_cast<const unsigned char*>(args.A) + (std::min<int64_t>(l16, M - 1) * args.lda + E * lq) * EB;
+  const unsigned char* wp[B_K ? 4 : 1];
   if constexpr (B_K) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) wp[c] = B + (std::min<int64_t>(n0 + 16 * c + l16, N - 1) * args.ldb + E * lq) * EB;
+    for (int c = 0; c < 4; ++c) wp[c] = B + (std::min<int64_t>(n0 + 16 * c + l16, N - 1) * args.ldb + E * lq) * EB;
   } else {
-    wp[0] = B + std::min<int64_t>(n0 + E * l16, N - E) * EB;
+    wp[0] = B + std::min<int64_t>(n0 + 4 * l16, N - 4) * EB;
   }
-  const auto load = [&](int64_t g, typename F::Group& to) {
+  typedef Group<DTYPE, B_K> G;
+  const auto load = [&](int64_t g, G& to) {
     const int64_t k = k0 + g * KG;          // wave-uniform
     const bool valid = k + E * lq < k1;     // all E of them: chunks and rows are whole sixteen bytes
-#pragma unroll
-    for (int r = 0; r < RB; ++r)
-      to.x[r] = valid ? *reinterpret_cast<const u32x4*>(xp[r] + k * EB) : u32x4{};
+    to.x = valid ? *reinterpret_cast<const u32x4*>(xp + k * EB) : u32x4{};
     if constexpr (B_K) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) to.w[c] = valid ? *reinterpret_cast<const u32x4*>(wp[c] + k * EB) : u32x4{};
+      for (int c = 0; c < 4; ++c) to.w[c] = valid ? *reinterpret_cast<const u32x4*>(wp[c] + k * EB) : u32x4{};
     } else {
 #pragma unroll
-      for (int i = 0; i < E; ++i)
-        to.w[i] = valid ? *reinterpret_cast<const u32x4*>(wp[0] + (k + E * lq + i) * args.ldb * EB) : u32x4{};
-    }
-  };
-
-  f32x4 acc[RB][NC];
-#pragma unroll
-  for (int r = 0; r < RB; ++r)
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[r][c] = f32x4{};
-  const auto compute = [&](const typename F::Group& g) {
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      u32x4 w = g.w[B_K ? c : 0];
-      if constexpr (!B_K) {
-        if constexpr (DTYPE == CLEAVE_BF16) {
-          // column c of the square: the low or high half of word c / 2 of the rows 2p and 2p + 1
-#pragma unroll
-          for (int p = 0; p < 4; ++p)
-            w[p] = __builtin_amdgcn_perm(g.w[2 * p + 1][c / 2], g.w[2 * p][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
-        } else {
-#pragma unroll
-          for (int p = 0; p < 4; ++p) w[p] = g.w[p][c];
-        }
+      for (int i = 0; i < E; ++i) {
+        typedef Columns4<DTYPE> C;
+        to.w[i] = valid ? *reinterpret_cast<const C*>(wp[0] + (k + E * lq + i) * args.ldb * EB) : C{};
       }
-#pragma unroll
-      for (int r = 0; r < RB; ++r) acc[r][c] = multiply<DTYPE>(g.x[r], w, acc[r][c]);
-      if constexpr (!B_K && RB > 1) __builtin_amdgcn_sched_barrier(0);   // (all fragments at once would spill)
     }
   };
-  if constexpr (!B_K && RB > 1 && DTYPE == CLEAVE_BF16) {
-    // (registers for one group: the other waves' loads cover this one's wait)
-    typename F::Group a;
-#pragma unroll 1
-    for (int64_t g = g0; g < g1; ++g) {
-      load(g, a);
-      compute(a);
-    }
-  } else if (g0 < g1) {   // the next group is on its way while one is multiplied
-    typename F::Group a, b;
-    load(g0, a);
-    int64_t g = g0;
-    for (; g + 2 < g1; g += 2) {
-      load(g + 1, b);
-      compute(a);
-      load(g + 2, a);
-      compute(b);
-    }
-    if (g + 1 < g1) {
-      load(g + 1, b);
-      compute(a);
-      compute(b);
-    } else {
-      compute(a);
-    }
-  }
-
-  // Lane (l16, lq) has rows 4 lq + j of columns E l16 + c (K x N) or 16 c + l16 (N x K).
+  f32x4 acc[4] = {};
+  const auto compute = [&](const G& g) {
 #pragma unroll
-  for (int r = 0; r < RB; ++r) {
-    if (16 * r >= M) break;
-    if (r > 0) __syncthreads();
+    for (int c = 0; c < 4; ++c) {
+      u32x4 w;
+      if constexpr (B_K) {
+        w = g.w[c];
+      } else if constexpr (DTYPE == CLEAVE_BF16) {
+        // column c: the low or high half of word c / 2 of the rows 2p and 2p + 1
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sums[wave][4 * lq + j][B_K ? 16 * c + l16 : E * l16 + c] = acc[r][c][j];
-    __syncthreads();
-    const int rows = static_cast<int>(std::min<int64_t>(16, M - 16 * r));
-    for (int at = threadIdx.x; at < rows * COLS; at += 64 * kWaves) {
-      const int row = at / COLS, col = at % COLS;
-      if (n0 + col >= N) continue;
-      float sum = sums[0][row][col];
-#pragma unroll
-      for (int w = 1; w < kWaves; ++w) sum += sums[w][row][col];
-      const int64_t m = 16 * r + row, n = n0 + col;
-      if (splits > 1) {
-        args.partials[(blockIdx.y * M + m) * N + n] = sum;
-      } else if (args.c_bf16) {
-        store_element<true>(args.C, m * args.ldc + n, finish_element<true>(epi, sum, m, n));
+        for (int p = 0; p < 4; ++p)
+          w[p] = __builtin_amdgcn_perm(g.w[2 * p + 1][c / 2], g.w[2 * p][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
       } else {
-        store_element<false>(args.C, m * args.ldc + n, finish_element<false>(epi, sum, m, n));
+#pragma unroll
+        for (int p = 0; p < 4; ++p) w[p] = g.w[p][c];
       }
+      acc[c] = multiply<DTYPE>(g.x, w, acc[c]);
     }
+  };
+  // the next groups are on their way while one is multiplied
+  G set[3];
+  int64_t g = g0;
+  if (g < g1) load(g, set[0]);
+  if (g + 1 < g1) load(g + 1, set[1]);
+  while (g < g1) {
+#pragma unroll
+    for (int s = 0; s < 3; ++s) {
+      if (g >= g1) break;
+      if (g + 2 < g1) load(g + 2, set[(s + 2) % 3]);
+      compute(set[s]);
+      ++g;
+    }
+  }
+
+  // Lane (l16, lq) has rows 4 lq + j of columns 4 l16 + c (K x N) or 16 c + l16 (N x K).
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (4 * lq + j < M) sums[wave][4 * lq + j][B_K ? 16 * c + l16 : 4 * l16 + c] = acc[c][j];
+  __syncthreads();
+  for (int at = threadIdx.x; at < static_cast<int>(M) * kColumns; at += 64 * WAVES) {
+    const int row = at / kColumns, col = at % kColumns;
+    const int64_t n = n0 + col;
+    if (n >= N) continue;
+    float sum = sums[0][row][col];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += sums[w][row][col];
+    if (splits > 1) args.partials[(blockIdx.y * M + row) * N + n] = sum;
+    else if (args.c_bf16) store_element<true>(args.C, row * args.ldc + n, finish_element<true>(epi, sum, row, n));
+    else store_element<false>(args.C, row * args.ldc + n, finish_element<false>(epi, sum, row, n));
   }
 }
 
-template <int DTYPE, bool B_K, int RB>
-hipError_t launch_rows(const ExecuteArgs& args, const LinearArgs& epi, int splits, hipStream_t stream) {
-  constexpr int COLS = FewRows<DTYPE, B_K, RB>::COLS;
-  hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, RB>), dim3(static_cast<uint32_t>((args.N + COLS - 1) / COLS), splits),
-                     dim3(64 * kWaves), 0, stream, args, epi, splits);
-  return hipGetLastError();
-}
 template <int DTYPE, bool B_K>
 hipError_t launch_layout(const ExecuteArgs& args, const LinearArgs& epi, int splits, hipStream_t stream) {
-  if (args.M <= 16) return launch_rows<DTYPE, B_K, 1>(args, epi, splits, stream);
-  if (args.M <= 32) return launch_rows<DTYPE, B_K, 2>(args, epi, splits, stream);
-  return launch_rows<DTYPE, B_K, 4>(args, epi, splits, stream);
+  const dim3 g(static_cast<uint32_t>((args.N + kColumns - 1) / kColumns), splits);
+  if (splits > 1) hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 4>), g, dim3(256), 0, stream, args, epi, splits);
+  else hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 16>), g, dim3(1024), 0, stream, args, epi, splits);
+  return hipGetLastError();
 }
 
 // ---- join ------------------------------------------------------------------------

@@ -57,7 +57,7 @@ def check(M, N, K, dtype=BF16, out=None, transA=0, transB=0, act="none", grad=Fa
     # sums of K products in fp32: 8 * 2^-24 |a| |b| (an eleven-sigma bound of a random walk), exact products
     s, t = (f64(sa), f64(sb)) if dtype == E4M3 else (np.ones(M), np.ones(N))
     err = 8 * U32 * np.outer(np.linalg.norm(opA, axis=1) * s, np.linalg.norm(opB, axis=0) * t)
-    if dtype == E4M3 and out == BF16 and M > 64:
+    if dtype == E4M3 and out == BF16 and M > 16:
         # the 8-bit instruction drops what lies below 2^-13 of the largest product of a group: up to that per product, of
         # either sign (uniform: standard deviation 2^-13 / sqrt(3)), six sigma
         most = np.outer(np.abs(opA).max(axis=1) * s, np.abs(opB).max(axis=0) * t)
@@ -97,7 +97,7 @@ EPILOGUES = [dict(), dict(bias=True, act="gelu_tanh", preact=True), dict(bias=Tr
              dict(act="relu", residual=True, preact=True), dict(grad=True, act="gelu_tanh"), dict(grad=True, act="silu", residual=True),
              dict(grad=True, act="relu")]
 FEW = [(1, 128, 256), (1, 1408, 64), (1, 8, 8), (3, 136, 72), (16, 256, 512), (17, 264, 520), (33, 128, 1000), (64, 512, 4096),
-       (2, 4096, 4096), (40, 96, 2048)]
+       (2, 4096, 4096), (40, 96, 2048), (1, 3076, 1024), (15, 11008, 160), (7, 3136, 40), (9, 100, 2056)]
 MANY = [(65, 128, 64), (128, 256, 64), (130, 264, 96), (256, 256, 256), (300, 520, 200), (513, 256, 64), (1000, 768, 1024),
         (2048, 512, 128), (1100, 4096, 512)]
 ODD = [(1, 1, 1), (5, 7, 3), (37, 53, 71), (1, 333, 1001), (200, 1, 50), (100, 100, 100), (129, 257, 65), (300, 77, 1000)]
@@ -172,9 +172,10 @@ def test_residual_in_place(size):
 
 def test_which_kernel():
     assert check(1, 128, 256)[2] == "linear_few_rows"
-    assert check(64, 128, 256, transB=1)[2] == "linear_few_rows"
-    assert check(64, 128, 256, dtype=F32)[2] == "linear_few_rows"
-    assert check(64, 131, 256, dtype=E4M3)[2] == "linear_few_rows"
+    assert check(16, 4096, 256, transB=1)[2] == "linear_few_rows"
+    assert check(16, 132, 256, dtype=F32)[2] == "linear_few_rows"
+    assert check(16, 131, 256, dtype=E4M3)[2] == "linear_few_rows"
+    assert "direct" in check(17, 128, 256, bias=True)[2]
     assert "direct" in check(512, 512, 512, bias=True)[2]
     assert "direct" in check(512, 512, 512, dtype=E4M3)[2]
     assert "direct" in check(512, 511, 512, transB=1, bias=True)[2]
