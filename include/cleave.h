@@ -423,7 +423,7 @@ int cleave_verify_grouped(cleave_plan* plan, int64_t n_members,
  * per row, from the unrounded h.  x, residual (or NULL), sum_out (h, or NULL): dtype
  * F32 or BF16; weight: cols floats; inv_rms: rows floats (i), or NULL.
  * y_dtype = dtype: scales must be NULL.  y_dtype = CLEAVE_E4M3: row t of y holds
- * h i w / s rounded to nearest even, with scales[t] = s = max|h i w| / 448 (a row whose
+ * h i w / s rounded to nearest even, with scales[t] = s = max|h i w| (1/448) (a row whose
  * largest magnitude is below 2^-100 is stored as zeros with s = 0; one that holds a NaN or
  * an infinity as NaN with s NaN).  sum_out may be x or residual, y too.
  * CLEAVE_EINVAL: negative rows, no column, a size above 2^31-1, NULL or misaligned
@@ -503,7 +503,7 @@ int cleave_linear(cleave_plan* plan, const cleave_linear_args* args, void* hip_s
  * States, updated in place: with m_scale and v_scale NULL, m and v are fp32.
  * Otherwise m[k] and v[k] are e4m3 values of m and of sqrt(v), and m_scale[k], v_scale[k] hold
  * one fp32 scale for every 256 consecutive elements of the tensor (the last one for what
- * is left): state = value * scale, scale = largest finite magnitude of the 256 / 448, rounded to
+ * is left): state = value * scale, scale = largest finite magnitude of the 256 times 1/448, rounded to
  * nearest even; what is above zero in sqrt(v) becomes at least 2^-9 of the scale; values that are
  * not finite become NaN; a block below 2^-100 is zeros with scale 0.  All zeros with scales 0
  * are the states of step 1.

@@ -28,84 +28,66 @@ constexpr int kWaves = kThreads / 64;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// A lane's four elements of a block of 256: neighbours (VEC), or 64 apart.
-template <bool VEC>
-__device__ __forceinline__ uint32_t place(int lane, int e) {
-  return VEC ? 4 * lane + e : lane + 64 * e;
-}
+// A lane's four neighbouring elements of a block, at any alignment; `left`: how many there are.  What is not there reads as zero
+// and is not written.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
 
-template <bool VEC>
-__device__ __forceinline__ f32x4 load_f32(const float* p, int lane, uint32_t n) {
-  if constexpr (VEC) {
-    if (4 * lane + 4u <= n) return *reinterpret_cast<const f32x4*>(p + 4 * lane);
+__device__ __forceinline__ f32x4 load_four(const float* p, int left) {
+  if (left >= 4) return *reinterpret_cast<const f32x4_any*>(p);
+  f32x4 x{};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < left) x[e] = p[e];
+  return x;
+}
+__device__ __forceinline__ f32x4 load_four(const uint16_t* p, int left) {
+  if (left >= 4) {
+    const u32x2 b = *reinterpret_cast<const u32x2_any*>(p);
+    return f32x4{__builtin_bit_cast(float, b[0] << 16), __builtin_bit_cast(float, b[0] & 0xffff0000u),
+                 __builtin_bit_cast(float, b[1] << 16), __builtin_bit_cast(float, b[1] & 0xffff0000u)};
   }
   f32x4 x{};
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (place<VEC>(lane, e) < n) x[e] = p[place<VEC>(lane, e)];
+    if (e < left) x[e] = __builtin_bit_cast(float, static_cast<uint32_t>(p[e]) << 16);
   return x;
 }
-template <bool VEC>
-__device__ __forceinline__ f32x4 load_bf16(const uint16_t* p, int lane, uint32_t n) {
-  if constexpr (VEC) {
-    if (4 * lane + 4u <= n) {
-      const u32x2 b = *reinterpret_cast<const u32x2*>(p + 4 * lane);
-      return f32x4{__builtin_bit_cast(float, b[0] << 16), __builtin_bit_cast(float, b[0] & 0xffff0000u),
-                   __builtin_bit_cast(float, b[1] << 16), __builtin_bit_cast(float, b[1] & 0xffff0000u)};
-    }
-  }
-  f32x4 x{};
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (place<VEC>(lane, e) < n) x[e] = __builtin_bit_cast(float, static_cast<uint32_t>(p[place<VEC>(lane, e)]) << 16);
-  return x;
-}
-template <bool VEC>
-__device__ __forceinline__ uint32_t load_bytes(const uint8_t* p, int lane, uint32_t n) {
-  if constexpr (VEC) {
-    if (4 * lane + 4u <= n) return *reinterpret_cast<const uint32_t*>(p + 4 * lane);
-  }
+__device__ __forceinline__ uint32_t load_four(const uint8_t* p, int left) {
+  if (left >= 4) return *reinterpret_cast<const u32_any*>(p);
   uint32_t x = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (place<VEC>(lane, e) < n) x |= static_cast<uint32_t>(p[place<VEC>(lane, e)]) << (8 * e);
+    if (e < left) x |= static_cast<uint32_t>(p[e]) << (8 * e);
   return x;
 }
-template <bool VEC>
-__device__ __forceinline__ void store_f32(float* p, f32x4 x, int lane, uint32_t n) {
-  if constexpr (VEC) {
-    if (4 * lane + 4u <= n) {
-      *reinterpret_cast<f32x4*>(p + 4 * lane) = x;
-      return;
-    }
+__device__ __forceinline__ void store_four(float* p, f32x4 x, int left) {
+  if (left >= 4) {
+    *reinterpret_cast<f32x4_any*>(p) = x;
+    return;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (place<VEC>(lane, e) < n) p[place<VEC>(lane, e)] = x[e];
+    if (e < left) p[e] = x[e];
 }
-template <bool VEC>
-__device__ __forceinline__ void store_bf16(uint16_t* p, f32x4 x, int lane, uint32_t n) {
-  if constexpr (VEC) {
-    if (4 * lane + 4u <= n) {
-      *reinterpret_cast<u32x2*>(p + 4 * lane) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-      return;
-    }
+__device__ __forceinline__ void store_four(uint16_t* p, f32x4 x, int left) {
+  if (left >= 4) {
+    *reinterpret_cast<u32x2_any*>(p) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    return;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (place<VEC>(lane, e) < n) p[place<VEC>(lane, e)] = to_bf16_bits(x[e]);
+    if (e < left) p[e] = to_bf16_bits(x[e]);
 }
-template <bool VEC>
-__device__ __forceinline__ void store_bytes(uint8_t* p, uint32_t x, int lane, uint32_t n) {
-  if constexpr (VEC) {
-    if (4 * lane + 4u <= n) {
-      *reinterpret_cast<uint32_t*>(p + 4 * lane) = x;
-      return;
-    }
+__device__ __forceinline__ void store_four(uint8_t* p, uint32_t x, int left) {
+  if (left >= 4) {
+    *reinterpret_cast<u32_any*>(p) = x;
+    return;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (place<VEC>(lane, e) < n) p[place<VEC>(lane, e)] = static_cast<uint8_t>(x >> (8 * e));
+    if (e < left) p[e] = static_cast<uint8_t>(x >> (8 * e));
 }
 
 __device__ __forceinline__ f32x4 decode(uint32_t q, float scale) {
@@ -144,32 +126,31 @@ struct Block {
   f32x4 w, g, m, v;
 };
 
-template <bool VEC, bool GRAD_BF16, bool STATES_8>
+template <bool GRAD_BF16, bool STATES_8>
 struct Update {
   const AdamTensor& t;
   const AdamWArgs& args;
   float clip;
 
-  __device__ __forceinline__ uint64_t elements() const { return (static_cast<uint64_t>(t.n_high) << 32) | t.n_low; }
-
-  __device__ __forceinline__ Block load(uint64_t at, int lane, uint32_t n) const {
+  // This lane's elements of the block that starts at element `first`: from `at` on, `left` of them there.
+  __device__ __forceinline__ Block load(uint64_t first, uint64_t at, int left) const {
     Block b;
-    b.w = load_f32<VEC>(t.w + at, lane, n);
-    if constexpr (GRAD_BF16) b.g = load_bf16<VEC>(static_cast<const uint16_t*>(t.g) + at, lane, n);
-    else b.g = load_f32<VEC>(static_cast<const float*>(t.g) + at, lane, n);
+    b.w = load_four(t.w + at, left);
+    if constexpr (GRAD_BF16) b.g = load_four(static_cast<const uint16_t*>(t.g) + at, left);
+    else b.g = load_four(static_cast<const float*>(t.g) + at, left);
     if constexpr (STATES_8) {
-      const uint32_t qm = load_bytes<VEC>(static_cast<const uint8_t*>(t.m) + at, lane, n);
-      const uint32_t qv = load_bytes<VEC>(static_cast<const uint8_t*>(t.v) + at, lane, n);
-      b.m = decode(qm, t.m_scale[at / kStateBlock]);
-      b.v = decode(qv, t.v_scale[at / kStateBlock]);
+      const uint32_t qm = load_four(static_cast<const uint8_t*>(t.m) + at, left);
+      const uint32_t qv = load_four(static_cast<const uint8_t*>(t.v) + at, left);
+      b.m = decode(qm, t.m_scale[first / kStateBlock]);
+      b.v = decode(qv, t.v_scale[first / kStateBlock]);
     } else {
-      b.m = load_f32<VEC>(static_cast<const float*>(t.m) + at, lane, n);
-      b.v = load_f32<VEC>(static_cast<const float*>(t.v) + at, lane, n);
+      b.m = load_four(static_cast<const float*>(t.m) + at, left);
+      b.v = load_four(static_cast<const float*>(t.v) + at, left);
     }
     return b;
   }
 
-  __device__ __forceinline__ void step(Block b, uint64_t at, int lane, uint32_t n) const {
+  __device__ __forceinline__ void step(Block b, uint64_t first, uint64_t at, int left, int lane) const {
 #pragma clang fp contract(off)
     f32x4 w1, m1, v1;
 #pragma unroll
@@ -181,31 +162,34 @@ struct Update {
       const float root = __builtin_sqrtf(v1[e] * args.inv_bias2) + args.eps;
       w1[e] = b.w[e] - args.lr * ((m1[e] * args.inv_bias1) / root + args.weight_decay * b.w[e]);
     }
-    store_f32<VEC>(t.w + at, w1, lane, n);
-    if (t.copy) store_bf16<VEC>(t.copy + at, w1, lane, n);
+    store_four(t.w + at, w1, left);
+    if (t.copy) store_four(t.copy + at, w1, left);
     if constexpr (STATES_8) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v1[e] = __builtin_sqrtf(v1[e]);
+      for (int e = 0; e < 4; ++e) {
+        v1[e] = __builtin_sqrtf(v1[e]);
+        if (e >= left) m1[e] = v1[e] = 0.0f;   // (0 times a scale of the gradients that is not finite)
+      }
       const BlockScale sm = block_scale(largest(m1)), sv = block_scale(largest(v1));
-      store_bytes<VEC>(static_cast<uint8_t*>(t.m) + at, encode<false>(m1, sm.inverse), lane, n);
-      store_bytes<VEC>(static_cast<uint8_t*>(t.v) + at, encode<true>(v1, sv.inverse), lane, n);
+      store_four(static_cast<uint8_t*>(t.m) + at, encode<false>(m1, sm.inverse), left);
+      store_four(static_cast<uint8_t*>(t.v) + at, encode<true>(v1, sv.inverse), left);
       if (lane == 0) {
-        t.m_scale[at / kStateBlock] = sm.scale;
-        t.v_scale[at / kStateBlock] = sv.scale;
+        t.m_scale[first / kStateBlock] = sm.scale;
+        t.v_scale[first / kStateBlock] = sv.scale;
       }
     } else {
-      store_f32<VEC>(static_cast<float*>(t.m) + at, m1, lane, n);
-      store_f32<VEC>(static_cast<float*>(t.v) + at, v1, lane, n);
+      store_four(static_cast<float*>(t.m) + at, m1, left);
+      store_four(static_cast<float*>(t.v) + at, v1, left);
     }
   }
 
   // Wave `wave` of the workgroup takes every kWaves-th block of 256 of the chunk.
-  __device__ __forceinline__ void chunk(uint64_t first, int wave, int lane) const {
-    const uint64_t n = elements();
-    const uint64_t end = first + kAdamChunk < n ? first + kAdamChunk : n;
-    for (uint64_t at = first + wave * kStateBlock; at < end; at += kWaves * kStateBlock) {
-      const uint32_t left = end - at < kStateBlock ? static_cast<uint32_t>(end - at) : kStateBlock;
-      step(load(at, lane, left), at, lane, left);
+  __device__ __forceinline__ void chunk(uint64_t start, int wave, int lane) const {
+    const uint64_t end = start + kAdamChunk < t.n ? start + kAdamChunk : t.n;
+    for (uint64_t first = start + wave * kStateBlock; first < end; first += kWaves * kStateBlock) {
+      const uint64_t at = first + 4 * lane;
+      const int left = at < end ? static_cast<int>(end - at < 4 ? end - at : 4) : 0;
+      step(load(first, at, left), first, at, left, lane);
     }
   }
 };
@@ -221,8 +205,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamWArgs args) {
   const uint32_t chunk0 = k > 0 ? args.chunk_end[k - 1] : 0;
   const uint64_t first = static_cast<uint64_t>(blockIdx.x - chunk0) * kAdamChunk;
   const float clip = args.grad_scale ? *args.grad_scale : 1.0f;
-  if (t.vec) Update<true, GRAD_BF16, STATES_8>{t, args, clip}.chunk(first, wave, lane);
-  else Update<false, GRAD_BF16, STATES_8>{t, args, clip}.chunk(first, wave, lane);
+  Update<GRAD_BF16, STATES_8>{t, args, clip}.chunk(first, wave, lane);
 }
 
 }  // namespace

@@ -1165,7 +1165,8 @@ int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e) {
   }
   for (int64_t S = want; S > 1; --S) {
     const int64_t chunk = (K + S - 1) / S;
-    if ((S - 1) * chunk < K && (chunk % e == 0 || K % e != 0)) return S;
+    // (what general tiles take at any length anyway is split at any)
+    if ((S - 1) * chunk < K && (chunk % e == 0 || K % e != 0 || (e == 4 && M > cleave::kFewRows))) return S;
   }
   return 1;
 }

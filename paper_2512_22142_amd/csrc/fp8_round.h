@@ -37,14 +37,14 @@ __device__ __forceinline__ auto bf16_of_e4m3(uint32_t lo, uint32_t hi) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// 448 / (the largest magnitude) as the scale's reciprocal; both zero below kLeastScaled.
-// NaN stays NaN.
+// The scale of values of which `most` is the largest magnitude, most * (1 / 448), and its reciprocal; both zero
+// below kLeastScaled.  NaN stays NaN.
 struct BlockScale {
   float scale, inverse;
 };
 __device__ __forceinline__ BlockScale block_scale(float most) {
   if (most < kLeastScaled) return {0.0f, 0.0f};
-  const float scale = most / kE4M3Max;
+  const float scale = most * (1.0f / kE4M3Max);
   return {scale, 1.0f / scale};
 }
 

@@ -24,19 +24,7 @@ namespace cleave {
 
 namespace {
 
-// e4m3 values of VEC elements, one scale.
-template <int VEC>
-__device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&y)[VEC]) {
-  if constexpr (VEC == 1) {
-    *p = static_cast<uint8_t>(pack_e4m3(y[0], y[0]));
-  } else {
-#pragma unroll
-    for (int q = 0; q < VEC / 4; ++q)
-      reinterpret_cast<uint32_t*>(p)[q] = pack_e4m3(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
-  }
-}
-
-// A row per group of NT threads, which holds up to NT * V * VEC elements of it; a wave (NT = 64)
+// A row per group of NT threads, which holds up to NT * V * N elements of it (N in sixteen bytes); a wave (NT = 64)
 // has its row to itself, four rows to a workgroup.
 template <int NT>
 struct RowGroup {
@@ -45,9 +33,10 @@ struct RowGroup {
   static constexpr int kWaves = NT / 64;
 };
 
-template <typename T, int VEC, int NT, int V, bool E4M3>
+template <typename T, int NT, int V, bool E4M3>
 __global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_kernel(NormArgs args) {
-  constexpr int NW = RowGroup<NT>::kWaves;
+  typedef Group16<T> G;
+  constexpr int NW = RowGroup<NT>::kWaves, N = G::N;
   __shared__ float slots[2][NW];
   const int t = threadIdx.x % NT;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * RowGroup<NT>::kRows + threadIdx.x / NT;
@@ -56,80 +45,79 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_kernel(NormAr
   const T* r = static_cast<const T*>(args.residual) + (args.residual ? row * args.ldr : 0);
   T* sum_out = static_cast<T*>(args.sum_out) + (args.sum_out ? row * args.lds : 0);
   const int cols = static_cast<int>(args.cols);
+  const auto at = [&](int j) { return (j * NT + t) * N; };
 
-  float h[V][VEC], w[V][VEC];
+  Raw16 x_raw[V], r_raw[V];
+  Floats16<N> w_raw[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int c = (j * NT + t) * VEC;
-    if (c < cols) load_elements<VEC>(x + c, h[j]);
-    else
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) h[j][e] = 0.0f;
+    x_raw[j] = G::read(x + at(j), cols - at(j));
+    if (args.residual) r_raw[j] = G::read(r + at(j), cols - at(j));
   }
+#pragma unroll
+  for (int j = 0; j < V; ++j) w_raw[j].read(args.weight + at(j), cols - at(j));
+  float h[V][N], w[V][N];
+#pragma unroll
+  for (int j = 0; j < V; ++j) G::unpack(x_raw[j], h[j]);
   if (args.residual) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int c = (j * NT + t) * VEC;
-      float add[VEC] = {};
-      if (c < cols) load_elements<VEC>(r + c, add);
+      float add[N];
+      G::unpack(r_raw[j], add);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) h[j][e] += add[e];
+      for (int e = 0; e < N; ++e) h[j][e] += add[e];
     }
-  }
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int c = (j * NT + t) * VEC;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) w[j][e] = 0.0f;
-    if (c < cols) load_elements<VEC>(args.weight + c, w[j]);
   }
   float squares = 0.0f;
 #pragma unroll
   for (int j = 0; j < V; ++j)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) squares += h[j][e] * h[j][e];
+    for (int e = 0; e < N; ++e) squares += h[j][e] * h[j][e];
   if (args.sum_out) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (j * NT + t) * VEC;
-      if (c < cols) store_elements<VEC>(sum_out + c, h[j]);
-    }
+    for (int j = 0; j < V; ++j) G::store(sum_out + at(j), cols - at(j), h[j]);
   }
   squares = group_sum<NW>(squares, slots[0]);
   const float inv = 1.0f / __builtin_sqrtf(squares / static_cast<float>(cols) + args.eps);
   if (args.inv_rms && t == 0) args.inv_rms[row] = inv;
 #pragma unroll
+  for (int j = 0; j < V; ++j) w_raw[j].unpack(w[j]);
+#pragma unroll
   for (int j = 0; j < V; ++j)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) h[j][e] = h[j][e] * inv * w[j][e];
+    for (int e = 0; e < N; ++e) h[j][e] = h[j][e] * inv * w[j][e];
   if constexpr (E4M3) {
     float most = 0.0f;
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) most = nan_max(most, __builtin_fabsf(h[j][e]));
+      for (int e = 0; e < N; ++e)
+        if (at(j) + e < cols) most = nan_max(most, __builtin_fabsf(h[j][e]));   // (inv may be infinite)
     const BlockScale s = block_scale(group_nan_max<NW>(most, slots[1]));
     if (t == 0) args.scales[row] = s.scale;
     uint8_t* y = static_cast<uint8_t*>(args.y) + row * args.ldy;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int c = (j * NT + t) * VEC;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) h[j][e] *= s.inverse;
-      if (c < cols) store_e4m3<VEC>(y + c, h[j]);
+      for (int e = 0; e < N; ++e) h[j][e] *= s.inverse;
+      store_e4m3<N>(y + at(j), cols - at(j), h[j]);
     }
   } else {
     T* y = static_cast<T*>(args.y) + row * args.ldy;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (j * NT + t) * VEC;
-      if (c < cols) store_elements<VEC>(y + c, h[j]);
-    }
+    for (int j = 0; j < V; ++j) G::store(y + at(j), cols - at(j), h[j]);
   }
 }
 
 // Rows that no group's registers hold: read again for each use (from the caches).
 constexpr int kLongThreads = 1024;
+__device__ __forceinline__ float element(const float* p) { return *p; }
+__device__ __forceinline__ float element(const Bf16* p) {
+  return __builtin_bit_cast(float, static_cast<uint32_t>(p->bits) << 16);
+}
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(Bf16* p, float x) { p->bits = to_bf16_bits(x); }
+
 template <typename T, bool E4M3>
 __global__ __launch_bounds__(kLongThreads) void rms_norm_long_kernel(NormArgs args) {
   constexpr int NW = kLongThreads / 64;
@@ -137,16 +125,7 @@ __global__ __launch_bounds__(kLongThreads) void rms_norm_long_kernel(NormArgs ar
   const int64_t row = blockIdx.x;
   const T* x = static_cast<const T*>(args.x) + row * args.ldx;
   const T* r = static_cast<const T*>(args.residual) + (args.residual ? row * args.ldr : 0);
-  const auto at = [&](int64_t c) {
-    float h[1];
-    load_elements<1>(x + c, h);
-    if (args.residual) {
-      float add[1];
-      load_elements<1>(r + c, add);
-      h[0] += add[0];
-    }
-    return h[0];
-  };
+  const auto at = [&](int64_t c) { return args.residual ? element(x + c) + element(r + c) : element(x + c); };
   float squares = 0.0f;
   for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
     const float h = at(c);
@@ -165,44 +144,34 @@ __global__ __launch_bounds__(kLongThreads) void rms_norm_long_kernel(NormArgs ar
   }
   // (an element is read, then written, by one thread: y or the sum may take x's or r's place)
   for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
-    const float h[1] = {at(c)};
-    float y[1] = {h[0] * inv * args.weight[c]};
-    if (args.sum_out) store_elements<1>(static_cast<T*>(args.sum_out) + row * args.lds + c, h);
-    if constexpr (E4M3) {
-      y[0] *= s.inverse;
-      store_e4m3<1>(static_cast<uint8_t*>(args.y) + row * args.ldy + c, y);
-    } else {
-      store_elements<1>(static_cast<T*>(args.y) + row * args.ldy + c, y);
-    }
+    const float h = at(c), y = h * inv * args.weight[c];
+    if (args.sum_out) put(static_cast<T*>(args.sum_out) + row * args.lds + c, h);
+    if constexpr (E4M3)
+      static_cast<uint8_t*>(args.y)[row * args.ldy + c] = static_cast<uint8_t>(pack_e4m3(y * s.inverse, 0.0f));
+    else
+      put(static_cast<T*>(args.y) + row * args.ldy + c, y);
   }
 }
 
-template <typename T, int VEC, int NT, int V>
+template <typename T, int NT, int V>
 hipError_t launch_norm(const NormArgs& args, hipStream_t stream) {
   constexpr int kRows = RowGroup<NT>::kRows;
   const dim3 g(static_cast<uint32_t>((args.rows + kRows - 1) / kRows)), b(RowGroup<NT>::kThreads);
-  if (args.scales) hipLaunchKernelGGL((rms_norm_kernel<T, VEC, NT, V, true>), g, b, 0, stream, args);
-  else hipLaunchKernelGGL((rms_norm_kernel<T, VEC, NT, V, false>), g, b, 0, stream, args);
+  if (args.scales) hipLaunchKernelGGL((rms_norm_kernel<T, NT, V, true>), g, b, 0, stream, args);
+  else hipLaunchKernelGGL((rms_norm_kernel<T, NT, V, false>), g, b, 0, stream, args);
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch_norm_of(const NormArgs& args, bool vec, hipStream_t stream) {
-  constexpr int E = Vec16<T>::N;
+hipError_t launch_norm_of(const NormArgs& args, hipStream_t stream) {
+  constexpr int N = Group16<T>::N;
   const int64_t n = args.cols;
-  if (vec) {
-    if (n <= 64 * E) return launch_norm<T, E, 64, 1>(args, stream);
-    if (n <= 256 * E) return launch_norm<T, E, 256, 1>(args, stream);
-    if (n <= 512 * E) return launch_norm<T, E, 256, 2>(args, stream);
-    if (n <= 1024 * E) return launch_norm<T, E, 512, 2>(args, stream);
-    if (n <= 2048 * E) return launch_norm<T, E, 1024, 2>(args, stream);
-    if (n <= 4096 * E) return launch_norm<T, E, 1024, 4>(args, stream);
-  } else {
-    if (n <= 512) return launch_norm<T, 1, 64, 8>(args, stream);
-    if (n <= 2048) return launch_norm<T, 1, 256, 8>(args, stream);
-    if (n <= 8192) return launch_norm<T, 1, 1024, 8>(args, stream);
-    if (n <= 16384) return launch_norm<T, 1, 1024, 16>(args, stream);
-  }
+  if (n <= 64 * N) return launch_norm<T, 64, 1>(args, stream);
+  if (n <= 256 * N) return launch_norm<T, 256, 1>(args, stream);
+  if (n <= 512 * N) return launch_norm<T, 256, 2>(args, stream);
+  if (n <= 1024 * N) return launch_norm<T, 512, 2>(args, stream);
+  if (n <= 2048 * N) return launch_norm<T, 1024, 2>(args, stream);
+  if (n <= 4096 * N) return launch_norm<T, 1024, 4>(args, stream);
   const dim3 g(static_cast<uint32_t>(args.rows)), b(kLongThreads);
   if (args.scales) hipLaunchKernelGGL((rms_norm_long_kernel<T, true>), g, b, 0, stream, args);
   else hipLaunchKernelGGL((rms_norm_long_kernel<T, false>), g, b, 0, stream, args);
@@ -213,48 +182,52 @@ hipError_t launch_norm_of(const NormArgs& args, bool vec, hipStream_t stream) {
 
 // Group `first` of the launch takes rows first, first + step, ... and holds its part of the weight's
 // gradient in registers until the last of them: one row of partial sums for each group.
-template <typename T, int VEC, int NT, int V>
+template <typename T, int NT, int V>
 __global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_backward_kernel(NormBackwardArgs args, int groups) {
-  constexpr int NW = RowGroup<NT>::kWaves;
+  typedef Group16<T> G;
+  constexpr int NW = RowGroup<NT>::kWaves, N = G::N;
   __shared__ float slots[2][NW];
   const int t = threadIdx.x % NT;
   const int group = blockIdx.x * RowGroup<NT>::kRows + threadIdx.x / NT;
   if (group >= groups) return;
   const int cols = static_cast<int>(args.cols);
-  float dw[V][VEC] = {}, w[V][VEC] = {};
+  const auto at = [&](int j) { return (j * NT + t) * N; };
+  float dw[V][N] = {}, w[V][N];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int c = (j * NT + t) * VEC;
-    if (c < cols) load_elements<VEC>(args.weight + c, w[j]);
+    Floats16<N> raw;
+    raw.read(args.weight + at(j), cols - at(j));
+    raw.unpack(w[j]);
   }
   int turn = 0;
   for (int64_t row = group; row < args.rows; row += groups, turn ^= 1) {
     const T* dy = static_cast<const T*>(args.dy) + row * args.lddy;
     const T* h = static_cast<const T*>(args.h) + row * args.ldh;
     const float inv = args.inv_rms[row];
-    float g[V][VEC] = {}, xhat[V][VEC] = {}, add[V][VEC] = {};
+    Raw16 g_raw[V], h_raw[V], add_raw[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int c = (j * NT + t) * VEC;
-      if (c < cols) {
-        load_elements<VEC>(dy + c, g[j]);
-        load_elements<VEC>(h + c, xhat[j]);
-      }
+      g_raw[j] = G::read(dy + at(j), cols - at(j));
+      h_raw[j] = G::read(h + at(j), cols - at(j));
     }
     if (args.dsum) {
       const T* dsum = static_cast<const T*>(args.dsum) + row * args.ldds;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int c = (j * NT + t) * VEC;
-        if (c < cols) load_elements<VEC>(dsum + c, add[j]);
-      }
+      for (int j = 0; j < V; ++j) add_raw[j] = G::read(dsum + at(j), cols - at(j));
+    }
+    float g[V][N], xhat[V][N];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      G::unpack(g_raw[j], g[j]);
+      G::unpack(h_raw[j], xhat[j]);
     }
     float dot = 0.0f;
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        xhat[j][e] *= inv;
+      for (int e = 0; e < N; ++e) {
+        if (at(j) + e >= cols) xhat[j][e] = 0.0f;   // (inv may be infinite)
+        else xhat[j][e] *= inv;
         dw[j][e] += g[j][e] * xhat[j][e];
         g[j][e] *= w[j][e];
         dot += g[j][e] * xhat[j][e];
@@ -264,21 +237,16 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_backward_kern
     T* dx = static_cast<T*>(args.dx) + row * args.lddx;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int c = (j * NT + t) * VEC;
+      float add[N] = {};
+      if (args.dsum) G::unpack(add_raw[j], add);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) g[j][e] = (g[j][e] - xhat[j][e] * mean) * inv + add[j][e];
-      if (c < cols) store_elements<VEC>(dx + c, g[j]);
+      for (int e = 0; e < N; ++e) g[j][e] = (g[j][e] - xhat[j][e] * mean) * inv + add[e];
+      G::store(dx + at(j), cols - at(j), g[j]);
     }
   }
   float* out = args.partials + static_cast<int64_t>(group) * args.cols;
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int c = (j * NT + t) * VEC;
-    if (c < cols) {
-      if constexpr (VEC == 1) out[c] = dw[j][0];
-      else store_elements<VEC>(out + c, dw[j]);
-    }
-  }
+  for (int j = 0; j < V; ++j) store_floats<N>(out + at(j), cols - at(j), dw[j]);
 }
 
 // Rows that no group's registers hold: the partial sums are kept in the group's row of them.
@@ -295,112 +263,116 @@ __global__ __launch_bounds__(kLongThreads) void rms_norm_backward_long_kernel(No
     const bool fresh = row == blockIdx.x;
     float dot = 0.0f;
     for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
-      float g[1], x[1];
-      load_elements<1>(dy + c, g);
-      load_elements<1>(h + c, x);
-      x[0] *= inv;
-      out[c] = (fresh ? 0.0f : out[c]) + g[0] * x[0];
-      dot += g[0] * args.weight[c] * x[0];
+      const float g = element(dy + c), x = element(h + c) * inv;
+      out[c] = (fresh ? 0.0f : out[c]) + g * x;
+      dot += g * args.weight[c] * x;
     }
     const float mean = group_sum<NW>(dot, slots[turn]) / static_cast<float>(args.cols);
     for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
-      float g[1], x[1], add[1] = {0.0f};
-      load_elements<1>(dy + c, g);
-      load_elements<1>(h + c, x);
-      if (args.dsum) load_elements<1>(static_cast<const T*>(args.dsum) + row * args.ldds + c, add);
-      g[0] = (g[0] * args.weight[c] - x[0] * inv * mean) * inv + add[0];
-      store_elements<1>(static_cast<T*>(args.dx) + row * args.lddx + c, g);
+      const float add = args.dsum ? element(static_cast<const T*>(args.dsum) + row * args.ldds + c) : 0.0f;
+      put(static_cast<T*>(args.dx) + row * args.lddx + c,
+          (element(dy + c) * args.weight[c] - element(h + c) * inv * mean) * inv + add);
     }
   }
 }
 
-template <typename T, int VEC, int NT, int V>
+template <typename T, int NT, int V>
 hipError_t launch_backward(const NormBackwardArgs& args, int groups, hipStream_t stream) {
   constexpr int kRows = RowGroup<NT>::kRows;
-  hipLaunchKernelGGL((rms_norm_backward_kernel<T, VEC, NT, V>), dim3((groups + kRows - 1) / kRows),
-                     dim3(RowGroup<NT>::kThreads), 0, stream, args, groups);
+  hipLaunchKernelGGL((rms_norm_backward_kernel<T, NT, V>), dim3((groups + kRows - 1) / kRows), dim3(RowGroup<NT>::kThreads), 0,
+                     stream, args, groups);
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch_backward_of(const NormBackwardArgs& args, bool vec, int groups, hipStream_t stream) {
-  constexpr int E = Vec16<T>::N;
+hipError_t launch_backward_of(const NormBackwardArgs& args, int groups, hipStream_t stream) {
+  constexpr int N = Group16<T>::N;
   const int64_t n = args.cols;
-  if (vec) {
-    if (n <= 64 * E) return launch_backward<T, E, 64, 1>(args, groups, stream);
-    if (n <= 256 * E) return launch_backward<T, E, 256, 1>(args, groups, stream);
-    if (n <= 512 * E) return launch_backward<T, E, 512, 1>(args, groups, stream);
-    if (n <= 1024 * E) return launch_backward<T, E, 1024, 1>(args, groups, stream);
-    if (n <= 2048 * E) return launch_backward<T, E, 1024, 2>(args, groups, stream);
-  } else {
-    if (n <= 512) return launch_backward<T, 1, 64, 8>(args, groups, stream);
-    if (n <= 2048) return launch_backward<T, 1, 256, 8>(args, groups, stream);
-    if (n <= 8192) return launch_backward<T, 1, 1024, 8>(args, groups, stream);
-  }
+  if (n <= 64 * N) return launch_backward<T, 64, 1>(args, groups, stream);
+  if (n <= 256 * N) return launch_backward<T, 256, 1>(args, groups, stream);
+  if (n <= 512 * N) return launch_backward<T, 512, 1>(args, groups, stream);
+  if (n <= 1024 * N) return launch_backward<T, 1024, 1>(args, groups, stream);
+  if (n <= 2048 * N) return launch_backward<T, 1024, 2>(args, groups, stream);
   hipLaunchKernelGGL((rms_norm_backward_long_kernel<T>), dim3(groups), dim3(kLongThreads), 0, stream, args, groups);
   return hipGetLastError();
 }
 
 // ---- sums of columns -------------------------------------------------------------
 
-// A workgroup sums one chunk of rows for 64 VEC columns: each of its NW waves every NW-th row, joined
+// A workgroup sums one chunk of rows for 64 groups of columns: each of its NW waves every NW-th row, joined
 // in wave order.
-template <typename T, int VEC, int NW>
+template <typename T, int NW>
 __global__ __launch_bounds__(64 * NW) void column_sum_kernel(ColumnSumArgs args) {
-  __shared__ float part[NW - 1][64 * VEC];
+  typedef Group16<T> G;
+  constexpr int N = G::N;
+  __shared__ float part[NW - 1][64 * N];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = (static_cast<int64_t>(blockIdx.x) * 64 + lane) * VEC;
+  const int64_t c = (static_cast<int64_t>(blockIdx.x) * 64 + lane) * N;
   const int64_t per = (args.rows + args.chunks - 1) / args.chunks;
   const int64_t first = blockIdx.y * per, end = std::min<int64_t>(first + per, args.rows);
-  float sum[VEC] = {};
-  if (c < args.cols) {
+  const int left = static_cast<int>(std::min<int64_t>(args.cols - c, N));
+  float sum[N] = {};
+  if (left > 0) {
     const T* p = static_cast<const T*>(args.in) + c;
 #pragma unroll 4
     for (int64_t row = first + wave; row < end; row += NW) {
-      float x[VEC];
-      load_elements<VEC>(p + row * args.ld, x);
+      float x[N];
+      G::unpack(G::read(p + row * args.ld, left), x);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) sum[e] += x[e];
+      for (int e = 0; e < N; ++e) sum[e] += x[e];
     }
   }
   if (wave > 0) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) part[wave - 1][e * 64 + lane] = sum[e];
+    for (int e = 0; e < N; ++e) part[wave - 1][e * 64 + lane] = sum[e];
   }
   __syncthreads();
-  if (wave > 0 || c >= args.cols) return;
+  if (wave > 0 || left <= 0) return;
 #pragma unroll
   for (int w = 0; w < NW - 1; ++w)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) sum[e] += part[w][e * 64 + lane];
-  float* out = args.chunks > 1 ? args.partials + blockIdx.y * args.cols : args.out;
-#pragma unroll
-  for (int e = 0; e < VEC; ++e)
-    if (c + e < args.cols) out[c + e] = sum[e];
+    for (int e = 0; e < N; ++e) sum[e] += part[w][e * 64 + lane];
+  store_floats<N>((args.chunks > 1 ? args.partials + blockIdx.y * args.cols : args.out) + c, left, sum);
 }
 
-template <typename T, int VEC, int NW>
+template <typename T, int NW>
 hipError_t launch_sum(const ColumnSumArgs& args, hipStream_t stream) {
-  const dim3 g(static_cast<uint32_t>((args.cols + 64 * VEC - 1) / (64 * VEC)), args.chunks);
-  hipLaunchKernelGGL((column_sum_kernel<T, VEC, NW>), g, dim3(64 * NW), 0, stream, args);
+  constexpr int kCols = 64 * Group16<T>::N;
+  const dim3 g(static_cast<uint32_t>((args.cols + kCols - 1) / kCols), args.chunks);
+  hipLaunchKernelGGL((column_sum_kernel<T, NW>), g, dim3(64 * NW), 0, stream, args);
   return hipGetLastError();
+}
+
+// The rows of partial sums: one column per lane and sixteen waves, as many loads in flight as there can be.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void join_rows_kernel(const float* in, int rows, int64_t cols, float* out) {
+  __shared__ float part[kJoinWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+  float sum = 0.0f;
+  if (c < cols) {
+#pragma unroll 8
+    for (int row = wave; row < rows; row += kJoinWaves) sum += in[row * cols + c];
+  }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (wave > 0 || c >= cols) return;
+#pragma unroll
+  for (int w = 1; w < kJoinWaves; ++w) sum += part[w][lane];
+  out[c] = sum;
 }
 
 }  // namespace
 
-hipError_t launch_rms_norm(const NormArgs& args, int dtype, bool vec, hipStream_t stream) {
-  return dtype == CLEAVE_BF16 ? launch_norm_of<Bf16>(args, vec, stream) : launch_norm_of<float>(args, vec, stream);
+hipError_t launch_rms_norm(const NormArgs& args, int dtype, hipStream_t stream) {
+  return dtype == CLEAVE_BF16 ? launch_norm_of<Bf16>(args, stream) : launch_norm_of<float>(args, stream);
 }
 
-int rms_norm_partial_rows(int64_t rows, int64_t cols) {
-  (void)cols;
-  return static_cast<int>(std::min<int64_t>(rows, 512));
-}
+int rms_norm_partial_rows(int64_t rows) { return static_cast<int>(std::min<int64_t>(rows, 512)); }
 
-hipError_t launch_rms_norm_backward(const NormBackwardArgs& args, int dtype, bool vec, int partial_rows,
-                                    hipStream_t stream) {
-  return dtype == CLEAVE_BF16 ? launch_backward_of<Bf16>(args, vec, partial_rows, stream)
-                              : launch_backward_of<float>(args, vec, partial_rows, stream);
+hipError_t launch_rms_norm_backward(const NormBackwardArgs& args, int dtype, int partial_rows, hipStream_t stream) {
+  return dtype == CLEAVE_BF16 ? launch_backward_of<Bf16>(args, partial_rows, stream)
+                              : launch_backward_of<float>(args, partial_rows, stream);
 }
 
 int column_sum_chunks(int64_t rows, int64_t cols) {
@@ -410,21 +382,13 @@ int column_sum_chunks(int64_t rows, int64_t cols) {
 }
 
 hipError_t launch_join_rows(const float* rows, int n, int64_t cols, float* out, hipStream_t stream) {
-  ColumnSumArgs join{};
-  join.in = rows;
-  join.ld = cols;
-  join.rows = n;
-  join.cols = cols;
-  join.out = out;
-  join.chunks = 1;
-  // one column per lane and sixteen waves: as many loads in flight as there can be
-  return launch_sum<float, 1, 16>(join, stream);
+  hipLaunchKernelGGL(join_rows_kernel, dim3(static_cast<uint32_t>((cols + 63) / 64)), dim3(64 * kJoinWaves), 0, stream, rows, n,
+                     cols, out);
+  return hipGetLastError();
 }
 
-hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, bool vec, hipStream_t stream) {
-  hipError_t e;
-  if (dtype == CLEAVE_BF16) e = vec ? launch_sum<Bf16, 8, 4>(args, stream) : launch_sum<Bf16, 1, 4>(args, stream);
-  else e = vec ? launch_sum<float, 4, 4>(args, stream) : launch_sum<float, 1, 4>(args, stream);
+hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, hipStream_t stream) {
+  const hipError_t e = dtype == CLEAVE_BF16 ? launch_sum<Bf16, 4>(args, stream) : launch_sum<float, 4>(args, stream);
   if (e != hipSuccess || args.chunks == 1) return e;
   return launch_join_rows(args.partials, args.chunks, args.cols, args.out, stream);
 }

@@ -25,30 +25,15 @@ int element_bytes(int dtype) { return dtype == CLEAVE_F32 ? 4 : dtype == CLEAVE_
 
 constexpr int64_t kMost = std::numeric_limits<int32_t>::max();
 
-// Matrices of rows x cols that one kernel walks: their checks, and whether every row of
-// all of them takes sixteen bytes of the input type at a time.
+// Checks of the matrices of rows x cols that one kernel walks.
 struct Matrices {
-  int64_t rows, cols;
-  int vec;          // elements in sixteen bytes of the input type
-  bool ok = true, wide;
-  Matrices(int64_t r, int64_t c, int dtype)
-      : rows(r), cols(c), vec(16 / element_bytes(dtype)), wide(c % vec == 0) {
-    ok = r >= 0 && c >= 1 && r <= kMost && c <= kMost;
-  }
+  int64_t cols;
+  bool ok;
+  Matrices(int64_t r, int64_t c) : cols(c), ok(r >= 0 && c >= 1 && r <= kMost && c <= kMost) {}
   void add(const void* p, int64_t ld, int dtype, bool optional = false) {
-    const int eb = element_bytes(dtype);
-    if (!p) {
-      ok = ok && optional;
-      return;
-    }
-    ok = ok && ld >= cols && aligned(p, eb);
-    // (an output of narrower elements takes as many of them)
-    wide = wide && ld % vec == 0 && aligned(p, static_cast<uintptr_t>(eb) * vec);
+    ok = ok && (p ? ld >= cols && aligned(p, element_bytes(dtype)) : optional);
   }
-  void add_vector(const float* p, bool read_wide, bool optional = false) {
-    ok = ok && (p ? aligned(p, 4) : optional);
-    if (read_wide) wide = wide && aligned(p, 16);
-  }
+  void add_vector(const float* p, bool optional = false) { ok = ok && (p ? aligned(p, 4) : optional); }
 };
 
 bool float_dtype(int dtype) { return dtype == CLEAVE_F32 || dtype == CLEAVE_BF16; }
@@ -61,45 +46,45 @@ extern "C" int cleave_rms_norm(int64_t rows, int64_t cols, const void* x, int64_
   if (!float_dtype(dtype) || (y_dtype != dtype && y_dtype != CLEAVE_E4M3)) return CLEAVE_EINVAL;
   if ((y_dtype == CLEAVE_E4M3) != (scales != nullptr)) return CLEAVE_EINVAL;
   if (!(eps >= 0.0f) || std::isinf(eps)) return CLEAVE_EINVAL;
-  Matrices m(rows, cols, dtype);
+  Matrices m(rows, cols);
   m.add(x, ldx, dtype);
   m.add(residual, ldr, dtype, true);
   m.add(y, ldy, y_dtype);
   m.add(sum_out, lds, dtype, true);
-  m.add_vector(weight, true);
-  m.add_vector(scales, false, true);
-  m.add_vector(inv_rms, false, true);
+  m.add_vector(weight);
+  m.add_vector(scales, true);
+  m.add_vector(inv_rms, true);
   if (!m.ok) return CLEAVE_EINVAL;
   if (rows == 0) return CLEAVE_OK;
   const cleave::NormArgs args{x, residual, weight, y, scales, sum_out, inv_rms, rows, cols, ldx, ldr, ldy, lds, eps};
-  CLEAVE_HIP(cleave::launch_rms_norm(args, dtype, m.wide, static_cast<hipStream_t>(hip_stream)));
+  CLEAVE_HIP(cleave::launch_rms_norm(args, dtype, static_cast<hipStream_t>(hip_stream)));
   return CLEAVE_OK;
 }
 
 extern "C" int64_t cleave_rms_norm_workspace(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 1 || rows > kMost || cols > kMost) return CLEAVE_EINVAL;
-  return cols * std::max(1, cleave::rms_norm_partial_rows(rows, cols));
+  return cols * std::max(1, cleave::rms_norm_partial_rows(rows));
 }
 
 extern "C" int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* h, int64_t ldh,
                                         const void* dsum, int64_t ldds, int dtype, const float* weight, const float* inv_rms,
                                         void* dx, int64_t lddx, float* dweight, float* workspace, void* hip_stream) {
   if (!float_dtype(dtype)) return CLEAVE_EINVAL;
-  Matrices m(rows, cols, dtype);
+  Matrices m(rows, cols);
   m.add(dy, lddy, dtype);
   m.add(h, ldh, dtype);
   m.add(dsum, ldds, dtype, true);
   m.add(dx, lddx, dtype);
-  m.add_vector(weight, true);
-  m.add_vector(inv_rms, false);
-  m.add_vector(dweight, false);
-  m.add_vector(workspace, true);
+  m.add_vector(weight);
+  m.add_vector(inv_rms);
+  m.add_vector(dweight);
+  m.add_vector(workspace);
   if (!m.ok) return CLEAVE_EINVAL;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const int partial_rows = cleave::rms_norm_partial_rows(rows, cols);
+  const int partial_rows = cleave::rms_norm_partial_rows(rows);
   if (rows > 0) {
     const cleave::NormBackwardArgs args{dy, h, dsum, weight, inv_rms, dx, workspace, rows, cols, lddy, ldh, ldds, lddx};
-    CLEAVE_HIP(cleave::launch_rms_norm_backward(args, dtype, m.wide, partial_rows, stream));
+    CLEAVE_HIP(cleave::launch_rms_norm_backward(args, dtype, partial_rows, stream));
   }
   CLEAVE_HIP(cleave::launch_join_rows(workspace, partial_rows, cols, dweight, stream));   // no rows: zeros
   return CLEAVE_OK;
@@ -113,13 +98,13 @@ extern "C" int64_t cleave_bias_grad_workspace(int64_t rows, int64_t cols) {
 extern "C" int cleave_bias_grad(int64_t rows, int64_t cols, const void* dy, int64_t lddy, int dtype, float* dbias,
                                 float* workspace, void* hip_stream) {
   if (!float_dtype(dtype)) return CLEAVE_EINVAL;
-  Matrices m(rows, cols, dtype);
+  Matrices m(rows, cols);
   m.add(dy, lddy, dtype);
-  m.add_vector(dbias, false);
-  m.add_vector(workspace, false);
+  m.add_vector(dbias);
+  m.add_vector(workspace);
   if (!m.ok) return CLEAVE_EINVAL;
   const cleave::ColumnSumArgs args{dy, lddy, rows, cols, dbias, workspace, cleave::column_sum_chunks(rows, cols)};
-  CLEAVE_HIP(cleave::launch_column_sum(args, dtype, m.wide, static_cast<hipStream_t>(hip_stream)));
+  CLEAVE_HIP(cleave::launch_column_sum(args, dtype, static_cast<hipStream_t>(hip_stream)));
   return CLEAVE_OK;
 }
 
@@ -178,10 +163,7 @@ extern "C" int cleave_adamw(int64_t n_tensors, const int64_t* sizes, float* cons
     t.m_scale = states_8bit ? m_scale[k] : nullptr;
     t.v_scale = states_8bit ? v_scale[k] : nullptr;
     t.copy = w_bf16 ? static_cast<uint16_t*>(w_bf16[k]) : nullptr;
-    t.n_low = static_cast<uint32_t>(n);
-    t.n_high = static_cast<uint32_t>(n >> 32);
-    // four neighbouring elements at a time
-    t.vec = aligned(t.w, 16) && aligned(t.g, 4 * gb) && aligned(t.m, 4 * sb) && aligned(t.v, 4 * sb) && aligned(t.copy, 8);
+    t.n = static_cast<uint64_t>(n);
     chunks += more;
     args.chunk_end[args.n_tensors++] = static_cast<uint32_t>(chunks);
   }

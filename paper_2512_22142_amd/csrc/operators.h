@@ -23,10 +23,10 @@ struct NormArgs {
   int64_t ldx, ldr, ldy, lds;   // elements
   float eps;
 };
-hipError_t launch_rms_norm(const NormArgs& args, int dtype, bool vec, hipStream_t stream);
+hipError_t launch_rms_norm(const NormArgs& args, int dtype, hipStream_t stream);
 
 // Rows of partial sums (each `cols` floats) that the gradient's first launch leaves for its second.
-int rms_norm_partial_rows(int64_t rows, int64_t cols);
+int rms_norm_partial_rows(int64_t rows);
 struct NormBackwardArgs {
   const void* dy;
   const void* h;
@@ -39,7 +39,7 @@ struct NormBackwardArgs {
   int64_t lddy, ldh, ldds, lddx;
 };
 // dx and the partial sums of the weight's gradient.
-hipError_t launch_rms_norm_backward(const NormBackwardArgs& args, int dtype, bool vec, int partial_rows, hipStream_t stream);
+hipError_t launch_rms_norm_backward(const NormBackwardArgs& args, int dtype, int partial_rows, hipStream_t stream);
 
 // ---- sums of columns ---------------------------------------------------------
 
@@ -56,7 +56,7 @@ struct ColumnSumArgs {
 int column_sum_chunks(int64_t rows, int64_t cols);
 // out[c] = sum of `n` contiguous rows of partial sums.
 hipError_t launch_join_rows(const float* rows, int n, int64_t cols, float* out, hipStream_t stream);
-hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, bool vec, hipStream_t stream);
+hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, hipStream_t stream);
 
 // ---- AdamW over many tensors -------------------------------------------------
 
@@ -73,9 +73,7 @@ struct AdamTensor {
   float* m_scale;
   float* v_scale;
   uint16_t* copy;          // bf16; may be null
-  uint32_t n_low;          // elements: 40 bits, and whether every array takes 16-byte accesses
-  uint32_t n_high : 8;
-  uint32_t vec : 1;
+  uint64_t n;              // elements
 };
 static_assert(sizeof(AdamTensor) == 64, "AdamTensor is 64 bytes");
 constexpr int kAdamTensors = 56;   // per launch

@@ -1,4 +1,4 @@
-// Elements of a row of fp32 or bf16 values, sixteen bytes or one element at a time.
+// Elements of a row of fp32 or bf16 values, sixteen bytes at a time, at any alignment of the elements.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -6,6 +6,7 @@
 #include <cstdint>
 
 #include "bf16_round.h"
+#include "fp8_round.h"
 
 namespace cleave {
 
@@ -13,66 +14,115 @@ struct Bf16 {
   uint16_t bits;
 };
 
+// N neighbouring elements in sixteen bytes.  `left`: how many there are from p on; what is not there reads as zero and is
+// not written.  (A row's last group is the only one that is not whole.)  read() and unpack() are apart so that several reads are
+// on their way before the first is waited for.
+typedef uint32_t Raw16 __attribute__((ext_vector_type(4)));
+
 template <typename T>
-struct Vec16;
+struct Group16;
+
 template <>
-struct Vec16<float> {
+struct Group16<float> {
   static constexpr int N = 4;
-};
-template <>
-struct Vec16<Bf16> {
-  static constexpr int N = 8;
-};
-
-typedef float row_f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t row_u32x4 __attribute__((ext_vector_type(4)));
-
-// VEC elements from p on: 1, or sixteen bytes' worth (p aligned to that).
-template <int VEC>
-__device__ __forceinline__ void load_elements(const float* p, float (&out)[VEC]) {
-  if constexpr (VEC == 1) {
-    out[0] = *p;
-  } else {
-    static_assert(VEC % 4 == 0, "whole 16 bytes");
+  typedef uint32_t Any __attribute__((ext_vector_type(4), aligned(4)));
+  static __device__ __forceinline__ Raw16 read(const float* p, int left) {
+    if (left >= N) return *reinterpret_cast<const Any*>(p);
+    Raw16 w{};
 #pragma unroll
-    for (int q = 0; q < VEC / 4; ++q) {
-      const row_f32x4 v = reinterpret_cast<const row_f32x4*>(p)[q];
+    for (int e = 0; e < N; ++e)
+      if (e < left) w[e] = reinterpret_cast<const uint32_t*>(p)[e];
+    return w;
+  }
+  static __device__ __forceinline__ void unpack(Raw16 w, float (&out)[N]) {
+    typedef float Floats __attribute__((ext_vector_type(4)));
+    const Floats v = __builtin_bit_cast(Floats, w);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) out[4 * q + e] = v[e];
+    for (int e = 0; e < N; ++e) out[e] = v[e];
+  }
+  static __device__ __forceinline__ void store(float* p, int left, const float (&in)[N]) {
+    typedef float FloatsAny __attribute__((ext_vector_type(4), aligned(4)));
+    if (left >= N) {
+      *reinterpret_cast<FloatsAny*>(p) = FloatsAny{in[0], in[1], in[2], in[3]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e < left) p[e] = in[e];
     }
   }
-}
-template <int VEC>
-__device__ __forceinline__ void load_elements(const Bf16* p, float (&out)[VEC]) {
-  if constexpr (VEC == 1) {
-    out[0] = __builtin_bit_cast(float, static_cast<uint32_t>(p->bits) << 16);
-  } else {
-    static_assert(VEC == 8, "16 bytes");
-    const row_u32x4 v = *reinterpret_cast<const row_u32x4*>(p);
+};
+
+template <>
+struct Group16<Bf16> {
+  static constexpr int N = 8;
+  typedef uint32_t Any __attribute__((ext_vector_type(4), aligned(2)));
+  static __device__ __forceinline__ Raw16 read(const Bf16* p, int left) {
+    if (left >= N) return *reinterpret_cast<const Any*>(p);
+    Raw16 w{};
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < left) w[e / 2] |= static_cast<uint32_t>(p[e].bits) << (16 * (e % 2));
+    return w;
+  }
+  static __device__ __forceinline__ void unpack(Raw16 w, float (&out)[N]) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      out[2 * q] = __builtin_bit_cast(float, v[q] << 16);
-      out[2 * q + 1] = __builtin_bit_cast(float, v[q] & 0xffff0000u);
+      out[2 * q] = __builtin_bit_cast(float, w[q] << 16);
+      out[2 * q + 1] = __builtin_bit_cast(float, w[q] & 0xffff0000u);
     }
   }
-}
-template <int VEC>
-__device__ __forceinline__ void store_elements(float* p, const float (&in)[VEC]) {
-  if constexpr (VEC == 1) {
-    *p = in[0];
-  } else {
+  static __device__ __forceinline__ void store(Bf16* p, int left, const float (&in)[N]) {
+    if (left >= N) {
+      *reinterpret_cast<Any*>(p) =
+          Any{pack_bf16(in[0], in[1]), pack_bf16(in[2], in[3]), pack_bf16(in[4], in[5]), pack_bf16(in[6], in[7])};
+    } else {
 #pragma unroll
-    for (int q = 0; q < VEC / 4; ++q)
-      reinterpret_cast<row_f32x4*>(p)[q] = row_f32x4{in[4 * q], in[4 * q + 1], in[4 * q + 2], in[4 * q + 3]};
+      for (int e = 0; e < N; ++e)
+        if (e < left) p[e].bits = to_bf16_bits(in[e]);
+    }
+  }
+};
+
+// N floats beside a group of either type.
+template <int N>
+struct Floats16 {
+  Raw16 raw[N / 4];
+  __device__ __forceinline__ void read(const float* p, int left) {
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) raw[q] = Group16<float>::read(p + 4 * q, left - 4 * q);
+  }
+  __device__ __forceinline__ void unpack(float (&out)[N]) const {
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) {
+      float four[4];
+      Group16<float>::unpack(raw[q], four);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[4 * q + e] = four[e];
+    }
+  }
+};
+template <int N>
+__device__ __forceinline__ void store_floats(float* p, int left, const float (&in)[N]) {
+#pragma unroll
+  for (int q = 0; q < N / 4; ++q) {
+    const float four[4] = {in[4 * q], in[4 * q + 1], in[4 * q + 2], in[4 * q + 3]};
+    Group16<float>::store(p + 4 * q, left - 4 * q, four);
   }
 }
-template <int VEC>
-__device__ __forceinline__ void store_elements(Bf16* p, const float (&in)[VEC]) {
-  if constexpr (VEC == 1) {
-    p->bits = to_bf16_bits(in[0]);
+// N e4m3 values.
+template <int N>
+__device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float (&in)[N]) {
+  typedef uint32_t Words __attribute__((ext_vector_type(N / 4)));
+  typedef uint32_t WordsAny __attribute__((ext_vector_type(N / 4), aligned(1)));
+  if (left >= N) {
+    Words w;
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) w[q] = pack_e4m3(in[4 * q], in[4 * q + 1], in[4 * q + 2], in[4 * q + 3]);
+    *reinterpret_cast<WordsAny*>(p) = w;
   } else {
-    *reinterpret_cast<row_u32x4*>(p) = row_u32x4{pack_bf16(in[0], in[1]), pack_bf16(in[2], in[3]),
-                                                 pack_bf16(in[4], in[5]), pack_bf16(in[6], in[7])};
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < left) p[e] = static_cast<uint8_t>(pack_e4m3(in[e], in[e]));
   }
 }
 

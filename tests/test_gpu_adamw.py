@@ -24,7 +24,7 @@ def to_blocks(x, up):
     b[:n] = x
     b = b.view(blocks, 256)
     most = torch.where(b.isfinite(), b.abs(), torch.zeros_like(b)).amax(dim=1)
-    scale = torch.where(most >= 2.0 ** -100, most / 448, torch.zeros_like(most))
+    scale = torch.where(most >= 2.0 ** -100, most * torch.tensor(1 / 448), torch.zeros_like(most))
     q = torch.where(scale[:, None] > 0, b * (1 / scale)[:, None], torch.zeros_like(b))
     if up:
         q = torch.where((b > 0) & (scale[:, None] > 0), q.clamp_min(2.0 ** -9), q)
