@@ -162,16 +162,26 @@ hipError_t launch_norm(const NormArgs& args, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// `v` groups to a thread, up to MOST: the least that holds a row.
+template <typename T, int NT, int MOST, int V = 1>
+hipError_t launch_norm_fit(const NormArgs& args, int64_t v, hipStream_t stream) {
+  if constexpr (V < MOST) {
+    if (v > V) return launch_norm_fit<T, NT, MOST, V + 1>(args, v, stream);
+  }
+  return launch_norm<T, NT, V>(args, stream);
+}
+
+// Which threads share a row.  Groups of sixteen bytes beyond the row's end leave lanes idle, so a thread holds as
+// many as fit the row; wide groups of threads serve few rows, whose latency counts, narrow ones many.  us, 256 and 512
+// threads with one or two groups each / these: 16384 x 5120 bf16 into 8 bits 111 / 106, 7247 x 9984 119 / 96, 7232 x 8960
+// 97 / 87; 20000 x 768, 256 threads / a wave to a row: see the figures beside the table of kernels.
 template <typename T>
 hipError_t launch_norm_of(const NormArgs& args, hipStream_t stream) {
-  constexpr int N = Group16<T>::N;
-  const int64_t n = args.cols;
-  if (n <= 64 * N) return launch_norm<T, 64, 1>(args, stream);
-  if (n <= 256 * N) return launch_norm<T, 256, 1>(args, stream);
-  if (n <= 512 * N) return launch_norm<T, 256, 2>(args, stream);
-  if (n <= 1024 * N) return launch_norm<T, 512, 2>(args, stream);
-  if (n <= 2048 * N) return launch_norm<T, 1024, 2>(args, stream);
-  if (n <= 4096 * N) return launch_norm<T, 1024, 4>(args, stream);
+  const int64_t groups = (args.cols + Group16<T>::N - 1) / Group16<T>::N;
+  if (groups <= 64) return launch_norm<T, 64, 1>(args, stream);
+  if (groups <= 4 * 64 && args.rows > 1024) return launch_norm_fit<T, 64, 4>(args, (groups + 63) / 64, stream);
+  if (groups <= 8 * 256 && args.rows > 256) return launch_norm_fit<T, 256, 8>(args, (groups + 255) / 256, stream);
+  if (groups <= 4 * 1024) return launch_norm_fit<T, 1024, 4>(args, (groups + 1023) / 1024, stream);
   const dim3 g(static_cast<uint32_t>(args.rows)), b(kLongThreads);
   if (args.scales) hipLaunchKernelGGL((rms_norm_long_kernel<T, true>), g, b, 0, stream, args);
   else hipLaunchKernelGGL((rms_norm_long_kernel<T, false>), g, b, 0, stream, args);
@@ -180,16 +190,16 @@ hipError_t launch_norm_of(const NormArgs& args, hipStream_t stream) {
 
 // ---- gradient ------------------------------------------------------------------
 
-// Group `first` of the launch takes rows first, first + step, ... and holds its part of the weight's
-// gradient in registers until the last of them: one row of partial sums for each group.
+// Every group of the launch takes every groups-th row and holds its part of the weight's gradient in registers until the
+// last of them: one row of partial sums for each workgroup, whose groups (a wave each, where there are several) are joined
+// in order.
 template <typename T, int NT, int V>
-__global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_backward_kernel(NormBackwardArgs args, int groups) {
+__global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_backward_kernel(NormBackwardArgs args) {
   typedef Group16<T> G;
-  constexpr int NW = RowGroup<NT>::kWaves, N = G::N;
+  constexpr int NW = RowGroup<NT>::kWaves, N = G::N, GROUPS = RowGroup<NT>::kRows;
   __shared__ float slots[2][NW];
   const int t = threadIdx.x % NT;
-  const int group = blockIdx.x * RowGroup<NT>::kRows + threadIdx.x / NT;
-  if (group >= groups) return;
+  const int group = blockIdx.x * GROUPS + threadIdx.x / NT, groups = gridDim.x * GROUPS;
   const int cols = static_cast<int>(args.cols);
   const auto at = [&](int j) { return (j * NT + t) * N; };
   float dw[V][N] = {}, w[V][N];
@@ -244,19 +254,36 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_backward_kern
       G::store(dx + at(j), cols - at(j), g[j]);
     }
   }
-  float* out = args.partials + static_cast<int64_t>(group) * args.cols;
+  if constexpr (GROUPS > 1) {
+    __shared__ float joined[GROUPS - 1][V * N][NT];
+    if (threadIdx.x >= NT) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) joined[threadIdx.x / NT - 1][j * N + e][t] = dw[j][e];
+    }
+    __syncthreads();
+    if (threadIdx.x >= NT) return;
+#pragma unroll
+    for (int g = 0; g < GROUPS - 1; ++g)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) dw[j][e] += joined[g][j * N + e][t];
+  }
+  float* out = args.partials + static_cast<int64_t>(blockIdx.x) * args.cols;
 #pragma unroll
   for (int j = 0; j < V; ++j) store_floats<N>(out + at(j), cols - at(j), dw[j]);
 }
 
 // Rows that no group's registers hold: the partial sums are kept in the group's row of them.
 template <typename T>
-__global__ __launch_bounds__(kLongThreads) void rms_norm_backward_long_kernel(NormBackwardArgs args, int groups) {
+__global__ __launch_bounds__(kLongThreads) void rms_norm_backward_long_kernel(NormBackwardArgs args) {
   constexpr int NW = kLongThreads / 64;
   __shared__ float slots[2][NW];
   float* out = args.partials + static_cast<int64_t>(blockIdx.x) * args.cols;
   int turn = 0;
-  for (int64_t row = blockIdx.x; row < args.rows; row += groups, turn ^= 1) {
+  for (int64_t row = blockIdx.x; row < args.rows; row += gridDim.x, turn ^= 1) {
     const T* dy = static_cast<const T*>(args.dy) + row * args.lddy;
     const T* h = static_cast<const T*>(args.h) + row * args.ldh;
     const float inv = args.inv_rms[row];
@@ -277,10 +304,8 @@ __global__ __launch_bounds__(kLongThreads) void rms_norm_backward_long_kernel(No
 }
 
 template <typename T, int NT, int V>
-hipError_t launch_backward(const NormBackwardArgs& args, int groups, hipStream_t stream) {
-  constexpr int kRows = RowGroup<NT>::kRows;
-  hipLaunchKernelGGL((rms_norm_backward_kernel<T, NT, V>), dim3((groups + kRows - 1) / kRows), dim3(RowGroup<NT>::kThreads), 0,
-                     stream, args, groups);
+hipError_t launch_backward(const NormBackwardArgs& args, int workgroups, hipStream_t stream) {
+  hipLaunchKernelGGL((rms_norm_backward_kernel<T, NT, V>), dim3(workgroups), dim3(RowGroup<NT>::kThreads), 0, stream, args);
   return hipGetLastError();
 }
 
@@ -289,11 +314,12 @@ hipError_t launch_backward_of(const NormBackwardArgs& args, int groups, hipStrea
   constexpr int N = Group16<T>::N;
   const int64_t n = args.cols;
   if (n <= 64 * N) return launch_backward<T, 64, 1>(args, groups, stream);
+  if (n <= 128 * N && args.rows > 2048) return launch_backward<T, 64, 2>(args, groups, stream);
   if (n <= 256 * N) return launch_backward<T, 256, 1>(args, groups, stream);
   if (n <= 512 * N) return launch_backward<T, 512, 1>(args, groups, stream);
   if (n <= 1024 * N) return launch_backward<T, 1024, 1>(args, groups, stream);
   if (n <= 2048 * N) return launch_backward<T, 1024, 2>(args, groups, stream);
-  hipLaunchKernelGGL((rms_norm_backward_long_kernel<T>), dim3(groups), dim3(kLongThreads), 0, stream, args, groups);
+  hipLaunchKernelGGL((rms_norm_backward_long_kernel<T>), dim3(groups), dim3(kLongThreads), 0, stream, args);
   return hipGetLastError();
 }
 
@@ -343,22 +369,28 @@ hipError_t launch_sum(const ColumnSumArgs& args, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// The rows of partial sums: one column per lane and sixteen waves, as many loads in flight as there can be.
-constexpr int kJoinWaves = 16;
-__global__ __launch_bounds__(64 * kJoinWaves) void join_rows_kernel(const float* in, int rows, int64_t cols, float* out) {
-  __shared__ float part[kJoinWaves][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+// The rows of partial sums: sixteen columns to a workgroup and 64 rows at a time, so that a few hundred rows are a few loads
+// of each thread.
+constexpr int kJoinThreads = 1024, kJoinCols = 16;
+__global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in, int rows, int64_t cols, float* out) {
+  constexpr int kRows = kJoinThreads / kJoinCols;
+  __shared__ float part[kJoinThreads / 64][kJoinCols];
+  const int at = threadIdx.x % kJoinCols, first = threadIdx.x / kJoinCols;
+  const int64_t c = static_cast<int64_t>(blockIdx.x) * kJoinCols + at;
   float sum = 0.0f;
   if (c < cols) {
 #pragma unroll 8
-    for (int row = wave; row < rows; row += kJoinWaves) sum += in[row * cols + c];
+    for (int row = first; row < rows; row += kRows) sum += in[row * cols + c];
   }
-  part[wave][lane] = sum;
+  // a wave's four rows, then the waves
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if ((threadIdx.x & 63) < kJoinCols) part[threadIdx.x / 64][at] = sum;
   __syncthreads();
-  if (wave > 0 || c >= cols) return;
+  if (threadIdx.x >= kJoinCols || c >= cols) return;
+  sum = part[0][at];
 #pragma unroll
-  for (int w = 1; w < kJoinWaves; ++w) sum += part[w][lane];
+  for (int w = 1; w < kJoinThreads / 64; ++w) sum += part[w][at];
   out[c] = sum;
 }
 
@@ -368,7 +400,13 @@ hipError_t launch_rms_norm(const NormArgs& args, int dtype, hipStream_t stream) 
   return dtype == CLEAVE_BF16 ? launch_norm_of<Bf16>(args, stream) : launch_norm_of<float>(args, stream);
 }
 
-int rms_norm_partial_rows(int64_t rows) { return static_cast<int>(std::min<int64_t>(rows, 512)); }
+// Workgroups of the gradient: what the CUs hold at a time, where every group of threads gets a few rows.  (Narrow rows have four
+// groups to a workgroup.)
+int rms_norm_partial_rows(int64_t rows, int64_t cols) {
+  const int64_t groups = cols <= 1024 ? 8192 : cols <= 2048 ? 1024 : 512;
+  const int64_t some = std::min(groups, rows <= 2048 ? rows : std::max<int64_t>((rows + 3) / 4, 2048));
+  return static_cast<int>(cols <= 1024 ? (some + 3) / 4 : std::min<int64_t>(some, groups));
+}
 
 hipError_t launch_rms_norm_backward(const NormBackwardArgs& args, int dtype, int partial_rows, hipStream_t stream) {
   return dtype == CLEAVE_BF16 ? launch_backward_of<Bf16>(args, partial_rows, stream)
@@ -382,8 +420,8 @@ int column_sum_chunks(int64_t rows, int64_t cols) {
 }
 
 hipError_t launch_join_rows(const float* rows, int n, int64_t cols, float* out, hipStream_t stream) {
-  hipLaunchKernelGGL(join_rows_kernel, dim3(static_cast<uint32_t>((cols + 63) / 64)), dim3(64 * kJoinWaves), 0, stream, rows, n,
-                     cols, out);
+  hipLaunchKernelGGL(join_rows_kernel, dim3(static_cast<uint32_t>((cols + kJoinCols - 1) / kJoinCols)), dim3(kJoinThreads), 0,
+                     stream, rows, n, cols, out);
   return hipGetLastError();
 }
 

@@ -63,7 +63,7 @@ extern "C" int cleave_rms_norm(int64_t rows, int64_t cols, const void* x, int64_
 
 extern "C" int64_t cleave_rms_norm_workspace(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 1 || rows > kMost || cols > kMost) return CLEAVE_EINVAL;
-  return cols * std::max(1, cleave::rms_norm_partial_rows(rows));
+  return cols * std::max(1, cleave::rms_norm_partial_rows(rows, cols));
 }
 
 extern "C" int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* h, int64_t ldh,
@@ -81,7 +81,7 @@ extern "C" int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* 
   m.add_vector(workspace);
   if (!m.ok) return CLEAVE_EINVAL;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const int partial_rows = cleave::rms_norm_partial_rows(rows);
+  const int partial_rows = cleave::rms_norm_partial_rows(rows, cols);
   if (rows > 0) {
     const cleave::NormBackwardArgs args{dy, h, dsum, weight, inv_rms, dx, workspace, rows, cols, lddy, ldh, ldds, lddx};
     CLEAVE_HIP(cleave::launch_rms_norm_backward(args, dtype, partial_rows, stream));

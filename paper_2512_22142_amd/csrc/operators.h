@@ -26,7 +26,7 @@ struct NormArgs {
 hipError_t launch_rms_norm(const NormArgs& args, int dtype, hipStream_t stream);
 
 // Rows of partial sums (each `cols` floats) that the gradient's first launch leaves for its second.
-int rms_norm_partial_rows(int64_t rows);
+int rms_norm_partial_rows(int64_t rows, int64_t cols);
 struct NormBackwardArgs {
   const void* dy;
   const void* h;
