@@ -237,6 +237,19 @@ __device__ __forceinline__ void spread_reads() {
   spread_reads_at<M, READS>(std::make_integer_sequence<int, M>{});
 }
 
+// The same with the reads behind the first half of the MFMAs.
+template <int M, int READS, int... I>
+__device__ __forceinline__ void early_reads_at(std::integer_sequence<int, I...>) {
+  constexpr int kSlots = M > 1 ? M / 2 : 1;
+  constexpr auto done = [](int m) { return m >= kSlots ? READS : (m * READS + kSlots - 1) / kSlots; };
+  ((__builtin_amdgcn_sched_group_barrier(0x008, 1, 0),
+    __builtin_amdgcn_sched_group_barrier(0x100, done(I + 1) - done(I), 0)), ...);
+}
+template <int M, int READS>
+__device__ __forceinline__ void early_reads() {
+  early_reads_at<M, READS>(std::make_integer_sequence<int, M>{});
+}
+
 // TAILS: some chunk of the launch ends within a K step (the code for that costs
 // scalar registers: an instantiation of its own).
 // Epi: what the sums go through on their way out (linear_epilogue.h).
@@ -469,7 +482,7 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
   f32x4 acc[MB][NB];
   u32x4 fa[kQuarters ? 1 : 2][MB], fb[kQuarters ? 1 : 2][NB];
   constexpr bool kWide = OPS == kE4M3;   // both sub-steps in one instruction
-  i32x8 wide_a[kWide ? MH : 1], wide_b[kWide ? NB : 1];
+  i32x8 wide_a[kWide ? MB : 1], wide_b[kWide ? NB : 1];
 
   // Fragment reads are ordinary (compiler-visible) LDS loads: the compiler
   // tracks their completion, and every address is a lane-constant register
@@ -537,14 +550,12 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
   };
   // The same for whole steps of 8-bit values: a lane's 32 bytes are its sixteen of either sub-step (any
   // order of k will do that both operands share).
-  // Rows I0 .. I0 + N - 1 of A into registers 0 .. N - 1.
-  auto read_wide_a = [&](uint32_t stage, auto to_tag, auto i0_tag, auto n_tag) {
+  auto read_wide_a = [&](uint32_t stage, auto i0_tag, auto n_tag) {
 #pragma unroll
-    for (int x = 0; x < decltype(n_tag)::value; ++x) {
-      const int i = decltype(i0_tag)::value + x;
+    for (int i = decltype(i0_tag)::value; i < decltype(i0_tag)::value + decltype(n_tag)::value; ++i) {
       const u32x4 lo = *reinterpret_cast<const u32x4*>(smem + (a_addr[0] + stage) + i * 16 * kRowBytes);
       const u32x4 hi = *reinterpret_cast<const u32x4*>(smem + (a_addr[1] + stage) + i * 16 * kRowBytes);
-      wide_a[decltype(to_tag)::value + x] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      wide_a[i] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   };
   auto read_wide_b = [&](uint32_t stage, auto j0_tag, auto n_tag) {
@@ -555,8 +566,7 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
       wide_b[j] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   };
-  // Rows I0 .. of the sums, whose fragments sit in registers R0 .., times columns J0 .. .
-  auto mma_wide = [&](auto i0_tag, auto r0_tag, auto m_tag, auto j0_tag, auto n_tag, auto fresh_tag) {
+  auto mma_wide = [&](auto i0_tag, auto m_tag, auto j0_tag, auto n_tag, auto fresh_tag) {
     constexpr int I0 = decltype(i0_tag)::value, J0 = decltype(j0_tag)::value, N = decltype(n_tag)::value;
 #pragma unroll
     for (int x = 0; x < decltype(m_tag)::value; ++x)
@@ -566,8 +576,7 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
         f32x4 sum = acc[i][j];
         if constexpr (decltype(fresh_tag)::value) sum = f32x4{};
         // (e4m3 both; no scales: the plain instruction)
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_b[j], wide_a[decltype(r0_tag)::value + x], sum, 0, 0, 0,
-                                                                    0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_b[j], wide_a[i], sum, 0, 0, 0, 0, 0, 0);
       }
   };
   constexpr int kReadsA = (A_K ? 1 : 2) * MB, kReadsB = (B_K ? 1 : 2) * NB;
@@ -593,7 +602,7 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
     // The fragments that a step begins with.
     auto first_frags = [&](uint32_t stage) {
       if constexpr (kWide) {
-        read_wide_a(stage, int_c<0>{}, int_c<0>{}, int_c<MH>{});
+        read_wide_a(stage, int_c<0>{}, int_c<MH>{});
         read_wide_b(stage, int_c<0>{}, int_c<NH>{});
       } else if constexpr (kQuarters) {
         read_a(stage, int_c<0>{}, int_c<0>{}, int_c<MH>{});
@@ -668,42 +677,30 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
       };
       constexpr int_c<0> k0{};
       constexpr int_c<1> k1{};
-      // 8-bit values: the second half of B times one half of A (rows I0 on), each row's registers being
-      // read anew behind its products: with A's second half of this stage, or the first half of the next.
-      [[maybe_unused]] auto rows_then_reads = [&](auto i0_tag, auto j0_tag, uint32_t stage, auto second_tag, bool on) {
-        const auto row = [&](auto x_tag) {
-          constexpr int X = decltype(x_tag)::value;
-          if constexpr (X < MH) {
-            mma_wide(int_c<decltype(i0_tag)::value + X>{}, x_tag, int_c<1>{}, j0_tag, int_c<NH>{}, fresh);
-            if (on) read_wide_a(stage, x_tag, int_c<(decltype(second_tag)::value ? MH : 0) + X>{}, int_c<1>{});
-            __builtin_amdgcn_sched_group_barrier(0x008, NH, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-          }
-        };
-        row(int_c<0>{});
-        row(int_c<1>{});
-        row(int_c<2>{});
-        row(int_c<3>{});
-        static_assert(MH <= 4, "the rows above");
-      };
       if constexpr (kWide) {
-        // Four quarters.  A's second half takes the registers of its first, row by row, in the second quarter, the
-        // next step's first half those of the second one in the last: with both halves at hand the large shape spills.
+        // Four quarters, each with a quarter of the reads in its first half: the waves run in step, and more than that at a
+        // time is more than the LDS gives.  The second halves are read in the first two quarters, the next step's
+        // first halves behind the barrier, where this step's are done with.
         constexpr int_c<0> lo{};
-        constexpr int_c<MH> mh{};
+        constexpr int_c<MH> a_hi{}, mh{};
         constexpr int_c<NH> b_hi{}, nh{};
         read_wide_b(cur, b_hi, nh);
-        mma_wide(lo, lo, mh, lo, nh, fresh);
-        spread_reads<MH * NH, NB>();
-        rows_then_reads(lo, b_hi, cur, std::true_type{}, true);
-        mma_wide(mh, lo, mh, lo, nh, fresh);
+        mma_wide(lo, mh, lo, nh, fresh);
+        early_reads<MH * NH, NB>();
+        read_wide_a(cur, a_hi, mh);
+        mma_wide(lo, mh, b_hi, nh, fresh);
+        early_reads<MH * NH, MB>();
         hand_over();
+        if (read_on) read_wide_a(oth, lo, mh);
+        mma_wide(a_hi, mh, lo, nh, fresh);
+        early_reads<MH * NH, MB>();
         if constexpr (MID && kQuarters) {
           if constexpr (!kPairs) issue_a(c, st, second_half);
           issue_b(c, st, whole);
         }
         if (read_on) read_wide_b(oth, lo, nh);
-        rows_then_reads(mh, b_hi, oth, std::false_type{}, read_on);
+        mma_wide(a_hi, mh, b_hi, nh, fresh);
+        early_reads<MH * NH, NB>();
       } else if constexpr (kQuarters) {
         // Four quarters per sub-step: (first half of A, one half of B), the other
         // half of B, then the second half of A with B's halves the other way
