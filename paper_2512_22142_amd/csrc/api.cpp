@@ -703,6 +703,20 @@ bool cut_small(const cleave_plan* plan, int cus) {
   }
 }
 
+// The same for 8-bit operands multiplied by their own instruction, whose large tile is four waves of 128 x 128: a round of
+// them against rounds of two small tiles to a CU, of which a last one with one each takes half.  us, large / small,
+// K = 4096: 3000 x 4096 65 / 56, 4096 x 4096 70 / 72, 4096 x 6144 117 / 98, 4096 x 11008 200 / 215, 16384 x 5120 x 5120
+// 375 / 419; short chains leave the large tile's stores uncovered: 8192 x 2048 x 1024 32 / 29.
+bool small_8bit(const cleave_plan* plan, int cus) {
+  const int64_t large = static_cast<int64_t>(plan->items[cleave::kTileLarge].size());
+  const int64_t fine = static_cast<int64_t>(plan->items_fine.size()), rest = fine % (2 * cus);
+  if (large == 0) return false;   // (all small already)
+  const double rounds_large = 1.85 * static_cast<double>((large + cus - 1) / cus);
+  const double rounds_small = 1.05 * (static_cast<double>(fine / (2 * cus)) + (rest == 0 ? 0.0 : rest <= cus ? 0.55 : 1.0));
+  const bool brief = plan->K <= 12 * cleave::kDirectKStep;
+  return rounds_small < rounds_large * (brief ? 1.2 : 1.0);
+}
+
 int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, const void* A,
                  int64_t lda, int transA, const void* B, int64_t ldb, int transB, int dtype,
                  float* partials, const BatchLayout& bl, void* hip_stream,
@@ -748,6 +762,9 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
                       // in-tile byte offsets are kept in 32 bits
                       lda * eb < (int64_t{1} << 22) && ldb * eb < (int64_t{1} << 22) &&
                       offsets_multiple_of(bl.a, bl.shape, e) && offsets_multiple_of(bl.b, bl.shape, e);
+  // 8-bit operands have no general kernel, and partial blocks leave theirs in whole eights of columns (cleave_linear
+  // refuses what would come here otherwise, and cleave_plan_linear does not plan it).
+  if (plan->pairs && (!direct || (!asm_to.C && !plan->all_n_mult8))) return CLEAVE_EINVAL;
   // An operand of the general kernel's 16-byte loads needs that much between the start of a
   // stored row and the end of any chunk (K-contiguous) or row (otherwise), and
   // in-tile byte offsets (up to 128 rows) that fit 32 bits.
@@ -763,7 +780,7 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
   int list_of[cleave::kNumTileClasses] = {task_ids ? -1 : 0, task_ids ? -1 : 1};
   // (8-bit operands multiplied as bf16 have no large shape)
   const bool no_large = plan->pairs && !(asm_to.C && asm_to.out_dtype == CLEAVE_BF16);
-  if (!task_ids && (!direct || no_large || cut_small(plan, cus))) {
+  if (!task_ids && (!direct || no_large || (plan->pairs ? small_8bit(plan, cus) : cut_small(plan, cus)))) {
     list_of[cleave::kTileSmall] = cleave::kNumTileClasses;
     d_lists[cleave::kTileLarge] = nullptr;
     counts[cleave::kTileLarge] = 0;
@@ -839,7 +856,6 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
     args.stream_below_k = task_ids ? 0 : streamed_below(plan, asm_to);
     args.c_bf16 = asm_to.out_dtype == CLEAVE_BF16 ? 1 : 0;
     const bool large = c == cleave::kTileLarge;
-    if (plan->pairs && !direct) return launch_failed(hipErrorInvalidValue);   // (cleave_linear has refused what leads here)
     if (direct) {
       // Persistent workgroups, as many as the chip holds at once: each walks
       // the item list with the grid as stride and fetches the head of its next
@@ -1144,18 +1160,20 @@ namespace {
 // where K is.
 //   Few rows, us, 1, 2, 4, 8, 16 splits: one row, bf16, K = 4096, N = 512 11.5, 11.1, 9.3, 8.5, 8.3, 2048 10.9, 10.9, 8.6, 8.6,
 // 9.1, 4096 11.7, 12.3, 9.3, 10.0, 10.6, 5120 12.9, 13.0, 13.2, 13.7, 13.7, 8192 13.2, 15.7, 15.1, 16.6, 16.9, 11008 17.6,
-// 19.8, 19.3, 19.9, 19.8: a CU's own loads are the limit of 64 workgroups, so up to 80 split, to one per CU.
+// 19.8, 19.3, 19.9, 19.8: a CU's own loads are the limit of 64 workgroups, so up to 80 split, to one per CU,
+// where a row of K has 5 KB or more.
 //   Tiles, us, 1, 2, 4, 8 splits: bf16, 64 x 512 x 11008 32.5, 20.6, 13.6, 14.2, 128 x 768 x 3072 11.8, 10.5, 9.1, 12.2, 300 x 512 x
 // 4096 14.8, 12.7, 10.3, 14.4, 64 x 4096 x 4096 16.8, 15.0, 15.3, 19.7, 500 x 1024 x 4096 15.4, 14.3, 15.3, 19.1, 256 x 4096 x 4096
 // 17.5, 21.7, 21.0, 26.0, 64 x 4096 x 1024 6.7, 9.2, 9.8, 15.2; where two splits make one 128 x 128 item per CU, 64 x 11008 x
 // 4096 29.1, 23.2, 24.7, 29.5, 128 x 11008 x 4096 29.3, 24.9, 27.9, 33.3, 256 x 8192 x 4096 29.3, 28.1, 30.9, 39.2; fp32, whose chains
 // are bound by their products, 64 x 4096 x 4096 72, 43, 28, 32, 167 x 1226 x 4793 84, 53, 51, 56.
-int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e) {
+int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e, bool pairs) {
   constexpr int64_t kCUs = 256;
+  if (pairs && M > cleave::kFewRows && N % 8 != 0) return 1;   // (partial blocks leave the 8-bit kernel in whole eights)
   int64_t want = 1;
   if (M <= cleave::kFewRows) {
     const int64_t groups = (N + 63) / 64;
-    if (groups <= 80) want = std::min<int64_t>({kCUs / groups, K / (32 * e), 16});
+    if (groups <= 80 && K * 16 / e >= 5120) want = std::min<int64_t>({kCUs / groups, K / (32 * e), 16});
   } else {
     const int64_t parts = ((M + 63) / 64) * ((N + 63) / 64);
     const int64_t items = ((M + 127) / 128) * ((N + 127) / 128);
@@ -1184,7 +1202,7 @@ extern "C" int cleave_plan_linear(int64_t M, int64_t N, int64_t K, int dtype, cl
   const int64_t k = pairs ? K / 2 : K;
   const int64_t tile = M <= cleave::kFewRows ? cleave::kSmallTileRows : cleave::kLargeTileRows;
   const int rc = cleave_plan_uniform(M, N, k, tile, tile,
-                                     static_cast<int32_t>(linear_splits(M, N, k, dtype == CLEAVE_F32 ? 4 : 8)), 0, out);
+                                     static_cast<int32_t>(linear_splits(M, N, k, dtype == CLEAVE_F32 ? 4 : 8, pairs)), 0, out);
   if (rc == CLEAVE_OK) (*out)->pairs = pairs;
   return rc;
 }
@@ -1234,7 +1252,8 @@ extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, voi
 
   // Few rows: every sixteen bytes along K belong to one chunk, and every four columns of a K x N operand to its rows.
   const int64_t e = 16 / eb;
-  const bool few_rows = M <= cleave::kFewRows && !a->transA && splits >= 1 && (K + splits - 1) / splits % e == 0 && K % e == 0 &&
+  const int64_t chunk = splits >= 1 ? (plan->K + splits - 1) / splits * (e4m3 ? 2 : 1) : 0;   // the plan's, in elements
+  const bool few_rows = M <= cleave::kFewRows && !a->transA && splits >= 1 && chunk % e == 0 && K % e == 0 &&
                         a->lda % e == 0 && aligned(a->A, 16) &&
                         (a->transB ? a->ldb % e == 0 && aligned(a->B, 16)
                                    : N % 4 == 0 && a->ldb % 4 == 0 && aligned(a->B, 4 * static_cast<uintptr_t>(eb)));
@@ -1256,7 +1275,7 @@ extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, voi
     args.M = M;
     args.N = N;
     args.K = K;
-    CLEAVE_HIP(cleave::launch_linear_few_rows(args, epi, a->dtype, static_cast<int>(splits), stream));
+    CLEAVE_HIP(cleave::launch_linear_few_rows(args, epi, a->dtype, static_cast<int>(splits), chunk, stream));
     plan->last_kernel = "linear_few_rows";
   } else {
     // (nothing to do behind the sums: the blocks themselves)

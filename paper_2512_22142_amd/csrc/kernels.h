@@ -234,9 +234,10 @@ hipError_t launch_linear_general(const ExecuteArgs& args, const LinearArgs& epi,
 
 // Few rows (at most kFewRows), transA = 0: B is read once, sixteen bytes at a time.  Into args.C through the epilogue
 // or, with splits > 1, into partials[s][row][column] for launch_linear_join.  The caller has checked that
-// every 16 bytes of a row of A, and of B, belong to one chunk (see few_rows_fit in api.cpp).
+// every 16 bytes along K belong to one chunk (of `chunk` elements), every four columns of a K x N operand to its rows.
 constexpr int64_t kFewRows = 16;
-hipError_t launch_linear_few_rows(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int splits, hipStream_t stream);
+hipError_t launch_linear_few_rows(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int splits, int64_t chunk,
+                                  hipStream_t stream);
 
 // Raises the dynamic-LDS limit of every execute kernel on the current device
 // (needed once per device and process, before the first launch).

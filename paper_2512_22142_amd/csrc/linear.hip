@@ -75,7 +75,7 @@ struct Group {   // what a lane holds of a group of k's
 };
 
 template <int DTYPE, bool B_K, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, LinearArgs epi, int splits) {
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, LinearArgs epi, int splits, int64_t chunk) {
   constexpr int E = Type<DTYPE>::E, KG = 4 * E, EB = 16 / E;
   __shared__ float sums[WAVES][kFewRows][kColumns];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -83,7 +83,6 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, 
   const int64_t M = args.M, N = args.N, K = args.K;
   const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kColumns;
   // this workgroup's chunk of k, this wave's groups of it
-  const int64_t chunk = (K + splits - 1) / splits;
   const int64_t k0 = blockIdx.y * chunk, k1 = std::min(k0 + chunk, K);
   const int64_t groups = (k1 - k0 + KG - 1) / KG, per = (groups + WAVES - 1) / WAVES;
   const int64_t g0 = std::min(wave * per, groups), g1 = std::min(g0 + per, groups);
@@ -170,10 +169,10 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, 
 }
 
 template <int DTYPE, bool B_K>
-hipError_t launch_layout(const ExecuteArgs& args, const LinearArgs& epi, int splits, hipStream_t stream) {
+hipError_t launch_layout(const ExecuteArgs& args, const LinearArgs& epi, int splits, int64_t chunk, hipStream_t stream) {
   const dim3 g(static_cast<uint32_t>((args.N + kColumns - 1) / kColumns), splits);
-  if (splits > 1) hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 4>), g, dim3(256), 0, stream, args, epi, splits);
-  else hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 16>), g, dim3(1024), 0, stream, args, epi, splits);
+  if (splits > 1) hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 4>), g, dim3(256), 0, stream, args, epi, splits, chunk);
+  else hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 16>), g, dim3(1024), 0, stream, args, epi, splits, chunk);
   return hipGetLastError();
 }
 
@@ -277,13 +276,14 @@ __global__ __launch_bounds__(kJoinThreads) void linear_join_kernel(ReduceArgs ar
 
 }  // namespace
 
-hipError_t launch_linear_few_rows(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int splits, hipStream_t stream) {
-  if (dtype == CLEAVE_E4M3) return launch_layout<CLEAVE_E4M3, true>(args, epi, splits, stream);
+hipError_t launch_linear_few_rows(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int splits, int64_t chunk,
+                                  hipStream_t stream) {
+  if (dtype == CLEAVE_E4M3) return launch_layout<CLEAVE_E4M3, true>(args, epi, splits, chunk, stream);
   if (dtype == CLEAVE_BF16)
-    return args.transB ? launch_layout<CLEAVE_BF16, true>(args, epi, splits, stream)
-                       : launch_layout<CLEAVE_BF16, false>(args, epi, splits, stream);
-  return args.transB ? launch_layout<CLEAVE_F32, true>(args, epi, splits, stream)
-                     : launch_layout<CLEAVE_F32, false>(args, epi, splits, stream);
+    return args.transB ? launch_layout<CLEAVE_BF16, true>(args, epi, splits, chunk, stream)
+                       : launch_layout<CLEAVE_BF16, false>(args, epi, splits, chunk, stream);
+  return args.transB ? launch_layout<CLEAVE_F32, true>(args, epi, splits, chunk, stream)
+                     : launch_layout<CLEAVE_F32, false>(args, epi, splits, chunk, stream);
 }
 
 hipError_t launch_linear_join(const ReduceArgs& args, const LinearArgs& epi, int64_t M, int64_t N, int splits, int out_dtype,

@@ -124,7 +124,8 @@ def test_fp32(size, epilogue, transB):
 
 
 E4M3_SIZES = [(1, 128, 256), (1, 11, 16), (3, 136, 80), (16, 257, 512), (33, 130, 1008), (64, 512, 4096), (65, 128, 64), (130, 261, 96),
-              (256, 256, 256), (300, 523, 208), (513, 256, 64), (1000, 768, 1024), (100, 64, 4096), (2048, 512, 128)]
+              (256, 256, 256), (300, 523, 208), (513, 256, 64), (1000, 768, 1024), (100, 64, 4096), (2048, 512, 128),
+              (100, 67, 8192), (16, 67, 8208), (9, 200, 11008), (300, 200, 8192), (1100, 203, 6016)]
 
 
 @pytest.mark.parametrize("size", E4M3_SIZES)
@@ -269,6 +270,22 @@ def test_what_is_not_finite_stays_in_its_row(size):
         cleave.linear(plan, A, B, C, act_grad=act, preact=z, partials=ws)
         cleave.linear(plan, A, B, plain, partials=ws)
         assert torch.all(C[0] == 0) and torch.equal(C[1:], plain[1:]), act
+
+
+def test_8_bit_values_that_are_not_a_number_stay_in_their_row():
+    for M, N, K in ((4, 128, 256), (100, 64, 8192), (300, 523, 208), (600, 512, 512)):
+        A, B = matrix(M, K, E4M3, 1, std=50.0)[0], matrix(N, K, E4M3, 2, std=5.0)[0]
+        A.view(torch.uint8)[1, K // 3] = 0x7f
+        B.view(torch.uint8)[5, K // 2] = 0xff
+        plan = cleave.plan_linear(M, N, K, E4M3)
+        ws = torch.empty(max(1, plan.linear_workspace), device="cuda")
+        for out in (BF16, F32):
+            C = torch.empty(M, N, dtype=out, device="cuda")
+            cleave.linear(plan, A, B, C, transB=1, scale_a=torch.ones(M, device="cuda"), scale_b=torch.ones(N, device="cuda"),
+                          partials=ws)
+            assert torch.all(C[1].isnan()) and torch.all(C[:, 5].isnan())
+            C[1], C[:, 5] = 0, 0
+            assert torch.all(C.isfinite())
 
 
 def test_a_leading_dimension_beyond_32_bits_of_bytes():
