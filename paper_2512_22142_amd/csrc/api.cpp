@@ -1166,7 +1166,9 @@ namespace {
 // 4096 14.8, 12.7, 10.3, 14.4, 64 x 4096 x 4096 16.8, 15.0, 15.3, 19.7, 500 x 1024 x 4096 15.4, 14.3, 15.3, 19.1, 256 x 4096 x 4096
 // 17.5, 21.7, 21.0, 26.0, 64 x 4096 x 1024 6.7, 9.2, 9.8, 15.2; where two splits make one 128 x 128 item per CU, 64 x 11008 x
 // 4096 29.1, 23.2, 24.7, 29.5, 128 x 11008 x 4096 29.3, 24.9, 27.9, 33.3, 256 x 8192 x 4096 29.3, 28.1, 30.9, 39.2; fp32, whose chains
-// are bound by their products, 64 x 4096 x 4096 72, 43, 28, 32, 167 x 1226 x 4793 84, 53, 51, 56.
+// are bound by their products, 64 x 4096 x 4096 72, 43, 28, 32, 167 x 1226 x 4793 84, 53, 51, 56, 500 x 1000 x 1000 24, 19, 20, 27:
+// to one item per CU, and long ones to two (two items of a CU fill each other's gaps), 1590 x 313 x 3890 74, 78, 60, 69,
+// 162 x 2752 x 7768 138, 132, 98, 103; 1000 x 1000 x 4000, a part per CU as it is, 81, 82, 77, 80.
 int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e, bool pairs) {
   constexpr int64_t kCUs = 256;
   if (pairs && M > cleave::kFewRows && N % 8 != 0) return 1;   // (partial blocks leave the 8-bit kernel in whole eights)
@@ -1177,14 +1179,15 @@ int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e, bool pairs) {
   } else {
     const int64_t parts = ((M + 63) / 64) * ((N + 63) / 64);
     const int64_t items = ((M + 127) / 128) * ((N + 127) / 128);
-    if (e == 4) want = std::min<int64_t>({kCUs / parts, K / 256, 4});
+    const int64_t per_cu = K >= 2048 && parts <= kCUs * 3 / 4 ? (2 * kCUs + parts - 1) / parts : kCUs / parts;
+    if (e == 4) want = std::min<int64_t>({per_cu, K / 256, 4});
     else if (K >= 3000 && parts <= 48) want = 4;
     else if (K >= 3000 && (parts <= kCUs / 2 || (items > kCUs / 4 && items <= kCUs / 2))) want = 2;
   }
   for (int64_t S = want; S > 1; --S) {
     const int64_t chunk = (K + S - 1) / S;
-    // (what general tiles take at any length anyway is split at any)
-    if ((S - 1) * chunk < K && (chunk % e == 0 || K % e != 0 || (e == 4 && M > cleave::kFewRows))) return S;
+    // (what takes chunks of any length anyway is split at any)
+    if ((S - 1) * chunk < K && (chunk % e == 0 || K % e != 0 || e == 4)) return S;
   }
   return 1;
 }
@@ -1250,13 +1253,8 @@ extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, voi
   int rc = ensure_uploaded(plan);
   if (rc != CLEAVE_OK) return rc;
 
-  // Few rows: every sixteen bytes along K belong to one chunk, and every four columns of a K x N operand to its rows.
-  const int64_t e = 16 / eb;
-  const int64_t chunk = splits >= 1 ? (plan->K + splits - 1) / splits * (e4m3 ? 2 : 1) : 0;   // the plan's, in elements
-  const bool few_rows = M <= cleave::kFewRows && !a->transA && splits >= 1 && chunk % e == 0 && K % e == 0 &&
-                        a->lda % e == 0 && aligned(a->A, 16) &&
-                        (a->transB ? a->ldb % e == 0 && aligned(a->B, 16)
-                                   : N % 4 == 0 && a->ldb % 4 == 0 && aligned(a->B, 4 * static_cast<uintptr_t>(eb)));
+  const bool few_rows = M <= cleave::kFewRows && !a->transA && splits >= 1;
+  const int64_t chunk = few_rows ? (plan->K + splits - 1) / splits * (e4m3 ? 2 : 1) : 0;   // the plan's, in elements
   AssembleTarget to;
   to.C = joined ? nullptr : a->C;
   to.ldc = a->ldc;

@@ -232,9 +232,8 @@ hipError_t launch_linear_8bit(const ExecuteArgs& args, const LinearArgs& epi, Di
 hipError_t launch_linear_general(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int tile_class,
                                  const GeneralLoads& how, hipStream_t stream);
 
-// Few rows (at most kFewRows), transA = 0: B is read once, sixteen bytes at a time.  Into args.C through the epilogue
-// or, with splits > 1, into partials[s][row][column] for launch_linear_join.  The caller has checked that
-// every 16 bytes along K belong to one chunk (of `chunk` elements), every four columns of a K x N operand to its rows.
+// Few rows (at most kFewRows), transA = 0, any size, stride and alignment: B is read once.  Into args.C through the
+// epilogue or, with splits > 1, chunks of `chunk` elements into partials[s][row][column] for launch_linear_join.
 constexpr int64_t kFewRows = 16;
 hipError_t launch_linear_few_rows(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int splits, int64_t chunk,
                                   hipStream_t stream);

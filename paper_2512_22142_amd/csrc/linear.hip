@@ -63,6 +63,28 @@ __device__ __forceinline__ f32x4 multiply(u32x4 x, u32x4 w, f32x4 acc) {
   }
 }
 
+// Reads at any alignment.
+template <typename V>
+__device__ __forceinline__ V read_any(const unsigned char* p) {
+  typedef uint32_t U4 __attribute__((ext_vector_type(4), aligned(1)));
+  typedef uint32_t U2 __attribute__((ext_vector_type(2), aligned(1)));
+  if constexpr (sizeof(V) == 16) return *reinterpret_cast<const U4*>(p);
+  else return *reinterpret_cast<const U2*>(p);
+}
+// The first `n` elements of EB bytes, fewer than V holds; zeros behind them.
+template <typename V, int EB>
+__device__ __forceinline__ V read_some(const unsigned char* p, int n) {
+  V w{};
+#pragma unroll
+  for (int e = 0; e < static_cast<int>(sizeof(V)) / EB; ++e) {
+    if (e >= n) continue;
+    if constexpr (EB == 4) w[e] = reinterpret_cast<const uint32_t*>(p)[e];
+    else if constexpr (EB == 2) w[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[e]) << (16 * (e % 2));
+    else w[e / 4] |= static_cast<uint32_t>(p[e]) << (8 * (e % 4));
+  }
+  return w;
+}
+
 // Sixteen bytes of a K x N operand's row, or the eight that hold four bf16.
 template <int DTYPE>
 using Columns4 = typename std::conditional<DTYPE == CLEAVE_BF16, u32x2, u32x4>::type;
@@ -87,31 +109,44 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, 
   const int64_t groups = (k1 - k0 + KG - 1) / KG, per = (groups + WAVES - 1) / WAVES;
   const int64_t g0 = std::min(wave * per, groups), g1 = std::min(g0 + per, groups);
 
-  // rows and columns that are not there repeat the last one: their sums are not stored
+  // rows and columns that are not there repeat the last ones: their sums are not stored, or are the same twice
   const unsigned char* const B = static_cast<const unsigned char*>(args.B);
   const unsigned char* const xp =
       static_cast<const unsigned char*>(args.A) + (std::min<int64_t>(l16, M - 1) * args.lda + E * lq) * EB;
+  const int first = static_cast<int>(std::min<int64_t>(4 * l16, std::max<int64_t>(N - 4, 0) - n0));   // of a K x N row's four
   const unsigned char* wp[B_K ? 4 : 1];
   if constexpr (B_K) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) wp[c] = B + (std::min<int64_t>(n0 + 16 * c + l16, N - 1) * args.ldb + E * lq) * EB;
   } else {
-    wp[0] = B + std::min<int64_t>(n0 + 4 * l16, N - 4) * EB;
+    wp[0] = B + (n0 + first) * EB;
   }
   typedef Group<DTYPE, B_K> G;
   const auto load = [&](int64_t g, G& to) {
     const int64_t k = k0 + g * KG;          // wave-uniform
-    const bool valid = k + E * lq < k1;     // all E of them: chunks and rows are whole sixteen bytes
-    to.x = valid ? *reinterpret_cast<const u32x4*>(xp + k * EB) : u32x4{};
+    typedef Columns4<DTYPE> C;
+    if (k + KG <= k1 && (B_K || N >= 4)) {
+      to.x = read_any<u32x4>(xp + k * EB);
+      if constexpr (B_K) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) to.w[c] = read_any<u32x4>(wp[c] + k * EB);
+      } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) to.w[i] = read_any<C>(wp[0] + (k + E * lq + i) * args.ldb * EB);
+      }
+      return;
+    }
+    // the chunk's last group, or rows of fewer than four: only what is there
+    const int left = static_cast<int>(std::min<int64_t>(std::max<int64_t>(k1 - k - E * lq, 0), E));
+    to.x = read_some<u32x4, EB>(xp + k * EB, left);
     if constexpr (B_K) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) to.w[c] = valid ? *reinterpret_cast<const u32x4*>(wp[c] + k * EB) : u32x4{};
+      for (int c = 0; c < 4; ++c) to.w[c] = read_some<u32x4, EB>(wp[c] + k * EB, left);
     } else {
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        typedef Columns4<DTYPE> C;
-        to.w[i] = valid ? *reinterpret_cast<const C*>(wp[0] + (k + E * lq + i) * args.ldb * EB) : C{};
-      }
+      for (int i = 0; i < E; ++i)
+        to.w[i] = i < left ? read_some<C, EB>(wp[0] + (k + E * lq + i) * args.ldb * EB, static_cast<int>(std::min<int64_t>(N, 4)))
+                           : C{};
     }
   };
   f32x4 acc[4] = {};
@@ -148,12 +183,14 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, 
     }
   }
 
-  // Lane (l16, lq) has rows 4 lq + j of columns 4 l16 + c (K x N) or 16 c + l16 (N x K).
+  // Lane (l16, lq) has rows 4 lq + j of columns first + c (K x N; some may be the workgroup's before) or 16 c + l16 (N x K).
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
+  for (int c = 0; c < 4; ++c) {
+    const int col = B_K ? 16 * c + l16 : first + c;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (4 * lq + j < M) sums[wave][4 * lq + j][B_K ? 16 * c + l16 : 4 * l16 + c] = acc[c][j];
+      if (4 * lq + j < M && col >= 0) sums[wave][4 * lq + j][col] = acc[c][j];
+  }
   __syncthreads();
   for (int at = threadIdx.x; at < static_cast<int>(M) * kColumns; at += 64 * WAVES) {
     const int row = at / kColumns, col = at % kColumns;

@@ -342,3 +342,20 @@ def test_refusals():
     with pytest.raises(cleave.CleaveError):                            # a plan of 8-bit operands is no other call's
         cleave.execute(plan8, torch.zeros(4, 8, device="cuda", dtype=BF16), torch.zeros(8, 8, device="cuda", dtype=BF16),
                        torch.empty(plan8.partial_elems, device="cuda"))
+
+
+@pytest.mark.parametrize("size", [(1, 1001, 333), (2, 1067, 674), (16, 130, 4099), (5, 3, 70), (4, 2, 1), (7, 65, 31)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("transB", [0, 1])
+@pytest.mark.parametrize("epilogue", [0, 1, 2])
+def test_few_rows_of_any_length(size, dtype, transB, epilogue):
+    assert check(*size, dtype=dtype, transB=transB, **EPILOGUES[epilogue])[2] == "linear_few_rows"
+    check(*size, dtype=dtype, transB=transB, pad=3, shift=1, **EPILOGUES[epilogue])
+
+
+@pytest.mark.parametrize("size,splits", [((3, 67, 1000), 3), ((16, 33, 515), 4), ((1, 5, 130), 2)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("transB", [0, 1])
+def test_few_rows_split_at_any_length(size, splits, dtype, transB):
+    plan = cleave.plan_uniform(*size, 64, 64, splits)
+    check(*size, dtype=dtype, transB=transB, plan=plan, **EPILOGUES[1])
