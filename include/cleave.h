@@ -467,7 +467,7 @@ int cleave_bias_grad(int64_t rows, int64_t cols, const void* dy, int64_t lddy, i
  *
  * plan: one GEMM (not batched), best cleave_plan_linear's, which chooses tiles and splits
  * of K for M, N, K and dtype; for CLEAVE_E4M3 it must be that (K a multiple of 16; its tasks
- * and dims count K in pairs of values, and the other calls refuse it).  partials: cleave_linear_workspace(plan)
+ * and dims count K in pairs of values; execute, verify and reduce calls refuse it).  partials: cleave_linear_workspace(plan)
  * floats (may be NULL if that is 0), of this call alone while it runs.
  * Few rows (M <= 16) read B once, as fast as memory gives it.  Bits: a function of the
  * arguments' values, sizes and alignment.  Asynchronous; the plan's tables are uploaded by the first call or

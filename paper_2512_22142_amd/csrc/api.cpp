@@ -996,7 +996,7 @@ struct ReduceEpilogue {
 int reduce_impl(cleave_plan* plan, const float* partials, void* C, int64_t ldc, int out_dtype,
                 const BatchLayout& bl, void* hip_stream,
                 const ReduceEpilogue& epi = ReduceEpilogue{}, bool members_aligned = true) {
-  if (!plan || !partials || !C) return CLEAVE_EINVAL;
+  if (!plan || plan->pairs || !partials || !C) return CLEAVE_EINVAL;   // (pairs: a plan of 8-bit operands)
   if (out_dtype != CLEAVE_F32 && out_dtype != CLEAVE_BF16) return CLEAVE_EINVAL;
   if (ldc < plan->N) return CLEAVE_EINVAL;
   const int ob = out_dtype == CLEAVE_BF16 ? 2 : 4;
@@ -1253,7 +1253,8 @@ extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, voi
   int rc = ensure_uploaded(plan);
   if (rc != CLEAVE_OK) return rc;
 
-  const bool few_rows = M <= cleave::kFewRows && !a->transA && splits >= 1;
+  // (a launch has fewer than 2^32 threads)
+  const bool few_rows = M <= cleave::kFewRows && !a->transA && splits >= 1 && N <= int64_t{1} << 27;
   const int64_t chunk = few_rows ? (plan->K + splits - 1) / splits * (e4m3 ? 2 : 1) : 0;   // the plan's, in elements
   AssembleTarget to;
   to.C = joined ? nullptr : a->C;
@@ -1441,6 +1442,7 @@ int verify_impl(cleave_plan* plan, const void* A, int64_t lda, int transA, const
                 double* lhs, double* rhs, double* scale, int32_t* accept, const BatchLayout& bl,
                 void* hip_stream, const AggregateTarget& agg = AggregateTarget{}) {
   if (!plan || !A || !B || !partials || !r || !s || !accept) return CLEAVE_EINVAL;
+  if (plan->pairs) return CLEAVE_EINVAL;   // a plan of 8-bit operands
   if (dtype != CLEAVE_F32 && dtype != CLEAVE_BF16) return CLEAVE_EINVAL;
   if ((transA != 0 && transA != 1) || (transB != 0 && transB != 1)) return CLEAVE_EINVAL;
   if (lda < (transA ? plan->M : plan->K) || ldb < (transB ? plan->K : plan->N)) return CLEAVE_EINVAL;

@@ -372,7 +372,7 @@ hipError_t launch_sum(const ColumnSumArgs& args, hipStream_t stream) {
 // The rows of partial sums: sixteen columns to a workgroup and 64 rows at a time, so that a few hundred rows are a few loads
 // of each thread.
 constexpr int kJoinThreads = 1024, kJoinCols = 16;
-__global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in, int rows, int64_t cols, float* out) {
+__global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in, int rows, int64_t ld, int64_t cols, float* out) {
   constexpr int kRows = kJoinThreads / kJoinCols;
   __shared__ float part[kJoinThreads / 64][kJoinCols];
   const int at = threadIdx.x % kJoinCols, first = threadIdx.x / kJoinCols;
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in
   float sum = 0.0f;
   if (c < cols) {
 #pragma unroll 8
-    for (int row = first; row < rows; row += kRows) sum += in[row * cols + c];
+    for (int row = first; row < rows; row += kRows) sum += in[row * ld + c];
   }
   // a wave's four rows, then the waves
   sum += __shfl_xor(sum, 16);
@@ -396,8 +396,27 @@ __global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in
 
 }  // namespace
 
+// A launch has fewer than 2^32 threads: more rows (columns, of a join) than these take several.
+constexpr int64_t kLaunchRows = int64_t{1} << 21, kLaunchCols = int64_t{1} << 25;
+
 hipError_t launch_rms_norm(const NormArgs& args, int dtype, hipStream_t stream) {
-  return dtype == CLEAVE_BF16 ? launch_norm_of<Bf16>(args, stream) : launch_norm_of<float>(args, stream);
+  const int64_t eb = dtype == CLEAVE_BF16 ? 2 : 4, yb = args.scales ? 1 : eb;
+  for (int64_t row = 0; row < args.rows; row += kLaunchRows) {
+    const auto down = [&](auto* p, int64_t bytes) {
+      return p ? reinterpret_cast<decltype(p)>(reinterpret_cast<uintptr_t>(p) + row * bytes) : p;
+    };
+    NormArgs some = args;
+    some.rows = std::min(args.rows - row, kLaunchRows);
+    some.x = down(args.x, args.ldx * eb);
+    some.residual = down(args.residual, args.ldr * eb);
+    some.sum_out = down(args.sum_out, args.lds * eb);
+    some.y = down(args.y, args.ldy * yb);
+    some.scales = down(args.scales, 4);
+    some.inv_rms = down(args.inv_rms, 4);
+    const hipError_t e = dtype == CLEAVE_BF16 ? launch_norm_of<Bf16>(some, stream) : launch_norm_of<float>(some, stream);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // Workgroups of the gradient: what the CUs hold at a time, where every group of threads gets a few rows.  (Narrow rows have four
@@ -420,9 +439,14 @@ int column_sum_chunks(int64_t rows, int64_t cols) {
 }
 
 hipError_t launch_join_rows(const float* rows, int n, int64_t cols, float* out, hipStream_t stream) {
-  hipLaunchKernelGGL(join_rows_kernel, dim3(static_cast<uint32_t>((cols + kJoinCols - 1) / kJoinCols)), dim3(kJoinThreads), 0,
-                     stream, rows, n, cols, out);
-  return hipGetLastError();
+  for (int64_t c = 0; c < cols; c += kLaunchCols) {
+    const int64_t some = std::min(cols - c, kLaunchCols);
+    hipLaunchKernelGGL(join_rows_kernel, dim3(static_cast<uint32_t>((some + kJoinCols - 1) / kJoinCols)), dim3(kJoinThreads), 0,
+                       stream, rows + c, n, cols, some, out + c);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, hipStream_t stream) {

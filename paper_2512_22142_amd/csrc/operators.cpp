@@ -150,23 +150,30 @@ extern "C" int cleave_adamw(int64_t n_tensors, const int64_t* sizes, float* cons
     chunks = 0;
     return e;
   };
-  for (int64_t k = 0; k < n_tensors; ++k) {
-    const int64_t n = sizes[k];
-    if (n == 0) continue;
+  // (a launch has fewer than 2^32 threads: a tensor of more chunks goes in pieces)
+  constexpr int64_t kChunks = int64_t{1} << 23, kPiece = kChunks * cleave::kAdamChunk;
+  const auto add = [&](int64_t k, int64_t from) -> hipError_t {
+    const int64_t n = std::min(sizes[k] - from, kPiece);
     const int64_t more = (n + cleave::kAdamChunk - 1) / cleave::kAdamChunk;
-    if (args.n_tensors == cleave::kAdamTensors || chunks + more > kMost) CLEAVE_HIP(launch());
+    if (args.n_tensors == cleave::kAdamTensors || chunks + more > kChunks) {
+      const hipError_t e = launch();
+      if (e != hipSuccess) return e;
+    }
     cleave::AdamTensor& t = args.tensors[args.n_tensors];
-    t.w = w[k];
-    t.g = g[k];
-    t.m = m[k];
-    t.v = v[k];
-    t.m_scale = states_8bit ? m_scale[k] : nullptr;
-    t.v_scale = states_8bit ? v_scale[k] : nullptr;
-    t.copy = w_bf16 ? static_cast<uint16_t*>(w_bf16[k]) : nullptr;
+    t.w = w[k] + from;
+    t.g = static_cast<const unsigned char*>(g[k]) + from * gb;
+    t.m = static_cast<unsigned char*>(m[k]) + from * static_cast<int64_t>(sb);
+    t.v = static_cast<unsigned char*>(v[k]) + from * static_cast<int64_t>(sb);
+    t.m_scale = states_8bit ? m_scale[k] + from / 256 : nullptr;
+    t.v_scale = states_8bit ? v_scale[k] + from / 256 : nullptr;
+    t.copy = w_bf16 ? static_cast<uint16_t*>(w_bf16[k]) + from : nullptr;
     t.n = static_cast<uint64_t>(n);
     chunks += more;
     args.chunk_end[args.n_tensors++] = static_cast<uint32_t>(chunks);
-  }
+    return hipSuccess;
+  };
+  for (int64_t k = 0; k < n_tensors; ++k)
+    for (int64_t from = 0; from < sizes[k]; from += kPiece) CLEAVE_HIP(add(k, from));
   CLEAVE_HIP(launch());
   return CLEAVE_OK;
 }

@@ -250,3 +250,8 @@ def test_refusals():
         cleave.rms_norm_backward(x, x, w, s, y, torch.empty(64, device="cuda"), torch.empty(3, device="cuda"))
     with pytest.raises(ValueError):
         cleave.bias_grad(x, torch.empty(63, device="cuda"), torch.empty(4096, device="cuda"))
+
+
+@pytest.mark.parametrize("out", [BF16, E4M3])
+def test_norm_of_more_rows_than_one_launch_takes(out):
+    run_norm(2 ** 21 + 77, 3, BF16, out, True)
