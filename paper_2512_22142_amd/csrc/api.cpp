@@ -1165,10 +1165,31 @@ namespace {
 //   Tiles, us, 1, 2, 4, 8 splits: bf16, 64 x 512 x 11008 32.5, 20.6, 13.6, 14.2, 128 x 768 x 3072 11.8, 10.5, 9.1, 12.2, 300 x 512 x
 // 4096 14.8, 12.7, 10.3, 14.4, 64 x 4096 x 4096 16.8, 15.0, 15.3, 19.7, 500 x 1024 x 4096 15.4, 14.3, 15.3, 19.1, 256 x 4096 x 4096
 // 17.5, 21.7, 21.0, 26.0, 64 x 4096 x 1024 6.7, 9.2, 9.8, 15.2; where two splits make one 128 x 128 item per CU, 64 x 11008 x
-// 4096 29.1, 23.2, 24.7, 29.5, 128 x 11008 x 4096 29.3, 24.9, 27.9, 33.3, 256 x 8192 x 4096 29.3, 28.1, 30.9, 39.2; fp32, whose chains
-// are bound by their products, 64 x 4096 x 4096 72, 43, 28, 32, 167 x 1226 x 4793 84, 53, 51, 56, 500 x 1000 x 1000 24, 19, 20, 27:
-// to one item per CU, and long ones to two (two items of a CU fill each other's gaps), 1590 x 313 x 3890 74, 78, 60, 69,
-// 162 x 2752 x 7768 138, 132, 98, 103; 1000 x 1000 x 4000, a part per CU as it is, 81, 82, 77, 80.
+// 4096 29.1, 23.2, 24.7, 29.5, 128 x 11008 x 4096 29.3, 24.9, 27.9, 33.3, 256 x 8192 x 4096 29.3, 28.1, 30.9, 39.2.
+//   fp32 is bound by its products: a 64 x 64 part takes 17.6 ns per k alone on its CU, two on one CU twice that, so the
+// time is the most parts that a CU gets times their chunks, and the join with the partial sums' way.  Up to three parts per CU,
+// beyond which the last round counts for little, the least of one to four splits is taken, us, 1, 2, 3, 4 splits: 64 x 4096 x 4096 71, 42, 32, 28, 500 x 1000 x 1000 24, 19, 22, 21, 1590 x 313 x 3890 75, 50,
+// 58, 50, 162 x 2752 x 7768 136, 122, 92, 101, 1300 x 1226 x 4793 153, 158, 139, 150, 3835 x 704 x 3904 250, 195, 179, 186,
+// 1000 x 1000 x 4000, a part per CU as it is, 73, 81, 78, 77.
+struct Fp32Splits {
+  int64_t splits, workgroups;
+};
+Fp32Splits fp32_splits(int64_t M, int64_t N, int64_t K) {
+  constexpr int64_t kCUs = 256;
+  const int64_t parts = ((M + 63) / 64) * ((N + 63) / 64);
+  int64_t best = 1;
+  double least = 0.0;
+  const int64_t most = parts <= 3 * kCUs ? std::min<int64_t>(4, K / 256) : 1;
+  for (int64_t S = 1; S <= std::max<int64_t>(most, 1); ++S) {
+    const int64_t chunk = (K + S - 1) / S;
+    double us = 0.0176 * static_cast<double>((parts * S + kCUs - 1) / kCUs * chunk);
+    if (S > 1) us += 4.0 + 2.0 * 16384.0 * static_cast<double>(parts * S) / 4.5e6;
+    if (S > 1 && us >= least) continue;
+    least = us;
+    best = S;
+  }
+  return {best, parts * best};
+}
 int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e, bool pairs) {
   constexpr int64_t kCUs = 256;
   if (pairs && M > cleave::kFewRows && N % 8 != 0) return 1;   // (partial blocks leave the 8-bit kernel in whole eights)
@@ -1179,9 +1200,8 @@ int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e, bool pairs) {
   } else {
     const int64_t parts = ((M + 63) / 64) * ((N + 63) / 64);
     const int64_t items = ((M + 127) / 128) * ((N + 127) / 128);
-    const int64_t per_cu = K >= 2048 && parts <= kCUs * 3 / 4 ? (2 * kCUs + parts - 1) / parts : kCUs / parts;
-    if (e == 4) want = std::min<int64_t>({per_cu, K / 256, 4});
-    else if (K >= 3000 && parts <= 48) want = 4;
+    if (e == 4) return fp32_splits(M, N, K).splits;
+    if (K >= 3000 && parts <= 48) want = 4;
     else if (K >= 3000 && (parts <= kCUs / 2 || (items > kCUs / 4 && items <= kCUs / 2))) want = 2;
   }
   for (int64_t S = want; S > 1; --S) {
@@ -1203,7 +1223,13 @@ extern "C" int cleave_plan_linear(int64_t M, int64_t N, int64_t K, int dtype, cl
   const bool pairs = dtype == CLEAVE_E4M3;
   if (pairs && K % 16 != 0) return CLEAVE_EINVAL;
   const int64_t k = pairs ? K / 2 : K;
-  const int64_t tile = M <= cleave::kFewRows ? cleave::kSmallTileRows : cleave::kLargeTileRows;
+  // (fp32 in tiles of one part each where several go to a CU: parts of larger tiles that hold nothing would take their turn
+  // among them.  us, 64 x 64 / 256 x 256: 167 x 1226 x 4793 in 4 splits 35 / 51, 162 x 2752 x 7768 in 3 92 / 126; in one split, and
+  // few parts, which are quartered, 2048 x 2048 x 2048 147 / 137, 124 x 768 x 2432 in 4 19 / 16)
+  const Fp32Splits parts = dtype == CLEAVE_F32 ? fp32_splits(M, N, K) : Fp32Splits{1, 0};
+  const int64_t tile = M <= cleave::kFewRows                        ? cleave::kSmallTileRows
+                       : parts.splits > 1 && parts.workgroups > 128 ? 64
+                                                                    : cleave::kLargeTileRows;
   const int rc = cleave_plan_uniform(M, N, k, tile, tile,
                                      static_cast<int32_t>(linear_splits(M, N, k, dtype == CLEAVE_F32 ? 4 : 8, pairs)), 0, out);
   if (rc == CLEAVE_OK) (*out)->pairs = pairs;
