@@ -1158,10 +1158,11 @@ namespace {
 // Splits of K for products whose tiles alone leave CUs idle: a second launch joins them (3 to 4 us with the partial sums'
 // way), so only chains of some length are split.  The chunks are whole sixteen bytes of the operands (`e` elements)
 // where K is.
-//   Few rows, us, 1, 2, 4, 8, 16 splits: one row, bf16, K = 4096, N = 512 11.5, 11.1, 9.3, 8.5, 8.3, 2048 10.9, 10.9, 8.6, 8.6,
-// 9.1, 4096 11.7, 12.3, 9.3, 10.0, 10.6, 5120 12.9, 13.0, 13.2, 13.7, 13.7, 8192 13.2, 15.7, 15.1, 16.6, 16.9, 11008 17.6,
-// 19.8, 19.3, 19.9, 19.8: a CU's own loads are the limit of 64 workgroups, so up to 80 split, to one per CU,
-// where a row of K has 5 KB or more.
+//   Few rows: up to 128 groups of 64 columns leave CUs without one, 257 to 384 give two to some and one to the others; where a
+// row of K has 5 KB or more those split, to one per CU, these in two.  One row, bf16, us, 1, 2, 4 splits, the weights from
+// memory / from the caches: K x N = 4096 x 4096 20, 16, 13 / 12, 12, 9, 4096 x 5632 22, 17, 17 / 14, 13, 8192 x 8192 40, 32, 32 / 24, 25,
+// stored N x K 46, 33, 35 / 34, 28, 4096 x 22016 49, 42, 43 / 34, 32; 4096 x 8192 21, 20, 19 / 14, 16, N x K 25, 19, 21 / 18, 16; as they
+// are 4096 x 11008 21, 25, 23 / 17.6, 20, 2048 x 6144 12.2, 11.7, 12.1 / 7.0, 7.7, 5120 x 27648 62, 65, 60 / 51, 53.
 //   Tiles, us, 1, 2, 4, 8 splits: bf16, 64 x 512 x 11008 32.5, 20.6, 13.6, 14.2, 128 x 768 x 3072 11.8, 10.5, 9.1, 12.2, 300 x 512 x
 // 4096 14.8, 12.7, 10.3, 14.4, 64 x 4096 x 4096 16.8, 15.0, 15.3, 19.7, 500 x 1024 x 4096 15.4, 14.3, 15.3, 19.1, 256 x 4096 x 4096
 // 17.5, 21.7, 21.0, 26.0, 64 x 4096 x 1024 6.7, 9.2, 9.8, 15.2; where two splits make one 128 x 128 item per CU, 64 x 11008 x
@@ -1196,7 +1197,10 @@ int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e, bool pairs) {
   int64_t want = 1;
   if (M <= cleave::kFewRows) {
     const int64_t groups = (N + 63) / 64;
-    if (groups <= 80 && K * 16 / e >= 5120) want = std::min<int64_t>({kCUs / groups, K / (32 * e), 16});
+    if (K * 16 / e >= 5120) {
+      if (groups <= kCUs / 2) want = std::min<int64_t>({kCUs / groups, K / (32 * e), 16});
+      else if (groups > kCUs && groups <= kCUs / 2 * 3) want = 2;
+    }
   } else {
     const int64_t parts = ((M + 63) / 64) * ((N + 63) / 64);
     const int64_t items = ((M + 127) / 128) * ((N + 127) / 128);
