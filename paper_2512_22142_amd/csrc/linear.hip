@@ -2,14 +2,16 @@
 // inner dimension with the epilogue.
 //
 // Few rows: y = x . W with at most 16 rows of x reads W once and does nothing else that counts, so it is
-// bound by memory.  A workgroup has 64 columns, its waves a run of k each; no LDS stands between the loads and the
+// bound by memory.  A workgroup has 64 columns, its waves take groups of k in turn; no LDS stands between the loads and the
 // matrix instructions (E: elements in 16 bytes; a group: 4 E k's):
 //   N x K: lane (n, q) loads the E k's from E q on of column n, and x's rows likewise: fragments as they are.
 //   K x N: lane (n, q) loads the columns 4 n .. 4 n + 3 of the rows k = E q .. E q + E - 1, sixteen lanes the 64
 //     columns of a row in one run.  It holds, for each of its four columns, the E k's of a fragment; bf16 are put
 //     together by v_perm, 4 per fragment, and fragment c belongs to the columns 4 n + c.
-// The waves are joined through LDS in wave order.  Sixteen of them leave the output itself, in one launch; where N has too
-// few columns to go round the CUs, four, whose workgroups split K and leave partial sums for a second kernel.
+// The waves are joined through LDS in wave order.  Sixteen of them leave the output itself, in one launch; where N's columns
+// go round the CUs unevenly, four, whose workgroups split K and leave partial sums for a second kernel.
+//   One row, bf16, K x N = 4096 x 11008 (90 MB): 17.6 us with the weights in the Infinity Cache (5.1 TB/s), 20.8 from memory (4.3; a
+// pass that only sums the columns takes 19 and a second launch); 8192 x 28672 97 us (4.8 TB/s).  16 rows: 18.6 and 24.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -104,10 +106,11 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, 
   const int l16 = lane & 15, lq = lane >> 4;
   const int64_t M = args.M, N = args.N, K = args.K;
   const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kColumns;
-  // this workgroup's chunk of k, this wave's groups of it
+  // this workgroup's chunk of k, of which its waves take every WAVES-th group: what they read at a time lies together.  (A run of
+  // groups each, with the weights from memory, us: 8192 x 28672 stored N x K 110 / 96, 4096 x 11008 27.1 / 23.6, K x N 21.2 / 20.8;
+  // 8192 x 8192 N x K in two chunks 33 / 36.5, K x N 31.6 / 30.0.)
   const int64_t k0 = blockIdx.y * chunk, k1 = std::min(k0 + chunk, K);
-  const int64_t groups = (k1 - k0 + KG - 1) / KG, per = (groups + WAVES - 1) / WAVES;
-  const int64_t g0 = std::min(wave * per, groups), g1 = std::min(g0 + per, groups);
+  const int64_t g1 = (k1 - k0 + KG - 1) / KG;
 
   // rows and columns that are not there repeat the last ones: their sums are not stored, or are the same twice
   const unsigned char* const B = static_cast<const unsigned char*>(args.B);
@@ -170,16 +173,16 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, 
   };
   // the next groups are on their way while one is multiplied
   G set[3];
-  int64_t g = g0;
+  int64_t g = wave;
   if (g < g1) load(g, set[0]);
-  if (g + 1 < g1) load(g + 1, set[1]);
+  if (g + WAVES < g1) load(g + WAVES, set[1]);
   while (g < g1) {
 #pragma unroll
     for (int s = 0; s < 3; ++s) {
       if (g >= g1) break;
-      if (g + 2 < g1) load(g + 2, set[(s + 2) % 3]);
+      if (g + 2 * WAVES < g1) load(g + 2 * WAVES, set[(s + 2) % 3]);
       compute(set[s]);
-      ++g;
+      g += WAVES;
     }
   }
 
