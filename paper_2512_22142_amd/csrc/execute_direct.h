@@ -907,7 +907,10 @@ using LargeShape = Shape<kLargeTileRows, kLargeTileCols, 2, 4, 64, 2, false>;
 using SmallShape = Shape<kSmallTileRows, kSmallTileCols, 2, 2, 64, 2, false>;
 // 8-bit operands have twice the products per byte, and what bounds them is the LDS: 256 x 256 in eight waves of 128 x 64
 // takes 125 bytes a clock of its 128 (reads and the ring's fill), in four of 128 x 128, one to a SIMD with 512
-// registers, 94.
+// registers, 94.  4096 x 11008 x 4096 178-193 us (2.0 PFLOP/s), 4096 x 4096 x 32768 2.6 PFLOP/s; the instruction from registers alone
+// gives 3.8.  A K step takes 1.57 us, its matrix instructions 1.1 of them; what bounds it is the fragments' way through the LDS
+// between two barriers, which no other wave of the SIMD covers.  Small tiles (two workgroups to a CU) serve the sizes that
+// small_8bit picks.
 using WideShape = Shape<kLargeTileRows, kLargeTileCols, 2, 2, 64, 2, false>;
 using DeepShape = Shape<kSmallTileRows, kSmallTileCols, 2, 2, 64, 4, true>;
 using PartsShape = Shape<64, 64, 2, 2, 64, 4, true>;

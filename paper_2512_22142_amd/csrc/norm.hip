@@ -9,7 +9,9 @@
 //   dx = i (g - xhat mean(g xhat)) + dsum;   dw = sum over rows of dy xhat
 //
 // Bound by memory: every row is read once and kept in registers between its statistics, the
-// scaling and the rounding.
+// scaling and the rounding.  A copy of 512 MB runs at 5.4 TB/s here.  bf16 with a residual, the sum stored:
+//   norm            4096 x 4096 27 us (5.0 TB/s); 16384 x 5120 into e4m3 103-106 (5.6); 1 x 4096 into e4m3 5.0, a launch
+//   gradient        8192 x 4096 with dsum 53-55 us, both launches (5.0 TB/s); fp32 3001 x 1001 13.1 (2.8)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -174,7 +176,7 @@ hipError_t launch_norm_fit(const NormArgs& args, int64_t v, hipStream_t stream) 
 // Which threads share a row.  Groups of sixteen bytes beyond the row's end leave lanes idle, so a thread holds as
 // many as fit the row; wide groups of threads serve few rows, whose latency counts, narrow ones many.  us, 256 and 512
 // threads with one or two groups each / these: 16384 x 5120 bf16 into 8 bits 111 / 106, 7247 x 9984 119 / 96, 7232 x 8960
-// 97 / 87; 20000 x 768, 256 threads / a wave to a row: see the figures beside the table of kernels.
+// 97 / 87; 20000 x 768 bf16 with a residual, 256 threads / a wave to a row, 32.4 / 24.5, into 8 bits 39 / 23.
 template <typename T>
 hipError_t launch_norm_of(const NormArgs& args, hipStream_t stream) {
   const int64_t groups = (args.cols + Group16<T>::N - 1) / Group16<T>::N;
@@ -190,8 +192,9 @@ hipError_t launch_norm_of(const NormArgs& args, hipStream_t stream) {
 
 // ---- gradient ------------------------------------------------------------------
 
-// Every group of the launch takes every groups-th row and holds its part of the weight's gradient in registers until the
-// last of them: one row of partial sums for each workgroup, whose groups (a wave each, where there are several) are joined
+// dx needs a row's whole sum, dw a sum over the rows: both leave one pass over dy and h.  Every group of the launch takes
+// every groups-th row and holds its part of the weight's gradient in registers until the last of them: one row of partial sums
+// for each workgroup (8192 x 4096: 512 rows of 16 KB, 8 MB beside the 268 MB of the pass; 5 us to join), whose groups (a wave each, where there are several) are joined
 // in order.
 template <typename T, int NT, int V>
 __global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_backward_kernel(NormBackwardArgs args) {
@@ -326,7 +329,7 @@ hipError_t launch_backward_of(const NormBackwardArgs& args, int groups, hipStrea
 // ---- sums of columns -------------------------------------------------------------
 
 // A workgroup sums one chunk of rows for 64 groups of columns: each of its NW waves every NW-th row, joined
-// in wave order.
+// in wave order; the chunks by the kernel below.  Bound by memory: 4096 x 11008 bf16, not in any cache, 19 us and 4 for the join.
 template <typename T, int NW>
 __global__ __launch_bounds__(64 * NW) void column_sum_kernel(ColumnSumArgs args) {
   typedef Group16<T> G;
