@@ -1210,8 +1210,8 @@ int64_t linear_splits(int64_t M, int64_t N, int64_t K, int64_t e, bool pairs) {
   }
   for (int64_t S = want; S > 1; --S) {
     const int64_t chunk = (K + S - 1) / S;
-    // (what takes chunks of any length anyway is split at any)
-    if ((S - 1) * chunk < K && (chunk % e == 0 || K % e != 0 || e == 4)) return S;
+    // (what takes chunks of any length anyway, or cuts its own, is split at any)
+    if ((S - 1) * chunk < K && (chunk % e == 0 || K % e != 0 || e == 4 || M <= cleave::kFewRows)) return S;
   }
   return 1;
 }
@@ -1285,7 +1285,8 @@ extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, voi
 
   // (a launch has fewer than 2^32 threads)
   const bool few_rows = M <= cleave::kFewRows && !a->transA && splits >= 1 && N <= int64_t{1} << 27;
-  const int64_t chunk = few_rows ? (plan->K + splits - 1) / splits * (e4m3 ? 2 : 1) : 0;   // the plan's, in elements
+  // (its chunks end on whole lines of 128 bytes; the last ones may be short, or empty, which leaves zeros)
+  const int64_t line = 128 / eb, chunk = few_rows ? ((K + splits - 1) / splits + line - 1) / line * line : 0;
   AssembleTarget to;
   to.C = joined ? nullptr : a->C;
   to.ldc = a->ldc;

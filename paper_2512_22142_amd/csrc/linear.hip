@@ -73,10 +73,12 @@ __device__ __forceinline__ V read_any(const unsigned char* p) {
   if constexpr (sizeof(V) == 16) return *reinterpret_cast<const U4*>(p);
   else return *reinterpret_cast<const U2*>(p);
 }
-// The first `n` elements of EB bytes, fewer than V holds; zeros behind them.
+// The first `n` elements of EB bytes; zeros behind them.
 template <typename V, int EB>
 __device__ __forceinline__ V read_some(const unsigned char* p, int n) {
+  if (n >= static_cast<int>(sizeof(V)) / EB) return read_any<V>(p);
   V w{};
+  if (n <= 0) return w;
 #pragma unroll
   for (int e = 0; e < static_cast<int>(sizeof(V)) / EB; ++e) {
     if (e >= n) continue;
