@@ -322,6 +322,10 @@ hipError_t launch_backward_of(const NormBackwardArgs& args, int groups, hipStrea
   if (n <= 512 * N) return launch_backward<T, 512, 1>(args, groups, stream);
   if (n <= 1024 * N) return launch_backward<T, 1024, 1>(args, groups, stream);
   if (n <= 2048 * N) return launch_backward<T, 1024, 2>(args, groups, stream);
+  if constexpr (N == 4) {   // (fp32 up to 16384 columns in registers, as bf16 above; us, read again / so, 887 x 8960 53.6 / 33.6)
+    if (n <= 3072 * N) return launch_backward<T, 1024, 3>(args, groups, stream);
+    if (n <= 4096 * N) return launch_backward<T, 1024, 4>(args, groups, stream);
+  }
   hipLaunchKernelGGL((rms_norm_backward_long_kernel<T>), dim3(groups), dim3(kLongThreads), 0, stream, args);
   return hipGetLastError();
 }

@@ -255,3 +255,10 @@ def test_refusals():
 @pytest.mark.parametrize("out", [BF16, E4M3])
 def test_norm_of_more_rows_than_one_launch_takes(out):
     run_norm(2 ** 21 + 77, 3, BF16, out, True)
+
+
+@pytest.mark.parametrize("cols", [8191, 8193, 12288, 12289, 16383, 16385])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_backward_of_wide_rows(cols, dtype):
+    run_backward(5, cols, dtype, True)
+    run_backward(700, cols, dtype, False, pad=1)
