@@ -194,8 +194,8 @@ hipError_t launch_norm_of(const NormArgs& args, hipStream_t stream) {
 
 // dx needs a row's whole sum, dw a sum over the rows: both leave one pass over dy and h.  Every group of the launch takes
 // every groups-th row and holds its part of the weight's gradient in registers until the last of them: one row of partial sums
-// for each workgroup (8192 x 4096: 512 rows of 16 KB, 8 MB beside the 268 MB of the pass; 5 us to join), whose groups (a wave each, where there are several) are joined
-// in order.
+// for each workgroup (8192 x 4096: 512 rows of 16 KB, 8 MB beside the 268 MB of the pass; 5 us to join), whose groups (a wave
+// each, where there are several) are joined in order.
 template <typename T, int NT, int V>
 __global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_backward_kernel(NormBackwardArgs args) {
   typedef Group16<T> G;
