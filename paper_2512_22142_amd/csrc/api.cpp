@@ -703,20 +703,6 @@ bool cut_small(const cleave_plan* plan, int cus) {
   }
 }
 
-// The same for 8-bit operands multiplied by their own instruction, whose large tile is four waves of 128 x 128: a round of
-// them against rounds of two small tiles to a CU, of which a last one with one each takes half.  us, large / small,
-// K = 4096: 3000 x 4096 65 / 56, 4096 x 4096 70 / 72, 4096 x 6144 117 / 98, 4096 x 11008 200 / 215, 16384 x 5120 x 5120
-// 375 / 419; short chains leave the large tile's stores uncovered: 8192 x 2048 x 1024 32 / 29.
-bool small_8bit(const cleave_plan* plan, int cus) {
-  const int64_t large = static_cast<int64_t>(plan->items[cleave::kTileLarge].size());
-  const int64_t fine = static_cast<int64_t>(plan->items_fine.size()), rest = fine % (2 * cus);
-  if (large == 0) return false;   // (all small already)
-  const double rounds_large = 1.85 * static_cast<double>((large + cus - 1) / cus);
-  const double rounds_small = 1.05 * (static_cast<double>(fine / (2 * cus)) + (rest == 0 ? 0.0 : rest <= cus ? 0.55 : 1.0));
-  const bool brief = plan->K <= 12 * cleave::kDirectKStep;
-  return rounds_small < rounds_large * (brief ? 1.2 : 1.0);
-}
-
 int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, const void* A,
                  int64_t lda, int transA, const void* B, int64_t ldb, int transB, int dtype,
                  float* partials, const BatchLayout& bl, void* hip_stream,
@@ -778,9 +764,8 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
   cleave::ListShape shapes[cleave::kNumTileClasses] = {plan->shape, plan->shape};   // (the general kernel runs all tasks, or a subset)
   // which of the plan's lists a class runs from (-1: a subset's own list)
   int list_of[cleave::kNumTileClasses] = {task_ids ? -1 : 0, task_ids ? -1 : 1};
-  // (8-bit operands multiplied as bf16 have no large shape)
-  const bool no_large = plan->pairs && !(asm_to.C && asm_to.out_dtype == CLEAVE_BF16);
-  if (!task_ids && (!direct || no_large || (plan->pairs ? small_8bit(plan, cus) : cut_small(plan, cus)))) {
+  // (8-bit operands have no large shape)
+  if (!task_ids && (!direct || plan->pairs || cut_small(plan, cus))) {
     list_of[cleave::kTileSmall] = cleave::kNumTileClasses;
     d_lists[cleave::kTileLarge] = nullptr;
     counts[cleave::kTileLarge] = 0;

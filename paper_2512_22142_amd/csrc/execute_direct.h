@@ -66,7 +66,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void* lds_void;
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
@@ -89,10 +88,7 @@ struct Shape {
   static constexpr int kLoadsA = kATile / 1024 / NW;   // wave-wide loads per wave and step
   static constexpr int kLoadsB = kBTile / 1024 / NW;
   static constexpr int kLoadsPerStep = kLoadsA + kLoadsB;
-  static constexpr int kImage = WTN > 64 ? 16 * WTN * 4 : kBlockImageBytes;   // a wave's image for the stores
-  static constexpr int kLds = STAGES * kStage + NW * kImage;
-  // Waves per SIMD: what a CU's workgroups come to.
-  static constexpr int kWavesPerSimd = TM * TN == 256 * 256 ? NW / 4 : 2;
+  static constexpr int kLds = STAGES * kStage + NW * kBlockImageBytes;
   // A tile smaller than the small class's: a workgroup computes one of the
   // PARTS_M x PARTS_N parts of a work item, and only that.
   static constexpr int PARTS_M = TM < kSmallTileRows ? kSmallTileRows / TM : 1;
@@ -174,17 +170,12 @@ struct DirectTile {
   __device__ __forceinline__ void issue(const unsigned char* gbase, uint32_t lds_tile, int wave) const {
     const uint32_t lds = lds_tile + wave * (kLoads * 1024);
     const unsigned char* base = gbase - (kLoads - 1) * 1024;
-    if constexpr (L == 8) {   // (the offset ends at 4095)
-      issue<FIRST, 4>(gbase, lds_tile, wave);
-      issue<FIRST + 4, 4>(gbase, lds_tile, wave);
-    } else if constexpr (L == 4) {
-      constexpr int kAt = FIRST * 1024;
+    if constexpr (L == 4) {
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
                    "global_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
                    "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
                    :
-                   : "s"(lds + kAt), "v"(goff[FIRST]), "v"(goff[FIRST + 1]), "v"(goff[FIRST + 2]), "v"(goff[FIRST + 3]),
-                     "s"(base + kAt)
+                   : "s"(lds), "v"(goff[0]), "v"(goff[1]), "v"(goff[2]), "v"(goff[3]), "s"(base)
                    : "memory", "m0");
     } else if constexpr (L == 2) {
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
@@ -237,30 +228,17 @@ __device__ __forceinline__ void spread_reads() {
   spread_reads_at<M, READS>(std::make_integer_sequence<int, M>{});
 }
 
-// The same with the reads behind the first half of the MFMAs.
-template <int M, int READS, int... I>
-__device__ __forceinline__ void early_reads_at(std::integer_sequence<int, I...>) {
-  constexpr int kSlots = M > 1 ? M / 2 : 1;
-  constexpr auto done = [](int m) { return m >= kSlots ? READS : (m * READS + kSlots - 1) / kSlots; };
-  ((__builtin_amdgcn_sched_group_barrier(0x008, 1, 0),
-    __builtin_amdgcn_sched_group_barrier(0x100, done(I + 1) - done(I), 0)), ...);
-}
-template <int M, int READS>
-__device__ __forceinline__ void early_reads() {
-  early_reads_at<M, READS>(std::make_integer_sequence<int, M>{});
-}
-
 // TAILS: some chunk of the launch ends within a K step (the code for that costs
 // scalar registers: an instantiation of its own).
 // Epi: what the sums go through on their way out (linear_epilogue.h).
-// OPS: with e4m3 operands a pair of values is what is written "bf16 element" below: both K-contiguous, and every
-// size and stride along K counts pairs.
-//   kE4M3: v_mfma_16x16x128, 32 bytes of each operand to a lane, at twice the rate of two bf16 instructions for the
-//     same bytes -- but it drops what lies below 2^-13 of the largest product of a group: sums of 4096 random values are
-//     1.6e-5 off (bf16: 9e-8).  For bf16 outputs, which are rounded to 2^-9.
-//   kE4M3Exact: the values as bf16 (v_cvt, exact), for fp32 outputs and partial sums.
+// OPS: with e4m3 operands (kE4M3) a pair of values is what is written "bf16 element" below: both K-contiguous, and every
+// size and stride along K counts pairs.  They are multiplied as bf16 (v_cvt, exact; a fragment's conversions serve all of its
+// products), so that the sums are fp32 sums.  The 8-bit instructions of twice the rate are not used: they drop what lies below
+// 2^-13 of the largest product of a group, so a row's outliers that cancel take the sum of its other products with them.
+// Bound like bf16 products, by the matrix instructions: 4096 x 11008 x 4096 286-350 us, 4096 x 4096 x 4096 118, 16384 x 5120 x 5120
+// 676 (1.06 to 1.3 PFLOP/s; a K step has 64 of them and 128 conversions to a wave).
 template <typename S, bool A_K, bool B_K, bool TAILS, DirectOperands OPS, typename Epi>
-__global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void execute_direct_kernel(ExecuteArgs args, Epi epi) {
+__global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(ExecuteArgs args, Epi epi) {
   constexpr int TM = S::TM, TN = S::TN, MB = S::MB, NB = S::NB, CPR = S::CPR, kSub = S::kSub;
   constexpr int kStage = S::kStage, kATile = S::kATile, STAGES = S::STAGES, LPS = S::kLoadsPerStep;
   constexpr int kRowBytes = CPR * 16;        // K-contiguous tile row
@@ -411,7 +389,7 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
   // Store instructions per lane of a full sub-tile.
   const bool bf16_out = args.C && args.c_bf16;
   const int tile_stores = bf16_out ? MB * NB / 2 : MB * NB;
-  unsigned char* const image = smem + STAGES * kStage + wave * S::kImage;
+  unsigned char* const image = smem + STAGES * kStage + wave * kBlockImageBytes;
 
   // This workgroup's items: first, first + stride, ... below it_end.
   int64_t it_first = blockIdx.x, it_end = args.n_items, stride = gridDim.x;
@@ -481,8 +459,6 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
   constexpr int MH = MB / 2, NH = NB / 2;
   f32x4 acc[MB][NB];
   u32x4 fa[kQuarters ? 1 : 2][MB], fb[kQuarters ? 1 : 2][NB];
-  constexpr bool kWide = OPS == kE4M3;   // both sub-steps in one instruction
-  i32x8 wide_a[kWide ? MB : 1], wide_b[kWide ? NB : 1];
 
   // Fragment reads are ordinary (compiler-visible) LDS loads: the compiler
   // tracks their completion, and every address is a lane-constant register
@@ -538,7 +514,7 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
         const int i = I0 + x, j = J0 + (i & 1 ? N - 1 - y : y);
         f32x4 sum = acc[i][j];
         if constexpr (FRESH) sum = f32x4{};
-        if constexpr (OPS == kE4M3Exact) {
+        if constexpr (OPS == kE4M3) {
           const u32x4 b = fb[SET][j], a = fa[SET][i];
           sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_e4m3(b[0], b[1]), bf16_of_e4m3(a[0], a[1]), sum, 0, 0, 0);
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_e4m3(b[2], b[3]), bf16_of_e4m3(a[2], a[3]), sum, 0, 0, 0);
@@ -546,37 +522,6 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
               __builtin_bit_cast(bf16x8, fb[SET][j]), __builtin_bit_cast(bf16x8, fa[SET][i]), sum, 0, 0, 0);
         }
-      }
-  };
-  // The same for whole steps of 8-bit values: a lane's 32 bytes are its sixteen of either sub-step (any
-  // order of k will do that both operands share).
-  auto read_wide_a = [&](uint32_t stage, auto i0_tag, auto n_tag) {
-#pragma unroll
-    for (int i = decltype(i0_tag)::value; i < decltype(i0_tag)::value + decltype(n_tag)::value; ++i) {
-      const u32x4 lo = *reinterpret_cast<const u32x4*>(smem + (a_addr[0] + stage) + i * 16 * kRowBytes);
-      const u32x4 hi = *reinterpret_cast<const u32x4*>(smem + (a_addr[1] + stage) + i * 16 * kRowBytes);
-      wide_a[i] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
-  };
-  auto read_wide_b = [&](uint32_t stage, auto j0_tag, auto n_tag) {
-#pragma unroll
-    for (int j = decltype(j0_tag)::value; j < decltype(j0_tag)::value + decltype(n_tag)::value; ++j) {
-      const u32x4 lo = *reinterpret_cast<const u32x4*>(smem + (b_addr[0] + stage) + j * 16 * kRowBytes);
-      const u32x4 hi = *reinterpret_cast<const u32x4*>(smem + (b_addr[1] + stage) + j * 16 * kRowBytes);
-      wide_b[j] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
-  };
-  auto mma_wide = [&](auto i0_tag, auto m_tag, auto j0_tag, auto n_tag, auto fresh_tag) {
-    constexpr int I0 = decltype(i0_tag)::value, J0 = decltype(j0_tag)::value, N = decltype(n_tag)::value;
-#pragma unroll
-    for (int x = 0; x < decltype(m_tag)::value; ++x)
-#pragma unroll
-      for (int y = 0; y < N; ++y) {
-        const int i = I0 + x, j = J0 + (i & 1 ? N - 1 - y : y);
-        f32x4 sum = acc[i][j];
-        if constexpr (decltype(fresh_tag)::value) sum = f32x4{};
-        // (e4m3 both; no scales: the plain instruction)
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_b[j], wide_a[i], sum, 0, 0, 0, 0, 0, 0);
       }
   };
   constexpr int kReadsA = (A_K ? 1 : 2) * MB, kReadsB = (B_K ? 1 : 2) * NB;
@@ -601,10 +546,7 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
 
     // The fragments that a step begins with.
     auto first_frags = [&](uint32_t stage) {
-      if constexpr (kWide) {
-        read_wide_a(stage, int_c<0>{}, int_c<MH>{});
-        read_wide_b(stage, int_c<0>{}, int_c<NH>{});
-      } else if constexpr (kQuarters) {
+      if constexpr (kQuarters) {
         read_a(stage, int_c<0>{}, int_c<0>{}, int_c<MH>{});
         read_b(stage, int_c<0>{}, int_c<0>{}, int_c<NH>{});
       } else {   // in the order in which they are multiplied
@@ -677,31 +619,7 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
       };
       constexpr int_c<0> k0{};
       constexpr int_c<1> k1{};
-      if constexpr (kWide) {
-        // Four quarters, each with a quarter of the reads in its first half: the waves run in step, and more than that at a
-        // time is more than the LDS gives.  The second halves are read in the first two quarters, the next step's
-        // first halves behind the barrier, where this step's are done with.
-        constexpr int_c<0> lo{};
-        constexpr int_c<MH> a_hi{}, mh{};
-        constexpr int_c<NH> b_hi{}, nh{};
-        read_wide_b(cur, b_hi, nh);
-        mma_wide(lo, mh, lo, nh, fresh);
-        early_reads<MH * NH, NB>();
-        read_wide_a(cur, a_hi, mh);
-        mma_wide(lo, mh, b_hi, nh, fresh);
-        early_reads<MH * NH, MB>();
-        hand_over();
-        if (read_on) read_wide_a(oth, lo, mh);
-        mma_wide(a_hi, mh, lo, nh, fresh);
-        early_reads<MH * NH, MB>();
-        if constexpr (MID && kQuarters) {
-          if constexpr (!kPairs) issue_a(c, st, second_half);
-          issue_b(c, st, whole);
-        }
-        if (read_on) read_wide_b(oth, lo, nh);
-        mma_wide(a_hi, mh, b_hi, nh, fresh);
-        early_reads<MH * NH, NB>();
-      } else if constexpr (kQuarters) {
+      if constexpr (kQuarters) {
         // Four quarters per sub-step: (first half of A, one half of B), the other
         // half of B, then the second half of A with B's halves the other way
         // round, so that each half of B changes once per sub-step.
@@ -814,7 +732,7 @@ __global__ __launch_bounds__(S::NT, S::NT == 512 ? 1 : S::kWavesPerSimd) void ex
     const auto leave = [&](auto bf16_tag, auto interior_tag, auto stream_tag) {
       // (an epilogue's loads and further stores come on top of the stores that the waits count: these
       // then wait for more than they need)
-      if constexpr (OPS == kE4M3Exact) {
+      if constexpr (OPS == kE4M3) {
         if (args.C == nullptr) {   // partial blocks, joined with the epilogue by another kernel
           store_rows<false, decltype(interior_tag)::value, false, MB, NB>(acc, target, image, wm * S::WTM, wn * S::WTN, lane,
                                                                           m_valid, n_valid);
@@ -859,8 +777,7 @@ hipError_t launch_one(const ExecuteArgs& args, const Epi& epi, int grid, hipStre
 template <typename S, bool A_K, bool B_K, bool TAILS, DirectOperands OPS, typename Epi>
 hipError_t configure_one() {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(execute_direct_kernel<S, A_K, B_K, TAILS, OPS, Epi>),
-                             hipFuncAttributeMaxDynamicSharedMemorySize,
-                             S::kLds);
+                             hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
 }
 
 // The layouts that there are: all four, with an epilogue those with A K-contiguous, in 8 bits those with B too.
@@ -905,13 +822,6 @@ hipError_t configure_shape() {
 //     items of 16 steps 164 / 237 us).
 using LargeShape = Shape<kLargeTileRows, kLargeTileCols, 2, 4, 64, 2, false>;
 using SmallShape = Shape<kSmallTileRows, kSmallTileCols, 2, 2, 64, 2, false>;
-// 8-bit operands have twice the products per byte, and what bounds them is the LDS: 256 x 256 in eight waves of 128 x 64
-// takes 125 bytes a clock of its 128 (reads and the ring's fill), in four of 128 x 128, one to a SIMD with 512
-// registers, 94.  4096 x 11008 x 4096 178-193 us (2.0 PFLOP/s), 4096 x 4096 x 32768 2.6 PFLOP/s; the instruction from registers alone
-// gives 3.8.  A K step takes 1.57 us, its matrix instructions 1.1 of them; what bounds it is the fragments' way through the LDS
-// between two barriers, which no other wave of the SIMD covers.  Small tiles (two workgroups to a CU) serve the sizes that
-// small_8bit picks.
-using WideShape = Shape<kLargeTileRows, kLargeTileCols, 2, 2, 64, 2, false>;
 using DeepShape = Shape<kSmallTileRows, kSmallTileCols, 2, 2, 64, 4, true>;
 using PartsShape = Shape<64, 64, 2, 2, 64, 4, true>;
 static_assert(kDirectKStep == LargeShape::BK && kDirectKStep == SmallShape::BK &&
@@ -940,8 +850,8 @@ template <DirectOperands OPS, typename Epi>
 hipError_t launch_with(const ExecuteArgs& args, const Epi& epi, DirectShape shape, bool tails, int grid, hipStream_t stream) {
   switch (shape) {
     case kDirectLarge:
-      if constexpr (OPS == kE4M3Exact) return hipErrorInvalidValue;
-      else return launch_shape<std::conditional_t<OPS == kE4M3, WideShape, LargeShape>, OPS>(args, epi, tails, grid, stream);
+      if constexpr (OPS == kE4M3) return hipErrorInvalidValue;   // 8-bit operands have no large shape
+      else return launch_shape<LargeShape, OPS>(args, epi, tails, grid, stream);
     case kDirectSmall: return launch_shape<SmallShape, OPS>(args, epi, tails, grid, stream);
     case kDirectDeep: return launch_shape<DeepShape, OPS>(args, epi, tails, static_cast<int>(args.n_items), stream);
     default: {   // one workgroup per part of an item; the list is padded to whole rounds of the XCDs
@@ -954,7 +864,7 @@ hipError_t launch_with(const ExecuteArgs& args, const Epi& epi, DirectShape shap
 template <DirectOperands OPS, typename Epi>
 hipError_t configure_all() {
   hipError_t e = hipSuccess;
-  if constexpr (OPS != kE4M3Exact) e = configure_shape<std::conditional_t<OPS == kE4M3, WideShape, LargeShape>, OPS, Epi>();
+  if constexpr (OPS != kE4M3) e = configure_shape<LargeShape, OPS, Epi>();
   if (e == hipSuccess) e = configure_shape<SmallShape, OPS, Epi>();
   if (e == hipSuccess) e = configure_shape<DeepShape, OPS, Epi>();
   if (e == hipSuccess) e = configure_shape<PartsShape, OPS, Epi>();

@@ -224,9 +224,8 @@ hipError_t launch_execute_direct(const ExecuteArgs& args, DirectShape shape, boo
 hipError_t launch_linear_direct(const ExecuteArgs& args, const LinearArgs& epi, DirectShape shape, bool tails, int grid,
                                 hipStream_t stream);
 // Operands of e4m3 values, both K-contiguous; K and the strides count pairs of them.  args.C null: partial blocks.
-// What the direct kernel multiplies.  e4m3 by its own instruction (kE4M3) is only as exact as
-// a bf16 output; as bf16 (kE4M3Exact) it has no large shape.
-enum DirectOperands : int { kBf16 = 0, kE4M3 = 1, kE4M3Exact = 2 };
+// (No large shape.)
+enum DirectOperands : int { kBf16 = 0, kE4M3 = 1 };   // what the direct kernel multiplies
 hipError_t launch_linear_8bit(const ExecuteArgs& args, const LinearArgs& epi, DirectShape shape, bool tails, int grid,
                               hipStream_t stream);
 hipError_t launch_linear_general(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int tile_class,

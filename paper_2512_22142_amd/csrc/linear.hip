@@ -54,7 +54,7 @@ __device__ __forceinline__ f32x4 multiply(u32x4 x, u32x4 w, f32x4 acc) {
   if constexpr (DTYPE == CLEAVE_BF16) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, w), acc, 0, 0, 0);
   } else if constexpr (DTYPE == CLEAVE_E4M3) {
-    // (as bf16, exactly: the 8-bit instruction drops bits, and memory bounds this kernel)
+    // (as bf16, exactly: the 8-bit instructions drop bits of the sum)
     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_e4m3(x[0], x[1]), bf16_of_e4m3(w[0], w[1]), acc, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_e4m3(x[2], x[3]), bf16_of_e4m3(w[2], w[3]), acc, 0, 0, 0);
   } else {

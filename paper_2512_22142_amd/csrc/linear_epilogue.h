@@ -251,11 +251,10 @@ __device__ __forceinline__ void emit_images(const LinearArgs& e, unsigned char* 
     }
   };
   if (e.bias) read_columns(e.bias, bias);
-  float scales[2] = {};   // of rows row0 + lane and row0 + 64 + lane
+  [[maybe_unused]] float scales = 0.0f;   // of row row0 + lane (SCALED: the images are 64 rows at most)
   if constexpr (SCALED) {
     read_columns(e.scale_b, scale_b);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) scales[h] = e.scale_a[m_base + min(row0 + 64 * h + lane, m_valid - 1)];
+    scales = e.scale_a[m_base + min(row0 + lane, m_valid - 1)];
   }
   const int64_t grow = m_base + row, gcol = n_base + col;
   unsigned char* out = out_base + (row * ld + col) * EB;
@@ -293,10 +292,7 @@ __device__ __forceinline__ void emit_images(const LinearArgs& e, unsigned char* 
       P y, z;
       read_image<ROWS, COLS, N>(image, r, rpiece, y.v);
       float scale_a = 0.0f;
-      if constexpr (SCALED) {
-        const int at = ROWS * i + r;   // (64 rows' worth in a register; an image does not straddle them)
-        scale_a = __shfl(ROWS * i < 64 ? scales[0] : scales[1], at & 63);
-      }
+      if constexpr (SCALED) scale_a = __shfl(scales, ROWS * i + r);
       if (reads_z) z = P::of(z_raw[0][k]);
       finish<SCALED>(e, y.v, z.v, bias, scale_b, scale_a);
       if (e.residual) {
@@ -331,6 +327,7 @@ template <bool BF16, bool INTERIOR, bool SCALED, int AHEAD, int MB, int NB>
 __device__ __forceinline__ void store_linear_rows(const tile_f32x4 (&acc)[MB][NB], const LinearArgs& e, const TileTarget& t,
                                                   unsigned char* image, int wave_row0, int wave_col0, int lane, int m_valid,
                                                   int n_valid, int64_t m_base, int64_t n_base) {
+  static_assert(!SCALED || MB * 16 <= 64, "the rows' scales are held one to a lane");
   const int row = lane & 15, quad = lane >> 4;   // lane's row and which four columns of a block
   emit_images<BF16, INTERIOR, SCALED, 16, NB * 16, AHEAD>(
       e, t.base, t.ld, image, MB, wave_row0, wave_col0, lane, m_valid, n_valid, m_base, n_base, [&](int i) {
