@@ -21,12 +21,18 @@ namespace cleave {
 
 // ---- activations -------------------------------------------------------------
 
-// 1 / (1 + e^-x).  The exponential and the reciprocal are the hardware's (an ulp or two);
-// e^-x may overflow: the reciprocal of infinity is zero.
+// 1 / (1 + e^-x), to a few ulps of itself for every x: e^-x = 2^t e^(-x - t ln 2) with t = -x log2(e) rounded, whose second
+// factor is 1 + rest (the rounding of t, up to 2^-18 at |x| = 87, would be an error of as much).  The exponential and the reciprocal are
+// the hardware's (an ulp each); 2^t may overflow: the reciprocal of infinity is zero, and what is below 2^-126 may be.
 __device__ __forceinline__ float sigmoid(float x) {
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896f * x));
+  constexpr float kLn2 = 0.693147180559945309f, kLn2Rest = -1.904654299957768e-9f;   // ln 2 - kLn2
+  const float t = -1.44269504088896f * x;
+  // (infinite x: no number, which the bounds take out)
+  const float rest = __builtin_amdgcn_fmed3f(__builtin_fmaf(-t, kLn2Rest, __builtin_fmaf(-t, kLn2, -x)), -0.5f, 0.5f);
+  return __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_amdgcn_exp2f(t), 1.0f + rest, 1.0f));
 }
 // gelu with tanh: z/2 (1 + tanh(u)) = z sigmoid(2 u), u = sqrt(2 / pi) (z + 0.044715 z^3).
+// (2 u is an fp32 value: its rounding is 2^-23 |2 u| of a small sigmoid.)
 constexpr float kGelu2 = 1.5957691216057308f;   // 2 sqrt(2 / pi)
 constexpr float kGelu3 = 0.044715f;
 
