@@ -38,12 +38,13 @@ __device__ __forceinline__ auto bf16_of_e4m3(uint32_t lo, uint32_t hi) {
 }
 
 // The scale of values of which `most` is the largest magnitude, most * (1 / 448), and its reciprocal; both zero
-// below kLeastScaled.  NaN stays NaN.
+// below kLeastScaled, both NaN where it is infinite or NaN.
 struct BlockScale {
   float scale, inverse;
 };
 __device__ __forceinline__ BlockScale block_scale(float most) {
   if (most < kLeastScaled) return {0.0f, 0.0f};
+  if (!(most < __builtin_inff())) return {__builtin_nanf(""), __builtin_nanf("")};
   const float scale = most * (1.0f / kE4M3Max);
   return {scale, 1.0f / scale};
 }
