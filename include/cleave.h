@@ -425,9 +425,10 @@ int cleave_verify_grouped(cleave_plan* plan, int64_t n_members,
  * y_dtype = dtype: scales must be NULL.  y_dtype = CLEAVE_E4M3: row t of y holds
  * h i w / s rounded to nearest even, with scales[t] = s = max|h i w| (1/448) (a row whose
  * largest magnitude is below 2^-100 is stored as zeros with s = 0; one that holds a NaN or
- * an infinity as NaN with s NaN).  sum_out may be x or residual, y too.
+ * an infinity as NaN with s NaN).  sum_out may be x or residual, with its leading dimension; y too, unless
+ * it is e4m3 (its rows would lie over other rows of x).  Otherwise outputs overlap nothing that the call reads or writes.
  * CLEAVE_EINVAL: negative rows, no column, a size above 2^31-1, NULL or misaligned
- * pointer, short leading dimension, negative, infinite or NaN eps, another dtype. */
+ * pointer, short leading dimension, negative, infinite or NaN eps, another dtype, an address shared otherwise. */
 int cleave_rms_norm(int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* residual,
                     int64_t ldr, int dtype, const float* weight, float eps,
                     void* y, int64_t ldy, int y_dtype, float* scales,
@@ -438,7 +439,7 @@ int cleave_rms_norm(int64_t rows, int64_t cols, const void* x, int64_t ldx, cons
  *   dx = i (g - xhat mean(g xhat)) + dsum;   dweight = sum over rows of dy xhat
  * dx is the gradient of x and of residual alike.  dsum (or NULL): the gradient that reaches h
  * itself, through the residual stream.  dy, h, dsum, dx: dtype F32 or BF16, dx may be
- * dy or dsum; dweight: cols floats.  workspace: cleave_rms_norm_workspace(rows, cols)
+ * dy, h or dsum, with its leading dimension; dweight: cols floats.  workspace: cleave_rms_norm_workspace(rows, cols)
  * floats, of this call alone while it runs.  CLEAVE_EINVAL as above. */
 int64_t cleave_rms_norm_workspace(int64_t rows, int64_t cols);
 int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* dy, int64_t lddy,
@@ -459,7 +460,8 @@ int cleave_bias_grad(int64_t rows, int64_t cols, const void* dy, int64_t lddy, i
  * The first is a layer's forward pass; preact (or NULL) gets z for its gradient.  The second is
  * the gradient of an activation's input, op(A) being the gradient behind the next layer's
  * weight.  Sums, bias and activation in fp32, z and C rounded once.  residual (or NULL), preact
- * and C: out_dtype F32 or BF16, M x N with leading dimensions ldr, ldz, ldc; residual may be C.
+ * and C: out_dtype F32 or BF16, M x N with leading dimensions ldr, ldz, ldc; residual may be C, and a
+ * preact that is read may be, with C's leading dimension.
  * bias: N floats or NULL.  A, B, transA, transB as for cleave_execute.
  * dtype CLEAVE_E4M3: A is M x K and B is N x K (transA = 0, transB = 1) of 8-bit values,
  * row m of A times scale_a[m], row n of B times scale_b[n] (as cleave_rms_norm leaves

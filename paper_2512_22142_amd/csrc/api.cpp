@@ -1247,6 +1247,9 @@ extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, voi
   if (!aligned(a->A, eb) || !aligned(a->B, eb) || !aligned(a->C, ob) || !aligned(a->residual, ob) || !aligned(a->preact, ob) ||
       !aligned(a->bias, 4) || !aligned(a->scale_a, 4) || !aligned(a->scale_b, 4) || !aligned(a->partials, 4))
     return CLEAVE_EINVAL;
+  // in place: the same elements at the same places, and not two outputs
+  if ((a->residual == a->C && M > 1 && a->ldr != a->ldc) || (a->preact == a->C && (!a->act_grad || (M > 1 && a->ldz != a->ldc))))
+    return CLEAVE_EINVAL;
   if (e4m3 && (a->transA || !a->transB || !aligned(a->A, 16) || !aligned(a->B, 16) || a->lda % 16 || a->ldb % 16 ||
                a->lda >= int64_t{1} << 22 || a->ldb >= int64_t{1} << 22))
     return CLEAVE_EINVAL;

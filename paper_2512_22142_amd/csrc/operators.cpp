@@ -36,6 +36,12 @@ struct Matrices {
   void add_vector(const float* p, bool optional = false) { ok = ok && (p ? aligned(p, 4) : optional); }
 };
 
+// Whether an output may take an input's place: the same elements at the same places, each read and written by one
+// thread.  (Rows of another pitch or type would lie over rows that others have yet to read.)
+bool in_place(const void* out, int64_t ldo, int out_dtype, const void* in, int64_t ldi, int dtype, int64_t rows) {
+  return !out || out != in || rows == 0 || (out_dtype == dtype && (ldo == ldi || rows == 1));
+}
+
 bool float_dtype(int dtype) { return dtype == CLEAVE_F32 || dtype == CLEAVE_BF16; }
 
 }  // namespace
@@ -55,6 +61,10 @@ extern "C" int cleave_rms_norm(int64_t rows, int64_t cols, const void* x, int64_
   m.add_vector(scales, true);
   m.add_vector(inv_rms, true);
   if (!m.ok) return CLEAVE_EINVAL;
+  if (!in_place(y, ldy, y_dtype, x, ldx, dtype, rows) || !in_place(y, ldy, y_dtype, residual, ldr, dtype, rows) ||
+      !in_place(sum_out, lds, dtype, x, ldx, dtype, rows) || !in_place(sum_out, lds, dtype, residual, ldr, dtype, rows) ||
+      (rows > 0 && y == sum_out))
+    return CLEAVE_EINVAL;
   if (rows == 0) return CLEAVE_OK;
   const cleave::NormArgs args{x, residual, weight, y, scales, sum_out, inv_rms, rows, cols, ldx, ldr, ldy, lds, eps};
   CLEAVE_HIP(cleave::launch_rms_norm(args, dtype, static_cast<hipStream_t>(hip_stream)));
@@ -80,6 +90,9 @@ extern "C" int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* 
   m.add_vector(dweight);
   m.add_vector(workspace);
   if (!m.ok) return CLEAVE_EINVAL;
+  if (!in_place(dx, lddx, dtype, dy, lddy, dtype, rows) || !in_place(dx, lddx, dtype, h, ldh, dtype, rows) ||
+      !in_place(dx, lddx, dtype, dsum, ldds, dtype, rows))
+    return CLEAVE_EINVAL;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const int partial_rows = cleave::rms_norm_partial_rows(rows, cols);
   if (rows > 0) {
