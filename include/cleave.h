@@ -601,7 +601,7 @@ const char* cleave_strerror(int status);
 int cleave_last_hip_error(void);
 /* Library ABI version (major*100 + minor). */
 int cleave_version(void);
-/* Name of the kernel variant the last cleave_execute of this plan chose for
+/* Name of the kernel variant the last cleave_execute or cleave_linear of this plan chose for
  * its dominant launch (for profiling reports); static string, never NULL. */
 const char* cleave_plan_last_kernel(const cleave_plan* plan);
 

@@ -353,6 +353,27 @@ const char* direct_kernel_name(cleave::DirectShape shape, int transA, int transB
   return names[shape][(transA ? 2 : 0) + (transB ? 1 : 0)];
 }
 
+// The kernels with an epilogue.
+const char* linear_kernel_name(int dtype, const cleave::GeneralLoads& how, int transA, int transB) {
+  static const char* names[2][2][4] = {
+      {{"linear_f32_128x128_nn", "linear_f32_128x128_nt", "linear_f32_128x128_tn", "linear_f32_128x128_tt"},
+       {"linear_f32_64x64_nn", "linear_f32_64x64_nt", "linear_f32_64x64_tn", "linear_f32_64x64_tt"}},
+      {{"linear_bf16_128x128_nn", "linear_bf16_128x128_nt", "linear_bf16_128x128_tn", "linear_bf16_128x128_tt"},
+       {"linear_bf16_64x64_nn", "linear_bf16_64x64_nt", "linear_bf16_64x64_tn", "linear_bf16_64x64_tt"}}};
+  const bool bf16 = dtype == CLEAVE_BF16;
+  if (how.a_elements || how.b_elements) return bf16 ? "linear_bf16_element" : "linear_f32_element";
+  return names[bf16 ? 1 : 0][how.tile == cleave::kTileLone ? 1 : 0][(transA ? 2 : 0) + (transB ? 1 : 0)];
+}
+
+const char* linear_direct_kernel_name(cleave::DirectShape shape, bool e4m3, int transB) {
+  static const char* names[4][3] = {   // (8-bit operands: no large shape, and B is N x K)
+      {"linear_direct_bf16_256x256_nn", "linear_direct_bf16_256x256_nt", "none"},
+      {"linear_direct_bf16_128x128_nn", "linear_direct_bf16_128x128_nt", "linear_direct_e4m3_128x128_nt"},
+      {"linear_direct_bf16_128x128_deep_nn", "linear_direct_bf16_128x128_deep_nt", "linear_direct_e4m3_128x128_deep_nt"},
+      {"linear_direct_bf16_64x64_nn", "linear_direct_bf16_64x64_nt", "linear_direct_e4m3_64x64_nt"}};
+  return names[shape][e4m3 ? 2 : transB ? 1 : 0];
+}
+
 }  // namespace
 
 int cleave::record_hip_error(hipError_t e) { return hip_fail(e); }
@@ -857,7 +878,8 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
                             : linear    ? cleave::launch_linear_direct(args, *linear, shape, plan->chunk_tails, grid, stream)
                                         : cleave::launch_execute_direct(args, shape, plan->chunk_tails, grid, stream);
       if (he != hipSuccess) return launch_failed(he);
-      if (counts[c] > most) plan->last_kernel = direct_kernel_name(shape, transA, transB);
+      if (counts[c] > most)
+        plan->last_kernel = linear ? linear_direct_kernel_name(shape, plan->pairs, transB) : direct_kernel_name(shape, transA, transB);
     } else {
       // in-tile byte offsets (256 rows) stay within 32 bits
       const bool by_k = !transA && transB && !a_elements && !b_elements && lda * eb < (int64_t{1} << 24) &&
@@ -878,7 +900,8 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
       const hipError_t he = linear ? cleave::launch_linear_general(args, *linear, dtype, c, how, stream)
                                    : cleave::launch_execute(args, dtype, c, how, stream);
       if (he != hipSuccess) return launch_failed(he);
-      if (counts[c] > most) plan->last_kernel = kernel_name(dtype, how, transA, transB);
+      if (counts[c] > most)
+        plan->last_kernel = linear ? linear_kernel_name(dtype, how, transA, transB) : kernel_name(dtype, how, transA, transB);
     }
     most = std::max(most, counts[c]);
   }
