@@ -164,9 +164,6 @@ int ensure_device_ready(int dev, int* cus) {
   if (g_device_cus[dev] == 0) {
     CLEAVE_HIP(cleave::configure_execute_kernels());
     CLEAVE_HIP(cleave::configure_execute_direct_kernels());
-    CLEAVE_HIP(cleave::configure_linear_general_kernels());
-    CLEAVE_HIP(cleave::configure_linear_direct_kernels());
-    CLEAVE_HIP(cleave::configure_linear_8bit_kernels());
     void* ptr = nullptr;   // `dev` is the current device: its copy of the array
     CLEAVE_HIP(hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch)));
     g_static_scratch[dev] = static_cast<cleave::WorkItem*>(ptr);
@@ -175,6 +172,21 @@ int ensure_device_ready(int dev, int* cus) {
     g_device_cus[dev] = std::max(n, 1);
   }
   if (cus) *cus = g_device_cus[dev];
+  return CLEAVE_OK;
+}
+
+// The kernels with an epilogue likewise, when a plan of cleave_plan_linear's is uploaded, or by the first cleave_linear: they would
+// cost who only executes another 4 ms.
+bool g_linear_ready[kMaxDevices] = {};
+
+int ensure_linear_ready(int dev) {
+  if (dev < 0 || dev >= kMaxDevices) return CLEAVE_EINVAL;
+  std::lock_guard<std::mutex> lock(g_device_mu);
+  if (g_linear_ready[dev]) return CLEAVE_OK;
+  CLEAVE_HIP(cleave::configure_linear_general_kernels());
+  CLEAVE_HIP(cleave::configure_linear_direct_kernels());
+  CLEAVE_HIP(cleave::configure_linear_8bit_kernels());
+  g_linear_ready[dev] = true;
   return CLEAVE_OK;
 }
 
@@ -211,6 +223,7 @@ int ensure_uploaded(cleave_plan* p) {
   if (p->device == dev) return CLEAVE_OK;
   if (p->device >= 0) free_device_tables(p);
   int rc = ensure_device_ready(dev, nullptr);
+  if (rc == CLEAVE_OK && p->linear) rc = ensure_linear_ready(dev);
   if (rc != CLEAVE_OK) return rc;
   rc = upload_vector(p->tasks, &p->d_tasks);
   hipStream_t writing = nullptr;
@@ -1244,8 +1257,10 @@ extern "C" int cleave_plan_linear(int64_t M, int64_t N, int64_t K, int dtype, cl
                                                                     : cleave::kLargeTileRows;
   const int rc = cleave_plan_uniform(M, N, k, tile, tile,
                                      static_cast<int32_t>(linear_splits(M, N, k, dtype == CLEAVE_F32 ? 4 : 8, pairs)), 0, out);
-  if (rc == CLEAVE_OK) (*out)->pairs = pairs;
-  return rc;
+  if (rc != CLEAVE_OK) return rc;
+  (*out)->linear = true;
+  (*out)->pairs = pairs;
+  return CLEAVE_OK;
 }
 
 extern "C" int64_t cleave_linear_workspace(const cleave_plan* plan) {
@@ -1292,6 +1307,7 @@ extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, voi
   epi.grad = a->act_grad;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   int rc = ensure_uploaded(plan);
+  if (rc == CLEAVE_OK) rc = ensure_linear_ready(plan->device);
   if (rc != CLEAVE_OK) return rc;
 
   // (a launch has fewer than 2^32 threads)
