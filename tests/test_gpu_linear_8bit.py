@@ -86,3 +86,21 @@ def test_bf16_outputs_are_the_rounded_sums(M, N):
     # that share of them, twice for those below the rms, is an ulp (2^-7 at most) off
     off = 2 * K ** 0.5 * U32 / U16
     assert np.linalg.norm(got - rounded) <= 2.0 ** -7 * off ** 0.5 * np.linalg.norm(rounded)
+
+
+@pytest.mark.parametrize("rows,N", [(16, 40), (256, 24), (4096, 1200)])
+def test_every_8_bit_value(rows, N):
+    """Each times one, and one times each: the value itself, NaN of both signs among them."""
+    every = torch.arange(rows, device="cuda", dtype=torch.int32) % 256
+    A = torch.zeros(rows, 256, device="cuda").to(E4M3)
+    at = torch.arange(rows, device="cuda")
+    A.view(torch.uint8)[at, at % 256] = every.to(torch.uint8)
+    B = torch.ones(N, 256, device="cuda").to(E4M3)
+    want = every.to(torch.uint8).view(E4M3).float()[:, None].expand(rows, N)
+    nan = want.isnan()
+    for out in (BF16, F32):
+        got = product(A, B, out).float()
+        assert torch.equal(got.isnan(), nan) and torch.equal(got[~nan], want[~nan])
+        if N > 16:
+            got = product(B, A, out).float()
+            assert torch.equal(got.isnan(), nan.t()) and torch.equal(got[~nan.t()], want.t()[~nan.t()])
