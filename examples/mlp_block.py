@@ -5,7 +5,7 @@
 The block is  h = x + r;  y = W2 gelu(W1 norm(h) + b1) + b2 + h,  trained towards a fixed random map of its
 input.  Forward: rms_norm (residual added on the way), linear with bias and gelu, linear with bias and
 residual.  Backward: the gradient of gelu's input out of the product with W2^T, weight gradients, bias
-gradients, the norm's gradient.  Update: one adamw call for all six tensors, states in 8 bits.
+gradients, the norm's gradient.  Update: one adamw call for all five tensors, states in 8 bits.
 Serving: the same norm leaves e4m3 rows for a product with the weight laid out once in e4m3.
 Every buffer is made once; a step allocates nothing.
 """

@@ -413,14 +413,14 @@ int cleave_verify_grouped(cleave_plan* plan, int64_t n_members,
  * parameter server (Sec. 4.1): the norm of the residual stream, bias gradients,
  * and the optimizer over all tensors of a layer at once.  Matrices are row-major, `rows` x
  * `cols`, with leading dimensions in elements; any size, stride and alignment of the
- * elements (rows that start on 16-byte boundaries, of whole 16 bytes of the input
- * type, take a faster path).  All are asynchronous on hip_stream, allocate
+ * elements.  All are asynchronous on hip_stream, allocate
  * nothing, keep nothing between calls and may be captured into a HIP graph.  Sums are
  * carried in fp32 in an order that depends on the sizes alone: the same call gives
  * the same bits.  rows = 0 is allowed: nothing is read, sums over rows are zero.
  *
  * cleave_rms_norm:  h = x + residual;  i = 1 / sqrt(mean(h^2) + eps);  y = h i w
- * per row, from the unrounded h.  x, residual (or NULL), sum_out (h, or NULL): dtype
+ * per row, from the unrounded h, the squares summed in fp32 (so i is 0 in a row whose h^2 pass
+ * fp32's range, |h| from 2^63 on).  x, residual (or NULL), sum_out (h, or NULL): dtype
  * F32 or BF16; weight: cols floats; inv_rms: rows floats (i), or NULL.
  * y_dtype = dtype: scales must be NULL.  y_dtype = CLEAVE_E4M3: row t of y holds
  * h i w / s rounded to nearest even, with scales[t] = s = max|h i w| (1/448) (a row whose
@@ -471,7 +471,7 @@ int cleave_bias_grad(int64_t rows, int64_t cols, const void* dy, int64_t lddy, i
  * of K for M, N, K and dtype; for CLEAVE_E4M3 it must be that (K a multiple of 16; its tasks
  * and dims count K in pairs of values; execute, verify and reduce calls refuse it).  partials: cleave_linear_workspace(plan)
  * floats (may be NULL if that is 0), of this call alone while it runs.
- * Few rows (M <= 16) read B once, as fast as memory gives it.  Bits: a function of the
+ * Few rows (M <= 16, transA = 0) read B once, as fast as memory gives it.  Bits: a function of the
  * arguments' values, sizes and alignment.  Asynchronous; the plan's tables are uploaded by the first call or
  * cleave_plan_upload, after which nothing is allocated.
  * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, act_grad with a
@@ -508,7 +508,8 @@ int cleave_linear(cleave_plan* plan, const cleave_linear_args* args, void* hip_s
  * is left): state = value * scale, scale = largest finite magnitude of the 256 times 1/448, rounded to
  * nearest even; what is above zero in sqrt(v) becomes at least 2^-9 of the scale; values that are
  * not finite become NaN; a block below 2^-100 is zeros with scale 0.  All zeros with scales 0
- * are the states of step 1.
+ * are the states of step 1.  lr, step and the others are the host's: a call recorded into a graph
+ * repeats the step that it was recorded with (record one per step, or launch it beside the graph).
  * Empty tensors are allowed (their pointers are not looked at).  CLEAVE_EINVAL: NULL or
  * misaligned pointer, a negative size or one of 2^40 and more, one of the two scale lists alone, step < 1,
  * beta outside [0, 1), negative eps, NaN, another dtype. */

@@ -14,8 +14,8 @@
 //
 // Bound by memory: 28 bytes per weight and step in 32 bits with a bf16 gradient and copy, 16 in 8 bits.  A wave has a block
 // of 256 weights, four to a lane, so a block's largest magnitude is a reduction over the wave and every access is a run of the
-// whole wave; a workgroup has 4096 weights, and the tensors' list travels in the kernel's arguments, so any number
-// of small ones shares a launch.  7.1 M weights in 32 bits 36-37 us (5.4 TB/s), 202 M in 8 bits 601-640 us (5.1 to 5.4).
+// whole wave; a workgroup has 4096 weights, and the tensors' list travels in the kernel's arguments, so up to
+// 56 of any sizes share a launch.  7.1 M weights in 32 bits 36-37 us (5.4 TB/s), 202 M in 8 bits 601-640 us (5.1 to 5.4).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>

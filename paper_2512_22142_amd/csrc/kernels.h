@@ -224,7 +224,7 @@ hipError_t launch_execute_direct(const ExecuteArgs& args, DirectShape shape, boo
 hipError_t launch_linear_direct(const ExecuteArgs& args, const LinearArgs& epi, DirectShape shape, bool tails, int grid,
                                 hipStream_t stream);
 // Operands of e4m3 values, both K-contiguous; K and the strides count pairs of them.  args.C null: partial blocks.
-// (No large shape.)
+// They have no large shape.
 enum DirectOperands : int { kBf16 = 0, kE4M3 = 1 };   // what the direct kernel multiplies
 hipError_t launch_linear_8bit(const ExecuteArgs& args, const LinearArgs& epi, DirectShape shape, bool tails, int grid,
                               hipStream_t stream);

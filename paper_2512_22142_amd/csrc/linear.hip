@@ -10,7 +10,7 @@
 //     together by v_perm, 4 per fragment, and fragment c belongs to the columns 4 n + c.
 // The waves are joined through LDS in wave order.  Sixteen of them leave the output itself, in one launch; where N's columns
 // go round the CUs unevenly, four, whose workgroups split K and leave partial sums for a second kernel.
-//   One row, bf16, K x N = 4096 x 11008 (90 MB): 17.6 us with the weights in the Infinity Cache (5.1 TB/s), 20.8 from memory (4.3; a
+//   One row, bf16, K x N = 4096 x 11008 (90 MB): 17.3-17.6 us with the weights in the Infinity Cache (5.2 TB/s), 20.8-22.8 from memory (4.0-4.3; a
 // pass that only sums the columns takes 19 and a second launch); 8192 x 28672 97 us (4.8 TB/s).  16 rows: 18.6 and 24.
 #include <hip/hip_runtime.h>
 

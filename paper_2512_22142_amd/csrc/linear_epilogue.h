@@ -213,7 +213,7 @@ __device__ __forceinline__ void read_image(const unsigned char* image, int row, 
 // cache and its addresses spill.  The vector-memory counter retires loads and stores in order, so a load waits for
 // the stores issued before it: what a turn reads is fetched AHEAD turns before, and nothing else is
 // loaded between stores (the rows' scales come from registers, across lanes).  4096 x 11008 x 4096 bf16 with bias, gelu and the stored
-// argument (180 MB out) takes 310-317 us (1.18 PFLOP/s), as long as with the bias alone.
+// argument (180 MB out) takes 309-321 us (1.15 to 1.2 PFLOP/s), as long as with the bias alone.
 //   row0, col0: the first image's place in the sub-tile, of which m_valid x n_valid elements exist.
 //   out: element (0, 0) of the sub-tile, `ld` elements to a row; m_base, n_base: its place in the output.
 template <bool BF16, bool INTERIOR, bool SCALED, int ROWS, int COLS, int AHEAD, typename Write>

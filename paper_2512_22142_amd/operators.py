@@ -54,7 +54,8 @@ def adamw(w, grads, m, v, lr, beta1, beta2, eps, weight_decay, step, m_scales=No
     """cleave_adamw: one AdamW step on the lists of tensors w (fp32, in place), grads (fp32 or bf16), m and v
     (in place: fp32, or float8_e4m3fn with a scale per 256 elements in m_scales and v_scales, v being
     held as its square root).  copies: bf16 tensors that get the new weights.  grad_scale: a
-    device tensor of one element that the gradients are multiplied by."""
+    device tensor of one element that the gradients are multiplied by.  lr, step and the others are host values, also in
+    a graph: a recorded call repeats its step."""
     _check(_native.adamw(w, grads, m, v, m_scales, v_scales, copies, grad_scale, lr, beta1, beta2, eps, weight_decay, step,
                          stream), "cleave_adamw")
 
