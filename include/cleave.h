@@ -447,6 +447,25 @@ int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* dy, int64_t
                              const float* weight, const float* inv_rms, void* dx, int64_t lddx,
                              float* dweight, float* workspace, void* hip_stream);
 
+/* Layer norm:  h = x + residual;  m = mean(h);  i = 1 / sqrt(mean((h - m)^2) + eps);  y = (h - m) i w + b
+ * per row, from the unrounded h (sums beyond fp32's range make the row NaN, or i zero).  Everything as for cleave_rms_norm, with
+ * bias: cols floats, or NULL; mean, inv_std: rows floats (m, i), each or NULL. */
+int cleave_layer_norm(int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* residual,
+                      int64_t ldr, int dtype, const float* weight, const float* bias, float eps,
+                      void* y, int64_t ldy, int y_dtype, float* scales, void* sum_out, int64_t lds,
+                      float* mean, float* inv_std, void* hip_stream);
+
+/* Its gradient, from dy, the stored h and its mean and inv_std:  xhat = (h - m) i;  g = dy w;
+ *   dx = i (g - mean(g) - xhat mean(g xhat)) + dsum;   dweight = sum over rows of dy xhat;
+ *   dbias (or NULL) = sum over rows of dy
+ * Everything as for cleave_rms_norm_backward; workspace: cleave_layer_norm_workspace(rows, cols) floats. */
+int64_t cleave_layer_norm_workspace(int64_t rows, int64_t cols);
+int cleave_layer_norm_backward(int64_t rows, int64_t cols, const void* dy, int64_t lddy,
+                               const void* h, int64_t ldh, const void* dsum, int64_t ldds, int dtype,
+                               const float* weight, const float* mean, const float* inv_std, void* dx,
+                               int64_t lddx, float* dweight, float* dbias, float* workspace,
+                               void* hip_stream);
+
 /* dbias = sum over rows of dy (the gradient of a bias that every row got).
  * workspace: cleave_bias_grad_workspace(rows, cols) floats, of this call alone while
  * it runs. */

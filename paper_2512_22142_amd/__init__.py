@@ -8,6 +8,7 @@
 and what a layer's step does between its GEMMs:
 
     rms_norm, rms_norm_backward   norm of the residual stream, its gradient
+    layer_norm, layer_norm_backward   the same with the mean taken off, and a bias
     linear (plan_linear)          product with bias, activation (or its gradient) and residual; 8-bit operands
     bias_grad                     sum of a gradient's rows
     adamw                         optimizer step over many tensors, states in 32 or 8 bits
@@ -63,6 +64,9 @@ _OPERATOR_NAMES = (
     "adamw",
     "bias_grad",
     "bias_grad_workspace",
+    "layer_norm",
+    "layer_norm_backward",
+    "layer_norm_workspace",
     "linear",
     "plan_linear",
     "rms_norm",

@@ -42,6 +42,7 @@ EXPORTS = (
     "cleave_execute_grouped", "cleave_reduce_grouped", "cleave_execute_noalloc", "cleave_reassign_sets", "cleave_reduce_adam_grouped", "cleave_verify_batched", "cleave_verify_grouped", "cleave_verify_reduce", "cleave_plan_schedule_loads",
     "cleave_rms_norm", "cleave_rms_norm_workspace", "cleave_rms_norm_backward", "cleave_bias_grad", "cleave_bias_grad_workspace",
     "cleave_adamw", "cleave_plan_linear", "cleave_linear_workspace", "cleave_linear",
+    "cleave_layer_norm", "cleave_layer_norm_workspace", "cleave_layer_norm_backward",
 )
 
 
@@ -152,7 +153,7 @@ def _load():
     lib.cleave_plan_linear.restype = ctypes.c_int
     lib.cleave_linear_workspace.argtypes = [p]
     lib.cleave_linear_workspace.restype = i64
-    for name in ("cleave_rms_norm_workspace", "cleave_bias_grad_workspace"):
+    for name in ("cleave_rms_norm_workspace", "cleave_bias_grad_workspace", "cleave_layer_norm_workspace"):
         getattr(lib, name).argtypes = [i64, i64]
         getattr(lib, name).restype = i64
     lib.cleave_reduce.restype = ctypes.c_int

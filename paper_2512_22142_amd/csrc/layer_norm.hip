@@ -1,0 +1,408 @@
+// Layer norm of a residual stream and its gradient (the paper keeps such operators on the parameter server, Sec. 4.1).
+//
+//   h = x + r;  m = mean(h);  i = 1 / sqrt(mean((h - m)^2) + eps);  y = (h - m) i w + b
+// over the columns of each row, in fp32 from the unrounded h; y in x's type or, for a product with 8-bit
+// operands, as e4m3 with the row's scale s = max|y| / 448.
+// The mean is taken twice: m0 from the sum of h, then, with d = h - m0, m = m0 + mean(d) and the variance
+// mean(d^2) - mean(d)^2, in which nothing cancels.  A mean that is large beside the deviations is then as good as fp32
+// holds it (m0 alone is off by a few roundings of the mean, all of which would reach y).
+//
+// Gradient, with the stored h, m and i, g = dy w and xhat = (h - m) i:
+//   dx = i (g - mean(g) - xhat mean(g xhat)) + dsum;   dw = sum over rows of dy xhat;   db = sum over rows of dy
+//
+// Bound by memory: every row is read once and kept in registers between its statistics, the scaling and the rounding.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "fp8_round.h"
+#include "operators.h"
+#include "row_access.h"
+#include "wave_reduce.h"
+
+namespace cleave {
+
+namespace {
+
+template <typename T, int NT, int V, bool E4M3>
+__global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(LayerNormArgs args) {
+  typedef Group16<T> G;
+  constexpr int NW = RowGroup<NT>::kWaves, N = G::N;
+  __shared__ float slots[4][NW];
+  const int t = threadIdx.x % NT;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * RowGroup<NT>::kRows + threadIdx.x / NT;
+  if (row >= args.rows) return;   // whole waves, and with several waves to a row whole workgroups
+  const T* x = static_cast<const T*>(args.x) + row * args.ldx;
+  const T* r = static_cast<const T*>(args.residual) + (args.residual ? row * args.ldr : 0);
+  T* sum_out = static_cast<T*>(args.sum_out) + (args.sum_out ? row * args.lds : 0);
+  const int cols = static_cast<int>(args.cols);
+  const float count = static_cast<float>(cols);
+  const auto at = [&](int j) { return (j * NT + t) * N; };
+
+  Raw16 x_raw[V], r_raw[V];
+  Floats16<N> w_raw[V], b_raw[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    x_raw[j] = G::read(x + at(j), cols - at(j));
+    if (args.residual) r_raw[j] = G::read(r + at(j), cols - at(j));
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    w_raw[j].read(args.weight + at(j), cols - at(j));
+    if (args.bias) b_raw[j].read(args.bias + at(j), cols - at(j));
+  }
+  float h[V][N];
+#pragma unroll
+  for (int j = 0; j < V; ++j) G::unpack(x_raw[j], h[j]);
+  if (args.residual) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float add[N];
+      G::unpack(r_raw[j], add);
+#pragma unroll
+      for (int e = 0; e < N; ++e) h[j][e] += add[e];
+    }
+  }
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum += h[j][e];
+  if (args.sum_out) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) G::store(sum_out + at(j), cols - at(j), h[j]);
+  }
+  const float first = group_sum<NW>(sum, slots[0]) / count;
+  float rest = 0.0f, squares = 0.0f;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      h[j][e] = at(j) + e < cols ? h[j][e] - first : 0.0f;
+      rest += h[j][e];
+      squares += h[j][e] * h[j][e];
+    }
+  group_sums<NW>(rest, squares, slots[1]);
+  rest /= count;
+  const float var = squares / count - rest * rest;
+  const float inv = 1.0f / __builtin_sqrtf((var < 0.0f ? 0.0f : var) + args.eps);   // (NaN stays)
+  if (t == 0) {
+    if (args.mean) args.mean[row] = first + rest;
+    if (args.inv_std) args.inv_std[row] = inv;
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    float w[N], b[N] = {};
+    w_raw[j].unpack(w);
+    if (args.bias) b_raw[j].unpack(b);
+#pragma unroll
+    for (int e = 0; e < N; ++e) h[j][e] = (h[j][e] - rest) * inv * w[e] + b[e];
+  }
+  if constexpr (E4M3) {
+    float most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (at(j) + e < cols) most = nan_max(most, __builtin_fabsf(h[j][e]));
+    const BlockScale s = block_scale(group_nan_max<NW>(most, slots[3]));
+    if (t == 0) args.scales[row] = s.scale;
+    uint8_t* y = static_cast<uint8_t*>(args.y) + row * args.ldy;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) h[j][e] *= s.inverse;
+      store_e4m3<N>(y + at(j), cols - at(j), h[j]);
+    }
+  } else {
+    T* y = static_cast<T*>(args.y) + row * args.ldy;
+#pragma unroll
+    for (int j = 0; j < V; ++j) G::store(y + at(j), cols - at(j), h[j]);
+  }
+}
+
+// Rows that no group's registers hold: read again for each use (from the caches).
+constexpr int kLongThreads = 1024;
+
+template <typename T, bool E4M3>
+__global__ __launch_bounds__(kLongThreads) void layer_norm_long_kernel(LayerNormArgs args) {
+  constexpr int NW = kLongThreads / 64;
+  __shared__ float slots[4][NW];
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(args.x) + row * args.ldx;
+  const T* r = static_cast<const T*>(args.residual) + (args.residual ? row * args.ldr : 0);
+  const float count = static_cast<float>(args.cols);
+  const auto at = [&](int64_t c) { return args.residual ? element(x + c) + element(r + c) : element(x + c); };
+  float sum = 0.0f;
+  for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) sum += at(c);
+  const float first = group_sum<NW>(sum, slots[0]) / count;
+  float rest = 0.0f, squares = 0.0f;
+  for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
+    const float d = at(c) - first;
+    rest += d;
+    squares += d * d;
+  }
+  group_sums<NW>(rest, squares, slots[1]);
+  rest /= count;
+  const float var = squares / count - rest * rest;
+  const float inv = 1.0f / __builtin_sqrtf((var < 0.0f ? 0.0f : var) + args.eps);
+  if (threadIdx.x == 0) {
+    if (args.mean) args.mean[row] = first + rest;
+    if (args.inv_std) args.inv_std[row] = inv;
+  }
+  const auto norm = [&](float h, int64_t c) {
+    return ((h - first) - rest) * inv * args.weight[c] + (args.bias ? args.bias[c] : 0.0f);
+  };
+  BlockScale s{1.0f, 1.0f};
+  if constexpr (E4M3) {
+    float most = 0.0f;
+    for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) most = nan_max(most, __builtin_fabsf(norm(at(c), c)));
+    s = block_scale(group_nan_max<NW>(most, slots[3]));
+    if (threadIdx.x == 0) args.scales[row] = s.scale;
+  }
+  // (an element is read, then written, by one thread: y or the sum may take x's or r's place)
+  for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
+    const float h = at(c), y = norm(h, c);
+    if (args.sum_out) put(static_cast<T*>(args.sum_out) + row * args.lds + c, h);
+    if constexpr (E4M3)
+      static_cast<uint8_t*>(args.y)[row * args.ldy + c] = static_cast<uint8_t>(pack_e4m3(y * s.inverse, 0.0f));
+    else
+      put(static_cast<T*>(args.y) + row * args.ldy + c, y);
+  }
+}
+
+template <typename T, int NT, int V>
+hipError_t launch_norm(const LayerNormArgs& args, hipStream_t stream) {
+  constexpr int kRows = RowGroup<NT>::kRows;
+  const dim3 g(static_cast<uint32_t>((args.rows + kRows - 1) / kRows)), b(RowGroup<NT>::kThreads);
+  if (args.scales) hipLaunchKernelGGL((layer_norm_kernel<T, NT, V, true>), g, b, 0, stream, args);
+  else hipLaunchKernelGGL((layer_norm_kernel<T, NT, V, false>), g, b, 0, stream, args);
+  return hipGetLastError();
+}
+
+// `v` groups to a thread, up to MOST: the least that holds a row.
+template <typename T, int NT, int MOST, int V = 1>
+hipError_t launch_norm_fit(const LayerNormArgs& args, int64_t v, hipStream_t stream) {
+  if constexpr (V < MOST) {
+    if (v > V) return launch_norm_fit<T, NT, MOST, V + 1>(args, v, stream);
+  }
+  return launch_norm<T, NT, V>(args, stream);
+}
+
+// Which threads share a row: as for the root-mean-square norm (norm.hip).
+template <typename T>
+hipError_t launch_norm_of(const LayerNormArgs& args, hipStream_t stream) {
+  const int64_t groups = (args.cols + Group16<T>::N - 1) / Group16<T>::N;
+  if (groups <= 64) return launch_norm<T, 64, 1>(args, stream);
+  if (groups <= 4 * 64 && args.rows > 1024) return launch_norm_fit<T, 64, 4>(args, (groups + 63) / 64, stream);
+  if (groups <= 8 * 256 && args.rows > 256) return launch_norm_fit<T, 256, 8>(args, (groups + 255) / 256, stream);
+  if (groups <= 4 * 1024) return launch_norm_fit<T, 1024, 4>(args, (groups + 1023) / 1024, stream);
+  const dim3 g(static_cast<uint32_t>(args.rows)), b(kLongThreads);
+  if (args.scales) hipLaunchKernelGGL((layer_norm_long_kernel<T, true>), g, b, 0, stream, args);
+  else hipLaunchKernelGGL((layer_norm_long_kernel<T, false>), g, b, 0, stream, args);
+  return hipGetLastError();
+}
+
+// ---- gradient ------------------------------------------------------------------
+
+// One pass over dy and h for dx and for the sums over rows: every group of the launch takes every groups-th row and holds its
+// part of dw and db in registers until the last of them, one row of partial sums for each workgroup, whose groups (a
+// wave each, where there are several) are joined in order.  The next row's loads are on their way while a row's sums are joined.
+template <typename T, int V>
+struct BackwardRow {
+  Raw16 dy[V], h[V], add[V];
+  float mean, inv;
+};
+template <typename T, int NT, int V>
+__global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_kernel(LayerNormBackwardArgs args) {
+  typedef Group16<T> G;
+  constexpr int NW = RowGroup<NT>::kWaves, N = G::N, GROUPS = RowGroup<NT>::kRows;
+  __shared__ float slots[2][2 * NW];
+  const int t = threadIdx.x % NT;
+  const int64_t group = static_cast<int64_t>(blockIdx.x) * GROUPS + threadIdx.x / NT, groups = static_cast<int64_t>(gridDim.x) * GROUPS;
+  const int cols = static_cast<int>(args.cols);
+  const float count = static_cast<float>(cols);
+  const auto at = [&](int j) { return (j * NT + t) * N; };
+  float dw[V][N] = {}, db[V][N] = {}, w[V][N];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    Floats16<N> raw;
+    raw.read(args.weight + at(j), cols - at(j));
+    raw.unpack(w[j]);
+  }
+  const auto fetch = [&](int64_t row, BackwardRow<T, V>& to) {
+    const T* dy = static_cast<const T*>(args.dy) + row * args.lddy;
+    const T* h = static_cast<const T*>(args.h) + row * args.ldh;
+    to.mean = args.mean[row];
+    to.inv = args.inv_std[row];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      to.dy[j] = G::read(dy + at(j), cols - at(j));
+      to.h[j] = G::read(h + at(j), cols - at(j));
+    }
+    if (args.dsum) {
+      const T* dsum = static_cast<const T*>(args.dsum) + row * args.ldds;
+#pragma unroll
+      for (int j = 0; j < V; ++j) to.add[j] = G::read(dsum + at(j), cols - at(j));
+    }
+  };
+  BackwardRow<T, V> cur, next;
+  if (group < args.rows) fetch(group, cur);
+  int turn = 0;
+  for (int64_t row = group; row < args.rows; row += groups, turn ^= 1) {
+    if (row + groups < args.rows) fetch(row + groups, next);
+    float g[V][N], xhat[V][N];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      G::unpack(cur.dy[j], g[j]);
+      G::unpack(cur.h[j], xhat[j]);
+    }
+    float sum = 0.0f, dot = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        xhat[j][e] = at(j) + e < cols ? (xhat[j][e] - cur.mean) * cur.inv : 0.0f;
+        dw[j][e] += g[j][e] * xhat[j][e];
+        db[j][e] += g[j][e];
+        g[j][e] *= w[j][e];
+        sum += g[j][e];
+        dot += g[j][e] * xhat[j][e];
+      }
+    // (the slots of the row before last are free: every wave has passed the barrier of the last one)
+    group_sums<NW>(sum, dot, slots[turn]);
+    sum /= count;
+    dot /= count;
+    T* dx = static_cast<T*>(args.dx) + row * args.lddx;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float add[N] = {};
+      if (args.dsum) G::unpack(cur.add[j], add);
+#pragma unroll
+      for (int e = 0; e < N; ++e) g[j][e] = (g[j][e] - sum - xhat[j][e] * dot) * cur.inv + add[e];
+      G::store(dx + at(j), cols - at(j), g[j]);
+    }
+    cur = next;
+  }
+  if constexpr (GROUPS > 1) {
+    __shared__ float joined[GROUPS - 1][2 * V * N][NT];
+    if (threadIdx.x >= NT) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          joined[threadIdx.x / NT - 1][j * N + e][t] = dw[j][e];
+          joined[threadIdx.x / NT - 1][(V + j) * N + e][t] = db[j][e];
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x >= NT) return;
+#pragma unroll
+    for (int g = 0; g < GROUPS - 1; ++g)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          dw[j][e] += joined[g][j * N + e][t];
+          db[j][e] += joined[g][(V + j) * N + e][t];
+        }
+  }
+  float* out = args.partials + static_cast<int64_t>(blockIdx.x) * 2 * args.cols;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    store_floats<N>(out + at(j), cols - at(j), dw[j]);
+    store_floats<N>(out + args.cols + at(j), cols - at(j), db[j]);
+  }
+}
+
+// Rows that no group's registers hold: the partial sums are kept in the group's row of them.
+template <typename T>
+__global__ __launch_bounds__(kLongThreads) void layer_norm_backward_long_kernel(LayerNormBackwardArgs args) {
+  constexpr int NW = kLongThreads / 64;
+  __shared__ float slots[2][2 * NW];
+  float* out = args.partials + static_cast<int64_t>(blockIdx.x) * 2 * args.cols;
+  const float count = static_cast<float>(args.cols);
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < args.rows; row += gridDim.x, turn ^= 1) {
+    const T* dy = static_cast<const T*>(args.dy) + row * args.lddy;
+    const T* h = static_cast<const T*>(args.h) + row * args.ldh;
+    const float inv = args.inv_std[row], mean = args.mean[row];
+    const bool fresh = row == blockIdx.x;
+    float sum = 0.0f, dot = 0.0f;
+    for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
+      const float d = element(dy + c), x = (element(h + c) - mean) * inv, g = d * args.weight[c];
+      out[c] = (fresh ? 0.0f : out[c]) + d * x;
+      out[args.cols + c] = (fresh ? 0.0f : out[args.cols + c]) + d;
+      sum += g;
+      dot += g * x;
+    }
+    group_sums<NW>(sum, dot, slots[turn]);
+    sum /= count;
+    dot /= count;
+    for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
+      const float add = args.dsum ? element(static_cast<const T*>(args.dsum) + row * args.ldds + c) : 0.0f;
+      put(static_cast<T*>(args.dx) + row * args.lddx + c,
+          (element(dy + c) * args.weight[c] - sum - (element(h + c) - mean) * inv * dot) * inv + add);
+    }
+  }
+}
+
+template <typename T, int NT, int V>
+hipError_t launch_backward(const LayerNormBackwardArgs& args, int workgroups, hipStream_t stream) {
+  hipLaunchKernelGGL((layer_norm_backward_kernel<T, NT, V>), dim3(workgroups), dim3(RowGroup<NT>::kThreads), 0, stream, args);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_backward_of(const LayerNormBackwardArgs& args, int workgroups, hipStream_t stream) {
+  constexpr int N = Group16<T>::N;
+  const int64_t n = args.cols;
+  if (n <= 64 * N) return launch_backward<T, 64, 1>(args, workgroups, stream);
+  if (n <= 128 * N && args.rows > 2048) return launch_backward<T, 64, 2>(args, workgroups, stream);
+  if (n <= 256 * N) return launch_backward<T, 256, 1>(args, workgroups, stream);
+  if (n <= 512 * N) return launch_backward<T, 512, 1>(args, workgroups, stream);
+  if (n <= 1024 * N) return launch_backward<T, 1024, 1>(args, workgroups, stream);
+  if (n <= 2048 * N) return launch_backward<T, 1024, 2>(args, workgroups, stream);
+  hipLaunchKernelGGL((layer_norm_backward_long_kernel<T>), dim3(workgroups), dim3(kLongThreads), 0, stream, args);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// A launch has fewer than 2^32 threads: more rows than these take several.
+constexpr int64_t kLaunchRows = int64_t{1} << 21;
+
+hipError_t launch_layer_norm(const LayerNormArgs& args, int dtype, hipStream_t stream) {
+  const int64_t eb = dtype == CLEAVE_BF16 ? 2 : 4, yb = args.scales ? 1 : eb;
+  for (int64_t row = 0; row < args.rows; row += kLaunchRows) {
+    const auto down = [&](auto* p, int64_t bytes) {
+      return p ? reinterpret_cast<decltype(p)>(reinterpret_cast<uintptr_t>(p) + row * bytes) : p;
+    };
+    LayerNormArgs some = args;
+    some.rows = std::min(args.rows - row, kLaunchRows);
+    some.x = down(args.x, args.ldx * eb);
+    some.residual = down(args.residual, args.ldr * eb);
+    some.sum_out = down(args.sum_out, args.lds * eb);
+    some.y = down(args.y, args.ldy * yb);
+    some.scales = down(args.scales, 4);
+    some.mean = down(args.mean, 4);
+    some.inv_std = down(args.inv_std, 4);
+    const hipError_t e = dtype == CLEAVE_BF16 ? launch_norm_of<Bf16>(some, stream) : launch_norm_of<float>(some, stream);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+int layer_norm_partial_rows(int64_t rows, int64_t cols) {
+  const int64_t groups = cols <= 1024 ? 8192 : cols <= 2048 ? 1024 : 512;
+  const int64_t some = std::min(groups, rows <= 2048 ? rows : std::max<int64_t>((rows + 3) / 4, 2048));
+  return static_cast<int>(cols <= 1024 ? (some + 3) / 4 : std::min<int64_t>(some, groups));
+}
+
+hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int dtype, int partial_rows, hipStream_t stream) {
+  return dtype == CLEAVE_BF16 ? launch_backward_of<Bf16>(args, partial_rows, stream)
+                              : launch_backward_of<float>(args, partial_rows, stream);
+}
+
+}  // namespace cleave

@@ -114,6 +114,64 @@ PyObject* py_rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// layer_norm(x, weight, y, bias, residual, sum_out, mean, inv_std, scales, eps, stream)
+PyObject* py_layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 11);
+    const Operand x = operand(a[0], "x");
+    const int dt = dtype_code(x.type);
+    const float* w = floats(a[1], "weight", x.cols);
+    const Operand y = operand(a[2], "y");
+    const int ydt = operand_code(y.type);
+    if (y.rows != x.rows || y.cols != x.cols || (ydt != dt && ydt != CLEAVE_E4M3))
+      raise(PyExc_ValueError, "y must have x's shape, and x's dtype or float8_e4m3fn");
+    const float* b = floats(a[3], "bias", x.cols, true);
+    const Operand r = like(a[4], "residual", x.rows, x.cols, x.type, true);
+    const Operand s = like(a[5], "sum_out", x.rows, x.cols, x.type, true);
+    float* mean = floats(a[6], "mean", x.rows, true);
+    float* inv = floats(a[7], "inv_std", x.rows, true);
+    float* scales = floats(a[8], "scales", x.rows, true);
+    if ((ydt == CLEAVE_E4M3) != (a[8] != Py_None)) raise(PyExc_ValueError, "scales belong to y in float8_e4m3fn, and only to that");
+    const float eps = static_cast<float>(real(a[9]));
+    void* stream = stream_of(a[10]);
+    if (x.rows == 0) return PyLong_FromLong(CLEAVE_OK);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = cleave_layer_norm(x.rows, x.cols, x.ptr, x.ld, r.ptr, r.ld, dt, w, b, eps, y.ptr, y.ld, ydt, scales, s.ptr, s.ld, mean,
+                           inv, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+  });
+}
+
+// layer_norm_backward(dy, h, weight, mean, inv_std, dx, dweight, workspace, dbias, dsum, stream)
+PyObject* py_layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 11);
+    const Operand dy = operand(a[0], "dy");
+    const int dt = dtype_code(dy.type);
+    const Operand h = like(a[1], "h", dy.rows, dy.cols, dy.type);
+    const float* w = floats(a[2], "weight", dy.cols);
+    const float* mean = floats(a[3], "mean", dy.rows);
+    const float* inv = floats(a[4], "inv_std", dy.rows);
+    const Operand dx = like(a[5], "dx", dy.rows, dy.cols, dy.type);
+    float* dw = floats(a[6], "dweight", dy.cols);
+    float* ws = floats(a[7], "workspace", cleave_layer_norm_workspace(dy.rows, dy.cols), false, true);
+    float* db = floats(a[8], "dbias", dy.cols, true);
+    const Operand ds = like(a[9], "dsum", dy.rows, dy.cols, dy.type, true);
+    void* stream = stream_of(a[10]);
+    // (tensors without elements have no address: any stands for them)
+    const auto some = [&](const void* p) { return dy.rows ? p : ws; };
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = cleave_layer_norm_backward(dy.rows, dy.cols, some(dy.ptr), dy.ld, some(h.ptr), h.ld, dy.rows ? ds.ptr : nullptr, ds.ld,
+                                    dt, w, static_cast<const float*>(some(mean)), static_cast<const float*>(some(inv)),
+                                    const_cast<void*>(some(dx.ptr)), dx.ld, dw, db, ws, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+  });
+}
+
 // bias_grad(dy, dbias, workspace, stream)
 PyObject* py_bias_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -260,6 +318,8 @@ PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef kOperatorMethods[] = {{"linear", as_function(py_linear), METH_FASTCALL, nullptr},
 {"rms_norm", as_function(py_rms_norm), METH_FASTCALL, nullptr},
                                   {"rms_norm_backward", as_function(py_rms_norm_backward), METH_FASTCALL, nullptr},
+                                  {"layer_norm", as_function(py_layer_norm), METH_FASTCALL, nullptr},
+                                  {"layer_norm_backward", as_function(py_layer_norm_backward), METH_FASTCALL, nullptr},
                                   {"bias_grad", as_function(py_bias_grad), METH_FASTCALL, nullptr},
                                   {"adamw", as_function(py_adamw), METH_FASTCALL, nullptr},
                                   {nullptr, nullptr, 0, nullptr}};

@@ -26,15 +26,6 @@ namespace cleave {
 
 namespace {
 
-// A row per group of NT threads, which holds up to NT * V * N elements of it (N in sixteen bytes); a wave (NT = 64)
-// has its row to itself, four rows to a workgroup.
-template <int NT>
-struct RowGroup {
-  static constexpr int kThreads = NT == 64 ? 256 : NT;
-  static constexpr int kRows = kThreads / NT;
-  static constexpr int kWaves = NT / 64;
-};
-
 template <typename T, int NT, int V, bool E4M3>
 __global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_kernel(NormArgs args) {
   typedef Group16<T> G;
@@ -113,12 +104,6 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void rms_norm_kernel(NormAr
 
 // Rows that no group's registers hold: read again for each use (from the caches).
 constexpr int kLongThreads = 1024;
-__device__ __forceinline__ float element(const float* p) { return *p; }
-__device__ __forceinline__ float element(const Bf16* p) {
-  return __builtin_bit_cast(float, static_cast<uint32_t>(p->bits) << 16);
-}
-__device__ __forceinline__ void put(float* p, float x) { *p = x; }
-__device__ __forceinline__ void put(Bf16* p, float x) { p->bits = to_bf16_bits(x); }
 
 template <typename T, bool E4M3>
 __global__ __launch_bounds__(kLongThreads) void rms_norm_long_kernel(NormArgs args) {
@@ -377,9 +362,10 @@ hipError_t launch_sum(const ColumnSumArgs& args, hipStream_t stream) {
 }
 
 // The rows of partial sums: sixteen columns to a workgroup and 64 rows at a time, so that a few hundred rows are a few loads
-// of each thread.
+// of each thread.  Columns from `split` on go to the second output.
 constexpr int kJoinThreads = 1024, kJoinCols = 16;
-__global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in, int rows, int64_t ld, int64_t cols, float* out) {
+__global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in, int rows, int64_t ld, int64_t cols, float* out,
+                                                                 int64_t split, float* second) {
   constexpr int kRows = kJoinThreads / kJoinCols;
   __shared__ float part[kJoinThreads / 64][kJoinCols];
   const int at = threadIdx.x % kJoinCols, first = threadIdx.x / kJoinCols;
@@ -398,7 +384,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in
   sum = part[0][at];
 #pragma unroll
   for (int w = 1; w < kJoinThreads / 64; ++w) sum += part[w][at];
-  out[c] = sum;
+  if (c < split) out[c] = sum;
+  else second[c - split] = sum;
 }
 
 }  // namespace
@@ -445,11 +432,15 @@ int column_sum_chunks(int64_t rows, int64_t cols) {
   return static_cast<int>(std::max<int64_t>(1, std::min({want, (rows + 31) / 32, int64_t{256}})));
 }
 
-hipError_t launch_join_rows(const float* rows, int n, int64_t cols, float* out, hipStream_t stream) {
-  for (int64_t c = 0; c < cols; c += kLaunchCols) {
-    const int64_t some = std::min(cols - c, kLaunchCols);
+hipError_t launch_join_rows(const float* rows, int n, int64_t ld, int64_t cols, float* out, hipStream_t stream, float* second) {
+  const int64_t all = second ? 2 * cols : cols;
+  for (int64_t c = 0; c < all; c += kLaunchCols) {
+    const int64_t some = std::min(all - c, kLaunchCols);
+    // (out is indexed by columns below the split only, the second output by those from it on)
+    const int64_t split = std::max<int64_t>(cols - c, 0);
     hipLaunchKernelGGL(join_rows_kernel, dim3(static_cast<uint32_t>((some + kJoinCols - 1) / kJoinCols)), dim3(kJoinThreads), 0,
-                       stream, rows + c, n, cols, some, out + c);
+                       stream, rows + c, n, ld, some, split > 0 ? out + c : out, split,
+                       second ? second + std::max<int64_t>(c - cols, 0) : second);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -459,7 +450,7 @@ hipError_t launch_join_rows(const float* rows, int n, int64_t cols, float* out, 
 hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, hipStream_t stream) {
   const hipError_t e = dtype == CLEAVE_BF16 ? launch_sum<Bf16, 4>(args, stream) : launch_sum<float, 4>(args, stream);
   if (e != hipSuccess || args.chunks == 1) return e;
-  return launch_join_rows(args.partials, args.chunks, args.cols, args.out, stream);
+  return launch_join_rows(args.partials, args.chunks, args.cols, args.cols, args.out, stream);
 }
 
 }  // namespace cleave

@@ -99,7 +99,70 @@ extern "C" int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* 
     const cleave::NormBackwardArgs args{dy, h, dsum, weight, inv_rms, dx, workspace, rows, cols, lddy, ldh, ldds, lddx};
     CLEAVE_HIP(cleave::launch_rms_norm_backward(args, dtype, partial_rows, stream));
   }
-  CLEAVE_HIP(cleave::launch_join_rows(workspace, partial_rows, cols, dweight, stream));   // no rows: zeros
+  CLEAVE_HIP(cleave::launch_join_rows(workspace, partial_rows, cols, cols, dweight, stream));   // no rows: zeros
+  return CLEAVE_OK;
+}
+
+extern "C" int cleave_layer_norm(int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                                 int dtype, const float* weight, const float* bias, float eps, void* y, int64_t ldy, int y_dtype,
+                                 float* scales, void* sum_out, int64_t lds, float* mean, float* inv_std, void* hip_stream) {
+  if (!float_dtype(dtype) || (y_dtype != dtype && y_dtype != CLEAVE_E4M3)) return CLEAVE_EINVAL;
+  if ((y_dtype == CLEAVE_E4M3) != (scales != nullptr)) return CLEAVE_EINVAL;
+  if (!(eps >= 0.0f) || std::isinf(eps)) return CLEAVE_EINVAL;
+  Matrices m(rows, cols);
+  m.add(x, ldx, dtype);
+  m.add(residual, ldr, dtype, true);
+  m.add(y, ldy, y_dtype);
+  m.add(sum_out, lds, dtype, true);
+  m.add_vector(weight);
+  m.add_vector(bias, true);
+  m.add_vector(scales, true);
+  m.add_vector(mean, true);
+  m.add_vector(inv_std, true);
+  if (!m.ok) return CLEAVE_EINVAL;
+  if (!in_place(y, ldy, y_dtype, x, ldx, dtype, rows) || !in_place(y, ldy, y_dtype, residual, ldr, dtype, rows) ||
+      !in_place(sum_out, lds, dtype, x, ldx, dtype, rows) || !in_place(sum_out, lds, dtype, residual, ldr, dtype, rows) ||
+      (rows > 0 && y == sum_out) || (rows > 0 && mean && mean == inv_std))
+    return CLEAVE_EINVAL;
+  if (rows == 0) return CLEAVE_OK;
+  const cleave::LayerNormArgs args{x,   residual, weight, bias, y,   scales, sum_out, mean,
+                                   inv_std, rows, cols, ldx, ldr, ldy, lds, eps};
+  CLEAVE_HIP(cleave::launch_layer_norm(args, dtype, static_cast<hipStream_t>(hip_stream)));
+  return CLEAVE_OK;
+}
+
+extern "C" int64_t cleave_layer_norm_workspace(int64_t rows, int64_t cols) {
+  if (rows < 0 || cols < 1 || rows > kMost || cols > kMost) return CLEAVE_EINVAL;
+  return 2 * cols * std::max(1, cleave::layer_norm_partial_rows(rows, cols));
+}
+
+extern "C" int cleave_layer_norm_backward(int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* h, int64_t ldh,
+                                          const void* dsum, int64_t ldds, int dtype, const float* weight, const float* mean,
+                                          const float* inv_std, void* dx, int64_t lddx, float* dweight, float* dbias,
+                                          float* workspace, void* hip_stream) {
+  if (!float_dtype(dtype)) return CLEAVE_EINVAL;
+  Matrices m(rows, cols);
+  m.add(dy, lddy, dtype);
+  m.add(h, ldh, dtype);
+  m.add(dsum, ldds, dtype, true);
+  m.add(dx, lddx, dtype);
+  m.add_vector(weight);
+  m.add_vector(mean);
+  m.add_vector(inv_std);
+  m.add_vector(dweight);
+  m.add_vector(dbias, true);
+  m.add_vector(workspace);
+  if (!m.ok || dweight == dbias) return CLEAVE_EINVAL;
+  if (!in_place(dx, lddx, dtype, dy, lddy, dtype, rows) || !in_place(dx, lddx, dtype, h, ldh, dtype, rows) ||
+      !in_place(dx, lddx, dtype, dsum, ldds, dtype, rows))
+    return CLEAVE_EINVAL;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const int partial_rows = cleave::layer_norm_partial_rows(rows, cols);
+  if (rows > 0) {
+    const cleave::LayerNormBackwardArgs args{dy, h, dsum, weight, mean, inv_std, dx, workspace, rows, cols, lddy, ldh, ldds, lddx};
+    CLEAVE_HIP(cleave::launch_layer_norm_backward(args, dtype, partial_rows, stream));
+  }
+  CLEAVE_HIP(cleave::launch_join_rows(workspace, partial_rows, 2 * cols, cols, dweight, stream, dbias));   // no rows: zeros
   return CLEAVE_OK;
 }
 

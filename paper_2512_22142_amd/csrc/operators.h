@@ -41,6 +41,40 @@ struct NormBackwardArgs {
 // dx and the partial sums of the weight's gradient.
 hipError_t launch_rms_norm_backward(const NormBackwardArgs& args, int dtype, int partial_rows, hipStream_t stream);
 
+// ---- layer norm --------------------------------------------------------------
+
+struct LayerNormArgs {
+  const void* x;
+  const void* residual;    // null: h = x
+  const float* weight;
+  const float* bias;       // may be null
+  void* y;                 // x's type, or e4m3 with `scales`
+  float* scales;           // null: y has x's type
+  void* sum_out;           // h in x's type; may be null
+  float* mean;             // may be null
+  float* inv_std;          // may be null
+  int64_t rows, cols;
+  int64_t ldx, ldr, ldy, lds;   // elements
+  float eps;
+};
+hipError_t launch_layer_norm(const LayerNormArgs& args, int dtype, hipStream_t stream);
+
+// Rows of partial sums (each 2 cols floats: the weight's, then the bias's) that the gradient's first launch leaves.
+int layer_norm_partial_rows(int64_t rows, int64_t cols);
+struct LayerNormBackwardArgs {
+  const void* dy;
+  const void* h;
+  const void* dsum;        // null: none
+  const float* weight;
+  const float* mean;
+  const float* inv_std;
+  void* dx;
+  float* partials;         // layer_norm_partial_rows x 2 cols
+  int64_t rows, cols;
+  int64_t lddy, ldh, ldds, lddx;
+};
+hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int dtype, int partial_rows, hipStream_t stream);
+
 // ---- sums of columns ---------------------------------------------------------
 
 // out[c] = sum over `rows` rows of in[., c], in a fixed order.
@@ -54,8 +88,9 @@ struct ColumnSumArgs {
 };
 // Chunks of rows that are summed apart.
 int column_sum_chunks(int64_t rows, int64_t cols);
-// out[c] = sum of `n` contiguous rows of partial sums.
-hipError_t launch_join_rows(const float* rows, int n, int64_t cols, float* out, hipStream_t stream);
+// out[c] = sum of `n` rows of partial sums, `ld` floats apart; a second output gets those of the next `cols` columns.
+hipError_t launch_join_rows(const float* rows, int n, int64_t ld, int64_t cols, float* out, hipStream_t stream,
+                            float* second = nullptr);
 hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, hipStream_t stream);
 
 // ---- AdamW over many tensors -------------------------------------------------

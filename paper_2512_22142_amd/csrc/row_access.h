@@ -83,6 +83,23 @@ struct Group16<Bf16> {
   }
 };
 
+// Single elements.
+__device__ __forceinline__ float element(const float* p) { return *p; }
+__device__ __forceinline__ float element(const Bf16* p) {
+  return __builtin_bit_cast(float, static_cast<uint32_t>(p->bits) << 16);
+}
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(Bf16* p, float x) { p->bits = to_bf16_bits(x); }
+
+// A row per group of NT threads, which holds up to NT * V * N elements of it (N in sixteen bytes); a wave (NT = 64)
+// has its row to itself, four rows to a workgroup.
+template <int NT>
+struct RowGroup {
+  static constexpr int kThreads = NT == 64 ? 256 : NT;
+  static constexpr int kRows = kThreads / NT;
+  static constexpr int kWaves = NT / 64;
+};
+
 // N floats beside a group of either type.
 template <int N>
 struct Floats16 {

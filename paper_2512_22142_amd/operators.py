@@ -39,6 +39,25 @@ def rms_norm_backward(dy, h, weight, inv_rms, dx, dweight, workspace, dsum=None,
     _check(_native.rms_norm_backward(dy, h, weight, inv_rms, dx, dweight, workspace, dsum, stream), "cleave_rms_norm_backward")
 
 
+def layer_norm(x, weight, y, bias=None, residual=None, sum_out=None, mean=None, inv_std=None, scales=None, eps=1e-5, stream=None):
+    """cleave_layer_norm: y = (h - mean(h)) / std(h) * weight + bias for the rows of h = x + residual (x, residual,
+    sum_out: fp32 or bf16; weight, bias: fp32).  y has x's dtype, or float8_e4m3fn with one fp32 scale per row in
+    `scales`.  sum_out gets h, mean and inv_std (1 / std) what the gradient needs."""
+    _check(_native.layer_norm(x, weight, y, bias, residual, sum_out, mean, inv_std, scales, eps, stream), "cleave_layer_norm")
+
+
+def layer_norm_workspace(rows, cols):
+    """fp32 elements of layer_norm_backward's workspace."""
+    return int(_lib.cleave_layer_norm_workspace(*_sizes(rows, cols)))
+
+
+def layer_norm_backward(dy, h, weight, mean, inv_std, dx, dweight, workspace, dbias=None, dsum=None, stream=None):
+    """cleave_layer_norm_backward: dx (the gradient of x and of the residual), dweight and dbias from dy, the h, mean and
+    inv_std that layer_norm left, and dsum, the gradient that reaches h through the residual stream."""
+    _check(_native.layer_norm_backward(dy, h, weight, mean, inv_std, dx, dweight, workspace, dbias, dsum, stream),
+           "cleave_layer_norm_backward")
+
+
 def bias_grad_workspace(rows, cols):
     """fp32 elements of bias_grad's workspace."""
     return int(_lib.cleave_bias_grad_workspace(*_sizes(rows, cols)))
