@@ -514,6 +514,64 @@ int cleave_plan_linear(int64_t M, int64_t N, int64_t K, int dtype, cleave_plan**
 int64_t cleave_linear_workspace(const cleave_plan* plan);
 int cleave_linear(cleave_plan* plan, const cleave_linear_args* args, void* hip_stream);
 
+/* Gated product (the two projections of a gated feed-forward block):
+ *   zg = A op(B_gate) + bias_gate;  zu = A op(B_up) + bias_up;   C = act(zg) zu
+ * with every weight read once.  gate and up (each or NULL) get zg and zu for the gradient.  A: M x K; B_gate, B_up: both as B of
+ * cleave_linear with one leading dimension ldb (halves of one matrix, or two); biases: N floats, each or NULL.  dtype, scales
+ * (scale_gate, scale_up: of the weights' rows), out_dtype and rounding as for cleave_linear; gate, up and C have out_dtype.
+ * plan: cleave_plan_gated's for M, N, K and dtype (a batched plan of two M x N x K members; dims in pairs of values for
+ * CLEAVE_E4M3, K a multiple of 16).  partials: cleave_gated_workspace(plan, whole) floats (may be NULL if that is 0), of this call
+ * alone while it runs.  whole = 1 serves bf16 calls of which A, B_gate and B_up lie on 16-byte boundaries, K, lda and ldb are
+ * multiples of 8, N too with transB = 0, and lda and ldb are below 2^21; whole = 0 serves all.  (8-bit operands: either.)
+ * Few rows (M <= 16) read the weights as fast as memory gives them.  Bits, upload, streams: as for cleave_linear.
+ * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, two outputs in one place, partials missing,
+ * a plan of another kind or type. */
+typedef struct {
+  const void* A;
+  const void* B_gate;
+  const void* B_up;
+  const float* scale_a;
+  const float* scale_gate;
+  const float* scale_up;
+  const float* bias_gate;
+  const float* bias_up;
+  void* gate;
+  void* up;
+  void* C;
+  float* partials;
+  int64_t lda, ldb, ld_gate, ld_up, ldc;
+  int32_t transB;
+  int32_t dtype, out_dtype;
+  int32_t act;
+} cleave_gated_args;
+int cleave_plan_gated(int64_t M, int64_t N, int64_t K, int dtype, cleave_plan** out);
+int64_t cleave_gated_workspace(const cleave_plan* plan, int whole);
+int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* args, void* hip_stream);
+
+/* The gradient of its two arguments, out of the product with the weight behind it:
+ *   p = A op(B);   dgate = p up act'(gate);   dup = p act(gate)
+ * A: M x K, the gradient behind the next weight; B: that weight, as B of cleave_linear (stored N x K of the next layer's
+ * N x K projection: transB = 1); gate, up: the kept zg and zu, M x N; dgate, dup: M x N; all four of out_dtype.  dgate may be
+ * gate and dup may be up, with its leading dimension.  dtype: F32 or BF16.  plan: cleave_plan_linear's for M, N, K and dtype.
+ * partials: cleave_gated_grad_workspace(plan, whole) floats, whole as above.  The gradients of A and of the two weights are
+ * products of dgate and dup (cleave_linear; one each where both lie side by side in one matrix, as the weights then do).
+ * CLEAVE_EINVAL as above, or an output in another one's place. */
+typedef struct {
+  const void* A;
+  const void* B;
+  const void* gate;
+  const void* up;
+  void* dgate;
+  void* dup;
+  float* partials;
+  int64_t lda, ldb, ld_gate, ld_up, ld_dgate, ld_dup;
+  int32_t transB;
+  int32_t dtype, out_dtype;
+  int32_t act;
+} cleave_gated_grad_args;
+int64_t cleave_gated_grad_workspace(const cleave_plan* plan, int whole);
+int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_grad_args* args, void* hip_stream);
+
 /* AdamW on n_tensors tensors of sizes[k] contiguous elements in one launch per 56
  * tensors: with c = *grad_scale (device; NULL: 1), per element
  *   g = c g;  m = beta1 m + (1-beta1) g;  v = beta2 v + (1-beta2) g^2;

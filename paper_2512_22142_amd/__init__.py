@@ -10,6 +10,7 @@ and what a layer's step does between its GEMMs:
     rms_norm, rms_norm_backward   norm of the residual stream, its gradient
     layer_norm, layer_norm_backward   the same with the mean taken off, and a bias
     linear (plan_linear)          product with bias, activation (or its gradient) and residual; 8-bit operands
+    linear_gated (plan_gated), linear_gated_grad   two products, an activation and the product of both; its gradient
     bias_grad                     sum of a gradient's rows
     adamw                         optimizer step over many tensors, states in 32 or 8 bits
 
@@ -67,7 +68,12 @@ _OPERATOR_NAMES = (
     "layer_norm",
     "layer_norm_backward",
     "layer_norm_workspace",
+    "gated_grad_workspace",
+    "gated_workspace",
     "linear",
+    "linear_gated",
+    "linear_gated_grad",
+    "plan_gated",
     "plan_linear",
     "rms_norm",
     "rms_norm_backward",

@@ -190,6 +190,20 @@ int ensure_linear_ready(int dev) {
   return CLEAVE_OK;
 }
 
+// And the gated product's and its gradient's.
+bool g_gated_ready[kMaxDevices] = {};
+
+int ensure_gated_ready(int dev) {
+  if (dev < 0 || dev >= kMaxDevices) return CLEAVE_EINVAL;
+  std::lock_guard<std::mutex> lock(g_device_mu);
+  if (g_gated_ready[dev]) return CLEAVE_OK;
+  CLEAVE_HIP(cleave::configure_gated_direct_kernels());
+  CLEAVE_HIP(cleave::configure_gated_8bit_kernels());
+  CLEAVE_HIP(cleave::configure_gated_grad_kernels());
+  g_gated_ready[dev] = true;
+  return CLEAVE_OK;
+}
+
 constexpr int kSubsetEvents = 16;
 
 int allocate_subset_ring(cleave_plan* p) {
@@ -220,10 +234,15 @@ bool cut_small(const cleave_plan* plan, int cus);
 int ensure_uploaded(cleave_plan* p) {
   int dev = 0;
   CLEAVE_HIP(hipGetDevice(&dev));
+  if (p->fused) {
+    const int rc = ensure_uploaded(p->fused);
+    if (rc != CLEAVE_OK) return rc;
+  }
   if (p->device == dev) return CLEAVE_OK;
   if (p->device >= 0) free_device_tables(p);
   int rc = ensure_device_ready(dev, nullptr);
   if (rc == CLEAVE_OK && p->linear) rc = ensure_linear_ready(dev);
+  if (rc == CLEAVE_OK && p->gated) rc = ensure_gated_ready(dev);
   if (rc != CLEAVE_OK) return rc;
   rc = upload_vector(p->tasks, &p->d_tasks);
   hipStream_t writing = nullptr;
@@ -378,6 +397,20 @@ const char* linear_kernel_name(int dtype, const cleave::GeneralLoads& how, int t
   return names[bf16 ? 1 : 0][how.tile == cleave::kTileLone ? 1 : 0][(transA ? 2 : 0) + (transB ? 1 : 0)];
 }
 
+// which: a gated product of bf16, of e4m3, the gradient
+const char* gated_kernel_name(cleave::DirectShape shape, int which, int transB) {
+  static const char* names[4][3][2] = {
+      {{"gated_direct_bf16_256x128_nn", "gated_direct_bf16_256x128_nt"}, {"none", "none"},
+       {"gated_grad_direct_bf16_256x256_nn", "gated_grad_direct_bf16_256x256_nt"}},
+      {{"gated_direct_bf16_128x64_nn", "gated_direct_bf16_128x64_nt"}, {"none", "gated_direct_e4m3_128x64_nt"},
+       {"gated_grad_direct_bf16_128x128_nn", "gated_grad_direct_bf16_128x128_nt"}},
+      {{"gated_direct_bf16_128x64_deep_nn", "gated_direct_bf16_128x64_deep_nt"}, {"none", "gated_direct_e4m3_128x64_deep_nt"},
+       {"gated_grad_direct_bf16_128x128_deep_nn", "gated_grad_direct_bf16_128x128_deep_nt"}},
+      {{"gated_direct_bf16_64x32_nn", "gated_direct_bf16_64x32_nt"}, {"none", "gated_direct_e4m3_64x32_nt"},
+       {"gated_grad_direct_bf16_64x64_nn", "gated_grad_direct_bf16_64x64_nt"}}};
+  return names[shape][which][transB ? 1 : 0];
+}
+
 const char* linear_direct_kernel_name(cleave::DirectShape shape, bool e4m3, int transB) {
   static const char* names[4][3] = {   // (8-bit operands: no large shape, and B is N x K)
       {"linear_direct_bf16_256x256_nn", "linear_direct_bf16_256x256_nt", "none"},
@@ -402,6 +435,7 @@ extern "C" int cleave_plan_upload(cleave_plan* plan) {
 
 extern "C" void cleave_plan_destroy(cleave_plan* plan) {
   if (!plan) return;
+  cleave_plan_destroy(plan->fused);
   if (plan->device >= 0) free_device_tables(plan);
   delete plan->verify;
   delete plan;
@@ -741,13 +775,15 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
                  int64_t lda, int transA, const void* B, int64_t ldb, int transB, int dtype,
                  float* partials, const BatchLayout& bl, void* hip_stream,
                  const AssembleTarget& asm_to = AssembleTarget{}, bool static_scratch = false,
-                 const cleave::LinearArgs* linear = nullptr) {
+                 const cleave::LinearArgs* linear = nullptr, const cleave::GatedArgs* gated = nullptr) {
   if (!plan || !A || !B || (!partials && !asm_to.C)) return CLEAVE_EINVAL;
+  const bool two = gated && gated->b_up;   // a gated product: the plan's columns are both operands'
+  const bool epilogue = linear || gated;
   if (dtype != CLEAVE_F32 && dtype != CLEAVE_BF16) return CLEAVE_EINVAL;
-  if (plan->pairs && !linear) return CLEAVE_EINVAL;   // a plan of 8-bit operands
+  if (plan->pairs && !epilogue) return CLEAVE_EINVAL;   // a plan of 8-bit operands
   if ((transA != 0 && transA != 1) || (transB != 0 && transB != 1)) return CLEAVE_EINVAL;
   if ((task_ids == nullptr) != (n_ids == 0) || n_ids < 0) return CLEAVE_EINVAL;
-  if (lda < (transA ? plan->M : plan->K) || ldb < (transB ? plan->K : plan->N)) return CLEAVE_EINVAL;
+  if (lda < (transA ? plan->M : plan->K) || ldb < (transB ? plan->K : two ? plan->N / 2 : plan->N)) return CLEAVE_EINVAL;
   const int eb = dtype == CLEAVE_BF16 ? 2 : 4;
   if (!aligned(A, eb) || !aligned(B, eb) || !aligned(partials, 4)) return CLEAVE_EINVAL;   // null partials: assemble mode
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -776,7 +812,7 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
   // x 2504 x 1024 in 4 37 / 30.
   const int e = 16 / eb;
   // (The epilogue's stores take any number of columns, and its kernels read A along K.)
-  const bool direct = dtype == CLEAVE_BF16 && (plan->all_n_mult8 || (linear && transB)) && !(linear && transA) && (transA ? plan->all_m_mult8 : plan->all_k_mult8) &&
+  const bool direct = dtype == CLEAVE_BF16 && ((two ? plan->N % 16 == 0 : plan->all_n_mult8) || (epilogue && transB)) && !(epilogue && transA) && (transA ? plan->all_m_mult8 : plan->all_k_mult8) &&
                       (!transB || plan->all_k_mult8) &&
                       lda % e == 0 && ldb % e == 0 && aligned(A, 16) && aligned(B, 16) &&
                       // in-tile byte offsets are kept in 32 bits
@@ -785,6 +821,7 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
   // 8-bit operands have no general kernel, and partial blocks leave theirs in whole eights of columns (cleave_linear
   // refuses what would come here otherwise, and cleave_plan_linear does not plan it).
   if (plan->pairs && (!direct || (!asm_to.C && !plan->all_n_mult8))) return CLEAVE_EINVAL;
+  if (gated && (!direct || !aligned(gated->b_up, 16) || plan->device < 0)) return CLEAVE_EINVAL;
   // An operand of the general kernel's 16-byte loads needs that much between the start of a
   // stored row and the end of any chunk (K-contiguous) or row (otherwise), and
   // in-tile byte offsets (up to 128 rows) that fit 32 bits.
@@ -887,12 +924,16 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
       args.wg_ranges = (list >= 0 && plan->wg_ranges_grid[list] == grid)
                            ? plan->d_wg_ranges[list] : nullptr;
       if (args.wg_ranges && list == cleave::kNumTileClasses) args.items += counts[c];   // behind the list as laid out
-      const hipError_t he = plan->pairs ? cleave::launch_linear_8bit(args, *linear, shape, plan->chunk_tails, grid, stream)
+      const hipError_t he = two && plan->pairs ? cleave::launch_gated_8bit(args, *gated, shape, plan->chunk_tails, grid, stream)
+                            : two       ? cleave::launch_gated_direct(args, *gated, shape, plan->chunk_tails, grid, stream)
+                            : gated     ? cleave::launch_gated_grad_direct(args, *gated, shape, plan->chunk_tails, grid, stream)
+                            : plan->pairs ? cleave::launch_linear_8bit(args, *linear, shape, plan->chunk_tails, grid, stream)
                             : linear    ? cleave::launch_linear_direct(args, *linear, shape, plan->chunk_tails, grid, stream)
                                         : cleave::launch_execute_direct(args, shape, plan->chunk_tails, grid, stream);
       if (he != hipSuccess) return launch_failed(he);
       if (counts[c] > most)
-        plan->last_kernel = linear ? linear_direct_kernel_name(shape, plan->pairs, transB) : direct_kernel_name(shape, transA, transB);
+        plan->last_kernel = gated ? gated_kernel_name(shape, two ? plan->pairs : 2, transB)
+                            : linear ? linear_direct_kernel_name(shape, plan->pairs, transB) : direct_kernel_name(shape, transA, transB);
     } else {
       // in-tile byte offsets (256 rows) stay within 32 bits
       const bool by_k = !transA && transB && !a_elements && !b_elements && lda * eb < (int64_t{1} << 24) &&
@@ -1259,6 +1300,7 @@ extern "C" int cleave_plan_linear(int64_t M, int64_t N, int64_t K, int dtype, cl
                                      static_cast<int32_t>(linear_splits(M, N, k, dtype == CLEAVE_F32 ? 4 : 8, pairs)), 0, out);
   if (rc != CLEAVE_OK) return rc;
   (*out)->linear = true;
+  (*out)->for_fp32 = dtype == CLEAVE_F32;
   (*out)->pairs = pairs;
   return CLEAVE_OK;
 }
@@ -1351,6 +1393,239 @@ extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, voi
   args.ldc = a->ldc;
   CLEAVE_HIP(cleave::launch_linear_join(args, epi, M, N, static_cast<int>(splits), a->out_dtype,
                                         plan->all_n_mult4 && aligned(a->partials, 16), stream));
+  return CLEAVE_OK;
+}
+
+// ---- gated product ---------------------------------------------------------------
+
+namespace {
+
+// Few rows are read as cleave_linear reads them.
+bool gated_few_rows(int64_t M, int64_t N) { return M <= cleave::kFewRows && N <= int64_t{1} << 27; }
+
+// What the direct kernel takes of bf16 operands (in units of it: pairs of e4m3): whole sixteen bytes, in-tile offsets of 32 bits.
+bool whole_operand(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld < int64_t{1} << 21; }
+
+bool floats_aligned(const float* const* list, int n) {
+  for (int k = 0; k < n; ++k)
+    if (!aligned(list[k], 4)) return false;
+  return true;
+}
+
+// The few-rows launch's operands: K is cut into chunks that end on whole lines of 128 bytes (the last ones may be short, or
+// empty, which leaves zeros).
+cleave::ExecuteArgs few_rows_args(int64_t M, int64_t N, int64_t K, int eb, int64_t splits, int64_t* chunk) {
+  const int64_t line = 128 / eb;
+  *chunk = ((K + splits - 1) / splits + line - 1) / line * line;
+  cleave::ExecuteArgs args{};
+  args.M = M;
+  args.N = N;
+  args.K = K;
+  return args;
+}
+
+}  // namespace
+
+extern "C" int cleave_plan_gated(int64_t M, int64_t N, int64_t K, int dtype, cleave_plan** out) {
+  if (!linear_dtype(dtype) || !out || M < 1 || N < 1 || K < 1) return CLEAVE_EINVAL;
+  constexpr int64_t kMost = std::numeric_limits<int32_t>::max();
+  if (M > kMost || N > kMost / 2 || K > kMost) return CLEAVE_EINVAL;
+  const bool pairs = dtype == CLEAVE_E4M3;
+  if (pairs && K % 16 != 0) return CLEAVE_EINVAL;
+  const int64_t k = pairs ? K / 2 : K;
+  const bool few = gated_few_rows(M, N);
+  // tiles and splits as for one product of both operands' columns; 8-bit operands with more than a few rows are not split
+  // (a workgroup of few rows has 64 columns of both)
+  const int64_t splits = pairs && !few ? 1 : linear_splits(M, few ? N : 2 * N, k, dtype == CLEAVE_F32 ? 4 : 8, pairs);
+  const int64_t tile = M <= cleave::kFewRows ? cleave::kSmallTileRows
+                       : dtype == CLEAVE_F32 && splits > 1 && fp32_splits(M, 2 * N, K).workgroups > 128 ? 64
+                                                                                                       : cleave::kLargeTileRows;
+  cleave_plan* plan = nullptr;
+  int rc = cleave_plan_batched(M, N, k, tile, tile, static_cast<int32_t>(splits), 2, &plan);
+  if (rc != CLEAVE_OK) return rc;
+  plan->gated = true;
+  plan->pairs = pairs;
+  plan->uniform_splits = splits;
+  if (!few && splits == 1 && dtype != CLEAVE_F32) {
+    rc = cleave_plan_uniform(M, 2 * N, k, cleave::kLargeTileRows, cleave::kLargeTileCols, 1, 0, &plan->fused);
+    if (rc != CLEAVE_OK) {
+      cleave_plan_destroy(plan);
+      return rc;
+    }
+    plan->fused->gated = true;
+    plan->fused->pairs = pairs;
+  }
+  *out = plan;
+  return CLEAVE_OK;
+}
+
+extern "C" int64_t cleave_gated_workspace(const cleave_plan* plan, int whole) {
+  if (!plan || !plan->gated || plan->batch != 2 || (whole != 0 && whole != 1)) return CLEAVE_EINVAL;
+  if (gated_few_rows(plan->M, plan->N)) return plan->uniform_splits == 1 ? 0 : plan->partial_elems;
+  if (plan->pairs || (plan->fused && whole)) return 0;
+  return plan->partial_elems;
+}
+
+extern "C" int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* a, void* hip_stream) {
+  if (!plan || !a || !plan->gated || plan->batch != 2 || !linear_dtype(a->dtype)) return CLEAVE_EINVAL;
+  const bool e4m3 = a->dtype == CLEAVE_E4M3;
+  if (plan->pairs != e4m3 || !a->A || !a->B_gate || !a->B_up || !a->C) return CLEAVE_EINVAL;
+  if ((a->transB != 0 && a->transB != 1) || (a->out_dtype != CLEAVE_F32 && a->out_dtype != CLEAVE_BF16)) return CLEAVE_EINVAL;
+  if (a->act < CLEAVE_ACT_NONE || a->act > CLEAVE_ACT_SILU) return CLEAVE_EINVAL;
+  if (e4m3 != (a->scale_a != nullptr) || e4m3 != (a->scale_gate != nullptr) || e4m3 != (a->scale_up != nullptr)) return CLEAVE_EINVAL;
+  const int ob = a->out_dtype == CLEAVE_BF16 ? 2 : 4, eb = e4m3 ? 1 : a->dtype == CLEAVE_BF16 ? 2 : 4;
+  const int64_t M = plan->M, N = plan->N, K = e4m3 ? 2 * plan->K : plan->K;
+  if (a->lda < K || a->ldb < (a->transB ? K : N) || a->ldc < N || (a->gate && a->ld_gate < N) || (a->up && a->ld_up < N))
+    return CLEAVE_EINVAL;
+  const float* const vectors[] = {a->scale_a, a->scale_gate, a->scale_up, a->bias_gate, a->bias_up, a->partials};
+  if (!aligned(a->A, eb) || !aligned(a->B_gate, eb) || !aligned(a->B_up, eb) || !aligned(a->C, ob) || !aligned(a->gate, ob) ||
+      !aligned(a->up, ob) || !floats_aligned(vectors, 6))
+    return CLEAVE_EINVAL;
+  if (a->C == a->gate || a->C == a->up || (a->gate && a->gate == a->up)) return CLEAVE_EINVAL;   // outputs in one place
+  if (e4m3 && (!a->transB || !aligned(a->A, 16) || !aligned(a->B_gate, 16) || !aligned(a->B_up, 16) || a->lda % 16 || a->ldb % 16 ||
+               a->lda >= int64_t{1} << 22 || a->ldb >= int64_t{1} << 22))
+    return CLEAVE_EINVAL;
+  cleave::GatedArgs epi{};
+  epi.b_up = a->B_up;
+  epi.bias_gate = a->bias_gate;
+  epi.bias_up = a->bias_up;
+  epi.scale_a = a->scale_a;
+  epi.scale_gate = a->scale_gate;
+  epi.scale_up = a->scale_up;
+  epi.gate = a->gate;
+  epi.up = a->up;
+  epi.ld_gate = a->ld_gate;
+  epi.ld_up = a->ld_up;
+  epi.act = a->act;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const int64_t splits = plan->uniform_splits;
+  const bool few = gated_few_rows(M, N);
+  const bool whole = e4m3 || (a->dtype == CLEAVE_BF16 && K % 8 == 0 && (a->transB || N % 8 == 0) && whole_operand(a->A, a->lda) &&
+                              whole_operand(a->B_gate, a->ldb) && whole_operand(a->B_up, a->ldb));
+  const bool fused = !few && plan->fused && whole;
+  if (!fused && (!few || splits > 1) && !a->partials) return CLEAVE_EINVAL;
+  if (fused) {
+    AssembleTarget to;
+    to.C = a->C;
+    to.ldc = a->ldc;
+    to.out_dtype = a->out_dtype;
+    int rc = ensure_uploaded(plan->fused);
+    if (rc == CLEAVE_OK)
+      rc = execute_impl(plan->fused, nullptr, 0, a->A, e4m3 ? a->lda / 2 : a->lda, 0, a->B_gate, e4m3 ? a->ldb / 2 : a->ldb,
+                        a->transB, CLEAVE_BF16, nullptr, BatchLayout{}, hip_stream, to, false, nullptr, &epi);
+    plan->last_kernel = plan->fused->last_kernel;
+    return rc;
+  }
+  cleave::ReduceArgs join{};
+  join.partials = a->partials;
+  join.C = a->C;
+  join.ldc = a->ldc;
+  const bool vec = N % 4 == 0 && aligned(a->partials, 16);
+  if (few) {
+    int64_t chunk = 0;
+    cleave::ExecuteArgs args = few_rows_args(M, N, K, eb, splits, &chunk);
+    args.A = a->A;
+    args.B = a->B_gate;
+    args.lda = a->lda;
+    args.ldb = a->ldb;
+    args.transB = a->transB;
+    args.partials = a->partials;
+    args.C = a->C;
+    args.ldc = a->ldc;
+    args.c_bf16 = a->out_dtype == CLEAVE_BF16;
+    CLEAVE_HIP(cleave::launch_gated_few_rows(args, epi, a->dtype, static_cast<int>(splits), chunk, stream));
+    plan->last_kernel = "gated_few_rows";
+    if (splits == 1) return CLEAVE_OK;
+    CLEAVE_HIP(cleave::launch_gated_join(join, epi, N, M, N, static_cast<int>(splits), a->out_dtype, vec, stream));
+    return CLEAVE_OK;
+  }
+  // both products' partial blocks, then one pass over them
+  const void* const As[2] = {a->A, a->A};
+  const void* const Bs[2] = {a->B_gate, a->B_up};
+  int rc = cleave_execute_grouped(plan, nullptr, 0, 2, As, a->lda, 0, Bs, a->ldb, a->transB, a->dtype, a->partials, hip_stream);
+  if (rc != CLEAVE_OK) return rc;
+  // (a long table of runs begins with the last member's)
+  const bool up_first = plan->tasks[plan->reduce_tiles[0].task].gemm_id != 0;
+  join.n_items = plan->reduce_runs / 2;
+  join.items = plan->d_reduce_items + (up_first ? join.n_items : 0);
+  CLEAVE_HIP(cleave::launch_gated_join(join, epi, plan->partial_elems / 2, M, N, static_cast<int>(splits), a->out_dtype,
+                                       plan->all_n_mult4 && vec, stream));
+  return CLEAVE_OK;
+}
+
+extern "C" int64_t cleave_gated_grad_workspace(const cleave_plan* plan, int whole) {
+  if (!plan || !plan->linear || plan->pairs || (whole != 0 && whole != 1)) return CLEAVE_EINVAL;
+  if (!gated_few_rows(plan->M, plan->N) && whole && plan->uniform_splits == 1 && !plan->for_fp32) return 0;
+  return plan->partial_elems;
+}
+
+extern "C" int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_grad_args* a, void* hip_stream) {
+  if (!plan || !a || !plan->linear || plan->pairs || (a->dtype != CLEAVE_F32 && a->dtype != CLEAVE_BF16)) return CLEAVE_EINVAL;
+  if (!a->A || !a->B || !a->gate || !a->up || !a->dgate || !a->dup) return CLEAVE_EINVAL;
+  if ((a->transB != 0 && a->transB != 1) || (a->out_dtype != CLEAVE_F32 && a->out_dtype != CLEAVE_BF16)) return CLEAVE_EINVAL;
+  if (a->act < CLEAVE_ACT_NONE || a->act > CLEAVE_ACT_SILU) return CLEAVE_EINVAL;
+  const int ob = a->out_dtype == CLEAVE_BF16 ? 2 : 4, eb = a->dtype == CLEAVE_BF16 ? 2 : 4;
+  const int64_t M = plan->M, N = plan->N, K = plan->K;
+  if (a->lda < K || a->ldb < (a->transB ? K : N) || a->ld_gate < N || a->ld_up < N || a->ld_dgate < N || a->ld_dup < N)
+    return CLEAVE_EINVAL;
+  if (!aligned(a->A, eb) || !aligned(a->B, eb) || !aligned(a->gate, ob) || !aligned(a->up, ob) || !aligned(a->dgate, ob) ||
+      !aligned(a->dup, ob) || !aligned(a->partials, 4))
+    return CLEAVE_EINVAL;
+  // in place: each over its own argument, the same elements at the same places
+  if (a->dgate == a->dup || a->dgate == a->up || a->dup == a->gate ||
+      (a->dgate == a->gate && M > 1 && a->ld_dgate != a->ld_gate) || (a->dup == a->up && M > 1 && a->ld_dup != a->ld_up))
+    return CLEAVE_EINVAL;
+  cleave::GatedArgs epi{};
+  epi.gate = const_cast<void*>(a->gate);
+  epi.up = const_cast<void*>(a->up);
+  epi.second = a->dup;
+  epi.ld_gate = a->ld_gate;
+  epi.ld_up = a->ld_up;
+  epi.ld_second = a->ld_dup;
+  epi.act = a->act;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const int64_t splits = plan->uniform_splits;
+  const bool few = gated_few_rows(M, N);
+  const bool whole = a->dtype == CLEAVE_BF16 && K % 8 == 0 && (a->transB || N % 8 == 0) && whole_operand(a->A, a->lda) &&
+                     whole_operand(a->B, a->ldb);
+  const bool fused = !few && whole && splits == 1;
+  if (!fused && !a->partials) return CLEAVE_EINVAL;
+  int rc = ensure_uploaded(plan);
+  if (rc == CLEAVE_OK) rc = ensure_gated_ready(plan->device);
+  if (rc != CLEAVE_OK) return rc;
+  if (fused) {
+    AssembleTarget to;
+    to.C = a->dgate;
+    to.ldc = a->ld_dgate;
+    to.out_dtype = a->out_dtype;
+    return execute_impl(plan, nullptr, 0, a->A, a->lda, 0, a->B, a->ldb, a->transB, a->dtype, nullptr, BatchLayout{}, hip_stream, to,
+                        false, nullptr, &epi);
+  }
+  if (few) {   // (the sums themselves, also where there is one chunk)
+    int64_t chunk = 0;
+    cleave::ExecuteArgs args = few_rows_args(M, N, K, eb, splits, &chunk);
+    args.A = a->A;
+    args.B = a->B;
+    args.lda = a->lda;
+    args.ldb = a->ldb;
+    args.transB = a->transB;
+    args.partials = a->partials;
+    args.C = a->partials;
+    args.ldc = N;
+    CLEAVE_HIP(cleave::launch_linear_few_rows(args, cleave::LinearArgs{}, a->dtype, static_cast<int>(splits), chunk, stream));
+    plan->last_kernel = "linear_few_rows";
+  } else {
+    rc = execute_impl(plan, nullptr, 0, a->A, a->lda, 0, a->B, a->ldb, a->transB, a->dtype, a->partials, BatchLayout{}, hip_stream);
+    if (rc != CLEAVE_OK) return rc;
+  }
+  cleave::ReduceArgs join{};
+  join.items = few ? nullptr : plan->d_reduce_items;
+  join.n_items = plan->reduce_runs;
+  join.partials = a->partials;
+  join.C = a->dgate;
+  join.ldc = a->ld_dgate;
+  CLEAVE_HIP(cleave::launch_gated_grad_join(join, epi, M, N, static_cast<int>(splits), a->out_dtype,
+                                            plan->all_n_mult4 && N % 4 == 0 && aligned(a->partials, 16), stream));
   return CLEAVE_OK;
 }
 

@@ -30,7 +30,7 @@
 //   * operand stored with the tile-row index contiguous (read "transposed"):
 //     the tile is kept as 64 k rows of R/8 chunks,
 //       slot = k*(R/8) + (chunk ^ swizzle(k)),
-//       swizzle = 4*(k & 3) ^ 2*((k >> 3) & 1),  for R = 64 4*((k >> 1) & 1) ^ 2*((k >> 3) & 1);
+//       swizzle = 4*(k & 3) ^ 2*((k >> 3) & 1),  for R = 64 4*((k >> 1) & 1) ^ 2*((k >> 3) & 1),  for R = 32 2*((k >> 3) & 1);
 //     fragments are gathered with the LDS transpose read (ds_read_b64_tr_b16:
 //     within 16 lanes, lane i supplies the address of 4 consecutive elements of
 //     k row i/4 and receives column i of the 4 x 16 block), two reads per
@@ -52,6 +52,7 @@
 #include <utility>
 
 #include "fp8_round.h"
+#include "gated_epilogue.h"
 #include "kernels.h"
 #include "linear_epilogue.h"
 #include "tile_store.h"
@@ -121,7 +122,7 @@ __device__ __forceinline__ int row_swizzle(int r) { return (r >> 1) & 7; }
 // read touches (four neighbours, and four of the next eight).
 template <int CH>
 __device__ __forceinline__ int k_swizzle(int k) {
-  return (CH == 8 ? 4 * ((k >> 1) & 1) : 4 * (k & 3)) ^ (2 * ((k >> 3) & 1));
+  return (CH == 4 ? 0 : CH == 8 ? 4 * ((k >> 1) & 1) : 4 * (k & 3)) ^ (2 * ((k >> 3) & 1));
 }
 
 __device__ __align__(16) const unsigned char g_zeros[16] = {};
@@ -230,7 +231,9 @@ __device__ __forceinline__ void spread_reads() {
 
 // TAILS: some chunk of the launch ends within a K step (the code for that costs
 // scalar registers: an instantiation of its own).
-// Epi: what the sums go through on their way out (linear_epilogue.h).
+// Epi: what the sums go through on their way out (linear_epilogue.h).  A gated product (Epi::kGated) has two operands B of one
+// layout: B's tile in LDS is one tile of TN / 2 columns behind the other, and a wave's NB blocks of columns are NB / 2 of the first
+// and the same NB / 2 of the second, so that both sums of an element are in one lane.  Its work items count both operands' columns.
 // OPS: with e4m3 operands (kE4M3) a pair of values is what is written "bf16 element" below: both K-contiguous, and every
 // size and stride along K counts pairs.  They are multiplied as bf16 (v_cvt, exact; a fragment's conversions serve all of its
 // products), so that the sums are fp32 sums.  The 8-bit instructions of twice the rate are not used: they drop what lies below
@@ -242,7 +245,9 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   constexpr int TM = S::TM, TN = S::TN, MB = S::MB, NB = S::NB, CPR = S::CPR, kSub = S::kSub;
   constexpr int kStage = S::kStage, kATile = S::kATile, STAGES = S::STAGES, LPS = S::kLoadsPerStep;
   constexpr int kRowBytes = CPR * 16;        // K-contiguous tile row
-  constexpr int CHA = TM / 8, CHB = TN / 8;  // chunks per k row, transposed tiles
+  constexpr int TNB = Epi::kGated ? TN / 2 : TN;   // columns of one operand B
+  constexpr int NBB = Epi::kGated ? NB / 2 : NB, WTNB = Epi::kGated ? S::WTN / 2 : S::WTN;
+  constexpr int CHA = TM / 8, CHB = TNB / 8; // chunks per k row, transposed tiles
 
   extern __shared__ __align__(16) unsigned char smem[];
 
@@ -277,12 +282,12 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   if constexpr (B_K) {
 #pragma unroll
     for (int ks = 0; ks < kSub; ++ks)
-      b_addr[ks] = kATile + (wn * S::WTN + l16) * kRowBytes + (((4 * ks + lq) ^ row_swizzle(l16)) * 16);
+      b_addr[ks] = kATile + (wn * WTNB + l16) * kRowBytes + (((4 * ks + lq) ^ row_swizzle(l16)) * 16);
   } else {
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      const int c = wn * (S::WTN / 8) + j * 2 + (cq >> 1);
-      b_addr[j] = kATile + ((8 * lq + kq) * CHB + (c ^ k_swizzle<CHB>(8 * lq + kq))) * 16 + (cq & 1) * 8;
+      const int c = wn * (WTNB / 8) + j % NBB * 2 + (cq >> 1);
+      b_addr[j] = kATile + j / NBB * (S::kBTile / 2) + ((8 * lq + kq) * CHB + (c ^ k_swizzle<CHB>(8 * lq + kq))) * 16 + (cq & 1) * 8;
     }
   }
 
@@ -301,7 +306,7 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
     int tail;                     // elements of the last step if it is not a whole one, else 0
     uint32_t m_base, n_base;      // its place in the output (read by an epilogue only)
   };
-  auto load_item = [&](int64_t idx) -> WorkItem {
+  auto load_part = [&](int64_t idx) -> WorkItem {
     if constexpr (S::PARTS == 1) {
       return load_work_item(args.items, idx);
     } else {
@@ -319,6 +324,14 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
       w.out_off += static_cast<uint64_t>(mo) * w.out_ld + no;
       return w;
     }
+  };
+  auto load_item = [&](int64_t idx) -> WorkItem {
+    WorkItem w = load_part(idx);
+    if constexpr (Epi::kGated) {   // the columns of one operand B
+      w.n_base /= 2;
+      w.n_valid /= 2;
+    }
+    return w;
   };
   auto make_ctx = [&](const WorkItem& w) -> ItemCtx {
     ItemCtx c;
@@ -341,7 +354,9 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   const int64_t b_step = b_ks * S::BK * 2;
 
   DirectTile<S, A_K, TM> ta;
-  DirectTile<S, B_K, TN> tb;
+  DirectTile<S, B_K, TNB> tb;
+  [[maybe_unused]] int64_t to_up = 0;   // bytes from the first operand B to the second
+  if constexpr (Epi::kGated) to_up = static_cast<const unsigned char*>(epi.b_up) - static_cast<const unsigned char*>(args.B);
   // Fetches the item's next step into ring stage st: A's part and B's, each at
   // once or in two halves.
   constexpr int_c<0> whole{};
@@ -354,13 +369,25 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   };
   auto issue_b = [&](ItemCtx& c, int st, auto what) {
     constexpr int W = decltype(what)::value, L = S::kLoadsB / (W ? 2 : 1);
-    tb.template issue<W == 2 ? L : 0, L>(c.b_ptr, smem_off + st * kStage + kATile, wave);
+    const uint32_t lds = smem_off + st * kStage + kATile;
+    if constexpr (Epi::kGated) {
+      constexpr int LB = S::kLoadsB / 2;
+      if (W != 2) tb.template issue<0, LB>(c.b_ptr, lds, wave);
+      if (W != 1) tb.template issue<0, LB>(c.b_ptr + to_up, lds + S::kBTile / 2, wave);
+    } else {
+      tb.template issue<W == 2 ? L : 0, L>(c.b_ptr, lds, wave);
+    }
     if (W != 1) c.b_ptr += b_step;
+  };
+  auto issue_tails = [&](ItemCtx& c, int st) {
+    const uint32_t lds = smem_off + st * kStage;
+    ta.issue_tail(c.a_ptr, lds, wave, lane, c.tail);
+    tb.issue_tail(c.b_ptr, lds + kATile, wave, lane, c.tail);
+    if constexpr (Epi::kGated) tb.issue_tail(c.b_ptr + to_up, lds + kATile + S::kBTile / 2, wave, lane, c.tail);
   };
   auto issue = [&](ItemCtx& c, int s, int st) {   // s: that step, which may be the chunk's last
     if (TAILS && c.tail != 0 && s == c.steps - 1) {
-      ta.issue_tail(c.a_ptr, smem_off + st * kStage, wave, lane, c.tail);
-      tb.issue_tail(c.b_ptr, smem_off + st * kStage + kATile, wave, lane, c.tail);
+      issue_tails(c, st);
       return;
     }
     issue_a(c, st, whole);
@@ -386,9 +413,10 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   // other lane offsets) the ring is filled from empty after the item's last
   // step, ahead of its stores.
   //
-  // Store instructions per lane of a full sub-tile.
+  // Store instructions per lane of a full sub-tile (with an epilogue: at least).
   const bool bf16_out = args.C && args.c_bf16;
-  const int tile_stores = bf16_out ? MB * NB / 2 : MB * NB;
+  int tile_stores = bf16_out ? MB * NB / 2 : MB * NB;
+  if constexpr (Epi::kGated) tile_stores = bf16_out ? gated_stores<true, MB, NB>() : gated_stores<false, MB, NB>();
   unsigned char* const image = smem + STAGES * kStage + wave * kBlockImageBytes;
 
   // This workgroup's items: first, first + stride, ... below it_end.
@@ -489,7 +517,8 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
 #pragma unroll
     for (int j = J0; j < J0 + decltype(n_tag)::value; ++j) {
       if constexpr (B_K) {
-        fb[SET][j] = *reinterpret_cast<const u32x4*>(smem + (b_addr[KS] + stage) + j * 16 * kRowBytes);
+        fb[SET][j] = *reinterpret_cast<const u32x4*>(smem + (b_addr[KS] + stage) + j % NBB * 16 * kRowBytes +
+                                                     j / NBB * (S::kBTile / 2));
       } else {
         const unsigned char* p = smem + (b_addr[j] + stage) + KS * (32 * CHB * 16);
         const u32x2 lo = tr_read(p);
@@ -538,9 +567,9 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   for (;;) {
     const int steps = c.steps;
     const bool has_next = !S::ONE_ITEM && it_next < it_end;
-    const bool interior = c.m_valid == TM && c.n_valid == TN;
+    const bool interior = c.m_valid == TM && c.n_valid == TNB;
     // hand the ring over without draining it
-    const bool cont = has_next && interior && nx.m_valid == TM && nx.n_valid == TN && steps >= STAGES && nx.steps >= STAGES;
+    const bool cont = has_next && interior && nx.m_valid == TM && nx.n_valid == TNB && steps >= STAGES && nx.steps >= STAGES;
     // stores between the steps fetched ahead of the item and its own
     const int stores_behind = entry == kFilled ? 0 : tile_stores;
 
@@ -598,8 +627,7 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
           }
         } else if constexpr (HOW == kRefilledLast) {
           CLEAVE_WAIT_BARRIER((STAGES - 2) * LPS);
-          ta.issue_tail(c.a_ptr, smem_off + st * kStage, wave, lane, c.tail);
-          tb.issue_tail(c.b_ptr, smem_off + st * kStage + kATile, wave, lane, c.tail);
+          issue_tails(c, st);
         } else if constexpr (HOW != kAnyStep) {
           if constexpr (HOW > 1) CLEAVE_WAIT_BARRIER((HOW - 2) * LPS);
         } else {
@@ -732,14 +760,22 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
     const auto leave = [&](auto bf16_tag, auto interior_tag, auto stream_tag) {
       // (an epilogue's loads and further stores come on top of the stores that the waits count: these
       // then wait for more than they need)
-      if constexpr (OPS == kE4M3) {
+      if constexpr (OPS == kE4M3 && !Epi::kGated) {
         if (args.C == nullptr) {   // partial blocks, joined with the epilogue by another kernel
           store_rows<false, decltype(interior_tag)::value, false, MB, NB>(acc, target, image, wm * S::WTM, wn * S::WTN, lane,
                                                                           m_valid, n_valid);
           return;
         }
       }
-      if constexpr (Epi::kLinear)
+      if constexpr (Epi::kGated)
+        store_gated_rows<decltype(bf16_tag)::value, decltype(interior_tag)::value, OPS != kBf16, MB, NB>(
+            acc, late_linear_args<sizeof(ExecuteArgs), GatedArgs>(), target, image, wm * S::WTM, wn * WTNB, lane, m_valid, n_valid,
+            m_base, n_base);
+      else if constexpr (std::is_same<Epi, GatedGradEpilogue>::value)
+        store_gated_grad_rows<decltype(bf16_tag)::value, decltype(interior_tag)::value, MB, NB>(
+            acc, late_linear_args<sizeof(ExecuteArgs), GatedArgs>(), target, image, wm * S::WTM, wn * S::WTN, lane, m_valid, n_valid,
+            m_base, n_base);
+      else if constexpr (Epi::kLinear)
         store_linear_rows<decltype(bf16_tag)::value, decltype(interior_tag)::value, OPS != kBf16, 1, MB, NB>(
             acc, late_linear_args<sizeof(ExecuteArgs)>(), target, image, wm * S::WTM, wn * S::WTN, lane, m_valid, n_valid,
             m_base, n_base);

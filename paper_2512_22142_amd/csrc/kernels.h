@@ -78,6 +78,21 @@ struct LinearArgs {
   int grad;
 };
 
+// The gated product's and its gradient's (gated_epilogue.h).  gate, up and second have the output's type.
+struct GatedArgs {
+  const void* b_up;           // the second operand B, stored as the first one is (the gradient: unused)
+  const float* bias_gate;     // N; may be null
+  const float* bias_up;
+  const float* scale_a;       // M and N, 8-bit operands; else null
+  const float* scale_gate;
+  const float* scale_up;
+  void* gate;                 // the arguments: written, or null; the gradient reads them
+  void* up;
+  void* second;               // the gradient's second output
+  int64_t ld_gate, ld_up, ld_second;   // elements
+  int64_t act;
+};
+
 // Bytes of the Infinity Cache: what is written last, up to that much, is still
 // there when the next launch reads it.
 constexpr int64_t kCacheBytes = int64_t{256} << 20;
@@ -231,11 +246,23 @@ hipError_t launch_linear_8bit(const ExecuteArgs& args, const LinearArgs& epi, Di
 hipError_t launch_linear_general(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int tile_class,
                                  const GeneralLoads& how, hipStream_t stream);
 
+// The gated product on the direct kernel, transA = 0: work items of M x 2N, of whose columns the kernel takes half for each
+// operand B.  e4m3: as for launch_linear_8bit.  And its gradient: work items of M x N.
+hipError_t launch_gated_direct(const ExecuteArgs& args, const GatedArgs& epi, DirectShape shape, bool tails, int grid,
+                               hipStream_t stream);
+hipError_t launch_gated_8bit(const ExecuteArgs& args, const GatedArgs& epi, DirectShape shape, bool tails, int grid,
+                             hipStream_t stream);
+hipError_t launch_gated_grad_direct(const ExecuteArgs& args, const GatedArgs& epi, DirectShape shape, bool tails, int grid,
+                                    hipStream_t stream);
+
 // Few rows (at most kFewRows), transA = 0, any size, stride and alignment: B is read once.  Into args.C through the
 // epilogue or, with splits > 1, chunks of `chunk` elements into partials[s][row][column] for launch_linear_join.
 constexpr int64_t kFewRows = 16;
 hipError_t launch_linear_few_rows(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int splits, int64_t chunk,
                                   hipStream_t stream);
+// The gated product likewise; partials[s][row][column of 2N], gate's columns first, for launch_gated_join.
+hipError_t launch_gated_few_rows(const ExecuteArgs& args, const GatedArgs& epi, int dtype, int splits, int64_t chunk,
+                                 hipStream_t stream);
 
 // Raises the dynamic-LDS limit of every execute kernel on the current device
 // (needed once per device and process, before the first launch).
@@ -244,6 +271,9 @@ hipError_t configure_execute_direct_kernels();
 hipError_t configure_linear_general_kernels();
 hipError_t configure_linear_direct_kernels();
 hipError_t configure_linear_8bit_kernels();
+hipError_t configure_gated_direct_kernels();
+hipError_t configure_gated_8bit_kernels();
+hipError_t configure_gated_grad_kernels();
 
 // ---- work-item lists of subset launches ---------------------------------------
 // One entry per re-issued task: which task, and where its work items go.  The
@@ -287,6 +317,13 @@ hipError_t launch_reduce(const ReduceArgs& args, int out_dtype, bool vec, int gr
 // M x N with `splits` blocks.  `vec`: four elements at a time.
 hipError_t launch_linear_join(const ReduceArgs& args, const LinearArgs& epi, int64_t M, int64_t N, int splits, int out_dtype,
                               bool vec, hipStream_t stream);
+
+// The gated product from partial blocks (`items`: the runs of gate's; up's lie `up_at` elements behind), or from
+// launch_gated_few_rows' (args.items null, up_at N).  And its gradient from those of one product.
+hipError_t launch_gated_join(const ReduceArgs& args, const GatedArgs& epi, int64_t up_at, int64_t M, int64_t N, int splits,
+                             int out_dtype, bool vec, hipStream_t stream);
+hipError_t launch_gated_grad_join(const ReduceArgs& args, const GatedArgs& epi, int64_t M, int64_t N, int splits, int out_dtype,
+                                  bool vec, hipStream_t stream);
 
 // Aggregation with a residual added: C = sum of partials + R; R has C's
 // element type, leading dimension and batch strides.

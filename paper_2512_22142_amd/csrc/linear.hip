@@ -19,6 +19,7 @@
 #include <type_traits>
 
 #include "fp8_round.h"
+#include "gated_epilogue.h"
 #include "kernels.h"
 #include "linear_epilogue.h"
 
@@ -100,9 +101,13 @@ struct Group {   // what a lane holds of a group of k's
   std::conditional_t<B_K, u32x4, Columns4<DTYPE>> w[B_K ? 4 : E];
 };
 
-template <int DTYPE, bool B_K, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, LinearArgs epi, int splits, int64_t chunk) {
+// Epi: LinearArgs, or GatedArgs: half of a workgroup's waves then read gate's columns and half the same columns of up, so that what a wave
+// holds, and what it reads at a time, is as for one operand.
+template <int DTYPE, bool B_K, int WAVES, typename Epi>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, Epi epi, int splits, int64_t chunk) {
   constexpr int E = Type<DTYPE>::E, KG = 4 * E, EB = 16 / E;
+  constexpr bool GATED = std::is_same<Epi, GatedArgs>::value;
+  constexpr int TURNS = GATED ? WAVES / 2 : WAVES;   // waves that share an operand
   __shared__ float sums[WAVES][kFewRows][kColumns];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, lq = lane >> 4;
@@ -115,7 +120,10 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, 
   const int64_t g1 = (k1 - k0 + KG - 1) / KG;
 
   // rows and columns that are not there repeat the last ones: their sums are not stored, or are the same twice
-  const unsigned char* const B = static_cast<const unsigned char*>(args.B);
+  const unsigned char* B = static_cast<const unsigned char*>(args.B);
+  if constexpr (GATED) {
+    if (wave >= TURNS) B = static_cast<const unsigned char*>(epi.b_up);
+  }
   const unsigned char* const xp =
       static_cast<const unsigned char*>(args.A) + (std::min<int64_t>(l16, M - 1) * args.lda + E * lq) * EB;
   const int first = static_cast<int>(std::min<int64_t>(4 * l16, std::max<int64_t>(N - 4, 0) - n0));   // of a K x N row's four
@@ -175,16 +183,16 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, 
   };
   // the next groups are on their way while one is multiplied
   G set[3];
-  int64_t g = wave;
+  int64_t g = GATED ? wave % TURNS : wave;
   if (g < g1) load(g, set[0]);
-  if (g + WAVES < g1) load(g + WAVES, set[1]);
+  if (g + TURNS < g1) load(g + TURNS, set[1]);
   while (g < g1) {
 #pragma unroll
     for (int s = 0; s < 3; ++s) {
       if (g >= g1) break;
-      if (g + 2 * WAVES < g1) load(g + 2 * WAVES, set[(s + 2) % 3]);
+      if (g + 2 * TURNS < g1) load(g + 2 * TURNS, set[(s + 2) % 3]);
       compute(set[s]);
-      g += WAVES;
+      g += TURNS;
     }
   }
 
@@ -203,19 +211,41 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, 
     if (n >= N) continue;
     float sum = sums[0][row][col];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) sum += sums[w][row][col];
-    if (splits > 1) args.partials[(blockIdx.y * M + row) * N + n] = sum;
+    for (int w = 1; w < TURNS; ++w) sum += sums[w][row][col];
+    if constexpr (GATED) {
+      float up = sums[TURNS][row][col];
+#pragma unroll
+      for (int w = TURNS + 1; w < WAVES; ++w) up += sums[w][row][col];
+      if (splits > 1) {
+        float* p = args.partials + (blockIdx.y * M + row) * 2 * N + n;
+        p[0] = sum;
+        p[N] = up;
+      } else if (args.c_bf16) {
+        store_element<true>(args.C, row * args.ldc + n, finish_gated_element<true>(epi, sum, up, row, n));
+      } else {
+        store_element<false>(args.C, row * args.ldc + n, finish_gated_element<false>(epi, sum, up, row, n));
+      }
+    } else if (splits > 1) args.partials[(blockIdx.y * M + row) * N + n] = sum;
     else if (args.c_bf16) store_element<true>(args.C, row * args.ldc + n, finish_element<true>(epi, sum, row, n));
     else store_element<false>(args.C, row * args.ldc + n, finish_element<false>(epi, sum, row, n));
   }
 }
 
-template <int DTYPE, bool B_K>
-hipError_t launch_layout(const ExecuteArgs& args, const LinearArgs& epi, int splits, int64_t chunk, hipStream_t stream) {
+template <int DTYPE, bool B_K, typename Epi>
+hipError_t launch_layout(const ExecuteArgs& args, const Epi& epi, int splits, int64_t chunk, hipStream_t stream) {
   const dim3 g(static_cast<uint32_t>((args.N + kColumns - 1) / kColumns), splits);
-  if (splits > 1) hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 4>), g, dim3(256), 0, stream, args, epi, splits, chunk);
-  else hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 16>), g, dim3(1024), 0, stream, args, epi, splits, chunk);
+  if (splits > 1) hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 4, Epi>), g, dim3(256), 0, stream, args, epi, splits, chunk);
+  else hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 16, Epi>), g, dim3(1024), 0, stream, args, epi, splits, chunk);
   return hipGetLastError();
+}
+template <typename Epi>
+hipError_t launch_few_rows(const ExecuteArgs& args, const Epi& epi, int dtype, int splits, int64_t chunk, hipStream_t stream) {
+  if (dtype == CLEAVE_E4M3) return launch_layout<CLEAVE_E4M3, true>(args, epi, splits, chunk, stream);
+  if (dtype == CLEAVE_BF16)
+    return args.transB ? launch_layout<CLEAVE_BF16, true>(args, epi, splits, chunk, stream)
+                       : launch_layout<CLEAVE_BF16, false>(args, epi, splits, chunk, stream);
+  return args.transB ? launch_layout<CLEAVE_F32, true>(args, epi, splits, chunk, stream)
+                     : launch_layout<CLEAVE_F32, false>(args, epi, splits, chunk, stream);
 }
 
 // ---- join ------------------------------------------------------------------------
@@ -316,16 +346,113 @@ __global__ __launch_bounds__(kJoinThreads) void linear_join_kernel(ReduceArgs ar
   }
 }
 
+// The same for a gated product (two sums to an element) or its gradient (two outputs).  Without a table an element's sums lie at
+// row * pitch + col of each of `splits` blocks.
+template <bool BF16, bool GRAD, bool VEC>
+__global__ __launch_bounds__(kJoinThreads) void gated_join_kernel(ReduceArgs args, GatedArgs epi, int64_t up_at, int64_t M, int64_t N,
+                                                                  int64_t pitch, int splits) {
+  constexpr int W = VEC ? 4 : 1;
+  for (int64_t it = blockIdx.x; it < args.n_items; it += gridDim.x) {
+    ReduceItem item{};
+    int64_t first = 0;
+    if (args.items) {
+      item = load_record(args.items, it);
+    } else {
+      first = it * kJoinRun;
+      item.block = static_cast<uint64_t>(M * pitch);
+      item.n_len = static_cast<uint32_t>(N);
+      item.m0 = static_cast<uint32_t>(first / N);
+      item.col0 = static_cast<uint32_t>(first % N);
+      item.count = static_cast<uint32_t>(std::min<int64_t>(kJoinRun, M * N - first));
+      item.ksplit_cnt = static_cast<uint32_t>(splits);
+    }
+    for (uint32_t e = threadIdx.x * W; e < item.count; e += kJoinThreads * W) {
+      const uint32_t r = (item.col0 + e) / item.n_len;
+      const int64_t row = int64_t{item.m0} + r, col = int64_t{item.n0} + (item.col0 + e - r * item.n_len);
+      const float* p = args.partials + (args.items ? static_cast<int64_t>(item.partial_off) + e : row * pitch + col);
+      if constexpr (VEC) {
+        f32x4 sum = *reinterpret_cast<const f32x4*>(p), other{};
+        if constexpr (!GRAD) other = *reinterpret_cast<const f32x4*>(p + up_at);
+#pragma unroll 4
+        for (uint32_t s = 1; s < item.ksplit_cnt; ++s) {
+          sum = sum + *reinterpret_cast<const f32x4*>(p + s * item.block);
+          if constexpr (!GRAD) other = other + *reinterpret_cast<const f32x4*>(p + up_at + s * item.block);
+        }
+        float a[4] = {sum[0], sum[1], sum[2], sum[3]}, b[4] = {other[0], other[1], other[2], other[3]};
+        if constexpr (GRAD) {
+          float zg[4];
+          Quad<BF16>::load(epi.gate, row * epi.ld_gate + col, zg);
+          Quad<BF16>::load(epi.up, row * epi.ld_up + col, b);
+          finish_gated_grad(static_cast<int>(epi.act), a, zg, b);
+          Quad<BF16>::store(epi.second, row * epi.ld_second + col, b);
+          Quad<BF16>::store(args.C, row * args.ldc + col, a);
+        } else {
+          float bg[4] = {}, bu[4] = {}, sg[4] = {}, su[4] = {}, y[4];
+          if (epi.bias_gate) Quad<false>::load(epi.bias_gate, col, bg);
+          if (epi.bias_up) Quad<false>::load(epi.bias_up, col, bu);
+          if (epi.scale_a) {
+            Quad<false>::load(epi.scale_gate, col, sg);
+            Quad<false>::load(epi.scale_up, col, su);
+            finish_gated<true>(static_cast<int>(epi.act), a, b, y, bg, bu, sg, su, epi.scale_a[row]);
+          } else {
+            finish_gated<false>(static_cast<int>(epi.act), a, b, y, bg, bu, sg, su, 0.0f);
+          }
+          if (epi.gate) Quad<BF16>::store(epi.gate, row * epi.ld_gate + col, a);
+          if (epi.up) Quad<BF16>::store(epi.up, row * epi.ld_up + col, b);
+          Quad<BF16>::store(args.C, row * args.ldc + col, y);
+        }
+      } else {
+        float sum = p[0], other = 0.0f;
+        if constexpr (!GRAD) other = p[up_at];
+        for (uint32_t s = 1; s < item.ksplit_cnt; ++s) {
+          sum += p[s * item.block];
+          if constexpr (!GRAD) other += p[up_at + s * item.block];
+        }
+        if constexpr (GRAD) {
+          float a[1] = {sum}, zg[1] = {load_element<BF16>(epi.gate, row * epi.ld_gate + col)},
+                b[1] = {load_element<BF16>(epi.up, row * epi.ld_up + col)};
+          finish_gated_grad(static_cast<int>(epi.act), a, zg, b);
+          store_element<BF16>(epi.second, row * epi.ld_second + col, b[0]);
+          store_element<BF16>(args.C, row * args.ldc + col, a[0]);
+        } else {
+          store_element<BF16>(args.C, row * args.ldc + col, finish_gated_element<BF16>(epi, sum, other, row, col));
+        }
+      }
+    }
+  }
+}
+
+template <bool GRAD>
+hipError_t launch_gated_joined(const ReduceArgs& args, const GatedArgs& epi, int64_t up_at, int64_t M, int64_t N, int splits,
+                               int out_dtype, bool vec, hipStream_t stream) {
+  ReduceArgs a = args;
+  if (!a.items) a.n_items = (M * N + kJoinRun - 1) / kJoinRun;
+  const int64_t pitch = GRAD ? N : 2 * N;
+  const dim3 g(static_cast<uint32_t>(std::min<int64_t>(a.n_items, int64_t{1} << 20))), b(kJoinThreads);
+  const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, g, b, 0, stream, a, epi, up_at, M, N, pitch, splits); };
+  if (out_dtype == CLEAVE_BF16) vec ? launch(gated_join_kernel<true, GRAD, true>) : launch(gated_join_kernel<true, GRAD, false>);
+  else vec ? launch(gated_join_kernel<false, GRAD, true>) : launch(gated_join_kernel<false, GRAD, false>);
+  return hipGetLastError();
+}
+
 }  // namespace
+
+hipError_t launch_gated_join(const ReduceArgs& args, const GatedArgs& epi, int64_t up_at, int64_t M, int64_t N, int splits,
+                             int out_dtype, bool vec, hipStream_t stream) {
+  return launch_gated_joined<false>(args, epi, up_at, M, N, splits, out_dtype, vec, stream);
+}
+hipError_t launch_gated_grad_join(const ReduceArgs& args, const GatedArgs& epi, int64_t M, int64_t N, int splits, int out_dtype,
+                                  bool vec, hipStream_t stream) {
+  return launch_gated_joined<true>(args, epi, 0, M, N, splits, out_dtype, vec, stream);
+}
 
 hipError_t launch_linear_few_rows(const ExecuteArgs& args, const LinearArgs& epi, int dtype, int splits, int64_t chunk,
                                   hipStream_t stream) {
-  if (dtype == CLEAVE_E4M3) return launch_layout<CLEAVE_E4M3, true>(args, epi, splits, chunk, stream);
-  if (dtype == CLEAVE_BF16)
-    return args.transB ? launch_layout<CLEAVE_BF16, true>(args, epi, splits, chunk, stream)
-                       : launch_layout<CLEAVE_BF16, false>(args, epi, splits, chunk, stream);
-  return args.transB ? launch_layout<CLEAVE_F32, true>(args, epi, splits, chunk, stream)
-                     : launch_layout<CLEAVE_F32, false>(args, epi, splits, chunk, stream);
+  return launch_few_rows(args, epi, dtype, splits, chunk, stream);
+}
+hipError_t launch_gated_few_rows(const ExecuteArgs& args, const GatedArgs& epi, int dtype, int splits, int64_t chunk,
+                                 hipStream_t stream) {
+  return launch_few_rows(args, epi, dtype, splits, chunk, stream);
 }
 
 hipError_t launch_linear_join(const ReduceArgs& args, const LinearArgs& epi, int64_t M, int64_t N, int splits, int out_dtype,

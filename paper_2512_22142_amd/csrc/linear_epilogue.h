@@ -52,26 +52,26 @@ __device__ __forceinline__ float silu_slope(float z) {
 
 // No epilogue: the kernels as cleave_execute and cleave_execute_assemble run them.
 struct NoEpilogue {
-  static constexpr bool kLinear = false;
+  static constexpr bool kLinear = false, kGated = false;
 };
 struct LinearEpilogue : LinearArgs {
-  static constexpr bool kLinear = true;
+  static constexpr bool kLinear = true, kGated = false;
 };
 
 // The epilogue's arguments, read from the kernel's argument segment (`OFFSET` bytes in) where they are needed:
 // held from the kernel's start on, they take scalar registers that the K loop then spills.
-template <size_t OFFSET>
-__device__ __forceinline__ LinearArgs late_linear_args() {
-  static_assert(OFFSET % 8 == 0 && sizeof(LinearArgs) % 8 == 0, "whole words");
+template <size_t OFFSET, typename Args = LinearArgs>
+__device__ __forceinline__ Args late_linear_args() {
+  static_assert(OFFSET % 8 == 0 && sizeof(Args) % 8 == 0, "whole words");
   typedef const __attribute__((address_space(4))) unsigned char* const_bytes;
   typedef const __attribute__((address_space(4))) uint64_t* const_words;
   const_bytes p = (const_bytes)__builtin_amdgcn_kernarg_segment_ptr() + OFFSET;
   asm volatile("" : "+s"(p));
   const_words src = (const_words)p;
-  uint64_t words[sizeof(LinearArgs) / 8];
+  uint64_t words[sizeof(Args) / 8];
 #pragma unroll
-  for (size_t k = 0; k < sizeof(LinearArgs) / 8; ++k) words[k] = src[k];
-  LinearArgs e;
+  for (size_t k = 0; k < sizeof(Args) / 8; ++k) words[k] = src[k];
+  Args e;
   __builtin_memcpy(&e, words, sizeof(e));
   return e;
 }

@@ -315,8 +315,114 @@ PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// The shape of a stored operand B.
+void expect_b(const Operand& b, bool transposed, int64_t N, int64_t K, const char* what) {
+  if (b.rows == (transposed ? N : K) && b.cols == (transposed ? K : N)) return;
+  PyErr_Format(PyExc_ValueError, "%s of shape (%lld, %lld) does not match the plan", what, static_cast<long long>(b.rows),
+               static_cast<long long>(b.cols));
+  throw Raised{};
+}
+
+// linear_gated(plan address, M, N, K, A, B_gate, B_up, C, transB, act, bias_gate, bias_up, gate, up, scale_a, scale_gate, scale_up,
+//              partials, stream)
+PyObject* py_linear_gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 19);
+    const int64_t M = integer(a[1]), N = integer(a[2]), K = integer(a[3]);
+    const Operand C = operand(a[7], "C");
+    const Operand A = like(a[4], "A", M, K, operand(a[4], "A").type), Bg = operand(a[5], "B_gate"), Bu = operand(a[6], "B_up");
+    cleave_gated_args args{};
+    args.transB = static_cast<int32_t>(integer(a[8]));
+    args.dtype = operand_code(A.type);
+    args.out_dtype = dtype_code(C.type);
+    if (A.type != Bg.type || A.type != Bu.type) raise(PyExc_TypeError, "A, B_gate and B_up must have the same dtype");
+    expect_b(Bg, args.transB != 0, N, K, "B_gate");
+    expect_b(Bu, args.transB != 0, N, K, "B_up");
+    if (Bg.rows > 1 && Bg.ld != Bu.ld) raise(PyExc_ValueError, "B_gate and B_up must have the same row stride");
+    if (C.rows != M || C.cols != N) raise(PyExc_ValueError, "C must be M x N");
+    const Operand gate = like(a[12], "gate", M, N, C.type, true), up = like(a[13], "up", M, N, C.type, true);
+    args.A = A.ptr;
+    args.lda = A.ld;
+    args.B_gate = Bg.ptr;
+    args.B_up = Bu.ptr;
+    args.ldb = Bg.ld;
+    args.C = C.ptr;
+    args.ldc = C.ld;
+    args.act = static_cast<int32_t>(integer(a[9]));
+    args.bias_gate = floats(a[10], "bias_gate", N, true);
+    args.bias_up = floats(a[11], "bias_up", N, true);
+    args.gate = gate.ptr;
+    args.ld_gate = gate.ld;
+    args.up = up.ptr;
+    args.ld_up = up.ld;
+    args.scale_a = floats(a[14], "scale_a", M, true);
+    args.scale_gate = floats(a[15], "scale_gate", N, true);
+    args.scale_up = floats(a[16], "scale_up", N, true);
+    const bool scaled = args.scale_a && args.scale_gate && args.scale_up;
+    if (args.dtype != CLEAVE_E4M3 && (args.scale_a || args.scale_gate || args.scale_up))
+      raise(PyExc_ValueError, "scales belong to operands in float8_e4m3fn");
+    if (args.dtype == CLEAVE_E4M3 && !scaled)
+      raise(PyExc_ValueError, "operands in float8_e4m3fn need scale_a, scale_gate and scale_up");
+    cleave_plan* plan = static_cast<cleave_plan*>(address(a[0]));
+    // (a workspace shorter than this call's is as good as none: the call says whether it needs one)
+    const int64_t least = cleave_gated_workspace(plan, 0);
+    if (a[17] != Py_None && least > 0 && tensor(a[17], "partials").numel() > 0 &&
+        (cleave_gated_workspace(plan, 1) > 0 || tensor(a[17], "partials").numel() >= least))
+      args.partials = floats(a[17], "partials", least, false, true);
+    void* stream = stream_of(a[18]);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = cleave_linear_gated(plan, &args, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+  });
+}
+
+// linear_gated_grad(plan address, M, N, K, A, B, gate, up, dgate, dup, transB, act, partials, stream)
+PyObject* py_linear_gated_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 14);
+    const int64_t M = integer(a[1]), N = integer(a[2]), K = integer(a[3]);
+    const Operand A = like(a[4], "A", M, K, operand(a[4], "A").type), B = operand(a[5], "B");
+    if (A.type != B.type) raise(PyExc_TypeError, "A and B must have the same dtype");
+    cleave_gated_grad_args args{};
+    args.transB = static_cast<int32_t>(integer(a[10]));
+    args.dtype = dtype_code(A.type);
+    expect_b(B, args.transB != 0, N, K, "B");
+    const Operand gate = like(a[6], "gate", M, N, operand(a[6], "gate").type), up = like(a[7], "up", M, N, gate.type);
+    const Operand dgate = like(a[8], "dgate", M, N, gate.type), dup = like(a[9], "dup", M, N, gate.type);
+    args.out_dtype = dtype_code(gate.type);
+    args.A = A.ptr;
+    args.lda = A.ld;
+    args.B = B.ptr;
+    args.ldb = B.ld;
+    args.gate = gate.ptr;
+    args.ld_gate = gate.ld;
+    args.up = up.ptr;
+    args.ld_up = up.ld;
+    args.dgate = dgate.ptr;
+    args.ld_dgate = dgate.ld;
+    args.dup = dup.ptr;
+    args.ld_dup = dup.ld;
+    args.act = static_cast<int32_t>(integer(a[11]));
+    cleave_plan* plan = static_cast<cleave_plan*>(address(a[0]));
+    const int64_t least = cleave_gated_grad_workspace(plan, 0);
+    if (a[12] != Py_None && least > 0 && tensor(a[12], "partials").numel() > 0 &&
+        (cleave_gated_grad_workspace(plan, 1) > 0 || tensor(a[12], "partials").numel() >= least))
+      args.partials = floats(a[12], "partials", least, false, true);
+    void* stream = stream_of(a[13]);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = cleave_linear_gated_grad(plan, &args, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+  });
+}
+
 PyMethodDef kOperatorMethods[] = {{"linear", as_function(py_linear), METH_FASTCALL, nullptr},
-{"rms_norm", as_function(py_rms_norm), METH_FASTCALL, nullptr},
+                                  {"linear_gated", as_function(py_linear_gated), METH_FASTCALL, nullptr},
+                                  {"linear_gated_grad", as_function(py_linear_gated_grad), METH_FASTCALL, nullptr},
+                                  {"rms_norm", as_function(py_rms_norm), METH_FASTCALL, nullptr},
                                   {"rms_norm_backward", as_function(py_rms_norm_backward), METH_FASTCALL, nullptr},
                                   {"layer_norm", as_function(py_layer_norm), METH_FASTCALL, nullptr},
                                   {"layer_norm_backward", as_function(py_layer_norm_backward), METH_FASTCALL, nullptr},

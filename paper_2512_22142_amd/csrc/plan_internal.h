@@ -299,8 +299,13 @@ struct cleave_plan {
   int64_t partial_elems = 0;
   int64_t num_tiles = 0;
   int64_t batch = 0;         // > 0: a batch of that many M x N x K GEMMs, task.gemm_id = member
-  bool linear = false;       // made by cleave_plan_linear
+  bool linear = false;       // made by cleave_plan_linear,
+  bool for_fp32 = false;     // for operands of fp32
   bool pairs = false;        // K counts pairs of 8-bit values (cleave_plan_linear)
+  // Made by cleave_plan_gated: two members (gate's product, up's), for operands that the direct kernel does not take, and the plan of
+  // M x 2N that it runs (null: none).
+  bool gated = false;
+  cleave_plan* fused = nullptr;
   int64_t uniform_splits = 0;   // plain plans whose tiles all have that many splits (0: others)
   bool all_k_mult8 = true;   // every k0 and k_len is a multiple of 8
   bool all_m_mult8 = true;   // every m0 and m_len is a multiple of 8

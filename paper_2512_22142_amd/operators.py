@@ -79,16 +79,20 @@ def adamw(w, grads, m, v, lr, beta1, beta2, eps, weight_decay, step, m_scales=No
                          stream), "cleave_adamw")
 
 
-def plan_linear(M, N, K, dtype):
-    """cleave_plan_linear: a plan for linear() with op(A) of M x K, op(B) of K x N and operands of torch dtype
-    `dtype` (float32, bfloat16 or float8_e4m3fn).  plan.linear_workspace: fp32 elements of
-    linear()'s `partials` (0: none needed)."""
+def _operand_code(dtype):
     import torch
     codes = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
     if dtype not in codes:
         raise TypeError("unsupported dtype %s" % dtype)
+    return codes[dtype]
+
+
+def plan_linear(M, N, K, dtype):
+    """cleave_plan_linear: a plan for linear() with op(A) of M x K, op(B) of K x N and operands of torch dtype
+    `dtype` (float32, bfloat16 or float8_e4m3fn).  plan.linear_workspace: fp32 elements of
+    linear()'s `partials` (0: none needed)."""
     out = ctypes.c_void_p()
-    _check(_lib.cleave_plan_linear(M, N, K, codes[dtype], ctypes.byref(out)), "cleave_plan_linear")
+    _check(_lib.cleave_plan_linear(M, N, K, _operand_code(dtype), ctypes.byref(out)), "cleave_plan_linear")
     plan = Plan(out.value)
     plan.linear_K = K
     return plan
@@ -111,3 +115,46 @@ def linear(plan, A, B, C, transA=0, transB=0, bias=None, act=None, act_grad=None
     _check(_native.linear(_plan_addr(plan), plan.M, plan.N, plan.linear_K, plan.linear_workspace, A, B, C, transA, transB, bias,
                           code, 0 if act_grad is None else 1, residual, preact, scale_a, scale_b, partials, stream),
            "cleave_linear")
+
+
+def plan_gated(M, N, K, dtype):
+    """cleave_plan_gated: a plan for linear_gated() with A of M x K, both weights of K x N and operands of torch dtype
+    `dtype` (float32, bfloat16 or float8_e4m3fn)."""
+    out = ctypes.c_void_p()
+    _check(_lib.cleave_plan_gated(M, N, K, _operand_code(dtype), ctypes.byref(out)), "cleave_plan_gated")
+    plan = Plan(out.value)
+    plan.linear_K = K
+    return plan
+
+
+def _workspace(elems, where):
+    if elems < 0:
+        _check(elems, where)
+    return int(elems)
+
+
+def gated_workspace(plan, whole=False):
+    """fp32 elements of linear_gated()'s `partials` (0: none needed).  whole=True: for bf16 operands that start on 16 bytes, with
+    row strides and K (and, with transB=0, N) in multiples of 8."""
+    return _workspace(_lib.cleave_gated_workspace(plan._h, int(bool(whole))), "cleave_gated_workspace")
+
+
+def linear_gated(plan, A, B_gate, B_up, C, transB=0, act="silu", bias_gate=None, bias_up=None, gate=None, up=None, scale_a=None,
+                 scale_gate=None, scale_up=None, partials=None, stream=None):
+    """cleave_linear_gated: C = act(A op(B_gate) + bias_gate) * (A op(B_up) + bias_up); `gate` and `up` (if given) get the
+    two factors' sums, which the gradient needs.  B_gate and B_up share their row stride.  Operands in float8_e4m3fn: both
+    weights N x K (transB=1), with fp32 scales of the rows of A and of the weights."""
+    _check(_native.linear_gated(_plan_addr(plan), plan.M, plan.N, plan.linear_K, A, B_gate, B_up, C, transB, _activation(act),
+                                bias_gate, bias_up, gate, up, scale_a, scale_gate, scale_up, partials, stream), "cleave_linear_gated")
+
+
+def gated_grad_workspace(plan, whole=False):
+    """fp32 elements of linear_gated_grad()'s `partials` (0: none needed) with plan_linear's plan; whole as for gated_workspace."""
+    return _workspace(_lib.cleave_gated_grad_workspace(plan._h, int(bool(whole))), "cleave_gated_grad_workspace")
+
+
+def linear_gated_grad(plan, A, B, gate, up, dgate, dup, transB=0, act="silu", partials=None, stream=None):
+    """cleave_linear_gated_grad: with p = A op(B), the gradient behind the gated product, dgate = p * up * act'(gate) and
+    dup = p * act(gate) from the gate and up that linear_gated kept.  plan: plan_linear's of that product."""
+    _check(_native.linear_gated_grad(_plan_addr(plan), plan.M, plan.N, plan.linear_K, A, B, gate, up, dgate, dup, transB,
+                                     _activation(act), partials, stream), "cleave_linear_gated_grad")
