@@ -572,6 +572,32 @@ typedef struct {
 int64_t cleave_gated_grad_workspace(const cleave_plan* plan, int whole);
 int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_grad_args* args, void* hip_stream);
 
+/* Log probabilities of given tokens: with l = scale * logits (rows x cols, F32 or BF16; scale > 0, the inverse of a temperature)
+ * and, per row, p = e^(l - lse),
+ *   lse = log sum e^l;   logp = l[id] - lse;   entropy = -sum p log p
+ * and the n_top most likely tokens in descending order (the lower id where logits are equal) with their log probabilities.
+ * ids: rows tokens, logp: rows floats, both or neither NULL; a negative id is no token (logp 0), one beyond the row gives
+ * NaN.  lse, entropy: rows floats, each or NULL.  top_ids, top_logp: rows x n_top (n_top <= 32 and <= cols; 0: both
+ * NULL).  Logits of minus infinity are masked tokens: they have no probability.  A row of nothing else has lse and log
+ * probabilities of minus infinity and entropy 0.  A row with a NaN or plus infinity is NaN; a NaN's place in its order is that of
+ * minus infinity.  workspace: cleave_log_probs_workspace(rows, cols, n_top) floats (may be NULL if that is 0), of this call alone
+ * while it runs.  No two outputs in one place.  CLEAVE_EINVAL as above, and more than 2^30 columns; CLEAVE_ELIMIT: n_top > 32. */
+int64_t cleave_log_probs_workspace(int64_t rows, int64_t cols, int64_t n_top);
+int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype, float scale,
+                     const int64_t* ids, float* logp, float* lse, float* entropy, int64_t n_top,
+                     int64_t* top_ids, float* top_logp, float* workspace, void* hip_stream);
+
+/* Its gradient, from the logits and the lse (and entropy) that it left:
+ *   dlogits_j = scale (dlogp (1[j = id] - p_j) - dentropy p_j (log p_j + entropy))
+ * ids and dlogp (rows floats; a row without a token gets none of it), entropy and dentropy: each pair or neither, one of the two
+ * at least.  p is as good as the fp32 lse: to 2^-24 |lse| of itself.  Rows whose logits are all minus infinity get zeros, as masked
+ * tokens do.  dlogits: rows x cols of dtype; may be logits, with its leading dimension.  (Cross-entropy averaged over n tokens:
+ * dlogp = -1 / n.)  CLEAVE_EINVAL as above. */
+int cleave_log_probs_backward(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype,
+                              float scale, const int64_t* ids, const float* lse, const float* dlogp,
+                              const float* entropy, const float* dentropy, void* dlogits, int64_t ldd,
+                              void* hip_stream);
+
 /* AdamW on n_tensors tensors of sizes[k] contiguous elements in one launch per 56
  * tensors: with c = *grad_scale (device; NULL: 1), per element
  *   g = c g;  m = beta1 m + (1-beta1) g;  v = beta2 v + (1-beta2) g^2;

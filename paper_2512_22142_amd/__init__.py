@@ -11,6 +11,7 @@ and what a layer's step does between its GEMMs:
     layer_norm, layer_norm_backward   the same with the mean taken off, and a bias
     linear (plan_linear)          product with bias, activation (or its gradient) and residual; 8-bit operands
     linear_gated (plan_gated), linear_gated_grad   two products, an activation and the product of both; its gradient
+    log_probs, log_probs_backward  log probabilities of tokens, entropy, the most likely ones; the gradient of the logits
     bias_grad                     sum of a gradient's rows
     adamw                         optimizer step over many tensors, states in 32 or 8 bits
 
@@ -73,6 +74,9 @@ _OPERATOR_NAMES = (
     "linear",
     "linear_gated",
     "linear_gated_grad",
+    "log_probs",
+    "log_probs_backward",
+    "log_probs_workspace",
     "plan_gated",
     "plan_linear",
     "rms_norm",

@@ -44,6 +44,7 @@ EXPORTS = (
     "cleave_adamw", "cleave_plan_linear", "cleave_linear_workspace", "cleave_linear",
     "cleave_layer_norm", "cleave_layer_norm_workspace", "cleave_layer_norm_backward",
     "cleave_plan_gated", "cleave_gated_workspace", "cleave_linear_gated", "cleave_gated_grad_workspace", "cleave_linear_gated_grad",
+    "cleave_log_probs_workspace", "cleave_log_probs", "cleave_log_probs_backward",
 )
 
 
@@ -156,6 +157,8 @@ def _load():
     lib.cleave_linear_workspace.restype = i64
     lib.cleave_plan_gated.argtypes = [i64, i64, i64, ctypes.c_int, ctypes.POINTER(p)]
     lib.cleave_plan_gated.restype = ctypes.c_int
+    lib.cleave_log_probs_workspace.argtypes = [i64, i64, i64]
+    lib.cleave_log_probs_workspace.restype = i64
     for name in ("cleave_gated_workspace", "cleave_gated_grad_workspace"):
         getattr(lib, name).argtypes = [p, ctypes.c_int]
         getattr(lib, name).restype = i64

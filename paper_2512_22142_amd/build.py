@@ -14,7 +14,7 @@ NATIVE = os.path.join(HERE, "_native.so")
 
 SOURCES = ["plan.cpp", "scheduler.cpp", "api.cpp", "operators.cpp", "execute.hip", "execute_direct.hip", "reduce.hip", "verify.hip",
            "subset.hip", "linear.hip", "linear_direct.hip", "linear_general.hip",
-           "linear_8bit.hip", "gated_direct.hip", "gated_8bit.hip", "gated_grad.hip", "norm.hip", "layer_norm.hip", "adamw.hip"]
+           "linear_8bit.hip", "gated_direct.hip", "gated_8bit.hip", "gated_grad.hip", "norm.hip", "layer_norm.hip", "log_probs.hip", "adamw.hip"]
 NATIVE_SOURCES = ["native.cpp", "native_operators.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -419,6 +419,80 @@ PyObject* py_linear_gated_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Contiguous int64 elements: one for each row, or rows x cols.
+int64_t* tokens(PyObject* o, const char* what, int64_t rows, int64_t cols, bool optional = false) {
+  if (optional && o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o, what);
+  on_current_device(t, what);
+  const bool shaped = cols < 0 ? t.dim() == 1 && t.size(0) == rows : t.dim() == 2 && t.size(0) == rows && t.size(1) == cols;
+  if (t.scalar_type() != at::kLong || !shaped || !t.is_contiguous()) {
+    PyErr_Format(PyExc_ValueError, "%s must be a contiguous int64 device tensor, one %s each of the %lld rows", what,
+                 cols < 0 ? "element for" : "row for", static_cast<long long>(rows));
+    throw Raised{};
+  }
+  return static_cast<int64_t*>(t.data_ptr());
+}
+
+// log_probs(logits, ids, logp, lse, entropy, top_ids, top_logp, scale, workspace, stream)
+PyObject* py_log_probs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 10);
+    const Operand l = operand(a[0], "logits");
+    const int dt = dtype_code(l.type);
+    const int64_t* ids = tokens(a[1], "ids", l.rows, -1, true);
+    float* logp = floats(a[2], "logp", l.rows, true);
+    if ((a[1] == Py_None) != (a[2] == Py_None)) raise(PyExc_ValueError, "ids and logp come together");
+    float* lse = floats(a[3], "lse", l.rows, true);
+    float* entropy = floats(a[4], "entropy", l.rows, true);
+    int64_t top = 0;
+    if ((a[5] == Py_None) != (a[6] == Py_None)) raise(PyExc_ValueError, "top_ids and top_logp come together");
+    if (a[5] != Py_None) {
+      const at::Tensor& t = tensor(a[5], "top_ids");
+      if (t.dim() != 2) raise(PyExc_ValueError, "top_ids must be rows x n_top");
+      top = t.size(1);
+    }
+    int64_t* top_ids = tokens(a[5], "top_ids", l.rows, top, true);
+    float* top_logp = floats(a[6], "top_logp", l.rows * top, true);
+    const float scale = static_cast<float>(real(a[7]));
+    const int64_t elems = cleave_log_probs_workspace(l.rows, l.cols, top);
+    float* ws = elems > 0 ? floats(a[8], "workspace", elems, false, true) : nullptr;
+    void* stream = stream_of(a[9]);
+    if (l.rows == 0) return PyLong_FromLong(CLEAVE_OK);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = cleave_log_probs(l.rows, l.cols, l.ptr, l.ld, dt, scale, ids, logp, lse, entropy, top, top ? top_ids : nullptr,
+                          top ? top_logp : nullptr, ws, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+  });
+}
+
+// log_probs_backward(logits, lse, dlogits, ids, dlogp, entropy, dentropy, scale, stream)
+PyObject* py_log_probs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 9);
+    const Operand l = operand(a[0], "logits");
+    const int dt = dtype_code(l.type);
+    const float* lse = floats(a[1], "lse", l.rows);
+    const Operand d = like(a[2], "dlogits", l.rows, l.cols, l.type);
+    const int64_t* ids = tokens(a[3], "ids", l.rows, -1, true);
+    const float* dlogp = floats(a[4], "dlogp", l.rows, true);
+    const float* entropy = floats(a[5], "entropy", l.rows, true);
+    const float* dentropy = floats(a[6], "dentropy", l.rows, true);
+    if ((a[3] == Py_None) != (a[4] == Py_None)) raise(PyExc_ValueError, "ids and dlogp come together");
+    if ((a[5] == Py_None) != (a[6] == Py_None)) raise(PyExc_ValueError, "entropy and dentropy come together");
+    if (a[3] == Py_None && a[5] == Py_None) raise(PyExc_ValueError, "a gradient of logp or of the entropy is needed");
+    const float scale = static_cast<float>(real(a[7]));
+    void* stream = stream_of(a[8]);
+    if (l.rows == 0) return PyLong_FromLong(CLEAVE_OK);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = cleave_log_probs_backward(l.rows, l.cols, l.ptr, l.ld, dt, scale, ids, lse, dlogp, entropy, dentropy, d.ptr, d.ld, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+  });
+}
+
 PyMethodDef kOperatorMethods[] = {{"linear", as_function(py_linear), METH_FASTCALL, nullptr},
                                   {"linear_gated", as_function(py_linear_gated), METH_FASTCALL, nullptr},
                                   {"linear_gated_grad", as_function(py_linear_gated_grad), METH_FASTCALL, nullptr},
@@ -426,6 +500,8 @@ PyMethodDef kOperatorMethods[] = {{"linear", as_function(py_linear), METH_FASTCA
                                   {"rms_norm_backward", as_function(py_rms_norm_backward), METH_FASTCALL, nullptr},
                                   {"layer_norm", as_function(py_layer_norm), METH_FASTCALL, nullptr},
                                   {"layer_norm_backward", as_function(py_layer_norm_backward), METH_FASTCALL, nullptr},
+                                  {"log_probs", as_function(py_log_probs), METH_FASTCALL, nullptr},
+                                  {"log_probs_backward", as_function(py_log_probs_backward), METH_FASTCALL, nullptr},
                                   {"bias_grad", as_function(py_bias_grad), METH_FASTCALL, nullptr},
                                   {"adamw", as_function(py_adamw), METH_FASTCALL, nullptr},
                                   {nullptr, nullptr, 0, nullptr}};

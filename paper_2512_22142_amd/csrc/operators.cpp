@@ -184,6 +184,73 @@ extern "C" int cleave_bias_grad(int64_t rows, int64_t cols, const void* dy, int6
   return CLEAVE_OK;
 }
 
+namespace {
+
+// (columns are counted in 32 bits beyond a row's end)
+constexpr int64_t kMostTokens = int64_t{1} << 30;
+
+// Columns of a part of a row: whole lines of sixteen bytes for every group of threads.
+int64_t log_probs_chunk(int64_t cols, int parts) { return ((cols + parts - 1) / parts + 511) / 512 * 512; }
+
+}  // namespace
+
+extern "C" int64_t cleave_log_probs_workspace(int64_t rows, int64_t cols, int64_t n_top) {
+  if (rows < 0 || cols < 1 || rows > kMost || cols > kMostTokens || n_top < 0 || n_top > cols) return CLEAVE_EINVAL;
+  if (n_top > cleave::kMostTop) return CLEAVE_ELIMIT;
+  const int64_t parts = cleave::log_probs_parts(rows, cols);
+  return parts == 1 ? 0 : rows * parts * (4 + 2 * n_top);
+}
+
+extern "C" int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype, float scale,
+                                const int64_t* ids, float* logp, float* lse, float* entropy, int64_t n_top, int64_t* top_ids,
+                                float* top_logp, float* workspace, void* hip_stream) {
+  if (!float_dtype(dtype) || !(scale > 0.0f) || std::isinf(scale)) return CLEAVE_EINVAL;
+  Matrices m(rows, cols);
+  m.add(logits, ld, dtype);
+  m.add_vector(logp, true);
+  m.add_vector(lse, true);
+  m.add_vector(entropy, true);
+  m.add_vector(top_logp, true);
+  m.add_vector(workspace, true);
+  if (!m.ok || cols > kMostTokens || !aligned(ids, 8) || !aligned(top_ids, 8)) return CLEAVE_EINVAL;
+  if ((ids != nullptr) != (logp != nullptr) || n_top < 0 || n_top > cols) return CLEAVE_EINVAL;
+  if (n_top > cleave::kMostTop) return CLEAVE_ELIMIT;
+  if ((n_top > 0) != (top_ids != nullptr) || (n_top > 0) != (top_logp != nullptr)) return CLEAVE_EINVAL;
+  if ((logp && (logp == lse || logp == entropy || logp == top_logp)) || (lse && (lse == entropy || lse == top_logp)) ||
+      (entropy && entropy == top_logp))
+    return CLEAVE_EINVAL;
+  if (rows == 0) return CLEAVE_OK;
+  int parts = cleave::log_probs_parts(rows, cols);
+  if (parts > 1 && !workspace) return CLEAVE_EINVAL;
+  const int64_t chunk = log_probs_chunk(cols, parts);
+  parts = static_cast<int>((cols + chunk - 1) / chunk);   // (rounding may leave the last ones empty)
+  const cleave::LogProbArgs args{logits, ids, logp, lse, entropy, top_ids, top_logp, workspace, rows, cols, ld, scale,
+                                 static_cast<int>(n_top), parts, static_cast<int>(std::min(chunk, cols))};
+  CLEAVE_HIP(cleave::launch_log_probs(args, dtype, static_cast<hipStream_t>(hip_stream)));
+  return CLEAVE_OK;
+}
+
+extern "C" int cleave_log_probs_backward(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype, float scale,
+                                         const int64_t* ids, const float* lse, const float* dlogp, const float* entropy,
+                                         const float* dentropy, void* dlogits, int64_t ldd, void* hip_stream) {
+  if (!float_dtype(dtype) || !(scale > 0.0f) || std::isinf(scale)) return CLEAVE_EINVAL;
+  Matrices m(rows, cols);
+  m.add(logits, ld, dtype);
+  m.add(dlogits, ldd, dtype);
+  m.add_vector(lse);
+  m.add_vector(dlogp, true);
+  m.add_vector(entropy, true);
+  m.add_vector(dentropy, true);
+  if (!m.ok || cols > kMostTokens || !aligned(ids, 8)) return CLEAVE_EINVAL;
+  if ((ids != nullptr) != (dlogp != nullptr) || (entropy != nullptr) != (dentropy != nullptr) || (!ids && !entropy))
+    return CLEAVE_EINVAL;
+  if (!in_place(dlogits, ldd, dtype, logits, ld, dtype, rows)) return CLEAVE_EINVAL;
+  if (rows == 0) return CLEAVE_OK;
+  const cleave::LogProbBackwardArgs args{logits, ids, lse, dlogp, entropy, dentropy, dlogits, rows, cols, ld, ldd, scale, 0};
+  CLEAVE_HIP(cleave::launch_log_probs_backward(args, dtype, static_cast<hipStream_t>(hip_stream)));
+  return CLEAVE_OK;
+}
+
 extern "C" int cleave_adamw(int64_t n_tensors, const int64_t* sizes, float* const* w, const void* const* g, int g_dtype,
                             void* const* m, void* const* v, float* const* m_scale, float* const* v_scale,
                             void* const* w_bf16, const float* grad_scale, double lr, double beta1, double beta2, double eps,

@@ -93,6 +93,41 @@ hipError_t launch_join_rows(const float* rows, int n, int64_t ld, int64_t cols, 
                             float* second = nullptr);
 hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, hipStream_t stream);
 
+// ---- log probabilities of tokens ---------------------------------------------
+
+constexpr int kMostTop = 32;      // most likely tokens of a row that are given
+constexpr int kMostParts = 32;    // of a row
+struct LogProbArgs {
+  const void* logits;
+  const int64_t* ids;      // null: no log probabilities
+  float* logp;             // null, with ids
+  float* lse;              // may be null
+  float* entropy;          // may be null
+  int64_t* top_ids;        // rows x n_top
+  float* top_logp;
+  float* workspace;        // parts > 1
+  int64_t rows, cols, ld;
+  float scale;
+  int n_top, parts;
+  int chunk;               // columns of a part
+};
+int log_probs_parts(int64_t rows, int64_t cols);
+hipError_t launch_log_probs(const LogProbArgs& args, int dtype, hipStream_t stream);
+
+struct LogProbBackwardArgs {
+  const void* logits;
+  const int64_t* ids;      // null, with dlogp
+  const float* lse;
+  const float* dlogp;
+  const float* entropy;    // null, with dentropy
+  const float* dentropy;
+  void* dlogits;
+  int64_t rows, cols, ld, ldd;
+  float scale;
+  int parts;               // workgroups of a row (filled in at the launch)
+};
+hipError_t launch_log_probs_backward(const LogProbBackwardArgs& args, int dtype, hipStream_t stream);
+
 // ---- AdamW over many tensors -------------------------------------------------
 
 // Elements of an 8-bit state that share a scale.

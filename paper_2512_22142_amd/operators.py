@@ -28,6 +28,12 @@ def _sizes(rows, cols):
     return rows, cols
 
 
+def _workspace(elems, where):
+    if elems < 0:
+        _check(elems, where)
+    return int(elems)
+
+
 def rms_norm_workspace(rows, cols):
     """fp32 elements of rms_norm_backward's workspace."""
     return int(_lib.cleave_rms_norm_workspace(*_sizes(rows, cols)))
@@ -66,6 +72,24 @@ def bias_grad_workspace(rows, cols):
 def bias_grad(dy, dbias, workspace, stream=None):
     """cleave_bias_grad: dbias (fp32) = sum of dy's rows."""
     _check(_native.bias_grad(dy, dbias, workspace, stream), "cleave_bias_grad")
+
+
+def log_probs_workspace(rows, cols, top=0):
+    """fp32 elements of log_probs()'s workspace (0: none needed)."""
+    return _workspace(_lib.cleave_log_probs_workspace(*_sizes(rows, cols), top), "cleave_log_probs_workspace")
+
+
+def log_probs(logits, ids=None, logp=None, lse=None, entropy=None, top_ids=None, top_logp=None, scale=1.0, workspace=None, stream=None):
+    """cleave_log_probs: for the rows of scale * logits (fp32 or bf16) the log probability of each row's token in ids (int64; negative:
+    no token, 0), the log of the sum of exponentials, the entropy, and the most likely tokens in descending order, as many
+    as top_ids (int64) and top_logp have columns.  The other outputs are fp32, one element per row; what is None is left out."""
+    _check(_native.log_probs(logits, ids, logp, lse, entropy, top_ids, top_logp, scale, workspace, stream), "cleave_log_probs")
+
+
+def log_probs_backward(logits, lse, dlogits, ids=None, dlogp=None, entropy=None, dentropy=None, scale=1.0, stream=None):
+    """cleave_log_probs_backward: dlogits (the logits' dtype; may be the logits themselves) from the gradients dlogp of the tokens'
+    log probabilities and dentropy of the entropy, with the lse and entropy that log_probs left."""
+    _check(_native.log_probs_backward(logits, lse, dlogits, ids, dlogp, entropy, dentropy, scale, stream), "cleave_log_probs_backward")
 
 
 def adamw(w, grads, m, v, lr, beta1, beta2, eps, weight_decay, step, m_scales=None, v_scales=None, copies=None,
@@ -125,12 +149,6 @@ def plan_gated(M, N, K, dtype):
     plan = Plan(out.value)
     plan.linear_K = K
     return plan
-
-
-def _workspace(elems, where):
-    if elems < 0:
-        _check(elems, where)
-    return int(elems)
 
 
 def gated_workspace(plan, whole=False):
