@@ -9,13 +9,15 @@
 // Gradient:  dx_j = a (dlogp (1[j = id] - p_j) - dH p_j (log p_j + H)).
 //
 // The most likely tokens: every thread also keeps its strip's first largest value.  Value and column make a 64-bit key, larger for a larger
-// value or a lower column, so no two are equal.  The k-th largest of the threads' keys is a bound that at least k elements
-// reach, and only the strips of the k threads that reach it hold such: those are read again, and their elements ranked.
+// value or a lower column, so no two are equal.  The k-th largest of the keys of groups of threads is a bound that at least k elements
+// reach, and only the strips of the few threads that reach it hold such: those are read again, and their elements ranked.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
+#include "kernels.h"
 #include "operators.h"
 #include "row_access.h"
 #include "wave_reduce.h"
@@ -66,89 +68,82 @@ __device__ __forceinline__ float value_of(Key k) {
   const uint32_t b = static_cast<uint32_t>(k >> 32);
   return __builtin_bit_cast(float, b & 0x80000000u ? b & 0x7fffffffu : ~b);
 }
-// A wave's keys in descending order of lanes (bitonic).
-__device__ __forceinline__ Key sort_wave(Key k) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int size = 2; size <= 64; size <<= 1)
-#pragma unroll
-    for (int d = size / 2; d > 0; d >>= 1) {
-      const Key other = static_cast<Key>(__shfl_xor(static_cast<uint32_t>(k >> 32), d)) << 32 | __shfl_xor(static_cast<uint32_t>(k), d);
-      const bool larger = ((lane & d) == 0) == ((lane & size) == 0);
-      k = larger == (k > other) ? k : other;
-    }
-  return k;
+__device__ __forceinline__ Key shuffle_xor(Key k, int d) {
+  return static_cast<Key>(__shfl_xor(static_cast<uint32_t>(k >> 32), d)) << 32 | __shfl_xor(static_cast<uint32_t>(k), d);
 }
 
-constexpr int kCandidates = 2048;   // held in LDS at a time
+constexpr int kCandidates = 1024;   // held in LDS at a time
 
-template <int NW>
+template <int NT>
 struct TopSpace {
-  Key lists[NW][kMostTop];   // the waves' largest keys
+  Key largest[64];           // the largest keys of 64 groups of neighbouring threads
   Key found[kCandidates];
   Key best[kMostTop];
-  Key bound;
-  int count;
+  uint16_t reach[NT];        // threads whose strips reach the bound
+  int count, reaching;
 };
 
-// The `n` keys of `found` that are largest go to `best`, in order.
-__device__ __forceinline__ void rank_keys(const Key* found, int count, Key* best, int n, int threads) {
-  for (int i = threadIdx.x; i < count; i += threads) {
-    const Key mine = found[i];
-    int rank = 0;
-    for (int j = 0; j < count; ++j) rank += found[j] > mine;
-    if (rank < n) best[rank] = mine;
+// How many of `list` (`count` keys, zeros behind them to a multiple of eight) are larger than `mine`.
+__device__ __forceinline__ int larger_than(const Key* list, int count, Key mine) {
+  int rank = 0;
+  for (int j = 0; j < count; j += 8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rank += list[j + i] > mine;
   }
+  return rank;
 }
 
-// space.best: the largest `n` keys of the workgroup's elements; zeros where there are fewer.  `mine`: this thread's largest, `push`:
-// (first, groups, take) calls take(key) for the elements of that many of this thread's groups, of `strip` at most.
-template <int NT, int N, typename Push>
-__device__ __forceinline__ void find_top(TopSpace<NT / 64>& space, Key mine, int n, int strip, Push push) {
-  constexpr int NW = NT / 64;
+// space.best: the largest `n` keys of the workgroup's elements; zeros where there are fewer.  `mine`: this thread's largest;
+// look(reaching, bound, take) calls take(key) once, from any thread, for every element that reaches the bound in the strips of the first
+// `reaching` threads of space.reach.
+//   The bound, which at least n elements reach: the n-th largest of the largest keys of 64 groups of threads; every wave finds it
+// itself (the rank of a lane's key by 64 reads).  Random logits leave some 1.4 n candidates, in the strips of as many threads, which all
+// threads share out among them.  Where more reach the bound than LDS holds (logits in an order that the strips follow), the n-th
+// largest of those that were held is the next bound: each round leaves out all that the last one held but n.
+template <int NT, typename Look>
+__device__ __forceinline__ void find_top(TopSpace<NT>& space, Key mine, int n, Look look) {
+  constexpr int kGroup = NT / 64;
+  static_assert(kCandidates % 8 == 0 && kGroup >= 1, "whole eights");
   const int t = threadIdx.x, lane = t & 63;
-  const Key sorted = sort_wave(mine);
-  if (lane < n) space.lists[t >> 6][lane] = sorted;
-  if (t == 0) {
-    space.bound = 0;
-    space.count = 0;
+  Key most = mine;
+#pragma unroll
+  for (int d = kGroup / 2; d > 0; d >>= 1) {
+    const Key other = shuffle_xor(most, d);
+    most = other > most ? other : most;
   }
+  if (t % kGroup == 0) space.largest[t / kGroup] = most;
   if (t < n) space.best[t] = 0;
+  if (t == 0) space.count = space.reaching = 0;
   __syncthreads();
-  for (int i = t; i < NW * n; i += NT) {
-    const Key k = space.lists[i / n][i % n];
-    int rank = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      // larger ones in a descending list
-      int lo = 0;
-#pragma unroll
-      for (int d = kMostTop; d > 0; d >>= 1)
-        if (lo + d <= n && space.lists[w][lo + d - 1] > k) lo += d;
-      rank += lo;
-    }
-    if (rank == n - 1 && k) space.bound = k;
+  const Key group = space.largest[lane];
+  const uint64_t is = __ballot(larger_than(space.largest, 64, group) == n - 1 && group != 0);
+  Key bound = 1;   // fewer groups than n have an element: all of them
+  if (is) {
+    const int at = __builtin_ctzll(is);
+    bound = static_cast<Key>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(group >> 32), at))) << 32 |
+            static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(group), at));
   }
+  if (mine >= bound) space.reach[atomicAdd(&space.reaching, 1)] = static_cast<uint16_t>(t);
   __syncthreads();
-  const Key bound = space.bound;
-  const bool reaches = mine && mine >= bound;
-  // at most n threads reach it: as many groups at a time as fit beside the best so far
-  const int some = max(1, (kCandidates / n - 1) / N);
-  for (int first = 0; first < strip; first += some) {
-    if (reaches)
-      push(first, min(some, strip - first), [&](Key k) {
-        if (k >= bound) space.found[atomicAdd(&space.count, 1)] = k;
-      });
+  const int reaching = space.reaching;
+  for (;;) {
+    look(reaching, bound, [&](Key k) {
+      const int at = atomicAdd(&space.count, 1);
+      if (at < kCandidates) space.found[at] = k;
+    });
     __syncthreads();
-    const int count = space.count;
-    rank_keys(space.found, count, space.best, n, NT);
+    const int all = space.count, count = min(all, kCandidates);
+    if (t < (8 - (count & 7)) % 8) space.found[count + t] = 0;
     __syncthreads();
-    if (first + some < strip) {
-      const int have = min(count, n);
-      if (t < have) space.found[t] = space.best[t];
-      if (t == 0) space.count = have;
-      __syncthreads();
+    for (int i = t; i < count; i += NT) {
+      const Key k = space.found[i];
+      const int rank = larger_than(space.found, count, k);
+      if (rank < n) space.best[rank] = k;
     }
+    if (t == 0) space.count = 0;
+    __syncthreads();
+    if (all <= kCandidates) return;
+    bound = space.best[n - 1];
   }
 }
 
@@ -183,13 +178,21 @@ __device__ __forceinline__ void put_top(const LogProbArgs& args, int64_t row, in
 // Floats of a part's record: m, s, w, then n_top keys.
 __host__ __device__ inline int record_floats(int n_top) { return 4 + 2 * n_top; }
 
-// Groups of sixteen bytes that a thread has on their way at a time.
-constexpr int kAhead = 4;
+// The largest of three.  (As one instruction: the compiler would first make quiet NaN of what is loaded.  A signaling one may become the
+// largest, beside which the sums are NaN.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// Groups of sixteen bytes of a thread that are taken together, while as many more are on their way.
+constexpr int kTogether = 4;
 
 template <typename T, int NT, bool TOP, bool ENTROPY>
 __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
   typedef Group16<T> G;
-  constexpr int N = G::N, NW = NT / 64, U = kAhead;
+  constexpr int N = G::N, NW = NT / 64, U = kTogether;
   __shared__ Stats slots[NW];
   const int t = threadIdx.x;
   const int64_t row = blockIdx.x / static_cast<uint32_t>(args.parts);
@@ -198,29 +201,32 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
   const int len = static_cast<int>(min(static_cast<int64_t>(args.chunk), args.cols - first));
   const T* x = static_cast<const T*>(args.logits) + row * args.ld + first;
   const float c = args.scale * kLog2e;
-  const int groups = (len + N - 1) / N;
+  const int groups = (len + N - 1) / N, whole = len / N;
+  // A row's last group, where it is not whole, is read so that it ends with the row; what the one before it has is left out.  (Fewer
+  // elements than a group are read one by one.)
+  const auto place = [&](int g) { return min(g * N, max(len - N, 0)); };
+  const auto read = [&](int g) { return len >= N ? G::read(x + place(g), N) : G::read(x, len); };
 
   Stats own{-kInf, 0.0f, 0.0f};
   float best = -kInf;
-  int best_at = t * N;
-  for (int g = t; g < groups; g += U * NT) {
-    Raw16 raw[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = G::read(x + static_cast<int64_t>(g + u * NT) * N, len - (g + u * NT) * N);
-    float v[U][N];
-    float most = -kInf;
+  int best_at = t * N;   // the first one that counts
+  const auto take = [&](const Raw16 (&raw)[U], int g, auto ragged_tag) {
+    constexpr bool RAGGED = decltype(ragged_tag)::value;
+    float v[U][N], most = -kInf;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       G::unpack(raw[u], v[u]);
-      const int at = (g + u * NT) * N;
-      if (at + N > len) {
+      const int i = g + u * NT;
+      int at = i * N;
+      if constexpr (RAGGED) {
+        at = place(i);
 #pragma unroll
         for (int e = 0; e < N; ++e)
-          if (at + e >= len) v[u][e] = -kInf;
+          if (i >= groups || at + e < i * N || at + e >= len) v[u][e] = -kInf;
       }
-      float here = v[u][0];
+      float here = max3(v[u][0], v[u][1], v[u][2]);
 #pragma unroll
-      for (int e = 1; e < N; ++e) here = __builtin_fmaxf(here, v[u][e]);
+      for (int e = 3; e < N; e += 2) here = e + 1 < N ? max3(here, v[u][e], v[u][e + 1]) : __builtin_fmaxf(here, v[u][e]);
       if constexpr (TOP) {
         if (here > best) {
           best = here;
@@ -235,15 +241,49 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
     }
     if (most > own.m) move_to(own, most, c);
     const float m = own.m > -kInf ? own.m : 0.0f;
+    float s[2] = {}, w[2] = {};
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const float d = c * (v[u][e] - m), p = __builtin_amdgcn_exp2f(d);
-        own.s += p;
-        if constexpr (ENTROPY) own.w += p * floored(d);
+        s[e % 2] += p;
+        if constexpr (ENTROPY) w[e % 2] += p * floored(d);
       }
+    own.s += s[0] + s[1];
+    if constexpr (ENTROPY) own.w += w[0] + w[1];
+  };
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  int g = t;
+  const int rounds = whole / (U * NT);   // of whole groups in every thread
+  Raw16 raw[U], next[U];
+  const auto fetch = [&](int from, Raw16 (&to)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) to[u] = G::read(x + static_cast<int64_t>(from + u * NT) * N, N);
+  };
+  const auto fetch_ragged = [&](int from, Raw16 (&to)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) to[u] = read(min(from + u * NT, groups - 1));
+  };
+  const bool rest = rounds * U * NT < groups;
+  if (rounds > 0) {
+    fetch(g, raw);
+    for (int r = 1; r < rounds; ++r) {
+      fetch(g + U * NT, next);
+      take(raw, g, no);
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = next[u];
+      g += U * NT;
+    }
+    if (rest) fetch_ragged(g + U * NT, next);
+    take(raw, g, no);
+    g += U * NT;
+  } else {
+    fetch_ragged(g, next);
   }
+  if (rest) take(next, g, yes);
+
   Stats all = own;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) all = join(all, {__shfl_xor(all.m, d), __shfl_xor(all.s, d), __shfl_xor(all.w, d)}, c);
@@ -264,17 +304,38 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
     }
   }
   if constexpr (TOP) {
-    __shared__ TopSpace<NW> space;
+    __shared__ TopSpace<NT> space;
     const Key mine = t < groups ? key_of(best, first + best_at) : 0;
-    find_top<NT, N>(space, mine, args.n_top, (groups + NT - 1) / NT, [&](int j0, int count, auto take) {
-      for (int j = j0; j < j0 + count; ++j) {
-        const int at = (t + j * NT) * N;
-        if (at >= len) break;
-        float v[N];
-        G::unpack(G::read(x + at, len - at), v);
+    const uint32_t strip = (groups + NT - 1) / NT;
+    find_top<NT>(space, mine, args.n_top, [&](uint32_t reaching, Key bound, auto take_key) {
+      const float least = value_of(bound);   // (of a bound that nothing sets: NaN, which is no bound)
+      const uint32_t count = reaching * strip;
+      for (uint32_t i = t; i < count; i += U * NT) {
+        int at_group[U];
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (at + e < len) take(key_of(v[e], first + at + e));
+        for (int u = 0; u < U; ++u) {
+          const uint32_t k = min(i + u * NT, count - 1), j = k / reaching;
+          at_group[u] = space.reach[k - j * reaching] + j * NT;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = read(min(at_group[u], groups - 1));
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (i + u * NT >= count || at_group[u] >= groups) continue;
+          float v[N];
+          G::unpack(raw[u], v);
+          float here = v[0];
+#pragma unroll
+          for (int e = 1; e < N; ++e) here = __builtin_fmaxf(here, v[e]);
+          if (here < least) continue;
+          const int at = place(at_group[u]);
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (at + e >= at_group[u] * N && at + e < len) {
+              const Key k = key_of(v[e], first + at + e);
+              if (k >= bound) take_key(k);
+            }
+        }
       }
     });
     if (t < args.n_top) {
@@ -294,7 +355,7 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
 constexpr int kJoinThreads = 256;
 template <typename T>
 __global__ __launch_bounds__(kJoinThreads) void log_probs_join_kernel(LogProbArgs args) {
-  __shared__ Key found[kMostParts * kMostTop], best[kMostTop];
+  __shared__ Key found[kMostParts * kMostTop + 8], best[kMostTop];
   const int64_t row = blockIdx.x;
   const int stride = record_floats(args.n_top);
   const float* records = args.workspace + row * args.parts * stride;
@@ -309,8 +370,13 @@ __global__ __launch_bounds__(kJoinThreads) void log_probs_join_kernel(LogProbArg
     const uint32_t* words = reinterpret_cast<const uint32_t*>(records + (i / args.n_top) * stride) + 4 + 2 * (i % args.n_top);
     found[i] = static_cast<Key>(words[1]) << 32 | words[0];
   }
+  if (threadIdx.x < 8) found[count + threadIdx.x] = 0;
   __syncthreads();
-  rank_keys(found, count, best, args.n_top, kJoinThreads);
+  for (int i = threadIdx.x; i < count; i += kJoinThreads) {
+    const Key k = found[i];
+    const int rank = larger_than(found, count, k);
+    if (rank < args.n_top) best[rank] = k;
+  }
   __syncthreads();
   if (static_cast<int>(threadIdx.x) < args.n_top) put_top(args, row, threadIdx.x, best[threadIdx.x], all, log_s);
 }
@@ -331,34 +397,48 @@ hipError_t launch_rows(const LogProbArgs& args, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Threads of a row.  Rows that fill the chip take few, whose sums are joined without a barrier (one wave) or a short one; few
+// rows take more, whose latency counts.  us, 64, 128, 256, 512, 1024 threads, bf16 with entropy: 16384 x 1024 19, 33, 55, 106, 239,
+// 8192 x 8192 27, 27, 29, 65, 146, 8192 x 32000 98, 103, 100, 117, 182, 1 x 8192 5.5, 4.8, 5.0, 6.2, 7.6, 1 x 32000 15, 10, 7.5, 7.3, 8.5,
+// 256 x 32000 15, 10, 8.4, 8.9, 10; with twenty tokens 16384 x 4096 (five) 44, 50, 95, 217, 632, 1100 x 32000 45, 31, 29, 32, 64,
+// 3001 x 50257 fp32 200, 175, 143, 124, 135, 1 x 8192 12.8, 8.9, 7.8, 9.7, 12.1, 1 x 32000 31, 18, 12.9, 11.7, 13.4.
 template <typename T>
 hipError_t launch_of(const LogProbArgs& args, hipStream_t stream) {
-  if (args.rows * args.parts > 1024) return launch_rows<T, 256>(args, stream);
-  return launch_rows<T, 1024>(args, stream);
+  const int64_t groups = (args.chunk + Group16<T>::N - 1) / Group16<T>::N;
+  const bool many = args.rows * args.parts > 1024;
+  if (many && groups <= 1024) return launch_rows<T, 64>(args, stream);
+  if (groups <= (args.n_top > 0 && !many ? 1024 : 4096) || (many && args.n_top == 0)) return launch_rows<T, 256>(args, stream);
+  return launch_rows<T, 512>(args, stream);
 }
 
 // ---- gradient ------------------------------------------------------------------
 
-constexpr int kGradThreads = 256;
-constexpr int kGradGroups = 4;   // of sixteen bytes, of a thread
-
-template <typename T>
-__global__ __launch_bounds__(kGradThreads) void log_probs_backward_kernel(LogProbBackwardArgs args) {
+// A thread takes U groups of sixteen bytes of a row, a workgroup of NT threads a part of one (a wave a short row of its own, four
+// to a workgroup).  STREAM: non-temporal stores.  An output that the Infinity Cache cannot hold pushes the logits out of it, and the
+// next launch waits for its write-backs; a smaller one is read from there next.  8192 x 32000 bf16 behind log_probs, both, us: plain 310,
+// streamed 281, streamed and from the last row on 274; the launch alone 188, 181, 180 (5.8 TB/s).
+template <typename T, int NT, int U, bool STREAM>
+__global__ __launch_bounds__(RowGroup<NT>::kThreads) void log_probs_backward_kernel(LogProbBackwardArgs args) {
   typedef Group16<T> G;
-  constexpr int N = G::N;
-  const int64_t row = blockIdx.x / static_cast<uint32_t>(args.parts);
+  constexpr int N = G::N, kRows = RowGroup<NT>::kRows;
+  const int t = threadIdx.x % NT;
+  // (from the last row on: what log_probs read last is what the Infinity Cache still holds)
+  const int64_t row = args.rows - 1 - (static_cast<int64_t>(blockIdx.x / static_cast<uint32_t>(args.parts)) * kRows + threadIdx.x / NT);
+  if (row < 0) return;
   const int part = static_cast<int>(blockIdx.x % static_cast<uint32_t>(args.parts));
   const int cols = static_cast<int>(args.cols);
   const T* x = static_cast<const T*>(args.logits) + row * args.ld;
   T* dx = static_cast<T*>(args.dlogits) + row * args.ldd;
-  const int64_t first = int64_t{part} * kGradThreads * kGradGroups * N;
-  Raw16 raw[kGradGroups];
+  const int first = part * (NT * U * N);   // below cols
+  Raw16 raw[U];
 #pragma unroll
-  for (int u = 0; u < kGradGroups; ++u) {
-    const int64_t at = first + (u * kGradThreads + threadIdx.x) * N;
-    raw[u] = G::read(x + at, static_cast<int>(max(int64_t{cols} - at, int64_t{0})));
+  for (int u = 0; u < U; ++u) {
+    const int at = first + (u * NT + t) * N;
+    raw[u] = G::read(x + at, max(cols - at, 0));
   }
-  const float lse = args.lse[row];
+  const float given = args.lse[row];
+  const bool none = given == -kInf;          // nothing left: no token has any of it
+  const float lse = none ? kInf : given;
   float d = 0.0f, dh = 0.0f, h = 0.0f;
   int64_t id = -1;
   if (args.ids) {
@@ -369,22 +449,25 @@ __global__ __launch_bounds__(kGradThreads) void log_probs_backward_kernel(LogPro
     h = args.entropy[row];
     dh = args.dentropy[row];
   }
-  const bool none = lse == -kInf;   // nothing left
 #pragma unroll
-  for (int u = 0; u < kGradGroups; ++u) {
-    const int64_t at = first + (u * kGradThreads + threadIdx.x) * N;
+  for (int u = 0; u < U; ++u) {
+    const int at = first + (u * NT + t) * N;
     if (at >= cols) break;
     float v[N];
     G::unpack(raw[u], v);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       const float logp = __builtin_fmaf(args.scale, v[e], -lse), p = __builtin_amdgcn_exp2f(kLog2e * logp);
-      float g = -p * (d + dh * (floored(logp) + h));
-      if (none) g = 0.0f * d;
-      if (at + e == id) g = none ? g : g + d;
-      v[e] = args.scale * g;
+      v[e] = -p * (d + dh * (floored(logp) + h));
     }
-    G::store(dx + at, static_cast<int>(cols - at), v);
+    if (id >= at && id < at + N && !none) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] += at + e == id ? d : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] *= args.scale;
+    if constexpr (STREAM) G::store_streamed(dx + at, cols - at, v);
+    else G::store(dx + at, cols - at, v);
   }
 }
 
@@ -393,11 +476,13 @@ __global__ __launch_bounds__(kGradThreads) void log_probs_backward_kernel(LogPro
 // A launch has fewer than 2^32 threads.
 constexpr int64_t kLaunchWorkgroups = int64_t{1} << 21;
 
-// Parts of a row: one, but where few rows leave most CUs idle and a row is long.
-int log_probs_parts(int64_t rows, int64_t cols) {
-  if (rows > 64) return 1;
-  const int64_t parts = std::min<int64_t>({cols / 16384, 256 / std::max<int64_t>(rows, 1), kMostParts});
-  return static_cast<int>(cols >= 131072 && parts > 1 ? parts : 1);
+// Parts of a row: one, but for few long rows, whose parts a second launch joins.  us, 1, 2, 4, 8, 16 parts, bf16 with entropy: 1 x 65536
+// 8.4, 7.9, 7.2, 7.8, 9.8, 1 x 131072 12.7, 10.0, 8.7, 7.7, 8.7, 16 x 262144 21.8, 15.0, 10.9, 9.4, 9.7, 64 x 131072 13.3, 11.2, 9.0, 9.5,
+// 11.6; with twenty tokens, which every part ranks, 1 x 65536 12.8, 13.5, 12.9, 14.9, 22.5, 1 x 131072 18.8, 16.5, 14.9, 15.4, 20.8,
+// 16 x 262144 30.6, 23.5, 18.3, 17.7, 23.5, 64 x 131072 19.7, 17.3, 16.7, 18.7, 25.6.
+int log_probs_parts(int64_t rows, int64_t cols, int64_t n_top) {
+  if (rows > 64 || cols < (n_top > 0 ? 131072 : 65536)) return 1;
+  return n_top > 0 || rows > 16 ? 4 : static_cast<int>(std::min<int64_t>(cols / 16384, kMostParts));
 }
 
 hipError_t launch_log_probs(const LogProbArgs& args, int dtype, hipStream_t stream) {
@@ -421,16 +506,21 @@ hipError_t launch_log_probs(const LogProbArgs& args, int dtype, hipStream_t stre
   return hipSuccess;
 }
 
-hipError_t launch_log_probs_backward(const LogProbBackwardArgs& args, int dtype, hipStream_t stream) {
-  const int64_t eb = dtype == CLEAVE_BF16 ? 2 : 4, n = dtype == CLEAVE_BF16 ? Group16<Bf16>::N : Group16<float>::N;
-  const int64_t of_workgroup = kGradThreads * kGradGroups * n, parts = (args.cols + of_workgroup - 1) / of_workgroup;
-  const int64_t most = std::max<int64_t>(1, (int64_t{1} << 23) / parts);
-  for (int64_t row = 0; row < args.rows; row += most) {
+namespace {
+
+template <typename T, int NT, int U>
+hipError_t launch_backward(const LogProbBackwardArgs& args, bool stream_out, hipStream_t stream) {
+  constexpr int kColumns = NT * U * Group16<T>::N, kRows = RowGroup<NT>::kRows;
+  const int64_t parts = (args.cols + kColumns - 1) / kColumns;
+  const int64_t most = std::max<int64_t>(1, (int64_t{1} << 23) / parts) * kRows;
+  // (the last rows first, over launches too)
+  for (int64_t end = args.rows; end > 0; end -= most) {
+    const int64_t row = std::max<int64_t>(end - most, 0);
     LogProbBackwardArgs some = args;
-    some.rows = std::min(args.rows - row, most);
+    some.rows = end - row;
     some.parts = static_cast<int>(parts);
-    some.logits = static_cast<const unsigned char*>(args.logits) + row * args.ld * eb;
-    some.dlogits = static_cast<unsigned char*>(args.dlogits) + row * args.ldd * eb;
+    some.logits = static_cast<const T*>(args.logits) + row * args.ld;
+    some.dlogits = static_cast<T*>(args.dlogits) + row * args.ldd;
     some.lse += row;
     if (args.ids) {
       some.ids += row;
@@ -440,13 +530,26 @@ hipError_t launch_log_probs_backward(const LogProbBackwardArgs& args, int dtype,
       some.entropy += row;
       some.dentropy += row;
     }
-    const dim3 g(static_cast<uint32_t>(some.rows * parts)), b(kGradThreads);
-    if (dtype == CLEAVE_BF16) hipLaunchKernelGGL((log_probs_backward_kernel<Bf16>), g, b, 0, stream, some);
-    else hipLaunchKernelGGL((log_probs_backward_kernel<float>), g, b, 0, stream, some);
+    const dim3 g(static_cast<uint32_t>((some.rows + kRows - 1) / kRows * parts)), b(RowGroup<NT>::kThreads);
+    if (stream_out) hipLaunchKernelGGL((log_probs_backward_kernel<T, NT, U, true>), g, b, 0, stream, some);
+    else hipLaunchKernelGGL((log_probs_backward_kernel<T, NT, U, false>), g, b, 0, stream, some);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+template <typename T>
+hipError_t launch_backward_of(const LogProbBackwardArgs& args, hipStream_t stream) {
+  const bool stream_out = args.rows * args.cols * static_cast<int64_t>(sizeof(T)) >= kCacheBytes;
+  if (args.cols <= 64 * 4 * Group16<T>::N) return launch_backward<T, 64, 4>(args, stream_out, stream);
+  return launch_backward<T, 256, 4>(args, stream_out, stream);
+}
+
+}  // namespace
+
+hipError_t launch_log_probs_backward(const LogProbBackwardArgs& args, int dtype, hipStream_t stream) {
+  return dtype == CLEAVE_BF16 ? launch_backward_of<Bf16>(args, stream) : launch_backward_of<float>(args, stream);
 }
 
 }  // namespace cleave

@@ -197,7 +197,7 @@ int64_t log_probs_chunk(int64_t cols, int parts) { return ((cols + parts - 1) / 
 extern "C" int64_t cleave_log_probs_workspace(int64_t rows, int64_t cols, int64_t n_top) {
   if (rows < 0 || cols < 1 || rows > kMost || cols > kMostTokens || n_top < 0 || n_top > cols) return CLEAVE_EINVAL;
   if (n_top > cleave::kMostTop) return CLEAVE_ELIMIT;
-  const int64_t parts = cleave::log_probs_parts(rows, cols);
+  const int64_t parts = cleave::log_probs_parts(rows, cols, n_top);
   return parts == 1 ? 0 : rows * parts * (4 + 2 * n_top);
 }
 
@@ -220,7 +220,7 @@ extern "C" int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, 
       (entropy && entropy == top_logp))
     return CLEAVE_EINVAL;
   if (rows == 0) return CLEAVE_OK;
-  int parts = cleave::log_probs_parts(rows, cols);
+  int parts = cleave::log_probs_parts(rows, cols, n_top);
   if (parts > 1 && !workspace) return CLEAVE_EINVAL;
   const int64_t chunk = log_probs_chunk(cols, parts);
   parts = static_cast<int>((cols + chunk - 1) / chunk);   // (rounding may leave the last ones empty)

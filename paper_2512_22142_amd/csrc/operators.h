@@ -96,7 +96,7 @@ hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, hipStream_t s
 // ---- log probabilities of tokens ---------------------------------------------
 
 constexpr int kMostTop = 32;      // most likely tokens of a row that are given
-constexpr int kMostParts = 32;    // of a row
+constexpr int kMostParts = 8;     // of a row
 struct LogProbArgs {
   const void* logits;
   const int64_t* ids;      // null: no log probabilities
@@ -111,7 +111,7 @@ struct LogProbArgs {
   int n_top, parts;
   int chunk;               // columns of a part
 };
-int log_probs_parts(int64_t rows, int64_t cols);
+int log_probs_parts(int64_t rows, int64_t cols, int64_t n_top);
 hipError_t launch_log_probs(const LogProbArgs& args, int dtype, hipStream_t stream);
 
 struct LogProbBackwardArgs {

@@ -40,6 +40,11 @@ struct Group16<float> {
 #pragma unroll
     for (int e = 0; e < N; ++e) out[e] = v[e];
   }
+  static __device__ __forceinline__ void store_streamed(float* p, int left, const float (&in)[N]) {
+    typedef float FloatsAny __attribute__((ext_vector_type(4), aligned(4)));
+    if (left >= N) __builtin_nontemporal_store(FloatsAny{in[0], in[1], in[2], in[3]}, reinterpret_cast<FloatsAny*>(p));
+    else store(p, left, in);
+  }
   static __device__ __forceinline__ void store(float* p, int left, const float (&in)[N]) {
     typedef float FloatsAny __attribute__((ext_vector_type(4), aligned(4)));
     if (left >= N) {
@@ -70,6 +75,15 @@ struct Group16<Bf16> {
       out[2 * q] = __builtin_bit_cast(float, w[q] << 16);
       out[2 * q + 1] = __builtin_bit_cast(float, w[q] & 0xffff0000u);
     }
+  }
+  // Non-temporal.
+  static __device__ __forceinline__ void store_streamed(Bf16* p, int left, const float (&in)[N]) {
+    if (left >= N)
+      __builtin_nontemporal_store(
+          Any{pack_bf16(in[0], in[1]), pack_bf16(in[2], in[3]), pack_bf16(in[4], in[5]), pack_bf16(in[6], in[7])},
+          reinterpret_cast<Any*>(p));
+    else
+      store(p, left, in);
   }
   static __device__ __forceinline__ void store(Bf16* p, int left, const float (&in)[N]) {
     if (left >= N) {
