@@ -234,10 +234,6 @@ bool cut_small(const cleave_plan* plan, int cus);
 int ensure_uploaded(cleave_plan* p) {
   int dev = 0;
   CLEAVE_HIP(hipGetDevice(&dev));
-  if (p->fused) {
-    const int rc = ensure_uploaded(p->fused);
-    if (rc != CLEAVE_OK) return rc;
-  }
   if (p->device == dev) return CLEAVE_OK;
   if (p->device >= 0) free_device_tables(p);
   int rc = ensure_device_ready(dev, nullptr);
@@ -428,9 +424,15 @@ extern "C" int cleave_last_hip_error(void) { return g_last_hip_error; }
 
 extern "C" int cleave_version(void) { return 107; }
 
+namespace {
+
+int upload_gated(cleave_plan* plan);
+
+}  // namespace
+
 extern "C" int cleave_plan_upload(cleave_plan* plan) {
   if (!plan) return CLEAVE_EINVAL;
-  return ensure_uploaded(plan);
+  return plan->gated ? upload_gated(plan) : ensure_uploaded(plan);
 }
 
 extern "C" void cleave_plan_destroy(cleave_plan* plan) {
@@ -778,9 +780,8 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
                  const cleave::LinearArgs* linear = nullptr, const cleave::GatedArgs* gated = nullptr) {
   if (!plan || !A || !B || (!partials && !asm_to.C)) return CLEAVE_EINVAL;
   const bool two = gated && gated->b_up;   // a gated product: the plan's columns are both operands'
-  const bool epilogue = linear || gated;
   if (dtype != CLEAVE_F32 && dtype != CLEAVE_BF16) return CLEAVE_EINVAL;
-  if (plan->pairs && !epilogue) return CLEAVE_EINVAL;   // a plan of 8-bit operands
+  if (plan->pairs && !linear && !gated) return CLEAVE_EINVAL;   // a plan of 8-bit operands
   if ((transA != 0 && transA != 1) || (transB != 0 && transB != 1)) return CLEAVE_EINVAL;
   if ((task_ids == nullptr) != (n_ids == 0) || n_ids < 0) return CLEAVE_EINVAL;
   if (lda < (transA ? plan->M : plan->K) || ldb < (transB ? plan->K : two ? plan->N / 2 : plan->N)) return CLEAVE_EINVAL;
@@ -812,16 +813,16 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
   // x 2504 x 1024 in 4 37 / 30.
   const int e = 16 / eb;
   // (The epilogue's stores take any number of columns, and its kernels read A along K.)
-  const bool direct = dtype == CLEAVE_BF16 && ((two ? plan->N % 16 == 0 : plan->all_n_mult8) || (epilogue && transB)) && !(epilogue && transA) && (transA ? plan->all_m_mult8 : plan->all_k_mult8) &&
+  // (Who asks for a gated product has seen to that.)
+  const bool direct = gated || (dtype == CLEAVE_BF16 && (plan->all_n_mult8 || (linear && transB)) && !(linear && transA) && (transA ? plan->all_m_mult8 : plan->all_k_mult8) &&
                       (!transB || plan->all_k_mult8) &&
                       lda % e == 0 && ldb % e == 0 && aligned(A, 16) && aligned(B, 16) &&
                       // in-tile byte offsets are kept in 32 bits
                       lda * eb < (int64_t{1} << 22) && ldb * eb < (int64_t{1} << 22) &&
-                      offsets_multiple_of(bl.a, bl.shape, e) && offsets_multiple_of(bl.b, bl.shape, e);
+                      offsets_multiple_of(bl.a, bl.shape, e) && offsets_multiple_of(bl.b, bl.shape, e));
   // 8-bit operands have no general kernel, and partial blocks leave theirs in whole eights of columns (cleave_linear
   // refuses what would come here otherwise, and cleave_plan_linear does not plan it).
   if (plan->pairs && (!direct || (!asm_to.C && !plan->all_n_mult8))) return CLEAVE_EINVAL;
-  if (gated && (!direct || !aligned(gated->b_up, 16) || plan->device < 0)) return CLEAVE_EINVAL;
   // An operand of the general kernel's 16-byte loads needs that much between the start of a
   // stored row and the end of any chunk (K-contiguous) or row (otherwise), and
   // in-tile byte offsets (up to 128 rows) that fit 32 bits.
@@ -1404,7 +1405,70 @@ namespace {
 bool gated_few_rows(int64_t M, int64_t N) { return M <= cleave::kFewRows && N <= int64_t{1} << 27; }
 
 // What the direct kernel takes of bf16 operands (in units of it: pairs of e4m3): whole sixteen bytes, in-tile offsets of 32 bits.
-bool whole_operand(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld < int64_t{1} << 21; }
+constexpr int64_t kMostPitch = (int64_t{1} << 21) - 8;
+bool whole_operand(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld <= kMostPitch; }
+
+// bf16 operands that are not whole are laid out again, in the workspace, in rows of whole sixteen bytes, zeros behind their ends (one pass
+// over what is not whole), for the direct kernel, where there are rows enough that the way through the general kernel
+// and fp32 partial blocks takes longer.  us, general / laid out, weights stored K x N:
+//   gated, K x N = 4096 x 11007, 512, 800, 1024, 1999, 4096 rows 146 / 169, 242 / 250, 286 / 252, 564 / 371, 1058 / 641; 1000 x 2500, 800, 1999, 4096
+// rows 30 / 30, 45.5 / 42.5, 78 / 70; 2048 x 4100, 800, 1200, 2048 rows 49 / 48, 68 / 73, 112 / 79.  An odd K costs the general kernel more:
+// 4097 x 11008, 200, 400, 800 rows 107 / 91, 151 / 102, 260 / 202 (stored N x K 135 / 147, 192 / 171, 308 / 271), 1001 x 2500, 200, 400, 800
+// rows 18.9 / 21.4, 24.3 / 23.0, 32.3 / 30.0.
+//   gradient, 4097 x 11008, 200, 400, 800, 2048 rows 60 / 51, 102 / 71, 150 / 150, 299 / 234 (N x K 74 / 78, 125 / 109, 183 / 171, 347 / 262), 2049 x
+// 4096, 200, 400, 800 rows 20.5 / 14.9, 29.0 / 24.8, 37.9 / 31.3.  Rows of the output that are not whole cost the direct kernel's stores more
+// than the join's: 4096 x 11007, 800, 1024, 1999, 4096 rows 149 / 199, 159 / 178, 299 / 293, 572 / 440, 2048 x 4100, 1200, 2048, 4096 rows 49 / 49,
+// 71 / 73, 126 / 91, 2048 x 2500 33 / 40, 49 / 49, 77 / 84, 1000 x 2500, 4096 rows 56 / 71.
+int64_t eights(int64_t n) { return (n + 7) / 8 * 8; }
+bool packs(int64_t M, int64_t N, int64_t K) {
+  return M >= (K % 8 != 0 ? 384 : 768) && eights(N) <= kMostPitch && eights(K) <= kMostPitch;
+}
+bool packs_grad(int64_t M, int64_t N, int64_t K) {
+  return (N % 8 == 0 ? M >= 384 : M >= 2048 && K >= 2048) && eights(N) <= kMostPitch && eights(K) <= kMostPitch;
+}
+// Floats of the workspace: A and `weights` operands B, in either layout, from a 16-byte boundary on.
+int64_t packed_floats(int64_t M, int64_t N, int64_t K, int64_t weights) {
+  return (M * eights(K) + weights * std::max(N * eights(K), K * eights(N))) / 2 + 4;
+}
+
+// What calls of the plan need on the device: few rows nothing.
+int upload_gated(cleave_plan* plan) {
+  if (gated_few_rows(plan->M, plan->N)) return CLEAVE_OK;
+  if (plan->fused) {
+    const int rc = ensure_uploaded(plan->fused);
+    if (rc != CLEAVE_OK || plan->pairs || packs(plan->M, plan->N, plan->K)) return rc;
+  }
+  return ensure_uploaded(plan);
+}
+
+// The operands of a call on the direct kernel, laid out again where they are not whole.
+struct Operands {
+  const void* a;
+  const void* b[2];
+  int64_t lda, ldb;
+};
+hipError_t pack_operands(Operands& o, int weights, int64_t M, int64_t N, int64_t K, int transB, float* workspace, hipStream_t stream) {
+  unsigned char* at = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(workspace) + 15) / 16 * 16);
+  cleave::PackArgs args{};
+  const auto add = [&](const void* from, int64_t ld, int64_t rows, int64_t cols) -> const void* {
+    cleave::PackMatrix& m = args.matrices[args.count++];
+    m = {from, at, ld, rows, cols};
+    at += rows * eights(cols) * 2;
+    return m.to;
+  };
+  if (K % 8 != 0 || !whole_operand(o.a, o.lda)) {
+    o.a = add(o.a, o.lda, M, K);
+    o.lda = eights(K);
+  }
+  bool whole = (transB ? K : N) % 8 == 0;
+  for (int w = 0; w < weights; ++w) whole = whole && whole_operand(o.b[w], o.ldb);
+  if (!whole) {
+    const int64_t rows = transB ? N : K, cols = transB ? K : N;
+    for (int w = 0; w < weights; ++w) o.b[w] = add(o.b[w], o.ldb, rows, cols);
+    o.ldb = eights(cols);
+  }
+  return cleave::launch_pack(args, stream);
+}
 
 bool floats_aligned(const float* const* list, int n) {
   for (int k = 0; k < n; ++k)
@@ -1446,7 +1510,7 @@ extern "C" int cleave_plan_gated(int64_t M, int64_t N, int64_t K, int dtype, cle
   plan->gated = true;
   plan->pairs = pairs;
   plan->uniform_splits = splits;
-  if (!few && splits == 1 && dtype != CLEAVE_F32) {
+  if (!few && splits == 1 && dtype != CLEAVE_F32 && (pairs || (eights(N) <= kMostPitch && eights(K) <= kMostPitch))) {
     rc = cleave_plan_uniform(M, 2 * N, k, cleave::kLargeTileRows, cleave::kLargeTileCols, 1, 0, &plan->fused);
     if (rc != CLEAVE_OK) {
       cleave_plan_destroy(plan);
@@ -1463,6 +1527,7 @@ extern "C" int64_t cleave_gated_workspace(const cleave_plan* plan, int whole) {
   if (!plan || !plan->gated || plan->batch != 2 || (whole != 0 && whole != 1)) return CLEAVE_EINVAL;
   if (gated_few_rows(plan->M, plan->N)) return plan->uniform_splits == 1 ? 0 : plan->partial_elems;
   if (plan->pairs || (plan->fused && whole)) return 0;
+  if (plan->fused && packs(plan->M, plan->N, plan->K)) return packed_floats(plan->M, plan->N, plan->K, 2);
   return plan->partial_elems;
 }
 
@@ -1502,17 +1567,20 @@ extern "C" int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* a
   const bool few = gated_few_rows(M, N);
   const bool whole = e4m3 || (a->dtype == CLEAVE_BF16 && K % 8 == 0 && (a->transB || N % 8 == 0) && whole_operand(a->A, a->lda) &&
                               whole_operand(a->B_gate, a->ldb) && whole_operand(a->B_up, a->ldb));
-  const bool fused = !few && plan->fused && whole;
-  if (!fused && (!few || splits > 1) && !a->partials) return CLEAVE_EINVAL;
+  const bool fused = !few && plan->fused && (whole || packs(M, N, K));
+  if (!(fused && whole) && (!few || splits > 1) && !a->partials) return CLEAVE_EINVAL;
   if (fused) {
     AssembleTarget to;
     to.C = a->C;
     to.ldc = a->ldc;
     to.out_dtype = a->out_dtype;
     int rc = ensure_uploaded(plan->fused);
-    if (rc == CLEAVE_OK)
-      rc = execute_impl(plan->fused, nullptr, 0, a->A, e4m3 ? a->lda / 2 : a->lda, 0, a->B_gate, e4m3 ? a->ldb / 2 : a->ldb,
-                        a->transB, CLEAVE_BF16, nullptr, BatchLayout{}, hip_stream, to, false, nullptr, &epi);
+    if (rc != CLEAVE_OK) return rc;
+    Operands o{a->A, {a->B_gate, a->B_up}, e4m3 ? a->lda / 2 : a->lda, e4m3 ? a->ldb / 2 : a->ldb};
+    if (!whole) CLEAVE_HIP(pack_operands(o, 2, M, N, K, a->transB, a->partials, stream));
+    epi.b_up = o.b[1];
+    rc = execute_impl(plan->fused, nullptr, 0, o.a, o.lda, 0, o.b[0], o.ldb, a->transB, CLEAVE_BF16, nullptr, BatchLayout{}, hip_stream,
+                      to, false, nullptr, &epi);
     plan->last_kernel = plan->fused->last_kernel;
     return rc;
   }
@@ -1555,7 +1623,10 @@ extern "C" int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* a
 
 extern "C" int64_t cleave_gated_grad_workspace(const cleave_plan* plan, int whole) {
   if (!plan || !plan->linear || plan->pairs || (whole != 0 && whole != 1)) return CLEAVE_EINVAL;
-  if (!gated_few_rows(plan->M, plan->N) && whole && plan->uniform_splits == 1 && !plan->for_fp32) return 0;
+  if (!gated_few_rows(plan->M, plan->N) && plan->uniform_splits == 1 && !plan->for_fp32) {
+    if (whole) return 0;
+    if (packs_grad(plan->M, plan->N, plan->K)) return packed_floats(plan->M, plan->N, plan->K, 1);
+  }
   return plan->partial_elems;
 }
 
@@ -1588,8 +1659,8 @@ extern "C" int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_gr
   const bool few = gated_few_rows(M, N);
   const bool whole = a->dtype == CLEAVE_BF16 && K % 8 == 0 && (a->transB || N % 8 == 0) && whole_operand(a->A, a->lda) &&
                      whole_operand(a->B, a->ldb);
-  const bool fused = !few && whole && splits == 1;
-  if (!fused && !a->partials) return CLEAVE_EINVAL;
+  const bool fused = !few && splits == 1 && !plan->for_fp32 && a->dtype == CLEAVE_BF16 && (whole || packs_grad(M, N, K));
+  if (!(fused && whole) && !a->partials) return CLEAVE_EINVAL;
   int rc = ensure_uploaded(plan);
   if (rc == CLEAVE_OK) rc = ensure_gated_ready(plan->device);
   if (rc != CLEAVE_OK) return rc;
@@ -1598,7 +1669,9 @@ extern "C" int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_gr
     to.C = a->dgate;
     to.ldc = a->ld_dgate;
     to.out_dtype = a->out_dtype;
-    return execute_impl(plan, nullptr, 0, a->A, a->lda, 0, a->B, a->ldb, a->transB, a->dtype, nullptr, BatchLayout{}, hip_stream, to,
+    Operands o{a->A, {a->B, nullptr}, a->lda, a->ldb};
+    if (!whole) CLEAVE_HIP(pack_operands(o, 1, M, N, K, a->transB, a->partials, stream));
+    return execute_impl(plan, nullptr, 0, o.a, o.lda, 0, o.b[0], o.ldb, a->transB, a->dtype, nullptr, BatchLayout{}, hip_stream, to,
                         false, nullptr, &epi);
   }
   if (few) {   // (the sums themselves, also where there is one chunk)

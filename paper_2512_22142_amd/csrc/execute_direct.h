@@ -397,7 +397,9 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
   // the first STAGES steps into the ring.
   auto fill_ring = [&](ItemCtx& c) {
     ta.init(a_rs, a_ks, c.m_valid, wave, lane);
-    tb.init(b_rs, b_ks, c.n_valid, wave, lane);
+    // (a gated call's operand B that is stored by rows of K is whole up to the next eight columns)
+    constexpr bool kEights = !B_K && (Epi::kGated || std::is_same<Epi, GatedGradEpilogue>::value);
+    tb.init(b_rs, b_ks, kEights ? (c.n_valid + 7) & ~7 : c.n_valid, wave, lane);
 #pragma unroll
     for (int st = 0; st < STAGES; ++st)
       if (st < c.steps) issue(c, st, st);
@@ -772,7 +774,7 @@ __global__ __launch_bounds__(S::NT, 512 / S::NT) void execute_direct_kernel(Exec
             acc, late_linear_args<sizeof(ExecuteArgs), GatedArgs>(), target, image, wm * S::WTM, wn * WTNB, lane, m_valid, n_valid,
             m_base, n_base);
       else if constexpr (std::is_same<Epi, GatedGradEpilogue>::value)
-        store_gated_grad_rows<decltype(bf16_tag)::value, decltype(interior_tag)::value, MB, NB>(
+        store_gated_grad_rows<decltype(bf16_tag)::value, decltype(interior_tag)::value, kGradAhead, MB, NB>(
             acc, late_linear_args<sizeof(ExecuteArgs), GatedArgs>(), target, image, wm * S::WTM, wn * S::WTN, lane, m_valid, n_valid,
             m_base, n_base);
       else if constexpr (Epi::kLinear)

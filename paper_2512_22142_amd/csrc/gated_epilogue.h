@@ -193,14 +193,16 @@ __device__ __forceinline__ void store_gated_rows(const tile_f32x4 (&acc)[MB][NB]
   }
 }
 
-// The gradient: a turn's arguments are fetched a turn ahead (emit_images).
-template <bool BF16, bool INTERIOR, int MB, int NB>
+// The gradient.  A turn takes the rows that the wave reads at a time (half an image of bf16), its arguments are fetched
+// AHEAD turns before (emit_images).
+constexpr int kGradAhead = 1;
+template <bool BF16, bool INTERIOR, int AHEAD, int MB, int NB>
 __device__ __forceinline__ void store_gated_grad_rows(const tile_f32x4 (&acc)[MB][NB], const GatedArgs& e, const TileTarget& t,
                                                       unsigned char* image, int wave_row0, int wave_col0, int lane, int m_valid,
                                                       int n_valid, int64_t m_base, int64_t n_base) {
   typedef Piece<BF16> P;
   constexpr int N = P::N, EB = BF16 ? 2 : 4, COLS = NB * 16;
-  constexpr int L = COLS / N, RR = 64 / L, K = 16 / RR;
+  constexpr int L = COLS / N, RR = 64 / L, K = 16 / RR;   // lanes to a row, rows of a turn, turns of an image
   static_assert(RR <= 16, "image");
   const int wrow = lane & 15, quad = lane >> 4;
   const int rrow = lane / L, rpiece = (lane % L) * (N / 4);
@@ -219,53 +221,48 @@ __device__ __forceinline__ void store_gated_grad_rows(const tile_f32x4 (&acc)[MB
   const unsigned char* gp = static_cast<const unsigned char*>(e.gate) + (grow * e.ld_gate + gcol) * EB;
   const unsigned char* up = static_cast<const unsigned char*>(e.up) + (grow * e.ld_up + gcol) * EB;
   const int64_t out_pitch = t.ld * EB, second_pitch = e.ld_second * EB, g_pitch = e.ld_gate * EB, u_pitch = e.ld_up * EB;
-  typename P::Raw g_raw[2][K], u_raw[2][K];
-  const auto fetch = [&](int ahead, int d) {   // row of blocks i + ahead, into place d
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int r = 16 * ahead + RR * k;
-      g_raw[d][k] = u_raw[d][k] = typename P::Raw{};
-      if (!valid(row + r)) continue;
-      g_raw[d][k] = read(gp + r * g_pitch);
-      u_raw[d][k] = read(up + r * u_pitch);
-    }
+  typename P::Raw g_raw[AHEAD + 1], u_raw[AHEAD + 1];
+  const auto fetch = [&](int ahead, int d) {   // of the turn that far on, into place d
+    g_raw[d] = u_raw[d] = typename P::Raw{};
+    if (!valid(row + RR * ahead)) return;
+    g_raw[d] = read(gp + RR * ahead * g_pitch);
+    u_raw[d] = read(up + RR * ahead * u_pitch);
   };
-  fetch(0, 0);
+#pragma unroll
+  for (int d = 0; d < AHEAD; ++d)
+    if (d < MB * K) fetch(d, d);
 #pragma unroll 1
-  for (int i = 0; i < MB; ++i) {
+  for (int i = 0; i < MB * K; ++i) {
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int ii = 0; ii < MB; ++ii)
-      if (ii == i) {
+      if (K * ii == i) {
 #pragma unroll
         for (int j = 0; j < NB; ++j)
           *reinterpret_cast<tile_f32x4*>(image + image_piece<NB * 4>(wrow, 4 * j + quad)) = acc[ii][j];
         CLEAVE_KEEP_APART(ii);
       }
     asm volatile("" ::: "memory");
-    if (i + 1 < MB) fetch(1, 1);
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      P p;
-      read_image<16, COLS, N>(image, rrow + RR * k, rpiece, p.v);
-      const P zg = P::of(g_raw[0][k]);
-      P zu = P::of(u_raw[0][k]);
-      finish_gated_grad(static_cast<int>(e.act), p.v, zg.v, zu.v);
-      if (valid(row + RR * k)) {
-        store(zu, second + RR * k * second_pitch);
-        store(p, out + RR * k * out_pitch);
-      }
+    if (i + AHEAD < MB * K) fetch(AHEAD, AHEAD);
+    P p;
+    read_image<16, COLS, N>(image, rrow + RR * (i % K), rpiece, p.v);
+    const P zg = P::of(g_raw[0]);
+    P zu = P::of(u_raw[0]);
+    finish_gated_grad(static_cast<int>(e.act), p.v, zg.v, zu.v);
+    if (valid(row)) {
+      store(zu, second);
+      store(p, out);
     }
     asm volatile("" ::: "memory");
-    row += 16;
-    out += 16 * out_pitch;
-    second += 16 * second_pitch;
-    gp += 16 * g_pitch;
-    up += 16 * u_pitch;
+    row += RR;
+    out += RR * out_pitch;
+    second += RR * second_pitch;
+    gp += RR * g_pitch;
+    up += RR * u_pitch;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      g_raw[0][k] = g_raw[1][k];
-      u_raw[0][k] = u_raw[1][k];
+    for (int d = 0; d < AHEAD; ++d) {
+      g_raw[d] = g_raw[d + 1];
+      u_raw[d] = u_raw[d + 1];
     }
   }
 }

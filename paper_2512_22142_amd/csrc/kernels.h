@@ -255,6 +255,19 @@ hipError_t launch_gated_8bit(const ExecuteArgs& args, const GatedArgs& epi, Dire
 hipError_t launch_gated_grad_direct(const ExecuteArgs& args, const GatedArgs& epi, DirectShape shape, bool tails, int grid,
                                     hipStream_t stream);
 
+// bf16 matrices laid out again in rows of whole eights, on 16-byte boundaries, zeros behind a row's end.
+struct PackMatrix {
+  const void* from;
+  void* to;
+  int64_t ld, rows, cols;   // of `from`, elements
+};
+struct PackArgs {
+  PackMatrix matrices[3];
+  int count;
+  int64_t first;   // row of all (filled in at the launch)
+};
+hipError_t launch_pack(const PackArgs& args, hipStream_t stream);
+
 // Few rows (at most kFewRows), transA = 0, any size, stride and alignment: B is read once.  Into args.C through the
 // epilogue or, with splits > 1, chunks of `chunk` elements into partials[s][row][column] for launch_linear_join.
 constexpr int64_t kFewRows = 16;

@@ -22,6 +22,7 @@
 #include "gated_epilogue.h"
 #include "kernels.h"
 #include "linear_epilogue.h"
+#include "row_access.h"
 
 namespace cleave {
 
@@ -435,7 +436,50 @@ hipError_t launch_gated_joined(const ReduceArgs& args, const GatedArgs& epi, int
   return hipGetLastError();
 }
 
+// ---- rows in whole sixteen bytes ---------------------------------------------------
+
+// A wave takes 64 kPackGroups groups of a row.
+constexpr int kPackGroups = 4;
+__global__ __launch_bounds__(256) void pack_kernel(PackArgs args) {
+  int64_t row = args.first + static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  int which = 0;
+  while (which < args.count && row >= args.matrices[which].rows) row -= args.matrices[which++].rows;
+  if (which == args.count) return;
+  const PackMatrix m = args.matrices[which];
+  const int64_t groups = (m.cols + 7) / 8;
+  const Bf16* from = static_cast<const Bf16*>(m.from) + row * m.ld;
+  u32x4* to = static_cast<u32x4*>(m.to) + row * groups;
+  const int64_t first = static_cast<int64_t>(blockIdx.y) * 64 * kPackGroups + (threadIdx.x & 63);
+  Raw16 raw[kPackGroups];
+#pragma unroll
+  for (int j = 0; j < kPackGroups; ++j) {
+    const int64_t g = first + 64 * j;
+    raw[j] = Group16<Bf16>::read(from + g * 8, static_cast<int>(max(min(m.cols - g * 8, int64_t{8}), int64_t{0})));
+  }
+#pragma unroll
+  for (int j = 0; j < kPackGroups; ++j)
+    if (first + 64 * j < groups) to[first + 64 * j] = raw[j];
+}
+
 }  // namespace
+
+hipError_t launch_pack(const PackArgs& args, hipStream_t stream) {
+  int64_t rows = 0, groups = 0;
+  for (int k = 0; k < args.count; ++k) {
+    rows += args.matrices[k].rows;
+    groups = std::max(groups, (args.matrices[k].cols + 7) / 8);
+  }
+  // (a launch has fewer than 2^32 threads)
+  const int64_t parts = (groups + 64 * kPackGroups - 1) / (64 * kPackGroups), most = std::max<int64_t>((int64_t{1} << 25) / parts / 4 * 4, 4);
+  PackArgs some = args;
+  for (some.first = 0; some.first < rows; some.first += most) {
+    const dim3 g(static_cast<uint32_t>((std::min(rows - some.first, most) + 3) / 4), static_cast<uint32_t>(parts));
+    hipLaunchKernelGGL(pack_kernel, g, dim3(256), 0, stream, some);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 hipError_t launch_gated_join(const ReduceArgs& args, const GatedArgs& epi, int64_t up_at, int64_t M, int64_t N, int splits,
                              int out_dtype, bool vec, hipStream_t stream) {

@@ -159,13 +159,38 @@ def test_few_rows(M, N, K, dtype, transB):
 
 
 @pytest.mark.parametrize("M,N,K", [(17, 1, 1), (37, 53, 71), (200, 50, 100), (129, 257, 65), (300, 77, 1000), (64, 512, 4096),
-                                   (33, 128, 3001), (500, 1000, 1000), (1100, 2052, 333), (2000, 2500, 200)])
+                                   (33, 128, 3001), (500, 1000, 1000), (1100, 2052, 333), (2000, 2500, 200), (400, 300, 1003),
+                                   (800, 1001, 328), (2049, 4100, 72), (900, 1, 9)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("transB", [0, 1])
 def test_any_size_and_alignment(M, N, K, dtype, transB):
     check(M, N, K, dtype, transB=transB, bias=True, keep=True)
     check(M, N, K, dtype, transB=transB, act="gelu_tanh", pad=3, shift=1, out=F32)
     check(M, N, K, dtype, transB=transB, act="relu", merged=True)
+
+
+def test_operands_that_are_laid_out_again():
+    """bf16 with rows, addresses or sizes that are not whole sixteen bytes run on the direct kernel where there are rows enough."""
+    for M, N, K, kw in ((400, 301, 203, dict(transB=0)), (400, 301, 203, dict(transB=1)), (800, 301, 200, dict(transB=0)),
+                        (800, 304, 200, dict(transB=1, pad=3)), (800, 304, 200, dict(transB=0, shift=1)), (800, 304, 200, dict(transB=1, shift=4))):
+        assert "gated_direct" in check(M, N, K, bias=True, keep=True, **kw)[1]
+        assert "gated_direct" in check(M, N, K, merged=True, **kw)[1]
+    for M, N, K, kw in ((400, 304, 203, dict(transB=0)), (400, 304, 203, dict(transB=1)), (400, 304, 200, dict(transB=0, pad=3)),
+                        (2050, 301, 2050, dict(transB=0)), (2050, 301, 2056, dict(transB=1, shift=1))):
+        assert "gated_grad_direct" in check_grad(M, N, K, **kw)
+
+
+def test_the_workspace_is_all_that_is_used():
+    """NaN behind the workspace stay, and what is in it does not count."""
+    for M, N, K in ((800, 301, 203), (300, 301, 203), (9, 300, 8192)):
+        plan = cleave.plan_gated(M, N, K, BF16)
+        n = cleave.gated_workspace(plan)
+        for shift in (0, 1, 3):          # floats of any alignment
+            whole = torch.full((n + 64,), float("nan"), device="cuda")
+            x, w = matrix(M, K, BF16, 1)[0], matrix(K, 2 * N, BF16, 2, 0, 0, 0.1)[0]
+            y = torch.empty(M, N, dtype=BF16, device="cuda")
+            cleave.linear_gated(plan, x, w[:, :N], w[:, N:], y, partials=whole[shift: shift + n])
+            assert torch.all(y.isfinite()) and torch.all(whole[shift + n:].isnan()) and torch.all(whole[:shift].isnan())
 
 
 @pytest.mark.parametrize("act", ACTS)
@@ -222,7 +247,8 @@ def test_gradient_in_every_shape_of_the_direct_kernel(M, N, K, name, transB, out
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 2752, 1024), (16, 1000, 77), (9, 300, 8192), (37, 53, 71), (129, 257, 65), (300, 77, 1000),
-                                   (64, 512, 4096), (33, 128, 3001), (1100, 2052, 333)])
+                                   (64, 512, 4096), (33, 128, 3001), (1100, 2052, 333), (400, 304, 1003), (2050, 1001, 2051),
+                                   (2050, 513, 2056), (500, 8, 9)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("transB", [0, 1])
 def test_gradient_of_any_size_and_alignment(M, N, K, dtype, transB):
