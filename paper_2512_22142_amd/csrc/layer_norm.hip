@@ -206,6 +206,9 @@ hipError_t launch_norm_of(const LayerNormArgs& args, hipStream_t stream) {
 
 // ---- gradient ------------------------------------------------------------------
 
+// Floats of the weight's sums in a row of partial sums, the bias's behind them: whole quads.
+__host__ __device__ __forceinline__ int64_t padded(int64_t cols) { return (cols + 3) / 4 * 4; }
+
 // One pass over dy and h for dx and for the sums over rows: every group of the launch takes every groups-th row and holds its
 // part of dw and db in registers until the last of them, one row of partial sums for each workgroup, whose groups (a
 // wave each, where there are several) are joined in order.  The next row's loads are on their way while a row's sums are joined.
@@ -247,11 +250,14 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
       for (int j = 0; j < V; ++j) to.add[j] = G::read(dsum + at(j), cols - at(j));
     }
   };
+  // (1024 threads have no registers for two rows: bf16 spilled 291)
+  constexpr bool AHEAD = NT < 1024;
   BackwardRow<T, V> cur, next;
-  if (group < args.rows) fetch(group, cur);
+  if (AHEAD && group < args.rows) fetch(group, cur);
   int turn = 0;
   for (int64_t row = group; row < args.rows; row += groups, turn ^= 1) {
-    if (row + groups < args.rows) fetch(row + groups, next);
+    if (!AHEAD) fetch(row, cur);
+    else if (row + groups < args.rows) fetch(row + groups, next);
     float g[V][N], xhat[V][N];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
@@ -283,7 +289,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
       for (int e = 0; e < N; ++e) g[j][e] = (g[j][e] - sum - xhat[j][e] * dot) * cur.inv + add[e];
       G::store(dx + at(j), cols - at(j), g[j]);
     }
-    cur = next;
+    if (AHEAD) cur = next;
   }
   if constexpr (GROUPS > 1) {
     __shared__ float joined[GROUPS - 1][2 * V * N][NT];
@@ -308,11 +314,12 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
           db[j][e] += joined[g][(V + j) * N + e][t];
         }
   }
-  float* out = args.partials + static_cast<int64_t>(blockIdx.x) * 2 * args.cols;
+  const int64_t half = padded(args.cols);
+  float* out = args.partials + static_cast<int64_t>(blockIdx.x) * 2 * half;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     store_floats<N>(out + at(j), cols - at(j), dw[j]);
-    store_floats<N>(out + args.cols + at(j), cols - at(j), db[j]);
+    store_floats<N>(out + half + at(j), cols - at(j), db[j]);
   }
 }
 
@@ -321,7 +328,8 @@ template <typename T>
 __global__ __launch_bounds__(kLongThreads) void layer_norm_backward_long_kernel(LayerNormBackwardArgs args) {
   constexpr int NW = kLongThreads / 64;
   __shared__ float slots[2][2 * NW];
-  float* out = args.partials + static_cast<int64_t>(blockIdx.x) * 2 * args.cols;
+  const int64_t half = padded(args.cols);
+  float* out = args.partials + static_cast<int64_t>(blockIdx.x) * 2 * half;
   const float count = static_cast<float>(args.cols);
   int turn = 0;
   for (int64_t row = blockIdx.x; row < args.rows; row += gridDim.x, turn ^= 1) {
@@ -333,7 +341,7 @@ __global__ __launch_bounds__(kLongThreads) void layer_norm_backward_long_kernel(
     for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
       const float d = element(dy + c), x = (element(h + c) - mean) * inv, g = d * args.weight[c];
       out[c] = (fresh ? 0.0f : out[c]) + d * x;
-      out[args.cols + c] = (fresh ? 0.0f : out[args.cols + c]) + d;
+      out[half + c] = (fresh ? 0.0f : out[half + c]) + d;
       sum += g;
       dot += g * x;
     }
@@ -348,6 +356,65 @@ __global__ __launch_bounds__(kLongThreads) void layer_norm_backward_long_kernel(
   }
 }
 
+// The rows of partial sums, in a fixed order: 64 columns to a workgroup, sixteen bytes to a thread, 64 rows at a time.  (What lies between a
+// half's end and the next quad is read and not used.)
+constexpr int kJoinThreads = 1024, kJoinCols = 64;
+__global__ __launch_bounds__(kJoinThreads) void layer_norm_join_kernel(const float* in, int rows, int64_t first, int64_t cols,
+                                                                       float* dweight, float* dbias) {
+  typedef Group16<float> G;
+  constexpr int kRows = kJoinThreads / 16;
+  __shared__ float part[kJoinThreads / 64][kJoinCols];
+  const int quad = threadIdx.x % 16;
+  const int64_t half = padded(cols), all = 2 * half, c0 = first + static_cast<int64_t>(blockIdx.x) * kJoinCols;
+  const float* p = in + min(c0 + 4 * quad, all - 4);
+  float sum[4] = {};
+#pragma unroll 8
+  for (int row = threadIdx.x / 16; row < rows; row += kRows) {
+    float x[4];
+    G::unpack(G::read(p + row * all, 4), x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += x[e];
+  }
+  // a wave's four rows, then the waves
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    sum[e] += __shfl_xor(sum[e], 16);
+    sum[e] += __shfl_xor(sum[e], 32);
+    if ((threadIdx.x & 63) < 16) part[threadIdx.x / 64][4 * quad + e] = sum[e];
+  }
+  __syncthreads();
+  const int64_t c = c0 + threadIdx.x;
+  if (threadIdx.x >= kJoinCols) return;
+  float total = part[0][threadIdx.x];
+#pragma unroll
+  for (int w = 1; w < kJoinThreads / 64; ++w) total += part[w][threadIdx.x];
+  if (c < cols) dweight[c] = total;
+  else if (dbias && c >= half && c < half + cols) dbias[c - half] = total;
+}
+
+// Threads of a row, groups of sixteen bytes of each, and workgroups: what the CUs hold at a time, so that a workgroup's rows
+// share one row of partial sums.  Narrow rows are a wave's, four to a workgroup, without a barrier.  us, the first launch alone: 16384 x 5120 bf16
+// with dsum (640 groups) 1024 x 1 (threads x groups) 155, 512 x 2 158, 128 x 5 145, 256 x 3 133, and in 256, 512, 768, 1024 workgroups > 160, 133,
+// 154, 140; 2999 x 1111 fp32 (278) 512 x 1 12.2, 256 x 2 10.8, 64 x 5 11.0, with half the rows of partial sums; 8192 x 768 bf16 (96) 256 x 1 17.2, 128 x 1 in
+// 2048 13.1, 64 x 2 in 512 13.7; 8192 x 4096 (512) 1024 x 1 71, 256 x 2 50.5, 512 x 1 49.9; 30000 x 256 (32) 128 x 1 28, 64 x 1 in 1024 17.4; 1000 x 8192
+// 512 x 2 in 256, 512 16.8, 21.4; 8192 x 1536 64 x 3 20.4, 256 x 1 in 512, 768, 1024 23.5, 20.1, 19.8.
+struct BackwardShape {
+  int threads, groups, workgroups;
+};
+BackwardShape backward_shape(int64_t rows, int64_t cols, int n) {
+  const int64_t g = (cols + n - 1) / n;
+  const auto at_most = [&](int most, int of_workgroup) {
+    return static_cast<int>(std::min<int64_t>(most, (rows + of_workgroup - 1) / of_workgroup));
+  };
+  if (g <= (n == 8 ? 192 : 320)) return {64, static_cast<int>((g + 63) / 64), at_most(g <= 64 ? 1024 : 512, 4)};
+  if (g <= 256) return {256, 1, at_most(768, 1)};
+  if (g <= 512) return {512, 1, at_most(512, 1)};
+  if (g <= 768) return {256, 3, at_most(512, 1)};
+  if (g <= 1024) return {512, 2, at_most(256, 1)};
+  if (g <= 2048) return {1024, 2, at_most(256, 1)};
+  return {kLongThreads, 0, at_most(512, 1)};
+}
+
 template <typename T, int NT, int V>
 hipError_t launch_backward(const LayerNormBackwardArgs& args, int workgroups, hipStream_t stream) {
   hipLaunchKernelGGL((layer_norm_backward_kernel<T, NT, V>), dim3(workgroups), dim3(RowGroup<NT>::kThreads), 0, stream, args);
@@ -355,16 +422,27 @@ hipError_t launch_backward(const LayerNormBackwardArgs& args, int workgroups, hi
 }
 
 template <typename T>
-hipError_t launch_backward_of(const LayerNormBackwardArgs& args, int workgroups, hipStream_t stream) {
-  constexpr int N = Group16<T>::N;
-  const int64_t n = args.cols;
-  if (n <= 64 * N) return launch_backward<T, 64, 1>(args, workgroups, stream);
-  if (n <= 128 * N && args.rows > 2048) return launch_backward<T, 64, 2>(args, workgroups, stream);
-  if (n <= 256 * N) return launch_backward<T, 256, 1>(args, workgroups, stream);
-  if (n <= 512 * N) return launch_backward<T, 512, 1>(args, workgroups, stream);
-  if (n <= 1024 * N) return launch_backward<T, 1024, 1>(args, workgroups, stream);
-  if (n <= 2048 * N) return launch_backward<T, 1024, 2>(args, workgroups, stream);
-  hipLaunchKernelGGL((layer_norm_backward_long_kernel<T>), dim3(workgroups), dim3(kLongThreads), 0, stream, args);
+hipError_t launch_backward_of(const LayerNormBackwardArgs& args, const BackwardShape& s, hipStream_t stream) {
+  switch (s.threads) {
+    case 64:
+      switch (s.groups) {
+        case 1: return launch_backward<T, 64, 1>(args, s.workgroups, stream);
+        case 2: return launch_backward<T, 64, 2>(args, s.workgroups, stream);
+        case 3: return launch_backward<T, 64, 3>(args, s.workgroups, stream);
+        default: break;
+      }
+      if constexpr (Group16<T>::N == 4)
+        return s.groups == 4 ? launch_backward<T, 64, 4>(args, s.workgroups, stream) : launch_backward<T, 64, 5>(args, s.workgroups, stream);
+      else
+        return hipErrorInvalidValue;   // (backward_shape gives bf16 three at most)
+    case 256:
+      return s.groups == 1 ? launch_backward<T, 256, 1>(args, s.workgroups, stream) : launch_backward<T, 256, 3>(args, s.workgroups, stream);
+    case 512:
+      return s.groups == 1 ? launch_backward<T, 512, 1>(args, s.workgroups, stream) : launch_backward<T, 512, 2>(args, s.workgroups, stream);
+    default: break;
+  }
+  if (s.groups == 2) return launch_backward<T, 1024, 2>(args, s.workgroups, stream);
+  hipLaunchKernelGGL((layer_norm_backward_long_kernel<T>), dim3(s.workgroups), dim3(kLongThreads), 0, stream, args);
   return hipGetLastError();
 }
 
@@ -395,14 +473,27 @@ hipError_t launch_layer_norm(const LayerNormArgs& args, int dtype, hipStream_t s
 }
 
 int layer_norm_partial_rows(int64_t rows, int64_t cols) {
-  const int64_t groups = cols <= 1024 ? 8192 : cols <= 2048 ? 1024 : 512;
-  const int64_t some = std::min(groups, rows <= 2048 ? rows : std::max<int64_t>((rows + 3) / 4, 2048));
-  return static_cast<int>(cols <= 1024 ? (some + 3) / 4 : std::min<int64_t>(some, groups));
+  return std::max(backward_shape(rows, cols, 4).workgroups, backward_shape(rows, cols, 8).workgroups);
 }
 
-hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int dtype, int partial_rows, hipStream_t stream) {
-  return dtype == CLEAVE_BF16 ? launch_backward_of<Bf16>(args, partial_rows, stream)
-                              : launch_backward_of<float>(args, partial_rows, stream);
+hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int dtype, hipStream_t stream) {
+  const bool bf16 = dtype == CLEAVE_BF16;
+  const BackwardShape s = backward_shape(args.rows, args.cols, bf16 ? 8 : 4);
+  if (args.rows > 0) {
+    const hipError_t e = bf16 ? launch_backward_of<Bf16>(args, s, stream) : launch_backward_of<float>(args, s, stream);
+    if (e != hipSuccess) return e;
+  }
+  // (no rows: zeros; a launch has fewer than 2^32 threads)
+  constexpr int64_t kLaunchCols = int64_t{1} << 27;
+  const int64_t all = args.dbias ? 2 * padded(args.cols) : args.cols;
+  for (int64_t c = 0; c < all; c += kLaunchCols) {
+    const dim3 g(static_cast<uint32_t>((std::min(all - c, kLaunchCols) + kJoinCols - 1) / kJoinCols));
+    hipLaunchKernelGGL(layer_norm_join_kernel, g, dim3(kJoinThreads), 0, stream, args.partials, s.workgroups, c, args.cols, args.dweight,
+                       args.dbias);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace cleave

@@ -362,10 +362,9 @@ hipError_t launch_sum(const ColumnSumArgs& args, hipStream_t stream) {
 }
 
 // The rows of partial sums: sixteen columns to a workgroup and 64 rows at a time, so that a few hundred rows are a few loads
-// of each thread.  Columns from `split` on go to the second output.
+// of each thread.
 constexpr int kJoinThreads = 1024, kJoinCols = 16;
-__global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in, int rows, int64_t ld, int64_t cols, float* out,
-                                                                 int64_t split, float* second) {
+__global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in, int rows, int64_t ld, int64_t cols, float* out) {
   constexpr int kRows = kJoinThreads / kJoinCols;
   __shared__ float part[kJoinThreads / 64][kJoinCols];
   const int at = threadIdx.x % kJoinCols, first = threadIdx.x / kJoinCols;
@@ -384,8 +383,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const float* in
   sum = part[0][at];
 #pragma unroll
   for (int w = 1; w < kJoinThreads / 64; ++w) sum += part[w][at];
-  if (c < split) out[c] = sum;
-  else second[c - split] = sum;
+  out[c] = sum;
 }
 
 }  // namespace
@@ -432,15 +430,11 @@ int column_sum_chunks(int64_t rows, int64_t cols) {
   return static_cast<int>(std::max<int64_t>(1, std::min({want, (rows + 31) / 32, int64_t{256}})));
 }
 
-hipError_t launch_join_rows(const float* rows, int n, int64_t ld, int64_t cols, float* out, hipStream_t stream, float* second) {
-  const int64_t all = second ? 2 * cols : cols;
-  for (int64_t c = 0; c < all; c += kLaunchCols) {
-    const int64_t some = std::min(all - c, kLaunchCols);
-    // (out is indexed by columns below the split only, the second output by those from it on)
-    const int64_t split = std::max<int64_t>(cols - c, 0);
+hipError_t launch_join_rows(const float* rows, int n, int64_t cols, float* out, hipStream_t stream) {
+  for (int64_t c = 0; c < cols; c += kLaunchCols) {
+    const int64_t some = std::min(cols - c, kLaunchCols);
     hipLaunchKernelGGL(join_rows_kernel, dim3(static_cast<uint32_t>((some + kJoinCols - 1) / kJoinCols)), dim3(kJoinThreads), 0,
-                       stream, rows + c, n, ld, some, split > 0 ? out + c : out, split,
-                       second ? second + std::max<int64_t>(c - cols, 0) : second);
+                       stream, rows + c, n, cols, some, out + c);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -450,7 +444,7 @@ hipError_t launch_join_rows(const float* rows, int n, int64_t ld, int64_t cols, 
 hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, hipStream_t stream) {
   const hipError_t e = dtype == CLEAVE_BF16 ? launch_sum<Bf16, 4>(args, stream) : launch_sum<float, 4>(args, stream);
   if (e != hipSuccess || args.chunks == 1) return e;
-  return launch_join_rows(args.partials, args.chunks, args.cols, args.cols, args.out, stream);
+  return launch_join_rows(args.partials, args.chunks, args.cols, args.out, stream);
 }
 
 }  // namespace cleave

@@ -99,7 +99,7 @@ extern "C" int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* 
     const cleave::NormBackwardArgs args{dy, h, dsum, weight, inv_rms, dx, workspace, rows, cols, lddy, ldh, ldds, lddx};
     CLEAVE_HIP(cleave::launch_rms_norm_backward(args, dtype, partial_rows, stream));
   }
-  CLEAVE_HIP(cleave::launch_join_rows(workspace, partial_rows, cols, cols, dweight, stream));   // no rows: zeros
+  CLEAVE_HIP(cleave::launch_join_rows(workspace, partial_rows, cols, dweight, stream));   // no rows: zeros
   return CLEAVE_OK;
 }
 
@@ -133,7 +133,7 @@ extern "C" int cleave_layer_norm(int64_t rows, int64_t cols, const void* x, int6
 
 extern "C" int64_t cleave_layer_norm_workspace(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 1 || rows > kMost || cols > kMost) return CLEAVE_EINVAL;
-  return 2 * cols * std::max(1, cleave::layer_norm_partial_rows(rows, cols));
+  return (cols + 3) / 4 * 8 * std::max(1, cleave::layer_norm_partial_rows(rows, cols));
 }
 
 extern "C" int cleave_layer_norm_backward(int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* h, int64_t ldh,
@@ -156,13 +156,9 @@ extern "C" int cleave_layer_norm_backward(int64_t rows, int64_t cols, const void
   if (!in_place(dx, lddx, dtype, dy, lddy, dtype, rows) || !in_place(dx, lddx, dtype, h, ldh, dtype, rows) ||
       !in_place(dx, lddx, dtype, dsum, ldds, dtype, rows))
     return CLEAVE_EINVAL;
-  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const int partial_rows = cleave::layer_norm_partial_rows(rows, cols);
-  if (rows > 0) {
-    const cleave::LayerNormBackwardArgs args{dy, h, dsum, weight, mean, inv_std, dx, workspace, rows, cols, lddy, ldh, ldds, lddx};
-    CLEAVE_HIP(cleave::launch_layer_norm_backward(args, dtype, partial_rows, stream));
-  }
-  CLEAVE_HIP(cleave::launch_join_rows(workspace, partial_rows, 2 * cols, cols, dweight, stream, dbias));   // no rows: zeros
+  const cleave::LayerNormBackwardArgs args{dy, h,       dsum,  weight, mean, inv_std, dx,   workspace,
+                                           dweight, dbias, rows,   cols, lddy,    ldh, ldds, lddx};
+  CLEAVE_HIP(cleave::launch_layer_norm_backward(args, dtype, static_cast<hipStream_t>(hip_stream)));
   return CLEAVE_OK;
 }
 

@@ -59,7 +59,7 @@ struct LayerNormArgs {
 };
 hipError_t launch_layer_norm(const LayerNormArgs& args, int dtype, hipStream_t stream);
 
-// Rows of partial sums (each 2 cols floats: the weight's, then the bias's) that the gradient's first launch leaves.
+// Rows of partial sums (the weight's, then the bias's, each in whole quads) that the gradient's first launch leaves for its second, at most.
 int layer_norm_partial_rows(int64_t rows, int64_t cols);
 struct LayerNormBackwardArgs {
   const void* dy;
@@ -69,11 +69,13 @@ struct LayerNormBackwardArgs {
   const float* mean;
   const float* inv_std;
   void* dx;
-  float* partials;         // layer_norm_partial_rows x 2 cols
+  float* partials;         // layer_norm_partial_rows rows
+  float* dweight;
+  float* dbias;            // null: none
   int64_t rows, cols;
   int64_t lddy, ldh, ldds, lddx;
 };
-hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int dtype, int partial_rows, hipStream_t stream);
+hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int dtype, hipStream_t stream);
 
 // ---- sums of columns ---------------------------------------------------------
 
@@ -88,9 +90,8 @@ struct ColumnSumArgs {
 };
 // Chunks of rows that are summed apart.
 int column_sum_chunks(int64_t rows, int64_t cols);
-// out[c] = sum of `n` rows of partial sums, `ld` floats apart; a second output gets those of the next `cols` columns.
-hipError_t launch_join_rows(const float* rows, int n, int64_t ld, int64_t cols, float* out, hipStream_t stream,
-                            float* second = nullptr);
+// out[c] = sum of `n` contiguous rows of partial sums.
+hipError_t launch_join_rows(const float* rows, int n, int64_t cols, float* out, hipStream_t stream);
 hipError_t launch_column_sum(const ColumnSumArgs& args, int dtype, hipStream_t stream);
 
 // ---- log probabilities of tokens ---------------------------------------------

@@ -50,4 +50,4 @@ def test_backward(change):
 def test_workspace():
     assert workspace(-1, 8) == EINVAL and workspace(8, 0) == EINVAL and workspace(2 ** 31, 8) == EINVAL and workspace(8, 2 ** 31) == EINVAL
     for rows, cols in ((0, 8), (1, 1), (5000, 4096), (2 ** 31 - 1, 2 ** 31 - 1)):
-        assert workspace(rows, cols) >= 2 * cols and workspace(rows, cols) % (2 * cols) == 0
+        assert workspace(rows, cols) >= 2 * cols and workspace(rows, cols) % 8 == 0
