@@ -10,7 +10,10 @@
 // Gradient, with the stored h, m and i, g = dy w and xhat = (h - m) i:
 //   dx = i (g - mean(g) - xhat mean(g xhat)) + dsum;   dw = sum over rows of dy xhat;   db = sum over rows of dy
 //
-// Bound by memory: every row is read once and kept in registers between its statistics, the scaling and the rounding.
+// Bound by memory: every row is read once and kept in registers between its statistics, the scaling and the rounding.  A copy of
+// 512 MB runs at 5.4 TB/s here.  bf16 with a residual, the sum stored: 8192 x 768 11.9 us (4.2 TB/s), 4096 x 4096 22.0 (from the caches), 16384 x 5120
+// 129 (5.2), into e4m3 118 (5.0); 1 x 4096 into e4m3 5.6, a launch; gradient with dsum and both launches 16384 x 5120 135 us (5.0 TB/s), fp32 2999 x
+// 1111 14.7 (2.7).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -37,20 +40,25 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
   const T* r = static_cast<const T*>(args.residual) + (args.residual ? row * args.ldr : 0);
   T* sum_out = static_cast<T*>(args.sum_out) + (args.sum_out ? row * args.lds : 0);
   const int cols = static_cast<int>(args.cols);
-  const float count = static_cast<float>(cols);
+  const float part = 1.0f / static_cast<float>(cols);
   const auto at = [&](int j) { return (j * NT + t) * N; };
 
+  // The weight and the bias of a thread's columns are on their way with the row where there are registers for them.
+  constexpr bool EARLY = V * N <= 16;
   Raw16 x_raw[V], r_raw[V];
-  Floats16<N> w_raw[V], b_raw[V];
+  [[maybe_unused]] Floats16<N> w_raw[V], b_raw[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     x_raw[j] = G::read(x + at(j), cols - at(j));
     if (args.residual) r_raw[j] = G::read(r + at(j), cols - at(j));
   }
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
+  const auto read_weights = [&](int j) {
     w_raw[j].read(args.weight + at(j), cols - at(j));
     if (args.bias) b_raw[j].read(args.bias + at(j), cols - at(j));
+  };
+  if constexpr (EARLY) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) read_weights(j);
   }
   float h[V][N];
 #pragma unroll
@@ -73,7 +81,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
 #pragma unroll
     for (int j = 0; j < V; ++j) G::store(sum_out + at(j), cols - at(j), h[j]);
   }
-  const float first = group_sum<NW>(sum, slots[0]) / count;
+  const float first = group_total<NW>(sum, slots[0]) * part;
   float rest = 0.0f, squares = 0.0f;
 #pragma unroll
   for (int j = 0; j < V; ++j)
@@ -83,9 +91,9 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
       rest += h[j][e];
       squares += h[j][e] * h[j][e];
     }
-  group_sums<NW>(rest, squares, slots[1]);
-  rest /= count;
-  const float var = squares / count - rest * rest;
+  group_totals<NW>(rest, squares, slots[1]);
+  rest *= part;
+  const float var = squares * part - rest * rest;
   const float inv = 1.0f / __builtin_sqrtf((var < 0.0f ? 0.0f : var) + args.eps);   // (NaN stays)
   if (t == 0) {
     if (args.mean) args.mean[row] = first + rest;
@@ -94,6 +102,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     float w[N], b[N] = {};
+    if constexpr (!EARLY) read_weights(j);
     w_raw[j].unpack(w);
     if (args.bias) b_raw[j].unpack(b);
 #pragma unroll
@@ -136,14 +145,14 @@ __global__ __launch_bounds__(kLongThreads) void layer_norm_long_kernel(LayerNorm
   const auto at = [&](int64_t c) { return args.residual ? element(x + c) + element(r + c) : element(x + c); };
   float sum = 0.0f;
   for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) sum += at(c);
-  const float first = group_sum<NW>(sum, slots[0]) / count;
+  const float first = group_total<NW>(sum, slots[0]) / count;
   float rest = 0.0f, squares = 0.0f;
   for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
     const float d = at(c) - first;
     rest += d;
     squares += d * d;
   }
-  group_sums<NW>(rest, squares, slots[1]);
+  group_totals<NW>(rest, squares, slots[1]);
   rest /= count;
   const float var = squares / count - rest * rest;
   const float inv = 1.0f / __builtin_sqrtf((var < 0.0f ? 0.0f : var) + args.eps);
@@ -190,12 +199,15 @@ hipError_t launch_norm_fit(const LayerNormArgs& args, int64_t v, hipStream_t str
   return launch_norm<T, NT, V>(args, stream);
 }
 
-// Which threads share a row: as for the root-mean-square norm (norm.hip).
+// Which threads share a row: a wave where it holds a narrow one and there are many, as few more as hold a wider one, many for few rows,
+// whose latency counts.  us, threads x groups, bf16 with a residual: 8192 x 768 64 x 2 11.9, 128 x 1 12.1, 256 x 1 17.2; 16384 x 5120 into 8
+// bits 64 x 10 192, 128 x 5 125, 256 x 3 118, 512 x 2 137, 1024 x 1 185, into bf16 154, 134, 129, 125, 149; 4096 x 4096 128 x 4 23.0, 256 x 2 21.9,
+// 1024 x 1 33; 20000 x 1000 fp32 64 x 4 65, 256 x 1 58; 200 x 9000 256 x 5 7.1, 1024 x 2 6.6; 1 x 768 64 x 2 5.6, 1024 x 1 4.3.
 template <typename T>
 hipError_t launch_norm_of(const LayerNormArgs& args, hipStream_t stream) {
   const int64_t groups = (args.cols + Group16<T>::N - 1) / Group16<T>::N;
   if (groups <= 64) return launch_norm<T, 64, 1>(args, stream);
-  if (groups <= 4 * 64 && args.rows > 1024) return launch_norm_fit<T, 64, 4>(args, (groups + 63) / 64, stream);
+  if (groups <= 3 * 64 && args.rows > 1024) return launch_norm_fit<T, 64, 3>(args, (groups + 63) / 64, stream);
   if (groups <= 8 * 256 && args.rows > 256) return launch_norm_fit<T, 256, 8>(args, (groups + 255) / 256, stream);
   if (groups <= 4 * 1024) return launch_norm_fit<T, 1024, 4>(args, (groups + 1023) / 1024, stream);
   const dim3 g(static_cast<uint32_t>(args.rows)), b(kLongThreads);
@@ -277,7 +289,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
         dot += g[j][e] * xhat[j][e];
       }
     // (the slots of the row before last are free: every wave has passed the barrier of the last one)
-    group_sums<NW>(sum, dot, slots[turn]);
+    group_totals<NW>(sum, dot, slots[turn]);
     sum /= count;
     dot /= count;
     T* dx = static_cast<T*>(args.dx) + row * args.lddx;
@@ -345,7 +357,7 @@ __global__ __launch_bounds__(kLongThreads) void layer_norm_backward_long_kernel(
       sum += g;
       dot += g * x;
     }
-    group_sums<NW>(sum, dot, slots[turn]);
+    group_totals<NW>(sum, dot, slots[turn]);
     sum /= count;
     dot /= count;
     for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {

@@ -284,14 +284,17 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
   }
   if (rest) take(next, g, yes);
 
-  Stats all = own;
+  // the wave's, then the waves'
+  const float of_wave = wave_join(own.m, [](float a, float b) { return __builtin_fmaxf(a, b); });
+  if (own.m != of_wave) move_to(own, of_wave, c);
+  Stats all{of_wave, wave_total(own.s), ENTROPY ? wave_total(own.w) : 0.0f};
+  if constexpr (NW > 1) {
+    if ((t & 63) == 0) slots[t >> 6] = all;
+    __syncthreads();
+    all = slots[0];
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) all = join(all, {__shfl_xor(all.m, d), __shfl_xor(all.s, d), __shfl_xor(all.w, d)}, c);
-  if ((t & 63) == 0) slots[t >> 6] = all;
-  __syncthreads();
-  all = slots[0];
-#pragma unroll
-  for (int w = 1; w < NW; ++w) all = join(all, slots[w], c);
+    for (int w = 1; w < NW; ++w) all = join(all, slots[w], c);
+  }
   const float log_s = __builtin_logf(all.s);
   float* record = args.workspace + static_cast<int64_t>(blockIdx.x) * record_floats(args.n_top);
   if (t == 0) {

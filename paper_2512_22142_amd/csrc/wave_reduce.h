@@ -35,15 +35,35 @@ template <int NW>
 __device__ __forceinline__ float group_sum(float x, float* slots) {
   return join_waves<NW>(wave_sum(x), slots, [](float a, float b) { return a + b; });
 }
+// The same sums across lanes without LDS: rows of sixteen lanes by DPP, the four rows through scalar registers.  (In another order than
+// wave_sum: kernels keep the one that they have.)
+template <int CTRL>
+__device__ __forceinline__ float dpp_of(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lane_of(float x, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+template <typename Join>
+__device__ __forceinline__ float wave_join(float x, Join join) {
+  x = join(x, dpp_of<0xb1>(x));    // quad_perm 1 0 3 2
+  x = join(x, dpp_of<0x4e>(x));    // quad_perm 2 3 0 1
+  x = join(x, dpp_of<0x141>(x));   // row_half_mirror
+  x = join(x, dpp_of<0x140>(x));   // row_mirror
+  return join(join(lane_of(x, 0), lane_of(x, 16)), join(lane_of(x, 32), lane_of(x, 48)));
+}
+__device__ __forceinline__ float wave_total(float x) {
+  return wave_join(x, [](float a, float b) { return a + b; });
+}
+template <int NW>
+__device__ __forceinline__ float group_total(float x, float* slots) {
+  return join_waves<NW>(wave_total(x), slots, [](float a, float b) { return a + b; });
+}
 // Two sums behind one barrier; 2 NW slots.
 template <int NW>
-__device__ __forceinline__ void group_sums(float& x, float& y, float* slots) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    const float a = __shfl_xor(x, d), b = __shfl_xor(y, d);
-    x += a;
-    y += b;
-  }
+__device__ __forceinline__ void group_totals(float& x, float& y, float* slots) {
+  x = wave_total(x);
+  y = wave_total(y);
   if constexpr (NW > 1) {
     if ((threadIdx.x & 63) == 0) {
       slots[threadIdx.x >> 6] = x;
