@@ -1470,6 +1470,20 @@ hipError_t pack_operands(Operands& o, int weights, int64_t M, int64_t N, int64_t
   return cleave::launch_pack(args, stream);
 }
 
+// Splits of K for few rows: a workgroup has 64 columns of both weights, so up to 128 of them leave CUs without one; where a
+// row of K has 4 KB or more they are split, to one per CU, and joined by a second launch.  (`k` elements of `bytes`: pairs of e4m3.)  One row, bf16,
+// weights from memory, us, 1, 2, 4, 8 splits: 4096 x 4096 26, 21, 18.7, 19.5, 11008 x 4096 58, 47, 38.3, 39.8, 2048 x 5632 21, 16.1, 17.1, 15.6,
+// 8192 x 8192 76, 51.6, 53.7, 54.7; as they are 4096 x 11008 36.1, 40, 36.9, 38.5, 5120 x 13824 54.4, 61, 62, 58.0, 1024 x 12000 13.9, 17.8, 18.0,
+// 19, 768 x 2048 7.1, 9.3, 9.2, 10.
+int64_t gated_few_splits(int64_t N, int64_t k, int64_t bytes) {
+  constexpr int64_t kCUs = 256;
+  const int64_t groups = (N + 63) / 64;
+  if (groups > kCUs / 2 || k * bytes < 4096) return 1;
+  for (int64_t S = std::min<int64_t>({kCUs / groups, k * bytes / 512, 16}); S > 1; --S)
+    if ((S - 1) * ((k + S - 1) / S) < k) return S;
+  return 1;
+}
+
 bool floats_aligned(const float* const* list, int n) {
   for (int k = 0; k < n; ++k)
     if (!aligned(list[k], 4)) return false;
@@ -1499,8 +1513,8 @@ extern "C" int cleave_plan_gated(int64_t M, int64_t N, int64_t K, int dtype, cle
   const int64_t k = pairs ? K / 2 : K;
   const bool few = gated_few_rows(M, N);
   // tiles and splits as for one product of both operands' columns; 8-bit operands with more than a few rows are not split
-  // (a workgroup of few rows has 64 columns of both)
-  const int64_t splits = pairs && !few ? 1 : linear_splits(M, few ? N : 2 * N, k, dtype == CLEAVE_F32 ? 4 : 8, pairs);
+  const int64_t splits = few ? gated_few_splits(N, k, dtype == CLEAVE_F32 ? 4 : 2)
+                         : pairs ? 1 : linear_splits(M, 2 * N, k, dtype == CLEAVE_F32 ? 4 : 8, false);
   const int64_t tile = M <= cleave::kFewRows ? cleave::kSmallTileRows
                        : dtype == CLEAVE_F32 && splits > 1 && fp32_splits(M, 2 * N, K).workgroups > 128 ? 64
                                                                                                        : cleave::kLargeTileRows;

@@ -235,6 +235,15 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(ExecuteArgs args, 
 template <int DTYPE, bool B_K, typename Epi>
 hipError_t launch_layout(const ExecuteArgs& args, const Epi& epi, int splits, int64_t chunk, hipStream_t stream) {
   const dim3 g(static_cast<uint32_t>((args.N + kColumns - 1) / kColumns), splits);
+  if constexpr (std::is_same<Epi, GatedArgs>::value) {
+    // One row, bf16, weights from memory, us, 4, 8, 16 waves: stored K x N, unsplit, 4096 x 11008 39, 36.1, 37.4, 5120 x 13824 60, 54.4, 55.8,
+    // 2048 x 16384 33, 25.3, 26.2 (N x K 33, 30.5, 28.6; 1024 x 12000 14.5, 13.3, 13.2); in 4 splits 4096 x 4096 23, 18.7, 19.3,
+    // 11008 x 4096 46, 38.3, 38.7, in 2 8192 x 8192 64, 51.6, 52.9.
+    constexpr int kWhole = B_K ? 16 : 8;
+    if (splits > 1) hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 8, Epi>), g, dim3(512), 0, stream, args, epi, splits, chunk);
+    else hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, kWhole, Epi>), g, dim3(64 * kWhole), 0, stream, args, epi, splits, chunk);
+    return hipGetLastError();
+  }
   if (splits > 1) hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 4, Epi>), g, dim3(256), 0, stream, args, epi, splits, chunk);
   else hipLaunchKernelGGL((few_rows_kernel<DTYPE, B_K, 16, Epi>), g, dim3(1024), 0, stream, args, epi, splits, chunk);
   return hipGetLastError();
