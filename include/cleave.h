@@ -524,7 +524,7 @@ int cleave_linear(cleave_plan* plan, const cleave_linear_args* args, void* hip_s
  * alone while it runs.  whole = 1 serves bf16 calls of which A, B_gate and B_up lie on 16-byte boundaries, K, lda and ldb are
  * multiples of 8, N too with transB = 0, and lda and ldb are below 2^21; whole = 0 serves all.  (8-bit operands: either.)
  * Few rows (M <= 16) read the weights as fast as memory gives them.  Bits, upload, streams: as for cleave_linear.
- * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, two outputs in one place, partials missing,
+ * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, an output in another one's or in an operand's place, partials missing,
  * a plan of another kind or type. */
 typedef struct {
   const void* A;
@@ -590,8 +590,8 @@ int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, int64_t ld,
 /* Its gradient, from the logits and the lse (and entropy) that it left:
  *   dlogits_j = scale (dlogp (1[j = id] - p_j) - dentropy p_j (log p_j + entropy))
  * ids and dlogp (rows floats; a row without a token gets none of it), entropy and dentropy: each pair or neither, one of the two
- * at least.  p is as good as the fp32 lse: to 2^-24 |lse| of itself.  Rows whose logits are all minus infinity get zeros, as masked
- * tokens do.  dlogits: rows x cols of dtype; may be logits, with its leading dimension.  (Cross-entropy averaged over n tokens:
+ * at least.  p is as good as the fp32 lse: to 2^-24 |lse| of itself.  Rows whose lse is below -1e30 (nothing but masked tokens, by minus
+ * infinity or by the type's lowest value) get zeros, as masked tokens do.  A row whose id is beyond it is NaN.  dlogits: rows x cols of dtype; may be logits, with its leading dimension.  (Cross-entropy averaged over n tokens:
  * dlogp = -1 / n.)  CLEAVE_EINVAL as above. */
 int cleave_log_probs_backward(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype,
                               float scale, const int64_t* ids, const float* lse, const float* dlogp,

@@ -1561,6 +1561,8 @@ extern "C" int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* a
       !aligned(a->up, ob) || !floats_aligned(vectors, 6))
     return CLEAVE_EINVAL;
   if (a->C == a->gate || a->C == a->up || (a->gate && a->gate == a->up)) return CLEAVE_EINVAL;   // outputs in one place
+  for (const void* out : {static_cast<const void*>(a->C), static_cast<const void*>(a->gate), static_cast<const void*>(a->up)})
+    if (out && (out == a->A || out == a->B_gate || out == a->B_up)) return CLEAVE_EINVAL;
   if (e4m3 && (!a->transB || !aligned(a->A, 16) || !aligned(a->B_gate, 16) || !aligned(a->B_up, 16) || a->lda % 16 || a->ldb % 16 ||
                a->lda >= int64_t{1} << 22 || a->ldb >= int64_t{1} << 22))
     return CLEAVE_EINVAL;
@@ -1657,7 +1659,8 @@ extern "C" int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_gr
       !aligned(a->dup, ob) || !aligned(a->partials, 4))
     return CLEAVE_EINVAL;
   // in place: each over its own argument, the same elements at the same places
-  if (a->dgate == a->dup || a->dgate == a->up || a->dup == a->gate ||
+  if (a->dgate == a->dup || a->dgate == a->up || a->dup == a->gate || a->dgate == a->A || a->dgate == a->B || a->dup == a->A ||
+      a->dup == a->B ||
       (a->dgate == a->gate && M > 1 && a->ld_dgate != a->ld_gate) || (a->dup == a->up && M > 1 && a->ld_dup != a->ld_up))
     return CLEAVE_EINVAL;
   cleave::GatedArgs epi{};

@@ -440,7 +440,8 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void log_probs_backward_ker
     raw[u] = G::read(x + at, max(cols - at, 0));
   }
   const float given = args.lse[row];
-  const bool none = given == -kInf;          // nothing left: no token has any of it
+  // Nothing left but masked tokens, by minus infinity or by the type's lowest value (of which lse holds no sum): none has any of it.
+  const bool none = given < -1e30f;
   const float lse = none ? kInf : given;
   float d = 0.0f, dh = 0.0f, h = 0.0f;
   int64_t id = -1;

@@ -211,7 +211,7 @@ extern "C" int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, 
   if (!m.ok || cols > kMostTokens || !aligned(ids, 8) || !aligned(top_ids, 8)) return CLEAVE_EINVAL;
   if ((ids != nullptr) != (logp != nullptr) || n_top < 0 || n_top > cols) return CLEAVE_EINVAL;
   if (n_top > cleave::kMostTop) return CLEAVE_ELIMIT;
-  if ((n_top > 0) != (top_ids != nullptr) || (n_top > 0) != (top_logp != nullptr)) return CLEAVE_EINVAL;
+  if ((n_top > 0) != (top_ids != nullptr) || (n_top > 0) != (top_logp != nullptr) || (ids && ids == top_ids)) return CLEAVE_EINVAL;
   if ((logp && (logp == lse || logp == entropy || logp == top_logp)) || (lse && (lse == entropy || lse == top_logp)) ||
       (entropy && entropy == top_logp))
     return CLEAVE_EINVAL;

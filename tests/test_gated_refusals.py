@@ -70,7 +70,7 @@ def test_workspace():
     dict(A=None), dict(B_gate=None), dict(B_up=None), dict(C=None), dict(lda=511), dict(ldb=511), dict(ldc=199), dict(ld_gate=199),
     dict(ld_up=199), dict(transB=2), dict(dtype=7), dict(out_dtype=E4M3), dict(act=-1), dict(act=4), dict(C=4 * P + 1), dict(gate=P + 1),
     dict(bias_gate=P + 2), dict(bias_up=P + 1), dict(partials=P + 2), dict(gate=4 * P), dict(up=4 * P), dict(up=5 * P),
-    dict(transB=0, ldb=199), dict(scale_gate="other"), dict(scale_a="other")])
+    dict(transB=0, ldb=199), dict(scale_gate="other"), dict(scale_a="other"), dict(C=P), dict(gate=2 * P), dict(up=3 * P)])
 def test_gated(dtype, change):
     plan = gated_plan(300, 200, 512, dtype)
     a = Args(A=P, B_gate=2 * P, B_up=3 * P, C=4 * P, gate=5 * P, up=6 * P, bias_gate=7 * P, bias_up=8 * P, partials=9 * P, lda=512, ldb=512,
@@ -111,7 +111,7 @@ def test_gated_without_a_workspace():
     dict(A=None), dict(B=None), dict(gate=None), dict(up=None), dict(dgate=None), dict(dup=None), dict(lda=511), dict(ldb=511),
     dict(ld_gate=199), dict(ld_up=199), dict(ld_dgate=199), dict(ld_dup=199), dict(transB=2), dict(dtype=E4M3), dict(out_dtype=E4M3),
     dict(act=4), dict(gate=P + 1), dict(dup=P + 1), dict(partials=P + 2), dict(dup=5 * P), dict(dgate=4 * P), dict(dup=3 * P),
-    dict(dgate=3 * P, ld_dgate=208), dict(dup=4 * P, ld_up=208), dict(A=P + 2, partials=None)])
+    dict(dgate=3 * P, ld_dgate=208), dict(dup=4 * P, ld_up=208), dict(A=P + 2, partials=None), dict(dgate=P), dict(dup=2 * P)])
 def test_grad(change):
     plan = made(300, 200, 512, BF16)
     a = GradArgs(A=P, B=2 * P, gate=3 * P, up=4 * P, dgate=5 * P, dup=6 * P, partials=7 * P, lda=512, ldb=512, ld_gate=200, ld_up=200,
@@ -134,3 +134,13 @@ def test_plans_of_other_calls():
                 setattr(a, name, 200)
         assert call(plan, ctypes.byref(a), None) == EINVAL
         lib.cleave_plan_destroy(plan)
+
+
+def test_other_calls_of_a_gated_plan_of_8_bit_operands():
+    plan = gated_plan(300, 200, 512, E4M3)
+    lists = ctypes.cast((p * 2)(P, 2 * P), p)
+    execute = declare("cleave_execute_grouped", [p, p, i64, i64, p, i64, c_int, p, i64, c_int, c_int, p, p])
+    reduce = declare("cleave_reduce_grouped", [p, p, i64, p, i64, c_int, p])
+    assert execute(plan, None, 0, 2, lists, 512, 0, lists, 512, 1, BF16, P, None) == EINVAL
+    assert reduce(plan, P, 2, lists, 200, F32, None) == EINVAL
+    lib.cleave_plan_destroy(plan)

@@ -307,6 +307,21 @@ def test_backward_of_masks(kind, dtype):
         assert torch.all(out[gone & ~hot] == 0)
 
 
+def test_backward_of_rows_without_a_token_left_and_of_tokens_beyond_the_row():
+    for dtype in (F32, BF16):
+        x = matrix(4, 1000, dtype, 1)[0].clone()
+        x[0], x[1] = -INF, torch.finfo(dtype).min
+        ids = torch.tensor([3, 4, 1000, -5], device="cuda")
+        logp, lse, ent = (torch.empty(4, device="cuda") for _ in range(3))
+        cleave.log_probs(x, ids, logp, lse=lse, entropy=ent)
+        d = torch.ones(4, device="cuda")
+        dx = torch.empty_like(x)
+        cleave.log_probs_backward(x, lse, dx, ids=ids, dlogp=d, entropy=ent, dentropy=d)
+        assert torch.all(dx[:2] == 0) and torch.all(dx[2].isnan()) and torch.all(dx[3].isfinite()) and torch.any(dx[3] != 0)
+        cleave.log_probs_backward(x, lse, dx, ids=ids, dlogp=d)
+        assert torch.all(dx[3] == 0)
+
+
 def test_backward_against_differences_of_the_kernel():
     rows, cols, step = 3, 50, 1.0 / 64
     x, u = matrix(rows, cols, F32, 1)[0].contiguous(), matrix(rows, cols, F32, 2, std=1.0)[0].contiguous()

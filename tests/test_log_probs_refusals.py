@@ -19,7 +19,7 @@ CALL = dict(rows=0, cols=100, x=P, ld=100, dtype=BF16, scale=1.0, ids=2 * P, log
     dict(dtype=5), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan), dict(ids=None), dict(logp=None),
     dict(n=-1), dict(n=0), dict(top=None), dict(tl=None), dict(n=20, cols=19), dict(x=P + 1), dict(ids=P + 4), dict(top=P + 4),
     dict(logp=P + 2), dict(lse=P + 2), dict(ent=P + 1), dict(tl=P + 2), dict(ws=P + 2), dict(dtype=F32, x=P + 2), dict(lse=3 * P),
-    dict(ent=3 * P), dict(tl=3 * P), dict(ent=4 * P), dict(tl=4 * P), dict(tl=5 * P)])
+    dict(ent=3 * P), dict(tl=3 * P), dict(ent=4 * P), dict(tl=4 * P), dict(tl=5 * P), dict(top=2 * P)])
 def test_log_probs(change):
     assert call(log_probs, CALL) == OK
     assert call(log_probs, CALL, ids=None, logp=None, lse=None, ent=None, n=0, top=None, tl=None) == OK
