@@ -239,6 +239,7 @@ int ensure_uploaded(cleave_plan* p) {
   int rc = ensure_device_ready(dev, nullptr);
   if (rc == CLEAVE_OK && p->linear) rc = ensure_linear_ready(dev);
   if (rc == CLEAVE_OK && p->gated) rc = ensure_gated_ready(dev);
+  if (rc == CLEAVE_OK && p->gated && p->pairs && p->uniform_splits > 1) rc = ensure_linear_ready(dev);
   if (rc != CLEAVE_OK) return rc;
   rc = upload_vector(p->tasks, &p->d_tasks);
   hipStream_t writing = nullptr;
@@ -1471,14 +1472,15 @@ hipError_t pack_operands(Operands& o, int weights, int64_t M, int64_t N, int64_t
 }
 
 // Splits of K for few rows: a workgroup has 64 columns of both weights, so up to 128 of them leave CUs without one; where a
-// row of K has 4 KB or more they are split, to one per CU, and joined by a second launch.  (`k` elements of `bytes`: pairs of e4m3.)  One row, bf16,
+// row of K has 2 KB or more they are split, to one per CU, and joined by a second launch.  (`k` elements of `bytes`: pairs of e4m3.)  One row, bf16,
 // weights from memory, us, 1, 2, 4, 8 splits: 4096 x 4096 26, 21, 18.7, 19.5, 11008 x 4096 58, 47, 38.3, 39.8, 2048 x 5632 21, 16.1, 17.1, 15.6,
 // 8192 x 8192 76, 51.6, 53.7, 54.7; as they are 4096 x 11008 36.1, 40, 36.9, 38.5, 5120 x 13824 54.4, 61, 62, 58.0, 1024 x 12000 13.9, 17.8, 18.0,
-// 19, 768 x 2048 7.1, 9.3, 9.2, 10.
+// 19, 768 x 2048 7.1, 9.3, 9.2, 10.  From the caches, one / as here (4 to 7): 1024 x 64 6.9 / 6.6, 1024 x 4096 8.8 / 9.3 (stored N x K 10.9 / 9.3),
+// 1408 x 1062 10.9 / 9.4, 2016 x 2048 13.4 / 10.3.
 int64_t gated_few_splits(int64_t N, int64_t k, int64_t bytes) {
   constexpr int64_t kCUs = 256;
   const int64_t groups = (N + 63) / 64;
-  if (groups > kCUs / 2 || k * bytes < 4096) return 1;
+  if (groups > kCUs / 2 || k * bytes < 2048) return 1;
   for (int64_t S = std::min<int64_t>({kCUs / groups, k * bytes / 512, 16}); S > 1; --S)
     if ((S - 1) * ((k + S - 1) / S) < k) return S;
   return 1;
@@ -1513,8 +1515,10 @@ extern "C" int cleave_plan_gated(int64_t M, int64_t N, int64_t K, int dtype, cle
   const int64_t k = pairs ? K / 2 : K;
   const bool few = gated_few_rows(M, N);
   // tiles and splits as for one product of both operands' columns; 8-bit operands with more than a few rows are not split
-  const int64_t splits = few ? gated_few_splits(N, k, dtype == CLEAVE_F32 ? 4 : 2)
-                         : pairs ? 1 : linear_splits(M, 2 * N, k, dtype == CLEAVE_F32 ? 4 : 8, false);
+  // (partial blocks leave the 8-bit kernel in whole eights of columns)
+  const int64_t splits = few                  ? gated_few_splits(N, k, dtype == CLEAVE_F32 ? 4 : 2)
+                         : pairs && N % 8 != 0 ? 1
+                                              : linear_splits(M, 2 * N, k, dtype == CLEAVE_F32 ? 4 : 8, pairs);
   const int64_t tile = M <= cleave::kFewRows ? cleave::kSmallTileRows
                        : dtype == CLEAVE_F32 && splits > 1 && fp32_splits(M, 2 * N, K).workgroups > 128 ? 64
                                                                                                        : cleave::kLargeTileRows;
@@ -1540,7 +1544,7 @@ extern "C" int cleave_plan_gated(int64_t M, int64_t N, int64_t K, int dtype, cle
 extern "C" int64_t cleave_gated_workspace(const cleave_plan* plan, int whole) {
   if (!plan || !plan->gated || plan->batch != 2 || (whole != 0 && whole != 1)) return CLEAVE_EINVAL;
   if (gated_few_rows(plan->M, plan->N)) return plan->uniform_splits == 1 ? 0 : plan->partial_elems;
-  if (plan->pairs || (plan->fused && whole)) return 0;
+  if (plan->fused && (plan->pairs || whole)) return 0;
   if (plan->fused && packs(plan->M, plan->N, plan->K)) return packed_floats(plan->M, plan->N, plan->K, 2);
   return plan->partial_elems;
 }
@@ -1624,9 +1628,16 @@ extern "C" int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* a
     return CLEAVE_OK;
   }
   // both products' partial blocks, then one pass over them
-  const void* const As[2] = {a->A, a->A};
   const void* const Bs[2] = {a->B_gate, a->B_up};
-  int rc = cleave_execute_grouped(plan, nullptr, 0, 2, As, a->lda, 0, Bs, a->ldb, a->transB, a->dtype, a->partials, hip_stream);
+  BatchLayout bl;
+  bl.shape.n_group = 2;
+  const void* B = nullptr;
+  int rc = group_offsets(Bs, 2, e4m3 ? 2 : eb, &bl.b, &B);
+  if (rc == CLEAVE_OK) rc = ensure_uploaded(plan);
+  const cleave::LinearArgs none{};   // (what the blocks of 8-bit operands go through)
+  if (rc == CLEAVE_OK)
+    rc = execute_impl(plan, nullptr, 0, a->A, e4m3 ? a->lda / 2 : a->lda, 0, B, e4m3 ? a->ldb / 2 : a->ldb, a->transB,
+                      e4m3 ? CLEAVE_BF16 : a->dtype, a->partials, bl, hip_stream, AssembleTarget{}, false, e4m3 ? &none : nullptr);
   if (rc != CLEAVE_OK) return rc;
   // (a long table of runs begins with the last member's)
   const bool up_first = plan->tasks[plan->reduce_tiles[0].task].gemm_id != 0;

@@ -262,8 +262,8 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
       for (int j = 0; j < V; ++j) to.add[j] = G::read(dsum + at(j), cols - at(j));
     }
   };
-  // (1024 threads have no registers for two rows: bf16 spilled 291)
-  constexpr bool AHEAD = NT < 1024;
+  // (where there are registers for two rows)
+  constexpr bool AHEAD = NT < 1024 && V * N <= 24;
   BackwardRow<T, V> cur, next;
   if (AHEAD && group < args.rows) fetch(group, cur);
   int turn = 0;
@@ -410,6 +410,9 @@ __global__ __launch_bounds__(kJoinThreads) void layer_norm_join_kernel(const flo
 // 154, 140; 2999 x 1111 fp32 (278) 512 x 1 12.2, 256 x 2 10.8, 64 x 5 11.0, with half the rows of partial sums; 8192 x 768 bf16 (96) 256 x 1 17.2, 128 x 1 in
 // 2048 13.1, 64 x 2 in 512 13.7; 8192 x 4096 (512) 1024 x 1 71, 256 x 2 50.5, 512 x 1 49.9; 30000 x 256 (32) 128 x 1 28, 64 x 1 in 1024 17.4; 1000 x 8192
 // 512 x 2 in 256, 512 16.8, 21.4; 8192 x 1536 64 x 3 20.4, 256 x 1 in 512, 768, 1024 23.5, 20.1, 19.8.
+// With the next row on its way 1024 threads have too few registers for two groups of bf16: 2048 x 12288 (1536) 1024 x 2 98, 512 x 3 44; 2048 x 16384
+// (2048), without the next row, 1024 x 2 114, 512 x 4 67 (with it 132).  Wider rows are fp32's only: 1024 x 8832 (2208) read twice (the long kernel) 63,
+// 512 x 5 27.4, 1024 x 3 32.3; 1024 x 12288 of fp32 85, 512 x 6 65, 1024 x 3 46.
 struct BackwardShape {
   int threads, groups, workgroups;
 };
@@ -423,7 +426,10 @@ BackwardShape backward_shape(int64_t rows, int64_t cols, int n) {
   if (g <= 512) return {512, 1, at_most(512, 1)};
   if (g <= 768) return {256, 3, at_most(512, 1)};
   if (g <= 1024) return {512, 2, at_most(256, 1)};
-  if (g <= 2048) return {1024, 2, at_most(256, 1)};
+  if (g <= 1536) return {512, 3, at_most(256, 1)};
+  if (g <= 2048) return {512, 4, at_most(256, 1)};
+  if (n == 4 && g <= 2560) return {512, 5, at_most(256, 1)};
+  if (n == 4 && g <= 3 * 1024) return {1024, 3, at_most(256, 1)};
   return {kLongThreads, 0, at_most(512, 1)};
 }
 
@@ -446,14 +452,24 @@ hipError_t launch_backward_of(const LayerNormBackwardArgs& args, const BackwardS
       if constexpr (Group16<T>::N == 4)
         return s.groups == 4 ? launch_backward<T, 64, 4>(args, s.workgroups, stream) : launch_backward<T, 64, 5>(args, s.workgroups, stream);
       else
-        return hipErrorInvalidValue;   // (backward_shape gives bf16 three at most)
+        return hipErrorInvalidValue;   // (backward_shape gives a wave three of bf16 at most)
     case 256:
       return s.groups == 1 ? launch_backward<T, 256, 1>(args, s.workgroups, stream) : launch_backward<T, 256, 3>(args, s.workgroups, stream);
     case 512:
-      return s.groups == 1 ? launch_backward<T, 512, 1>(args, s.workgroups, stream) : launch_backward<T, 512, 2>(args, s.workgroups, stream);
+      switch (s.groups) {
+        case 1: return launch_backward<T, 512, 1>(args, s.workgroups, stream);
+        case 2: return launch_backward<T, 512, 2>(args, s.workgroups, stream);
+        case 3: return launch_backward<T, 512, 3>(args, s.workgroups, stream);
+        case 4: return launch_backward<T, 512, 4>(args, s.workgroups, stream);
+        default: break;
+      }
+      break;
     default: break;
   }
-  if (s.groups == 2) return launch_backward<T, 1024, 2>(args, s.workgroups, stream);
+  if constexpr (Group16<T>::N == 4) {   // (rows of bf16 are read twice from 2049 groups on)
+    if (s.groups == 5) return launch_backward<T, 512, 5>(args, s.workgroups, stream);
+    if (s.groups == 3) return launch_backward<T, 1024, 3>(args, s.workgroups, stream);
+  }
   hipLaunchKernelGGL((layer_norm_backward_long_kernel<T>), dim3(s.workgroups), dim3(kLongThreads), 0, stream, args);
   return hipGetLastError();
 }

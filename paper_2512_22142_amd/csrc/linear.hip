@@ -361,19 +361,19 @@ __global__ __launch_bounds__(kJoinThreads) void linear_join_kernel(ReduceArgs ar
 template <bool BF16, bool GRAD, bool VEC>
 __global__ __launch_bounds__(kJoinThreads) void gated_join_kernel(ReduceArgs args, GatedArgs epi, int64_t up_at, int64_t M, int64_t N,
                                                                   int64_t pitch, int splits) {
-  constexpr int W = VEC ? 4 : 1;
+  constexpr int W = VEC ? 4 : 1, kRun = kJoinThreads * W;   // (one turn of every thread: few rows have few elements)
   for (int64_t it = blockIdx.x; it < args.n_items; it += gridDim.x) {
     ReduceItem item{};
     int64_t first = 0;
     if (args.items) {
       item = load_record(args.items, it);
     } else {
-      first = it * kJoinRun;
+      first = it * kRun;
       item.block = static_cast<uint64_t>(M * pitch);
       item.n_len = static_cast<uint32_t>(N);
       item.m0 = static_cast<uint32_t>(first / N);
       item.col0 = static_cast<uint32_t>(first % N);
-      item.count = static_cast<uint32_t>(std::min<int64_t>(kJoinRun, M * N - first));
+      item.count = static_cast<uint32_t>(std::min<int64_t>(kRun, M * N - first));
       item.ksplit_cnt = static_cast<uint32_t>(splits);
     }
     for (uint32_t e = threadIdx.x * W; e < item.count; e += kJoinThreads * W) {
@@ -383,7 +383,7 @@ __global__ __launch_bounds__(kJoinThreads) void gated_join_kernel(ReduceArgs arg
       if constexpr (VEC) {
         f32x4 sum = *reinterpret_cast<const f32x4*>(p), other{};
         if constexpr (!GRAD) other = *reinterpret_cast<const f32x4*>(p + up_at);
-#pragma unroll 4
+#pragma unroll 8
         for (uint32_t s = 1; s < item.ksplit_cnt; ++s) {
           sum = sum + *reinterpret_cast<const f32x4*>(p + s * item.block);
           if constexpr (!GRAD) other = other + *reinterpret_cast<const f32x4*>(p + up_at + s * item.block);
@@ -414,6 +414,7 @@ __global__ __launch_bounds__(kJoinThreads) void gated_join_kernel(ReduceArgs arg
       } else {
         float sum = p[0], other = 0.0f;
         if constexpr (!GRAD) other = p[up_at];
+#pragma unroll 8
         for (uint32_t s = 1; s < item.ksplit_cnt; ++s) {
           sum += p[s * item.block];
           if constexpr (!GRAD) other += p[up_at + s * item.block];
@@ -436,7 +437,8 @@ template <bool GRAD>
 hipError_t launch_gated_joined(const ReduceArgs& args, const GatedArgs& epi, int64_t up_at, int64_t M, int64_t N, int splits,
                                int out_dtype, bool vec, hipStream_t stream) {
   ReduceArgs a = args;
-  if (!a.items) a.n_items = (M * N + kJoinRun - 1) / kJoinRun;
+  const int run = kJoinThreads * (vec ? 4 : 1);
+  if (!a.items) a.n_items = (M * N + run - 1) / run;
   const int64_t pitch = GRAD ? N : 2 * N;
   const dim3 g(static_cast<uint32_t>(std::min<int64_t>(a.n_items, int64_t{1} << 20))), b(kJoinThreads);
   const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, g, b, 0, stream, a, epi, up_at, M, N, pitch, splits); };
@@ -460,10 +462,13 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs args) {
   u32x4* to = static_cast<u32x4*>(m.to) + row * groups;
   const int64_t first = static_cast<int64_t>(blockIdx.y) * 64 * kPackGroups + (threadIdx.x & 63);
   Raw16 raw[kPackGroups];
+  const auto left = [&](int j) { return static_cast<int>(max(min(m.cols - (first + 64 * j) * 8, int64_t{8}), int64_t{0})); };
+  if (off_word(from)) {   // (uniform: a wave's row)
 #pragma unroll
-  for (int j = 0; j < kPackGroups; ++j) {
-    const int64_t g = first + 64 * j;
-    raw[j] = Group16<Bf16>::read(from + g * 8, static_cast<int>(max(min(m.cols - g * 8, int64_t{8}), int64_t{0})));
+    for (int j = 0; j < kPackGroups; ++j) raw[j] = read_off_word(from + (first + 64 * j) * 8, left(j));
+  } else {
+#pragma unroll
+    for (int j = 0; j < kPackGroups; ++j) raw[j] = Group16<Bf16>::read(from + (first + 64 * j) * 8, left(j));
   }
 #pragma unroll
   for (int j = 0; j < kPackGroups; ++j)

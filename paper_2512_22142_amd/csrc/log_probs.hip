@@ -205,7 +205,11 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
   // A row's last group, where it is not whole, is read so that it ends with the row; what the one before it has is left out.  (Fewer
   // elements than a group are read one by one.)
   const auto place = [&](int g) { return min(g * N, max(len - N, 0)); };
-  const auto read = [&](int g) { return len >= N ? G::read(x + place(g), N) : G::read(x, len); };
+  const bool off = off_word(x);
+  const auto read = [&](int g) {
+    if (len < N) return G::read(x, len);
+    return off ? read_off_word(x + place(g), N) : G::read(x + place(g), N);
+  };
 
   Stats own{-kInf, 0.0f, 0.0f};
   float best = -kInf;
@@ -258,24 +262,32 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
   int g = t;
   const int rounds = whole / (U * NT);   // of whole groups in every thread
   Raw16 raw[U], next[U];
-  const auto fetch = [&](int from, Raw16 (&to)[U]) {
+  const auto fetch = [&](int from, Raw16 (&to)[U], auto off_tag) {
+    constexpr bool OFF = decltype(off_tag)::value;
 #pragma unroll
-    for (int u = 0; u < U; ++u) to[u] = G::read(x + static_cast<int64_t>(from + u * NT) * N, N);
+    for (int u = 0; u < U; ++u) {
+      const T* p = x + static_cast<int64_t>(from + u * NT) * N;
+      to[u] = OFF ? read_off_word(p, N) : G::read(p, N);
+    }
   };
   const auto fetch_ragged = [&](int from, Raw16 (&to)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) to[u] = read(min(from + u * NT, groups - 1));
   };
   const bool rest = rounds * U * NT < groups;
-  if (rounds > 0) {
-    fetch(g, raw);
+  const auto run = [&](auto off_tag) {
+    fetch(g, raw, off_tag);
     for (int r = 1; r < rounds; ++r) {
-      fetch(g + U * NT, next);
+      fetch(g + U * NT, next, off_tag);
       take(raw, g, no);
 #pragma unroll
       for (int u = 0; u < U; ++u) raw[u] = next[u];
       g += U * NT;
     }
+  };
+  if (rounds > 0) {
+    if (sizeof(T) == 2 && off) run(std::integral_constant<bool, sizeof(T) == 2>{});
+    else run(no);
     if (rest) fetch_ragged(g + U * NT, next);
     take(raw, g, no);
     g += U * NT;
@@ -485,7 +497,7 @@ constexpr int64_t kLaunchWorkgroups = int64_t{1} << 21;
 // 11.6; with twenty tokens, which every part ranks, 1 x 65536 12.8, 13.5, 12.9, 14.9, 22.5, 1 x 131072 18.8, 16.5, 14.9, 15.4, 20.8,
 // 16 x 262144 30.6, 23.5, 18.3, 17.7, 23.5, 64 x 131072 19.7, 17.3, 16.7, 18.7, 25.6.
 int log_probs_parts(int64_t rows, int64_t cols, int64_t n_top) {
-  if (rows > 64 || cols < (n_top > 0 ? 131072 : 65536)) return 1;
+  if (rows > 64 || cols < (n_top > 0 ? 98304 : 65536)) return 1;
   return n_top > 0 || rows > 16 ? 4 : static_cast<int>(std::min<int64_t>(cols / 16384, kMostParts));
 }
 

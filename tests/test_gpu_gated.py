@@ -145,6 +145,15 @@ def test_8_bit_operands(M, N, K, name, out):
         assert check(M, N, K, E4M3, out, **kw)[1] == name
 
 
+@pytest.mark.parametrize("M,N,K", [(169, 256, 7680), (64, 128, 6192), (4086, 64, 10880), (33, 264, 6016)])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_8_bit_operands_with_a_split_inner_dimension(M, N, K, out):
+    plan = cleave.plan_gated(M, N, K, E4M3)
+    assert cleave.gated_workspace(plan) > 2 * M * N and cleave.gated_workspace(plan, whole=True) == cleave.gated_workspace(plan)
+    for kw in (dict(), dict(act="gelu_tanh", bias=True, keep=True), dict(pad=1, shift=1), dict(merged=True, up_first=True)):
+        check(M, N, K, E4M3, out, **kw)
+
+
 FEW = [(1, 11008, 256), (1, 64, 64), (2, 1, 16), (16, 1000, 512), (5, 4096, 4096), (3, 300, 4096), (16, 77, 8192), (7, 9000, 48)]
 
 

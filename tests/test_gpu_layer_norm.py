@@ -194,7 +194,7 @@ def check_backward(rows, cols, dtype, dsum, bias=True, pad=0, shift=0):
 
 @pytest.mark.parametrize("rows,cols", SIZES + [(2500, 64), (2500, 500), (2500, 768), (2500, 1024), (2500, 1111), (2500, 1280),
                                                (2500, 1281), (2500, 1537), (2500, 2000), (2500, 2072), (2100, 4096), (2050, 5120),
-                                               (2100, 6145), (1100, 8193), (5000, 256), (9000, 40), (30, 70000)])
+                                               (2100, 6145), (1100, 8193), (300, 10241), (300, 12290), (5000, 256), (9000, 40), (30, 70000)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_backward(rows, cols, dtype):
     check_backward(rows, cols, dtype, dsum=cols % 2 == 0, bias=rows % 3 > 0)

@@ -119,6 +119,13 @@ def test_strides_and_alignment(pad, shift, dtype, rows, cols):
     check(rows, cols, dtype, 7, pad=pad, shift=shift)
 
 
+@pytest.mark.parametrize("rows,cols", [(40, 50257), (1100, 4099), (3, 9001), (2, 100001)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_rows_that_begin_within_a_word(rows, cols, shift):
+    check(rows, cols, BF16, 5, shift=shift)
+    check(rows, cols, BF16, 0, shift=shift)
+
+
 def masks(kind):
     def change(logits, ids):
         rows, cols = logits.shape
