@@ -462,13 +462,10 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs args) {
   u32x4* to = static_cast<u32x4*>(m.to) + row * groups;
   const int64_t first = static_cast<int64_t>(blockIdx.y) * 64 * kPackGroups + (threadIdx.x & 63);
   Raw16 raw[kPackGroups];
-  const auto left = [&](int j) { return static_cast<int>(max(min(m.cols - (first + 64 * j) * 8, int64_t{8}), int64_t{0})); };
-  if (off_word(from)) {   // (uniform: a wave's row)
 #pragma unroll
-    for (int j = 0; j < kPackGroups; ++j) raw[j] = read_off_word(from + (first + 64 * j) * 8, left(j));
-  } else {
-#pragma unroll
-    for (int j = 0; j < kPackGroups; ++j) raw[j] = Group16<Bf16>::read(from + (first + 64 * j) * 8, left(j));
+  for (int j = 0; j < kPackGroups; ++j) {
+    const int64_t g = first + 64 * j;
+    raw[j] = Group16<Bf16>::read(from + g * 8, static_cast<int>(max(min(m.cols - g * 8, int64_t{8}), int64_t{0})));
   }
 #pragma unroll
   for (int j = 0; j < kPackGroups; ++j)

@@ -205,11 +205,7 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
   // A row's last group, where it is not whole, is read so that it ends with the row; what the one before it has is left out.  (Fewer
   // elements than a group are read one by one.)
   const auto place = [&](int g) { return min(g * N, max(len - N, 0)); };
-  const bool off = off_word(x);
-  const auto read = [&](int g) {
-    if (len < N) return G::read(x, len);
-    return off ? read_off_word(x + place(g), N) : G::read(x + place(g), N);
-  };
+  const auto read = [&](int g) { return len >= N ? G::read(x + place(g), N) : G::read(x, len); };
 
   Stats own{-kInf, 0.0f, 0.0f};
   float best = -kInf;
@@ -262,32 +258,24 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
   int g = t;
   const int rounds = whole / (U * NT);   // of whole groups in every thread
   Raw16 raw[U], next[U];
-  const auto fetch = [&](int from, Raw16 (&to)[U], auto off_tag) {
-    constexpr bool OFF = decltype(off_tag)::value;
+  const auto fetch = [&](int from, Raw16 (&to)[U]) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const T* p = x + static_cast<int64_t>(from + u * NT) * N;
-      to[u] = OFF ? read_off_word(p, N) : G::read(p, N);
-    }
+    for (int u = 0; u < U; ++u) to[u] = G::read(x + static_cast<int64_t>(from + u * NT) * N, N);
   };
   const auto fetch_ragged = [&](int from, Raw16 (&to)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) to[u] = read(min(from + u * NT, groups - 1));
   };
   const bool rest = rounds * U * NT < groups;
-  const auto run = [&](auto off_tag) {
-    fetch(g, raw, off_tag);
+  if (rounds > 0) {
+    fetch(g, raw);
     for (int r = 1; r < rounds; ++r) {
-      fetch(g + U * NT, next, off_tag);
+      fetch(g + U * NT, next);
       take(raw, g, no);
 #pragma unroll
       for (int u = 0; u < U; ++u) raw[u] = next[u];
       g += U * NT;
     }
-  };
-  if (rounds > 0) {
-    if (sizeof(T) == 2 && off) run(std::integral_constant<bool, sizeof(T) == 2>{});
-    else run(no);
     if (rest) fetch_ragged(g + U * NT, next);
     take(raw, g, no);
     g += U * NT;

@@ -97,26 +97,6 @@ struct Group16<Bf16> {
   }
 };
 
-// Whether rows of bf16 begin in the middle of a word, where sixteen bytes at a time are read at less than half the rate (11092 x 8503 laid
-// out again, half of the rows so, 340 us as they are, 93 by the words that hold them); a whole wave's or workgroup's row.
-__device__ __forceinline__ bool off_word(const Bf16* row) {
-  return __builtin_amdgcn_readfirstlane(static_cast<int>(reinterpret_cast<uintptr_t>(row) & 2)) != 0;
-}
-__device__ __forceinline__ bool off_word(const float*) { return false; }
-// A group of such a row by the five words that hold it.  (Each of them holds an element of the row.)
-__device__ __forceinline__ Raw16 read_off_word(const Bf16* p, int left) {
-  if (left < 8) return Group16<Bf16>::read(p, left);
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(p - 1);
-  typedef uint32_t Any __attribute__((ext_vector_type(4), aligned(4)));
-  const Raw16 lo = *reinterpret_cast<const Any*>(words);
-  const uint32_t last = words[4];
-  Raw16 w;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) w[q] = __builtin_amdgcn_alignbit(q < 3 ? lo[q + 1] : last, lo[q], 16);
-  return w;
-}
-__device__ __forceinline__ Raw16 read_off_word(const float* p, int left) { return Group16<float>::read(p, left); }
-
 // Single elements.
 __device__ __forceinline__ float element(const float* p) { return *p; }
 __device__ __forceinline__ float element(const Bf16* p) {
