@@ -44,26 +44,6 @@ def rms_norm_backward(dy, h, w, inv, dsum=None):
     return dx, (dy * xhat).sum(axis=0)
 
 
-def layer_norm(x, w, eps, b=None, residual=None):
-    """(y, h, mean, 1 / std) of the rows of h = x + residual."""
-    h = x if residual is None else x + residual
-    mean = h.mean(axis=1)
-    d = h - mean[:, None]
-    inv = 1.0 / np.sqrt((d * d).mean(axis=1) + eps)
-    y = d * inv[:, None] * w
-    return (y if b is None else y + b), h, mean, inv
-
-
-def layer_norm_backward(dy, h, w, mean, inv, dsum=None):
-    """(dx, dw, db) with the given statistics."""
-    xhat = (h - mean[:, None]) * inv[:, None]
-    g = dy * w
-    dx = inv[:, None] * (g - g.mean(axis=1, keepdims=True) - xhat * (g * xhat).mean(axis=1, keepdims=True))
-    if dsum is not None:
-        dx = dx + dsum
-    return dx, (dy * xhat).sum(axis=0), dy.sum(axis=0)
-
-
 _K = math.sqrt(2.0 / math.pi)
 
 

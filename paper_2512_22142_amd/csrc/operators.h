@@ -1,4 +1,4 @@
-// Launch interface of the operators around the GEMMs: norm, bias gradient, AdamW.
+// Launch interface of the operators around the GEMMs: norms, bias gradient, log probabilities, AdamW.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -1,4 +1,4 @@
-"""Operators around the GEMMs of a layer's step: norm, linear product, bias gradient, AdamW.
+"""Operators around the GEMMs of a layer's step: norms, linear and gated products, bias gradient, log probabilities, AdamW.
 
 Arguments are torch tensors on the current device, outputs and workspaces
 included: nothing is allocated here.  `stream` is torch's current stream unless

@@ -329,6 +329,19 @@ def test_backward_of_rows_without_a_token_left_and_of_tokens_beyond_the_row():
         assert torch.all(dx[3] == 0)
 
 
+@pytest.mark.parametrize("mask", [-INF, -3e38])
+def test_masked_tokens_have_no_gradient_however_large_the_given_one(mask):
+    x = matrix(3, 1000, BF16, 1)[0].clone()
+    x[:, 100:900] = mask
+    ids = torch.tensor([3, 950, -1], device="cuda")
+    logp, lse, ent = (torch.empty(3, device="cuda") for _ in range(3))
+    cleave.log_probs(x, ids, logp, lse=lse, entropy=ent)
+    d = torch.full((3,), 1e20, device="cuda")
+    dx = torch.empty_like(x)
+    cleave.log_probs_backward(x, lse, dx, ids=ids, dlogp=d, entropy=ent, dentropy=d)
+    assert torch.all(dx[:, 100:900] == 0) and torch.all(dx.isfinite())
+
+
 def test_backward_against_differences_of_the_kernel():
     rows, cols, step = 3, 50, 1.0 / 64
     x, u = matrix(rows, cols, F32, 1)[0].contiguous(), matrix(rows, cols, F32, 2, std=1.0)[0].contiguous()
