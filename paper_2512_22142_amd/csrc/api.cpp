@@ -1526,6 +1526,7 @@ extern "C" int cleave_plan_gated(int64_t M, int64_t N, int64_t K, int dtype, cle
   int rc = cleave_plan_batched(M, N, k, tile, tile, static_cast<int32_t>(splits), 2, &plan);
   if (rc != CLEAVE_OK) return rc;
   plan->gated = true;
+  plan->for_fp32 = dtype == CLEAVE_F32;
   plan->pairs = pairs;
   plan->uniform_splits = splits;
   if (!few && splits == 1 && dtype != CLEAVE_F32 && (pairs || (eights(N) <= kMostPitch && eights(K) <= kMostPitch))) {
@@ -1552,7 +1553,7 @@ extern "C" int64_t cleave_gated_workspace(const cleave_plan* plan, int whole) {
 extern "C" int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* a, void* hip_stream) {
   if (!plan || !a || !plan->gated || plan->batch != 2 || !linear_dtype(a->dtype)) return CLEAVE_EINVAL;
   const bool e4m3 = a->dtype == CLEAVE_E4M3;
-  if (plan->pairs != e4m3 || !a->A || !a->B_gate || !a->B_up || !a->C) return CLEAVE_EINVAL;
+  if (plan->pairs != e4m3 || plan->for_fp32 != (a->dtype == CLEAVE_F32) || !a->A || !a->B_gate || !a->B_up || !a->C) return CLEAVE_EINVAL;
   if ((a->transB != 0 && a->transB != 1) || (a->out_dtype != CLEAVE_F32 && a->out_dtype != CLEAVE_BF16)) return CLEAVE_EINVAL;
   if (a->act < CLEAVE_ACT_NONE || a->act > CLEAVE_ACT_SILU) return CLEAVE_EINVAL;
   if (e4m3 != (a->scale_a != nullptr) || e4m3 != (a->scale_gate != nullptr) || e4m3 != (a->scale_up != nullptr)) return CLEAVE_EINVAL;
@@ -1658,7 +1659,7 @@ extern "C" int64_t cleave_gated_grad_workspace(const cleave_plan* plan, int whol
 }
 
 extern "C" int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_grad_args* a, void* hip_stream) {
-  if (!plan || !a || !plan->linear || plan->pairs || (a->dtype != CLEAVE_F32 && a->dtype != CLEAVE_BF16)) return CLEAVE_EINVAL;
+  if (!plan || !a || !plan->linear || plan->pairs || a->dtype != (plan->for_fp32 ? CLEAVE_F32 : CLEAVE_BF16)) return CLEAVE_EINVAL;
   if (!a->A || !a->B || !a->gate || !a->up || !a->dgate || !a->dup) return CLEAVE_EINVAL;
   if ((a->transB != 0 && a->transB != 1) || (a->out_dtype != CLEAVE_F32 && a->out_dtype != CLEAVE_BF16)) return CLEAVE_EINVAL;
   if (a->act < CLEAVE_ACT_NONE || a->act > CLEAVE_ACT_SILU) return CLEAVE_EINVAL;
@@ -1687,7 +1688,7 @@ extern "C" int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_gr
   const bool few = gated_few_rows(M, N);
   const bool whole = a->dtype == CLEAVE_BF16 && K % 8 == 0 && (a->transB || N % 8 == 0) && whole_operand(a->A, a->lda) &&
                      whole_operand(a->B, a->ldb);
-  const bool fused = !few && splits == 1 && !plan->for_fp32 && a->dtype == CLEAVE_BF16 && (whole || packs_grad(M, N, K));
+  const bool fused = !few && splits == 1 && !plan->for_fp32 && (whole || packs_grad(M, N, K));
   if (!(fused && whole) && !a->partials) return CLEAVE_EINVAL;
   int rc = ensure_uploaded(plan);
   if (rc == CLEAVE_OK) rc = ensure_gated_ready(plan->device);

@@ -136,6 +136,20 @@ def test_plans_of_other_calls():
         lib.cleave_plan_destroy(plan)
 
 
+@pytest.mark.parametrize("M", [4, 40, 900])
+def test_plans_of_another_type(M):
+    for plan_dtype, dtype in ((BF16, F32), (F32, BF16)):
+        plan = gated_plan(M, 200, 512, plan_dtype)
+        a = Args(A=P, B_gate=2 * P, B_up=3 * P, C=4 * P, partials=5 * P, lda=512, ldb=512, ldc=200, transB=1, dtype=dtype, out_dtype=BF16)
+        assert gated(plan, ctypes.byref(a), None) == EINVAL
+        lib.cleave_plan_destroy(plan)
+        plan = made(M, 200, 512, plan_dtype)
+        a = GradArgs(A=P, B=2 * P, gate=3 * P, up=4 * P, dgate=5 * P, dup=6 * P, partials=7 * P, lda=512, ldb=512, ld_gate=200, ld_up=200,
+                     ld_dgate=200, ld_dup=200, transB=1, dtype=dtype, out_dtype=BF16)
+        assert grad(plan, ctypes.byref(a), None) == EINVAL
+        lib.cleave_plan_destroy(plan)
+
+
 def test_other_calls_of_a_gated_plan_of_8_bit_operands():
     plan = gated_plan(300, 200, 512, E4M3)
     lists = ctypes.cast((p * 2)(P, 2 * P), p)
