@@ -1486,6 +1486,41 @@ int64_t gated_few_splits(int64_t N, int64_t k, int64_t bytes) {
   return 1;
 }
 
+// Splits of K for more rows, `k` in elements of two bytes.  Few items of 128 x 128: what takes least by the time of a K step (up to 64 items run as a part a
+// CU, up to 128 as two, up to 256 as one item; K x N's half tiles of 32 columns are half lines, which only whole products have) and of the join
+// (5 us, and both products' partial blocks written and read at 4.5 TB/s).  Otherwise as many as fill the CUs with large tiles.  bf16, weights from
+// memory, us, K x N / N x K, unsplit; 2; 4 splits: 17 rows, 2560 x 5120 (columns x K) 52 / 25; 34 / 27; 19 / 19, 4096 x 11008 91 / 51; 61 / 53; 48 / 40,
+// 5632 x 2048 34 / 18; 17 / 17; 19 / 19, 2816 x 1024 8.5 / 7.0; 10.6 / 10.6; 10.8 / 10.2; 128 rows, 4096 x 4096 39 / 23; 32 / 27; 28 / 27, 2048 x 2048
+// 15.6 / 11.4; 12.3 / 12.6; 14.9 / 14.1; 256 rows, 2048 x 5632 50 / 30; 38 / 34; 27 / 26, 4096 x 2048 27 / 20; 22 / 22; 27 / 25; 1289 rows, 192 x 2880 15.1 /
+// 12.3 and in 4 17.2 / 17.9; large tiles: 256 rows, 11008 x 4096 83 / 78; 67 / 67; 90 / 87, 512 rows, 4096 x 11008 118 / 109; 120 / 119; 96 / 92,
+// 8192 x 4096 86 / 77; 73 / 77; 94 / 94, 5632 x 4096 63 / 62; 67 / 66; 83 / 81, 1159 rows, 1920 x 9920 134 / 131; 152 / 178.
+// e4m3, 17 rows, 1024 x 4096 14.8; 12.0; 9.3, 2048 x 5632 18.8; 14.1; 13.3, 4096 x 4096 15.7; 16.3; 18.2; 256 rows, 2048 x 2048 10.5; 15.8; 20.3.
+int64_t gated_splits(int64_t M, int64_t N, int64_t k, bool pairs) {
+  constexpr int64_t kCUs = 256;
+  const int64_t items = ((M + 127) / 128) * ((2 * N + 127) / 128), large = ((M + 255) / 256) * ((2 * N + 255) / 256);
+  const auto whole = [&](int64_t S) { return (k + S - 1) / S % 8 == 0 && (S - 1) * ((k + S - 1) / S) < k; };   // (chunks in sixteen bytes)
+  if (items <= (pairs ? kCUs / 8 : kCUs / 2)) {
+    int64_t best = 1;
+    double least = 0.0;
+    for (int64_t S = 1; S <= 4 && items * S <= kCUs; ++S) {
+      if (S > 1 && !whole(S)) continue;
+      const double step = S == 1                   ? (pairs ? 0.25 : items <= kCUs / 4 ? 0.3 : 0.65)
+                          : items * S <= kCUs / 4  ? 0.25
+                          : items * S <= kCUs / 2  ? 0.52
+                                                   : 0.6;
+      double us = step * static_cast<double>(k) / static_cast<double>(64 * S);
+      if (S > 1) us += 5.0 + 8.0 * static_cast<double>(S * M * 2 * N) / 4.5e6;
+      if (S > 1 && us >= least) continue;
+      least = us;
+      best = S;
+    }
+    return best;
+  }
+  if (pairs || items < kCUs || large > kCUs / 2) return 1;
+  const int64_t S = large <= kCUs / 4 ? 4 : 2;
+  return k >= 2048 * S && whole(S) && large * S >= (M <= 256 ? 160 : 192) ? S : 1;
+}
+
 bool floats_aligned(const float* const* list, int n) {
   for (int k = 0; k < n; ++k)
     if (!aligned(list[k], 4)) return false;
@@ -1514,11 +1549,12 @@ extern "C" int cleave_plan_gated(int64_t M, int64_t N, int64_t K, int dtype, cle
   if (pairs && K % 16 != 0) return CLEAVE_EINVAL;
   const int64_t k = pairs ? K / 2 : K;
   const bool few = gated_few_rows(M, N);
-  // tiles and splits as for one product of both operands' columns; 8-bit operands with more than a few rows are not split
-  // (partial blocks leave the 8-bit kernel in whole eights of columns)
-  const int64_t splits = few                  ? gated_few_splits(N, k, dtype == CLEAVE_F32 ? 4 : 2)
-                         : pairs && N % 8 != 0 ? 1
-                                              : linear_splits(M, 2 * N, k, dtype == CLEAVE_F32 ? 4 : 8, pairs);
+  // (partial blocks leave the 8-bit kernel in whole eights of columns; what the general kernel takes is split as one product of both
+  // operands' columns)
+  const int64_t splits = few                                      ? gated_few_splits(N, k, dtype == CLEAVE_F32 ? 4 : 2)
+                         : pairs && N % 8 != 0                    ? 1
+                         : dtype == CLEAVE_F32 || k % 8 != 0      ? linear_splits(M, 2 * N, k, dtype == CLEAVE_F32 ? 4 : 8, pairs)
+                                                                  : gated_splits(M, N, k, pairs);
   const int64_t tile = M <= cleave::kFewRows ? cleave::kSmallTileRows
                        : dtype == CLEAVE_F32 && splits > 1 && fp32_splits(M, 2 * N, K).workgroups > 128 ? 64
                                                                                                        : cleave::kLargeTileRows;
