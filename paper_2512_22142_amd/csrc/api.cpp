@@ -1432,9 +1432,9 @@ int64_t packed_floats(int64_t M, int64_t N, int64_t K, int64_t weights) {
   return (M * eights(K) + weights * std::max(N * eights(K), K * eights(N))) / 2 + 4;
 }
 
-// What calls of the plan need on the device: few rows nothing.
+// What calls of the plan need on the device: few rows nothing, but for the direct kernel.
 int upload_gated(cleave_plan* plan) {
-  if (gated_few_rows(plan->M, plan->N)) return CLEAVE_OK;
+  if (gated_few_rows(plan->M, plan->N)) return plan->fused ? ensure_uploaded(plan->fused) : CLEAVE_OK;
   if (plan->fused) {
     const int rc = ensure_uploaded(plan->fused);
     if (rc != CLEAVE_OK || plan->pairs || packs(plan->M, plan->N, plan->K)) return rc;
@@ -1521,6 +1521,20 @@ int64_t gated_splits(int64_t M, int64_t N, int64_t k, bool pairs) {
   return k >= 2048 * S && whole(S) && large * S >= (M <= 256 ? 160 : 192) ? S : 1;
 }
 
+// Few rows of whole bf16 operands that the direct kernel takes in less time, though its tiles are mostly empty: short K, whose loads it has on
+// their way sooner, where every part has a CU; and long rows of K stored N x K, of which it reads whole lines, where every CU has an item and few
+// have two.  us, weights from memory, few rows / direct, K x N and N x K, one row (16): 768 x 768 7.0, 8.7 (8.1, 10.2) / 6.3, 6.2 (6.4, 6.2), 4096 x 1024 9.3,
+// 9.4 (10.5, 10.3) / 8.5, 7.1 (8.9, 7.2), 4096 x 256 5.0, 5.2 (5.7, 6.0) / 5.2, 5.1 (5.3, 5.1), 5632 x 1024 10.2, 10.9 / 14.5, 9.5, 2816 x 2048 10.9, 11.8 / 12.8,
+// 11.0; 11008 x 8192 80, 86 (84, 97) / 74, 70 (77, 69), 11008 x 4096 43, 48 (44, 50) / 40, 43 (41, 43), 8192 x 8192 60, 65 / 111, 67, 16384 x 4096 57, 57 / 54, 64.
+enum FewDirect { kFewNever, kFewByColumn, kFewAlways };   // ByColumn: stored N x K
+FewDirect gated_few_direct(int64_t N, int64_t K) {
+  constexpr int64_t kCUs = 256;
+  const int64_t items = (2 * N + 127) / 128;
+  if (K % 8 != 0) return kFewNever;
+  if (items <= kCUs / 4) return K <= 1024 ? kFewAlways : kFewNever;
+  return items > kCUs / 2 && items <= kCUs / 4 * 3 && K >= 4096 ? kFewByColumn : kFewNever;
+}
+
 bool floats_aligned(const float* const* list, int n) {
   for (int k = 0; k < n; ++k)
     if (!aligned(list[k], 4)) return false;
@@ -1565,7 +1579,8 @@ extern "C" int cleave_plan_gated(int64_t M, int64_t N, int64_t K, int dtype, cle
   plan->for_fp32 = dtype == CLEAVE_F32;
   plan->pairs = pairs;
   plan->uniform_splits = splits;
-  if (!few && splits == 1 && dtype != CLEAVE_F32 && (pairs || (eights(N) <= kMostPitch && eights(K) <= kMostPitch))) {
+  const FewDirect few_direct = few && dtype == CLEAVE_BF16 ? gated_few_direct(N, K) : kFewNever;
+  if ((few ? few_direct != kFewNever : splits == 1) && dtype != CLEAVE_F32 && (pairs || (eights(N) <= kMostPitch && eights(K) <= kMostPitch))) {
     rc = cleave_plan_uniform(M, 2 * N, k, cleave::kLargeTileRows, cleave::kLargeTileCols, 1, 0, &plan->fused);
     if (rc != CLEAVE_OK) {
       cleave_plan_destroy(plan);
@@ -1580,7 +1595,10 @@ extern "C" int cleave_plan_gated(int64_t M, int64_t N, int64_t K, int dtype, cle
 
 extern "C" int64_t cleave_gated_workspace(const cleave_plan* plan, int whole) {
   if (!plan || !plan->gated || plan->batch != 2 || (whole != 0 && whole != 1)) return CLEAVE_EINVAL;
-  if (gated_few_rows(plan->M, plan->N)) return plan->uniform_splits == 1 ? 0 : plan->partial_elems;
+  if (gated_few_rows(plan->M, plan->N)) {
+    const bool direct = plan->fused && whole && gated_few_direct(plan->N, plan->K) == kFewAlways;
+    return direct || plan->uniform_splits == 1 ? 0 : plan->partial_elems;
+  }
   if (plan->fused && (plan->pairs || whole)) return 0;
   if (plan->fused && packs(plan->M, plan->N, plan->K)) return packed_floats(plan->M, plan->N, plan->K, 2);
   return plan->partial_elems;
@@ -1624,7 +1642,7 @@ extern "C" int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* a
   const bool few = gated_few_rows(M, N);
   const bool whole = e4m3 || (a->dtype == CLEAVE_BF16 && K % 8 == 0 && (a->transB || N % 8 == 0) && whole_operand(a->A, a->lda) &&
                               whole_operand(a->B_gate, a->ldb) && whole_operand(a->B_up, a->ldb));
-  const bool fused = !few && plan->fused && (whole || packs(M, N, K));
+  const bool fused = plan->fused && (few ? whole && (a->transB || gated_few_direct(N, K) == kFewAlways) : whole || packs(M, N, K));
   if (!(fused && whole) && (!few || splits > 1) && !a->partials) return CLEAVE_EINVAL;
   if (fused) {
     AssembleTarget to;

@@ -160,11 +160,30 @@ FEW = [(1, 11008, 256), (1, 64, 64), (2, 1, 16), (16, 1000, 512), (5, 4096, 4096
 @pytest.mark.parametrize("M,N,K", FEW)
 @pytest.mark.parametrize("dtype,transB", [(BF16, 0), (BF16, 1), (F32, 0), (F32, 1), (E4M3, 1)])
 def test_few_rows(M, N, K, dtype, transB):
+    direct = dtype == BF16 and K <= 1024 and N <= 4096 and (transB or N % 8 == 0)     # (whole operands, short K)
     for kw in (dict(), dict(act="gelu_tanh", bias=True, keep=True, out=F32)):
-        assert check(M, N, K, dtype, transB=transB, **kw)[1] == "gated_few_rows"
+        name = check(M, N, K, dtype, transB=transB, **kw)[1]
+        assert name == "gated_few_rows" if not direct else name.startswith("gated_direct_bf16_64x32"), name
     if dtype != E4M3:
         check(M, N, K, dtype, transB=transB, pad=3, shift=1, keep=True)
         check(M, N, K - 1, dtype, transB=transB, act="relu")
+
+
+@pytest.mark.parametrize("M,N,K,names", [(1, 8200, 4104, ("few", "direct")), (13, 12200, 4096, ("few", "direct")), (16, 12296, 4096, ("few", "few")),
+                                         (3, 4096, 1024, ("direct", "direct")), (15, 4104, 1024, ("few", "few")), (1, 8, 8, ("direct", "direct")),
+                                         (16, 1000, 1000, ("direct", "direct")), (2, 1003, 96, ("few", "direct")), (4, 8200, 4088, ("few", "few"))])
+def test_few_rows_on_the_direct_kernel(M, N, K, names):
+    for transB in (0, 1):
+        for kw in (dict(), dict(bias=True, keep=True, act="gelu_tanh", out=F32), dict(merged=True)):
+            if kw.get("merged") and N % 8 and not transB:
+                continue
+            name = check(M, N, K, transB=transB, **kw)[1]
+            assert ("gated_direct" in name) == (names[transB] == "direct"), name
+        check(M, N, K, transB=transB, shift=1)
+        check(M, N, K, transB=transB, pad=1)
+    plan = cleave.plan_gated(M, N, K, BF16)
+    if names == ("direct", "direct"):
+        assert cleave.gated_workspace(plan, whole=True) == 0
 
 
 @pytest.mark.parametrize("M,N,K", [(17, 1, 1), (37, 53, 71), (200, 50, 100), (129, 257, 65), (300, 77, 1000), (64, 512, 4096),

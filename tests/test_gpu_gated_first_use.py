@@ -48,7 +48,7 @@ print("same", plan.last_kernel)
 """
 
 
-@pytest.mark.parametrize("M,K,N", [(512, 256, 512), (900, 250, 300), (40, 250, 300), (4, 4096, 512)])
+@pytest.mark.parametrize("M,K,N", [(512, 256, 512), (900, 250, 300), (40, 250, 300), (4, 4096, 512), (4, 1024, 512)])
 @pytest.mark.parametrize("what", [GATED, GRAD])
 def test_first_use_in_a_graph(what, M, K, N):
     child = START.format(M=M, K=K, N=N) + what + END
