@@ -35,7 +35,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
   __shared__ float slots[4][NW];
   const int t = threadIdx.x % NT;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * RowGroup<NT>::kRows + threadIdx.x / NT;
-  if (row >= args.rows) return;   // whole waves, and with several waves to a row whole workgroups
+  if (row >= args.rows) return;   // whole sixteens of lanes, waves, or with several waves to a row workgroups
   const T* x = static_cast<const T*>(args.x) + row * args.ldx;
   const T* r = static_cast<const T*>(args.residual) + (args.residual ? row * args.ldr : 0);
   T* sum_out = static_cast<T*>(args.sum_out) + (args.sum_out ? row * args.lds : 0);
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
 #pragma unroll
     for (int j = 0; j < V; ++j) G::store(sum_out + at(j), cols - at(j), h[j]);
   }
-  const float first = group_total<NW>(sum, slots[0]) * part;
+  const float first = group_total<NT>(sum, slots[0]) * part;
   float rest = 0.0f, squares = 0.0f;
 #pragma unroll
   for (int j = 0; j < V; ++j)
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
       rest += h[j][e];
       squares += h[j][e] * h[j][e];
     }
-  group_totals<NW>(rest, squares, slots[1]);
+  group_totals<NT>(rest, squares, slots[1]);
   rest *= part;
   const float var = squares * part - rest * rest;
   const float inv = 1.0f / __builtin_sqrtf((var < 0.0f ? 0.0f : var) + args.eps);   // (NaN stays)
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
 #pragma unroll
       for (int e = 0; e < N; ++e)
         if (at(j) + e < cols) most = nan_max(most, __builtin_fabsf(h[j][e]));
-    const BlockScale s = block_scale(group_nan_max<NW>(most, slots[3]));
+    const BlockScale s = block_scale(row_nan_max<NT>(most, slots[3]));
     if (t == 0) args.scales[row] = s.scale;
     uint8_t* y = static_cast<uint8_t*>(args.y) + row * args.ldy;
 #pragma unroll
@@ -145,14 +145,14 @@ __global__ __launch_bounds__(kLongThreads) void layer_norm_long_kernel(LayerNorm
   const auto at = [&](int64_t c) { return args.residual ? element(x + c) + element(r + c) : element(x + c); };
   float sum = 0.0f;
   for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) sum += at(c);
-  const float first = group_total<NW>(sum, slots[0]) / count;
+  const float first = group_total<kLongThreads>(sum, slots[0]) / count;
   float rest = 0.0f, squares = 0.0f;
   for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
     const float d = at(c) - first;
     rest += d;
     squares += d * d;
   }
-  group_totals<NW>(rest, squares, slots[1]);
+  group_totals<kLongThreads>(rest, squares, slots[1]);
   rest /= count;
   const float var = squares / count - rest * rest;
   const float inv = 1.0f / __builtin_sqrtf((var < 0.0f ? 0.0f : var) + args.eps);
@@ -202,10 +202,15 @@ hipError_t launch_norm_fit(const LayerNormArgs& args, int64_t v, hipStream_t str
 // Which threads share a row: a wave where it holds a narrow one and there are many, as few more as hold a wider one, many for few rows,
 // whose latency counts.  us, threads x groups, bf16 with a residual: 8192 x 768 64 x 2 11.9, 128 x 1 12.1, 256 x 1 17.2; 16384 x 5120 into 8
 // bits 64 x 10 192, 128 x 5 125, 256 x 3 118, 512 x 2 137, 1024 x 1 185, into bf16 154, 134, 129, 125, 149; 4096 x 4096 128 x 4 23.0, 256 x 2 21.9,
-// 1024 x 1 33; 20000 x 1000 fp32 64 x 4 65, 256 x 1 58; 200 x 9000 256 x 5 7.1, 1024 x 2 6.6; 1 x 768 64 x 2 5.6, 1024 x 1 4.3.
+// 1024 x 1 33; 20000 x 1000 fp32 64 x 4 65, 256 x 1 58; 200 x 9000 256 x 5 7.1, 1024 x 2 6.6; 1 x 768 64 x 2 5.6, 1024 x 1 4.3.  Rows of a head's
+// width, without a residual, 64 x 1, 16 x 1, 8 x 1: 262144 x 64 86, 22.2, 14.0 (4.8 TB/s), 16 x 64 3.0, 2.8, 2.4; 131072 x 128 43, 13.6, 8 x 2 13.4; 65536 x
+// 256 24.4, 16 x 2 13.6, 8 x 4 14.6; 300 x 128 3.1, 2.6, 8 x 2 3.0; fp32 131072 x 128 33.8, 16 x 2 21.2.
 template <typename T>
 hipError_t launch_norm_of(const LayerNormArgs& args, hipStream_t stream) {
   const int64_t groups = (args.cols + Group16<T>::N - 1) / Group16<T>::N;
+  if (groups <= 8) return launch_norm<T, 8, 1>(args, stream);
+  if (groups <= 16) return launch_norm<T, 16, 1>(args, stream);
+  if (groups <= 32) return launch_norm<T, 16, 2>(args, stream);
   if (groups <= 64) return launch_norm<T, 64, 1>(args, stream);
   if (groups <= 3 * 64 && args.rows > 1024) return launch_norm_fit<T, 64, 3>(args, (groups + 63) / 64, stream);
   if (groups <= 8 * 256 && args.rows > 256) return launch_norm_fit<T, 256, 8>(args, (groups + 255) / 256, stream);
@@ -224,6 +229,7 @@ __host__ __device__ __forceinline__ int64_t padded(int64_t cols) { return (cols 
 // One pass over dy and h for dx and for the sums over rows: every group of the launch takes every groups-th row and holds its
 // part of dw and db in registers until the last of them, one row of partial sums for each workgroup, whose groups (a
 // wave each, where there are several) are joined in order.  The next row's loads are on their way while a row's sums are joined.
+// (Groups of fewer than 64 threads add theirs by columns.)
 template <typename T, int V>
 struct BackwardRow {
   Raw16 dy[V], h[V], add[V];
@@ -289,7 +295,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
         dot += g[j][e] * xhat[j][e];
       }
     // (the slots of the row before last are free: every wave has passed the barrier of the last one)
-    group_totals<NW>(sum, dot, slots[turn]);
+    group_totals<NT>(sum, dot, slots[turn]);
     sum /= count;
     dot /= count;
     T* dx = static_cast<T*>(args.dx) + row * args.lddx;
@@ -303,7 +309,32 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
     }
     if (AHEAD) cur = next;
   }
-  if constexpr (GROUPS > 1) {
+  const int64_t half = padded(args.cols);
+  float* out = args.partials + static_cast<int64_t>(blockIdx.x) * 2 * half;
+  if constexpr (NT < 64) {   // a column to a thread
+    constexpr int kWide = NT * V * N;
+    __shared__ float joined[GROUPS][2][kWide];
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        joined[threadIdx.x / NT][0][at(j) + e] = dw[j][e];
+        joined[threadIdx.x / NT][1][at(j) + e] = db[j][e];
+      }
+    __syncthreads();
+    for (int c = threadIdx.x; c < cols; c += RowGroup<NT>::kThreads) {
+      float sums[2] = {};
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        sums[0] += joined[g][0][c];
+        sums[1] += joined[g][1][c];
+      }
+      out[c] = sums[0];
+      out[half + c] = sums[1];
+    }
+    return;
+  }
+  if constexpr (NT == 64) {
     __shared__ float joined[GROUPS - 1][2 * V * N][NT];
     if (threadIdx.x >= NT) {
 #pragma unroll
@@ -326,8 +357,6 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
           db[j][e] += joined[g][(V + j) * N + e][t];
         }
   }
-  const int64_t half = padded(args.cols);
-  float* out = args.partials + static_cast<int64_t>(blockIdx.x) * 2 * half;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     store_floats<N>(out + at(j), cols - at(j), dw[j]);
@@ -357,7 +386,7 @@ __global__ __launch_bounds__(kLongThreads) void layer_norm_backward_long_kernel(
       sum += g;
       dot += g * x;
     }
-    group_totals<NW>(sum, dot, slots[turn]);
+    group_totals<kLongThreads>(sum, dot, slots[turn]);
     sum /= count;
     dot /= count;
     for (int64_t c = threadIdx.x; c < args.cols; c += kLongThreads) {
@@ -405,14 +434,16 @@ __global__ __launch_bounds__(kJoinThreads) void layer_norm_join_kernel(const flo
 }
 
 // Threads of a row, groups of sixteen bytes of each, and workgroups: what the CUs hold at a time, so that a workgroup's rows
-// share one row of partial sums.  Narrow rows are a wave's, four to a workgroup, without a barrier.  us, the first launch alone: 16384 x 5120 bf16
+// share one row of partial sums.  Narrow rows are a wave's, four to a workgroup, without a barrier, or eight or sixteen lanes'.  us, the first launch alone: 16384 x 5120 bf16
 // with dsum (640 groups) 1024 x 1 (threads x groups) 155, 512 x 2 158, 128 x 5 145, 256 x 3 133, and in 256, 512, 768, 1024 workgroups > 160, 133,
 // 154, 140; 2999 x 1111 fp32 (278) 512 x 1 12.2, 256 x 2 10.8, 64 x 5 11.0, with half the rows of partial sums; 8192 x 768 bf16 (96) 256 x 1 17.2, 128 x 1 in
 // 2048 13.1, 64 x 2 in 512 13.7; 8192 x 4096 (512) 1024 x 1 71, 256 x 2 50.5, 512 x 1 49.9; 30000 x 256 (32) 128 x 1 28, 64 x 1 in 1024 17.4; 1000 x 8192
 // 512 x 2 in 256, 512 16.8, 21.4; 8192 x 1536 64 x 3 20.4, 256 x 1 in 512, 768, 1024 23.5, 20.1, 19.8.
 // With the next row on its way 1024 threads have too few registers for two groups of bf16: 2048 x 12288 (1536) 1024 x 2 98, 512 x 3 44; 2048 x 16384
 // (2048), without the next row, 1024 x 2 114, 512 x 4 67 (with it 132).  Wider rows are fp32's only: 1024 x 8832 (2208) read twice (the long kernel) 63,
-// 512 x 5 27.4, 1024 x 3 32.3; 1024 x 12288 of fp32 85, 512 x 6 65, 1024 x 3 46.
+// 512 x 5 27.4, 1024 x 3 32.3; 1024 x 12288 of fp32 85, 512 x 6 65, 1024 x 3 46; 1024 x 16384 108, 512 x 8 78, 1024 x 4 89.
+// Rows of a head's width, without dsum, 64 x 1 in 1024, 16 x 1 in 512, 1024, 8 x 1 in 512, 1024: 262144 x 64 100, 36.2, 26.8, 19.4, 18.1 (5.2 TB/s),
+// 32768 x 64 16.4, 7.0, 6.3, 5.0, 5.3; 65536 x 100 47, 20.9, 15.1, 8 x 2 14.5, 17.1; 65536 x 256 30.3, 16 x 2 19.2, 21.1.
 struct BackwardShape {
   int threads, groups, workgroups;
 };
@@ -421,6 +452,9 @@ BackwardShape backward_shape(int64_t rows, int64_t cols, int n) {
   const auto at_most = [&](int most, int of_workgroup) {
     return static_cast<int>(std::min<int64_t>(most, (rows + of_workgroup - 1) / of_workgroup));
   };
+  if (g <= 8) return {8, 1, at_most(512, 32)};
+  if (g <= 16) return {16, 1, at_most(1024, 16)};
+  if (g <= 32) return {16, 2, at_most(512, 16)};
   if (g <= (n == 8 ? 192 : 320)) return {64, static_cast<int>((g + 63) / 64), at_most(g <= 64 ? 1024 : 512, 4)};
   if (g <= 256) return {256, 1, at_most(768, 1)};
   if (g <= 512) return {512, 1, at_most(512, 1)};
@@ -430,6 +464,7 @@ BackwardShape backward_shape(int64_t rows, int64_t cols, int n) {
   if (g <= 2048) return {512, 4, at_most(256, 1)};
   if (n == 4 && g <= 2560) return {512, 5, at_most(256, 1)};
   if (n == 4 && g <= 3 * 1024) return {1024, 3, at_most(256, 1)};
+  if (n == 4 && g <= 4096) return {512, 8, at_most(256, 1)};
   return {kLongThreads, 0, at_most(512, 1)};
 }
 
@@ -442,6 +477,9 @@ hipError_t launch_backward(const LayerNormBackwardArgs& args, int workgroups, hi
 template <typename T>
 hipError_t launch_backward_of(const LayerNormBackwardArgs& args, const BackwardShape& s, hipStream_t stream) {
   switch (s.threads) {
+    case 8: return launch_backward<T, 8, 1>(args, s.workgroups, stream);
+    case 16:
+      return s.groups == 1 ? launch_backward<T, 16, 1>(args, s.workgroups, stream) : launch_backward<T, 16, 2>(args, s.workgroups, stream);
     case 64:
       switch (s.groups) {
         case 1: return launch_backward<T, 64, 1>(args, s.workgroups, stream);
@@ -468,6 +506,7 @@ hipError_t launch_backward_of(const LayerNormBackwardArgs& args, const BackwardS
   }
   if constexpr (Group16<T>::N == 4) {   // (rows of bf16 are read twice from 2049 groups on)
     if (s.groups == 5) return launch_backward<T, 512, 5>(args, s.workgroups, stream);
+    if (s.groups == 8) return launch_backward<T, 512, 8>(args, s.workgroups, stream);
     if (s.groups == 3) return launch_backward<T, 1024, 3>(args, s.workgroups, stream);
   }
   hipLaunchKernelGGL((layer_norm_backward_long_kernel<T>), dim3(s.workgroups), dim3(kLongThreads), 0, stream, args);

@@ -106,12 +106,12 @@ __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(Bf16* p, float x) { p->bits = to_bf16_bits(x); }
 
 // A row per group of NT threads, which holds up to NT * V * N elements of it (N in sixteen bytes); a wave (NT = 64)
-// has its row to itself, four rows to a workgroup.
+// has its row to itself, four rows to a workgroup, and eight or sixteen lanes a narrow one.
 template <int NT>
 struct RowGroup {
-  static constexpr int kThreads = NT == 64 ? 256 : NT;
+  static constexpr int kThreads = NT <= 64 ? 256 : NT;
   static constexpr int kRows = kThreads / NT;
-  static constexpr int kWaves = NT / 64;
+  static constexpr int kWaves = NT < 64 ? 1 : NT / 64;
 };
 
 // N floats beside a group of either type.

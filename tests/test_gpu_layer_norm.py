@@ -100,6 +100,18 @@ def test_norm(rows, cols, dtype, out):
     check_norm(rows, cols, dtype, out, residual=rows % 2 == 1, bias=cols % 3 > 0 or cols == 1)
 
 
+# rows that eight or sixteen lanes share, and the next wider ones; numbers of them that end within a wave
+NARROW = [(1, 2), (33, 8), (100, 31), (4099, 32), (35, 33), (1000, 63), (4097, 64), (2055, 65), (70, 100), (515, 127), (9001, 128), (129, 129),
+          (47, 200), (3003, 255), (5001, 256), (14, 257)]
+
+
+@pytest.mark.parametrize("rows,cols", NARROW)
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (BF16, E4M3), (F32, F32), (F32, E4M3)])
+def test_narrow_rows(rows, cols, dtype, out):
+    check_norm(rows, cols, dtype, out, residual=rows % 2 == 1, bias=cols % 2 == 0)
+    check_norm(rows, cols, dtype, out, residual=rows % 2 == 0, pad=3, shift=1)
+
+
 @pytest.mark.parametrize("pad,shift", [(8, 0), (3, 0), (8, 1), (0, 4), (5, 7)])
 @pytest.mark.parametrize("dtype,out", [(BF16, BF16), (BF16, E4M3), (F32, F32)])
 @pytest.mark.parametrize("cols", [768, 70001])
@@ -194,7 +206,7 @@ def check_backward(rows, cols, dtype, dsum, bias=True, pad=0, shift=0):
 
 @pytest.mark.parametrize("rows,cols", SIZES + [(2500, 64), (2500, 500), (2500, 768), (2500, 1024), (2500, 1111), (2500, 1280),
                                                (2500, 1281), (2500, 1537), (2500, 2000), (2500, 2072), (2100, 4096), (2050, 5120),
-                                               (2100, 6145), (1100, 8193), (300, 10241), (300, 12290), (5000, 256), (9000, 40), (30, 70000)])
+                                               (2100, 6145), (1100, 8193), (300, 10241), (300, 12290), (270, 16001), (5000, 256), (9000, 40), (30, 70000)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_backward(rows, cols, dtype):
     check_backward(rows, cols, dtype, dsum=cols % 2 == 0, bias=rows % 3 > 0)
@@ -205,6 +217,13 @@ def test_backward(rows, cols, dtype):
 def test_backward_strides_and_alignment(pad, shift, dtype):
     check_backward(9, 768, dtype, True, True, pad, shift)
     check_backward(3000, 100, dtype, True, True, pad, shift)
+
+
+@pytest.mark.parametrize("rows,cols", NARROW + [(20000, 64), (40000, 24), (17000, 128), (9000, 200)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_backward_of_narrow_rows(rows, cols, dtype):
+    check_backward(rows, cols, dtype, dsum=rows % 2 == 0, bias=cols % 2 == 0)
+    check_backward(rows, cols, dtype, True, True, 3, 1)
 
 
 def test_backward_repeats_its_bits_and_writes_over_its_inputs():
