@@ -28,7 +28,22 @@ namespace cleave {
 
 namespace {
 
-template <typename T, int NT, int V, bool E4M3>
+// A row's group from column `at` on.  ENDING: rows of bf16 that are not in whole groups, few of them to a thread.  The branches of a last group's
+// elements wait one after the other there, so wide loads that end with the row are put in place instead (fp32's do not wait, and threads with many
+// groups have no registers for it).  us, branches / wide loads: 8313 x 789 16.8 / 14.5, its gradient 28.7 / 19.4, 1689 x 2596 12.2 / 9.8, 22.0 / 16.7, 7353 x
+// 9235's gradient (512 x 3) 192 / 169; with whole groups 8192 x 768 11.0 / 11.7; 512 x 4, 4566 x 13859's 168 / 227; fp32 2999 x 1111's 14.5 / 19.
+template <bool ENDING, typename T>
+__device__ __forceinline__ Raw16 read_group(const T* row, int at, int cols) {
+  if constexpr (ENDING) return read_ending(row + at, cols - at);
+  else return Group16<T>::read(row + at, cols - at);
+}
+template <typename T, bool ENDING>
+__device__ __forceinline__ Raw16 settle_group(Raw16 w, int at, int cols) {
+  return ENDING ? settle<T>(w, cols - at) : w;
+}
+bool takes_ending(int64_t cols) { return cols % 8 != 0 && cols > 8; }
+
+template <typename T, int NT, int V, bool E4M3, bool ENDING>
 __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(LayerNormArgs args) {
   typedef Group16<T> G;
   constexpr int NW = RowGroup<NT>::kWaves, N = G::N;
@@ -49,8 +64,8 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
   [[maybe_unused]] Floats16<N> w_raw[V], b_raw[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    x_raw[j] = G::read(x + at(j), cols - at(j));
-    if (args.residual) r_raw[j] = G::read(r + at(j), cols - at(j));
+    x_raw[j] = read_group<ENDING>(x, at(j), cols);
+    if (args.residual) r_raw[j] = read_group<ENDING>(r, at(j), cols);
   }
   const auto read_weights = [&](int j) {
     w_raw[j].read(args.weight + at(j), cols - at(j));
@@ -62,12 +77,12 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
   }
   float h[V][N];
 #pragma unroll
-  for (int j = 0; j < V; ++j) G::unpack(x_raw[j], h[j]);
+  for (int j = 0; j < V; ++j) G::unpack(settle_group<T, ENDING>(x_raw[j], at(j), cols), h[j]);
   if (args.residual) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       float add[N];
-      G::unpack(r_raw[j], add);
+      G::unpack(settle_group<T, ENDING>(r_raw[j], at(j), cols), add);
 #pragma unroll
       for (int e = 0; e < N; ++e) h[j][e] += add[e];
     }
@@ -185,8 +200,15 @@ template <typename T, int NT, int V>
 hipError_t launch_norm(const LayerNormArgs& args, hipStream_t stream) {
   constexpr int kRows = RowGroup<NT>::kRows;
   const dim3 g(static_cast<uint32_t>((args.rows + kRows - 1) / kRows)), b(RowGroup<NT>::kThreads);
-  if (args.scales) hipLaunchKernelGGL((layer_norm_kernel<T, NT, V, true>), g, b, 0, stream, args);
-  else hipLaunchKernelGGL((layer_norm_kernel<T, NT, V, false>), g, b, 0, stream, args);
+  if constexpr (Group16<T>::N == 8 && V <= 3) {
+    if (takes_ending(args.cols)) {
+      if (args.scales) hipLaunchKernelGGL((layer_norm_kernel<T, NT, V, true, true>), g, b, 0, stream, args);
+      else hipLaunchKernelGGL((layer_norm_kernel<T, NT, V, false, true>), g, b, 0, stream, args);
+      return hipGetLastError();
+    }
+  }
+  if (args.scales) hipLaunchKernelGGL((layer_norm_kernel<T, NT, V, true, false>), g, b, 0, stream, args);
+  else hipLaunchKernelGGL((layer_norm_kernel<T, NT, V, false, false>), g, b, 0, stream, args);
   return hipGetLastError();
 }
 
@@ -235,7 +257,7 @@ struct BackwardRow {
   Raw16 dy[V], h[V], add[V];
   float mean, inv;
 };
-template <typename T, int NT, int V>
+template <typename T, int NT, int V, bool ENDING>
 __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_kernel(LayerNormBackwardArgs args) {
   typedef Group16<T> G;
   constexpr int NW = RowGroup<NT>::kWaves, N = G::N, GROUPS = RowGroup<NT>::kRows;
@@ -259,13 +281,13 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
     to.inv = args.inv_std[row];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      to.dy[j] = G::read(dy + at(j), cols - at(j));
-      to.h[j] = G::read(h + at(j), cols - at(j));
+      to.dy[j] = read_group<ENDING>(dy, at(j), cols);
+      to.h[j] = read_group<ENDING>(h, at(j), cols);
     }
     if (args.dsum) {
       const T* dsum = static_cast<const T*>(args.dsum) + row * args.ldds;
 #pragma unroll
-      for (int j = 0; j < V; ++j) to.add[j] = G::read(dsum + at(j), cols - at(j));
+      for (int j = 0; j < V; ++j) to.add[j] = read_group<ENDING>(dsum, at(j), cols);
     }
   };
   // (where there are registers for two rows)
@@ -279,8 +301,8 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
     float g[V][N], xhat[V][N];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      G::unpack(cur.dy[j], g[j]);
-      G::unpack(cur.h[j], xhat[j]);
+      G::unpack(settle_group<T, ENDING>(cur.dy[j], at(j), cols), g[j]);
+      G::unpack(settle_group<T, ENDING>(cur.h[j], at(j), cols), xhat[j]);
     }
     float sum = 0.0f, dot = 0.0f;
 #pragma unroll
@@ -302,7 +324,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       float add[N] = {};
-      if (args.dsum) G::unpack(cur.add[j], add);
+      if (args.dsum) G::unpack(settle_group<T, ENDING>(cur.add[j], at(j), cols), add);
 #pragma unroll
       for (int e = 0; e < N; ++e) g[j][e] = (g[j][e] - sum - xhat[j][e] * dot) * cur.inv + add[e];
       G::store(dx + at(j), cols - at(j), g[j]);
@@ -470,7 +492,14 @@ BackwardShape backward_shape(int64_t rows, int64_t cols, int n) {
 
 template <typename T, int NT, int V>
 hipError_t launch_backward(const LayerNormBackwardArgs& args, int workgroups, hipStream_t stream) {
-  hipLaunchKernelGGL((layer_norm_backward_kernel<T, NT, V>), dim3(workgroups), dim3(RowGroup<NT>::kThreads), 0, stream, args);
+  const dim3 g(workgroups), b(RowGroup<NT>::kThreads);
+  if constexpr (Group16<T>::N == 8 && V <= 3) {
+    if (takes_ending(args.cols)) {
+      hipLaunchKernelGGL((layer_norm_backward_kernel<T, NT, V, true>), g, b, 0, stream, args);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((layer_norm_backward_kernel<T, NT, V, false>), g, b, 0, stream, args);
   return hipGetLastError();
 }
 
