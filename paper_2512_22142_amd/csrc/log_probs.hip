@@ -490,7 +490,7 @@ constexpr int64_t kLaunchWorkgroups = int64_t{1} << 21;
 // 11.6; with twenty tokens, which every part ranks, 1 x 65536 12.8, 13.5, 12.9, 14.9, 22.5, 1 x 131072 18.8, 16.5, 14.9, 15.4, 20.8,
 // 16 x 262144 30.6, 23.5, 18.3, 17.7, 23.5, 64 x 131072 19.7, 17.3, 16.7, 18.7, 25.6.
 int log_probs_parts(int64_t rows, int64_t cols, int64_t n_top) {
-  if (rows > 64 || cols < (n_top > 0 ? 98304 : 65536)) return 1;
+  if (rows > 64 || cols < 65536) return 1;
   return n_top > 0 || rows > 16 ? 4 : static_cast<int>(std::min<int64_t>(cols / 16384, kMostParts));
 }
 
