@@ -191,13 +191,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// Groups of sixteen bytes of a thread that are taken together, while as many more are on their way.
-constexpr int kTogether = 4;
-
-template <typename T, int NT, bool TOP, bool ENTROPY>
+// U: groups of sixteen bytes of a thread that are taken together, while as many more are on their way.
+template <typename T, int NT, int U, bool TOP, bool ENTROPY>
 __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs args) {
   typedef Group16<T> G;
-  constexpr int N = G::N, NW = NT / 64, U = kTogether;
+  constexpr int N = G::N, NW = NT / 64;
   __shared__ Stats slots[NW];
   const int t = threadIdx.x;
   const int64_t row = blockIdx.x / static_cast<uint32_t>(args.parts);
@@ -389,15 +387,15 @@ __global__ __launch_bounds__(kJoinThreads) void log_probs_join_kernel(LogProbArg
   if (static_cast<int>(threadIdx.x) < args.n_top) put_top(args, row, threadIdx.x, best[threadIdx.x], all, log_s);
 }
 
-template <typename T, int NT>
+template <typename T, int NT, int U = 4>
 hipError_t launch_rows(const LogProbArgs& args, hipStream_t stream) {
   const dim3 g(static_cast<uint32_t>(args.rows * args.parts)), b(NT);
   if (args.n_top > 0) {
-    if (args.entropy) hipLaunchKernelGGL((log_probs_kernel<T, NT, true, true>), g, b, 0, stream, args);
-    else hipLaunchKernelGGL((log_probs_kernel<T, NT, true, false>), g, b, 0, stream, args);
+    if (args.entropy) hipLaunchKernelGGL((log_probs_kernel<T, NT, U, true, true>), g, b, 0, stream, args);
+    else hipLaunchKernelGGL((log_probs_kernel<T, NT, U, true, false>), g, b, 0, stream, args);
   } else {
-    if (args.entropy) hipLaunchKernelGGL((log_probs_kernel<T, NT, false, true>), g, b, 0, stream, args);
-    else hipLaunchKernelGGL((log_probs_kernel<T, NT, false, false>), g, b, 0, stream, args);
+    if (args.entropy) hipLaunchKernelGGL((log_probs_kernel<T, NT, U, false, true>), g, b, 0, stream, args);
+    else hipLaunchKernelGGL((log_probs_kernel<T, NT, U, false, false>), g, b, 0, stream, args);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || args.parts == 1) return e;
@@ -410,10 +408,14 @@ hipError_t launch_rows(const LogProbArgs& args, hipStream_t stream) {
 // 8192 x 8192 27, 27, 29, 65, 146, 8192 x 32000 98, 103, 100, 117, 182, 1 x 8192 5.5, 4.8, 5.0, 6.2, 7.6, 1 x 32000 15, 10, 7.5, 7.3, 8.5,
 // 256 x 32000 15, 10, 8.4, 8.9, 10; with twenty tokens 16384 x 4096 (five) 44, 50, 95, 217, 632, 1100 x 32000 45, 31, 29, 32, 64,
 // 3001 x 50257 fp32 200, 175, 143, 124, 135, 1 x 8192 12.8, 8.9, 7.8, 9.7, 12.1, 1 x 32000 31, 18, 12.9, 11.7, 13.4.
+// Short rows take fewer groups together, since what is not there costs as much as what is: 64 threads, four and as here (one up to 64 groups, two up to
+// 128), 16384 x 1024 bf16 15.3, 9.7 (with eight tokens 36.9, 27.2), 16384 x 512 13.6, 7.2 (34.0, 24.0), 65536 x 128 43, 23.8 (123, 93).
 template <typename T>
 hipError_t launch_of(const LogProbArgs& args, hipStream_t stream) {
   const int64_t groups = (args.chunk + Group16<T>::N - 1) / Group16<T>::N;
   const bool many = args.rows * args.parts > 1024;
+  if (many && groups <= 64) return launch_rows<T, 64, 1>(args, stream);
+  if (many && groups <= 128) return launch_rows<T, 64, 2>(args, stream);
   if (many && groups <= 1024) return launch_rows<T, 64>(args, stream);
   if (groups <= (args.n_top > 0 && !many ? 1024 : 4096) || (many && args.n_top == 0)) return launch_rows<T, 256>(args, stream);
   return launch_rows<T, 512>(args, stream);

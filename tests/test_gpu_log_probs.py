@@ -112,6 +112,16 @@ def test_log_probs(rows, cols, dtype, top):
     check(rows, cols, dtype, min(top, cols), scale=1.0 if top != 1 else 0.7, entropy=top != 20)
 
 
+@pytest.mark.parametrize("rows,cols", [(3000, 1), (1100, 7), (2001, 64), (1500, 255), (1026, 256), (1030, 257), (1500, 512), (1100, 513),
+                                       (1025, 777), (1111, 1024), (1100, 1025)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_many_short_rows(rows, cols, dtype):
+    check(rows, cols, dtype, 0)
+    check(rows, cols, dtype, min(8, cols), shift=1)
+    check(rows, cols, dtype, min(32, cols), pad=3)
+    check(rows, cols, dtype, 1, entropy=False)
+
+
 @pytest.mark.parametrize("pad,shift", [(8, 0), (3, 0), (8, 1), (0, 4), (5, 7)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,cols", [(9, 1000), (3, 131100), (1200, 300)])
