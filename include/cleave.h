@@ -524,8 +524,8 @@ int cleave_linear(cleave_plan* plan, const cleave_linear_args* args, void* hip_s
  * alone while it runs.  whole = 1 serves bf16 calls of which A, B_gate and B_up lie on 16-byte boundaries, K, lda and ldb are
  * multiples of 8, N too with transB = 0, and lda and ldb are below 2^21; whole = 0 serves all.  (8-bit operands: either.)
  * Few rows (M <= 16) read the weights as fast as memory gives them.  Bits, upload, streams: as for cleave_linear.
- * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, an output in another one's or in an operand's place, partials missing,
- * a plan of another kind or type. */
+ * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, an output in another one's or in an operand's place,
+ * partials missing, a plan of another kind or type. */
 typedef struct {
   const void* A;
   const void* B_gate;
@@ -580,8 +580,9 @@ int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_grad_args* ar
  * NaN.  lse, entropy: rows floats, each or NULL.  top_ids, top_logp: rows x n_top (n_top <= 32 and <= cols; 0: both
  * NULL).  Logits of minus infinity are masked tokens: they have no probability.  A row of nothing else has lse and log
  * probabilities of minus infinity and entropy 0.  A row with a NaN or plus infinity is NaN; a NaN's place in its order is that of
- * minus infinity (beside a signaling one the order is open).  workspace: cleave_log_probs_workspace(rows, cols, n_top) floats (may be NULL if that is 0), of this call alone
- * while it runs.  No two outputs in one place.  CLEAVE_EINVAL as above, and more than 2^30 columns; CLEAVE_ELIMIT: n_top > 32. */
+ * minus infinity (beside a signaling one the order is open).  workspace: cleave_log_probs_workspace(rows, cols, n_top) floats (may be NULL
+ * if that is 0), of this call alone while it runs.  No two outputs in one place.  CLEAVE_EINVAL as above, and more than 2^30 columns;
+ * CLEAVE_ELIMIT: n_top > 32. */
 int64_t cleave_log_probs_workspace(int64_t rows, int64_t cols, int64_t n_top);
 int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype, float scale,
                      const int64_t* ids, float* logp, float* lse, float* entropy, int64_t n_top,
@@ -591,7 +592,8 @@ int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, int64_t ld,
  *   dlogits_j = scale (dlogp (1[j = id] - p_j) - dentropy p_j (log p_j + entropy))
  * ids and dlogp (rows floats; a row without a token gets none of it), entropy and dentropy: each pair or neither, one of the two
  * at least.  p is as good as the fp32 lse: to 2^-24 |lse| of itself.  Rows whose lse is below -1e30 (nothing but masked tokens, by minus
- * infinity or by the type's lowest value) get zeros, as masked tokens do.  A row whose id is beyond it is NaN.  dlogits: rows x cols of dtype; may be logits, with its leading dimension.  (Cross-entropy averaged over n tokens:
+ * infinity or by the type's lowest value) get zeros, as masked tokens do.  A row whose id is beyond it is NaN.  dlogits: rows x cols of
+ * dtype; may be logits, with its leading dimension.  (Cross-entropy averaged over n tokens:
  * dlogp = -1 / n.)  CLEAVE_EINVAL as above. */
 int cleave_log_probs_backward(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype,
                               float scale, const int64_t* ids, const float* lse, const float* dlogp,

@@ -1413,13 +1413,13 @@ bool whole_operand(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 
 // over what is not whole), for the direct kernel, where there are rows enough that the way through the general kernel
 // and fp32 partial blocks takes longer.  us, general / laid out, weights stored K x N:
 //   gated, K x N = 4096 x 11007, 512, 800, 1024, 1999, 4096 rows 146 / 169, 242 / 250, 286 / 252, 564 / 371, 1058 / 641; 1000 x 2500, 800, 1999, 4096
-// rows 30 / 30, 45.5 / 42.5, 78 / 70; 2048 x 4100, 800, 1200, 2048 rows 49 / 48, 68 / 73, 112 / 79.  An odd K costs the general kernel more:
-// 4097 x 11008, 200, 400, 800 rows 107 / 91, 151 / 102, 260 / 202 (stored N x K 135 / 147, 192 / 171, 308 / 271), 1001 x 2500, 200, 400, 800
-// rows 18.9 / 21.4, 24.3 / 23.0, 32.3 / 30.0.
+// rows 30 / 30, 45.5 / 42.5, 78 / 70; 2048 x 4100, 800, 1200, 2048 rows 49 / 48, 68 / 73, 112 / 79.  An odd K costs the general kernel
+// more: 4097 x 11008, 200, 400, 800 rows 107 / 91, 151 / 102, 260 / 202 (stored N x K 135 / 147, 192 / 171, 308 / 271), 1001 x 2500, 200,
+// 400, 800 rows 18.9 / 21.4, 24.3 / 23.0, 32.3 / 30.0.
 //   gradient, 4097 x 11008, 200, 400, 800, 2048 rows 60 / 51, 102 / 71, 150 / 150, 299 / 234 (N x K 74 / 78, 125 / 109, 183 / 171, 347 / 262), 2049 x
-// 4096, 200, 400, 800 rows 20.5 / 14.9, 29.0 / 24.8, 37.9 / 31.3.  Rows of the output that are not whole cost the direct kernel's stores more
-// than the join's: 4096 x 11007, 800, 1024, 1999, 4096 rows 149 / 199, 159 / 178, 299 / 293, 572 / 440, 2048 x 4100, 1200, 2048, 4096 rows 49 / 49,
-// 71 / 73, 126 / 91, 2048 x 2500 33 / 40, 49 / 49, 77 / 84, 1000 x 2500, 4096 rows 56 / 71.
+// 4096, 200, 400, 800 rows 20.5 / 14.9, 29.0 / 24.8, 37.9 / 31.3.  Rows of the output that are not whole cost the direct kernel's stores
+// more than the join's: 4096 x 11007, 800, 1024, 1999, 4096 rows 149 / 199, 159 / 178, 299 / 293, 572 / 440, 2048 x 4100, 1200, 2048, 4096
+// rows 49 / 49, 71 / 73, 126 / 91, 2048 x 2500 33 / 40, 49 / 49, 77 / 84, 1000 x 2500, 4096 rows 56 / 71.
 int64_t eights(int64_t n) { return (n + 7) / 8 * 8; }
 bool packs(int64_t M, int64_t N, int64_t K) {
   return M >= (K % 8 != 0 ? 384 : 768) && eights(N) <= kMostPitch && eights(K) <= kMostPitch;
@@ -1472,11 +1472,11 @@ hipError_t pack_operands(Operands& o, int weights, int64_t M, int64_t N, int64_t
 }
 
 // Splits of K for few rows: a workgroup has 64 columns of both weights, so up to 128 of them leave CUs without one; where a
-// row of K has 2 KB or more they are split, to one per CU, and joined by a second launch.  (`k` elements of `bytes`: pairs of e4m3.)  One row, bf16,
-// weights from memory, us, 1, 2, 4, 8 splits: 4096 x 4096 26, 21, 18.7, 19.5, 11008 x 4096 58, 47, 38.3, 39.8, 2048 x 5632 21, 16.1, 17.1, 15.6,
-// 8192 x 8192 76, 51.6, 53.7, 54.7; as they are 4096 x 11008 36.1, 40, 36.9, 38.5, 5120 x 13824 54.4, 61, 62, 58.0, 1024 x 12000 13.9, 17.8, 18.0,
-// 19, 768 x 2048 7.1, 9.3, 9.2, 10.  From the caches, one / as here (4 to 7): 1024 x 64 6.9 / 6.6, 1024 x 4096 8.8 / 9.3 (stored N x K 10.9 / 9.3),
-// 1408 x 1062 10.9 / 9.4, 2016 x 2048 13.4 / 10.3.
+// row of K has 2 KB or more they are split, to one per CU, and joined by a second launch.  (`k` elements of `bytes`: pairs of e4m3.)  One
+// row, bf16, weights from memory, us, 1, 2, 4, 8 splits: 4096 x 4096 26, 21, 18.7, 19.5, 11008 x 4096 58, 47, 38.3, 39.8, 2048 x 5632 21,
+// 16.1, 17.1, 15.6, 8192 x 8192 76, 51.6, 53.7, 54.7; as they are 4096 x 11008 36.1, 40, 36.9, 38.5, 5120 x 13824 54.4, 61, 62, 58.0, 1024
+// x 12000 13.9, 17.8, 18.0, 19, 768 x 2048 7.1, 9.3, 9.2, 10.  From the caches, one / as here (4 to 7): 1024 x 64 6.9 / 6.6, 1024 x 4096
+// 8.8 / 9.3 (stored N x K 10.9 / 9.3), 1408 x 1062 10.9 / 9.4, 2016 x 2048 13.4 / 10.3.
 int64_t gated_few_splits(int64_t N, int64_t k, int64_t bytes) {
   constexpr int64_t kCUs = 256;
   const int64_t groups = (N + 63) / 64;
@@ -1486,15 +1486,17 @@ int64_t gated_few_splits(int64_t N, int64_t k, int64_t bytes) {
   return 1;
 }
 
-// Splits of K for more rows, `k` in elements of two bytes.  Few items of 128 x 128: what takes least by the time of a K step (up to 64 items run as a part a
-// CU, up to 128 as two, up to 256 as one item; K x N's half tiles of 32 columns are half lines, which only whole products have) and of the join
-// (5 us, and both products' partial blocks written and read at 4.5 TB/s).  Otherwise as many as fill the CUs with large tiles.  bf16, weights from
-// memory, us, K x N / N x K, unsplit; 2; 4 splits: 17 rows, 2560 x 5120 (columns x K) 52 / 25; 34 / 27; 19 / 19, 4096 x 11008 91 / 51; 61 / 53; 48 / 40,
-// 5632 x 2048 34 / 18; 17 / 17; 19 / 19, 2816 x 1024 8.5 / 7.0; 10.6 / 10.6; 10.8 / 10.2; 128 rows, 4096 x 4096 39 / 23; 32 / 27; 28 / 27, 2048 x 2048
-// 15.6 / 11.4; 12.3 / 12.6; 14.9 / 14.1; 256 rows, 2048 x 5632 50 / 30; 38 / 34; 27 / 26, 4096 x 2048 27 / 20; 22 / 22; 27 / 25; 1289 rows, 192 x 2880 15.1 /
-// 12.3 and in 4 17.2 / 17.9; large tiles: 256 rows, 11008 x 4096 83 / 78; 67 / 67; 90 / 87, 512 rows, 4096 x 11008 118 / 109; 120 / 119; 96 / 92,
-// 8192 x 4096 86 / 77; 73 / 77; 94 / 94, 5632 x 4096 63 / 62; 67 / 66; 83 / 81, 1159 rows, 1920 x 9920 134 / 131; 152 / 178.
-// e4m3, 17 rows, 1024 x 4096 14.8; 12.0; 9.3, 2048 x 5632 18.8; 14.1; 13.3, 4096 x 4096 15.7; 16.3; 18.2; 256 rows, 2048 x 2048 10.5; 15.8; 20.3.
+// Splits of K for more rows, `k` in elements of two bytes.  Few items of 128 x 128: what takes least by the time of a K step (up to 64
+// items run as a part a CU, up to 128 as two, up to 256 as one item; K x N's half tiles of 32 columns are half lines, which only whole
+// products have) and of the join
+// (5 us, and both products' partial blocks written and read at 4.5 TB/s).  Otherwise as many as fill the CUs with large tiles.  bf16,
+// weights from memory, us, K x N / N x K, unsplit; 2; 4 splits: 17 rows, 2560 x 5120 (columns x K) 52 / 25; 34 / 27; 19 / 19, 4096 x 11008
+// 91 / 51; 61 / 53; 48 / 40, 5632 x 2048 34 / 18; 17 / 17; 19 / 19, 2816 x 1024 8.5 / 7.0; 10.6 / 10.6; 10.8 / 10.2; 128 rows, 4096 x 4096
+// 39 / 23; 32 / 27; 28 / 27, 2048 x 2048 15.6 / 11.4; 12.3 / 12.6; 14.9 / 14.1; 256 rows, 2048 x 5632 50 / 30; 38 / 34; 27 / 26, 4096 x
+// 2048 27 / 20; 22 / 22; 27 / 25; 1289 rows, 192 x 2880 15.1 / 12.3 and in 4 17.2 / 17.9; large tiles: 256 rows, 11008 x 4096 83 / 78; 67
+// / 67; 90 / 87, 512 rows, 4096 x 11008 118 / 109; 120 / 119; 96 / 92, 8192 x 4096 86 / 77; 73 / 77; 94 / 94, 5632 x 4096 63 / 62; 67 /
+// 66; 83 / 81, 1159 rows, 1920 x 9920 134 / 131; 152 / 178. e4m3, 17 rows, 1024 x 4096 14.8; 12.0; 9.3, 2048 x 5632 18.8; 14.1; 13.3, 4096
+// x 4096 15.7; 16.3; 18.2; 256 rows, 2048 x 2048 10.5; 15.8; 20.3.
 int64_t gated_splits(int64_t M, int64_t N, int64_t k, bool pairs) {
   constexpr int64_t kCUs = 256;
   const int64_t items = ((M + 127) / 128) * ((2 * N + 127) / 128), large = ((M + 255) / 256) * ((2 * N + 255) / 256);
@@ -1521,11 +1523,12 @@ int64_t gated_splits(int64_t M, int64_t N, int64_t k, bool pairs) {
   return k >= 2048 * S && whole(S) && large * S >= (M <= 256 ? 160 : 192) ? S : 1;
 }
 
-// Few rows of whole bf16 operands that the direct kernel takes in less time, though its tiles are mostly empty: short K, whose loads it has on
-// their way sooner, where every part has a CU; and long rows of K stored N x K, of which it reads whole lines, where every CU has an item and few
-// have two.  us, weights from memory, few rows / direct, K x N and N x K, one row (16): 768 x 768 7.0, 8.7 (8.1, 10.2) / 6.3, 6.2 (6.4, 6.2), 4096 x 1024 9.3,
-// 9.4 (10.5, 10.3) / 8.5, 7.1 (8.9, 7.2), 4096 x 256 5.0, 5.2 (5.7, 6.0) / 5.2, 5.1 (5.3, 5.1), 5632 x 1024 10.2, 10.9 / 14.5, 9.5, 2816 x 2048 10.9, 11.8 / 12.8,
-// 11.0; 11008 x 8192 80, 86 (84, 97) / 74, 70 (77, 69), 11008 x 4096 43, 48 (44, 50) / 40, 43 (41, 43), 8192 x 8192 60, 65 / 111, 67, 16384 x 4096 57, 57 / 54, 64.
+// Few rows of whole bf16 operands that the direct kernel takes in less time, though its tiles are mostly empty: short K, whose loads it
+// has on their way sooner, where every part has a CU; and long rows of K stored N x K, of which it reads whole lines, where every CU has
+// an item and few have two.  us, weights from memory, few rows / direct, K x N and N x K, one row (16): 768 x 768 7.0, 8.7 (8.1, 10.2) /
+// 6.3, 6.2 (6.4, 6.2), 4096 x 1024 9.3, 9.4 (10.5, 10.3) / 8.5, 7.1 (8.9, 7.2), 4096 x 256 5.0, 5.2 (5.7, 6.0) / 5.2, 5.1 (5.3, 5.1), 5632
+// x 1024 10.2, 10.9 / 14.5, 9.5, 2816 x 2048 10.9, 11.8 / 12.8, 11.0; 11008 x 8192 80, 86 (84, 97) / 74, 70 (77, 69), 11008 x 4096 43, 48
+// (44, 50) / 40, 43 (41, 43), 8192 x 8192 60, 65 / 111, 67, 16384 x 4096 57, 57 / 54, 64.
 enum FewDirect { kFewNever, kFewByColumn, kFewAlways };   // ByColumn: stored N x K
 FewDirect gated_few_direct(int64_t N, int64_t K) {
   constexpr int64_t kCUs = 256;

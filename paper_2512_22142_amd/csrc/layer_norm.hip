@@ -11,9 +11,9 @@
 //   dx = i (g - mean(g) - xhat mean(g xhat)) + dsum;   dw = sum over rows of dy xhat;   db = sum over rows of dy
 //
 // Bound by memory: every row is read once and kept in registers between its statistics, the scaling and the rounding.  A copy of
-// 512 MB runs at 5.4 TB/s here.  bf16 with a residual, the sum stored: 8192 x 768 11.9 us (4.2 TB/s), 4096 x 4096 22.0 (from the caches), 16384 x 5120
-// 129 (5.2), into e4m3 118 (5.0); 1 x 4096 into e4m3 5.6, a launch; gradient with dsum and both launches 16384 x 5120 135 us (5.0 TB/s), fp32 2999 x
-// 1111 14.7 (2.7).
+// 512 MB runs at 5.4 TB/s here.  bf16 with a residual, the sum stored: 8192 x 768 11.0 us (4.6 TB/s), 4096 x 4096 22.0 (from the caches),
+// 16384 x 5120 129 (5.2), into e4m3 118 (5.0); 1 x 4096 into e4m3 5.6, a launch; gradient with dsum and both launches 16384 x 5120 135 us
+// (5.0 TB/s), fp32 2999 x 1111 14.5 (2.8).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -28,10 +28,11 @@ namespace cleave {
 
 namespace {
 
-// A row's group from column `at` on.  ENDING: rows of bf16 that are not in whole groups, few of them to a thread.  The branches of a last group's
-// elements wait one after the other there, so wide loads that end with the row are put in place instead (fp32's do not wait, and threads with many
-// groups have no registers for it).  us, branches / wide loads: 8313 x 789 16.8 / 14.5, its gradient 28.7 / 19.4, 1689 x 2596 12.2 / 9.8, 22.0 / 16.7, 7353 x
-// 9235's gradient (512 x 3) 192 / 169; with whole groups 8192 x 768 11.0 / 11.7; 512 x 4, 4566 x 13859's 168 / 227; fp32 2999 x 1111's 14.5 / 19.
+// A row's group from column `at` on.  ENDING: rows of bf16 that are not in whole groups, few of them to a thread.  The branches of a last
+// group's elements wait one after the other there, so wide loads that end with the row are put in place instead (fp32's do not wait, and
+// threads with many groups have no registers for it).  us, branches / wide loads: 8313 x 789 16.8 / 14.5, its gradient 28.7 / 19.4, 1689 x
+// 2596 12.2 / 9.8, 22.0 / 16.7, 7353 x 9235's gradient (512 x 3) 192 / 169; with whole groups 8192 x 768 11.0 / 11.7; 512 x 4, 4566 x
+// 13859's 168 / 227; fp32 2999 x 1111's 14.5 / 19.
 template <bool ENDING, typename T>
 __device__ __forceinline__ Raw16 read_group(const T* row, int at, int cols) {
   if constexpr (ENDING) return read_ending(row + at, cols - at);
@@ -222,11 +223,12 @@ hipError_t launch_norm_fit(const LayerNormArgs& args, int64_t v, hipStream_t str
 }
 
 // Which threads share a row: a wave where it holds a narrow one and there are many, as few more as hold a wider one, many for few rows,
-// whose latency counts.  us, threads x groups, bf16 with a residual: 8192 x 768 64 x 2 11.9, 128 x 1 12.1, 256 x 1 17.2; 16384 x 5120 into 8
-// bits 64 x 10 192, 128 x 5 125, 256 x 3 118, 512 x 2 137, 1024 x 1 185, into bf16 154, 134, 129, 125, 149; 4096 x 4096 128 x 4 23.0, 256 x 2 21.9,
-// 1024 x 1 33; 20000 x 1000 fp32 64 x 4 65, 256 x 1 58; 200 x 9000 256 x 5 7.1, 1024 x 2 6.6; 1 x 768 64 x 2 5.6, 1024 x 1 4.3.  Rows of a head's
-// width, without a residual, 64 x 1, 16 x 1, 8 x 1: 262144 x 64 86, 22.2, 14.0 (4.8 TB/s), 16 x 64 3.0, 2.8, 2.4; 131072 x 128 43, 13.6, 8 x 2 13.4; 65536 x
-// 256 24.4, 16 x 2 13.6, 8 x 4 14.6; 300 x 128 3.1, 2.6, 8 x 2 3.0; fp32 131072 x 128 33.8, 16 x 2 21.2.
+// whose latency counts.  us, threads x groups, bf16 with a residual: 8192 x 768 64 x 2 11.9, 128 x 1 12.1, 256 x 1 17.2; 16384 x 5120 into
+// 8 bits 64 x 10 192, 128 x 5 125, 256 x 3 118, 512 x 2 137, 1024 x 1 185, into bf16 154, 134, 129, 125, 149; 4096 x 4096 128 x 4 23.0,
+// 256 x 2 21.9, 1024 x 1 33; 20000 x 1000 fp32 64 x 4 65, 256 x 1 58; 200 x 9000 256 x 5 7.1, 1024 x 2 6.6; 1 x 768 64 x 2 5.6, 1024 x 1
+// 4.3.  Rows of a head's width, without a residual, 64 x 1, 16 x 1, 8 x 1: 262144 x 64 86, 22.2, 14.0 (4.8 TB/s), 16 x 64 3.0, 2.8, 2.4;
+// 131072 x 128 43, 13.6, 8 x 2 13.4; 65536 x 256 24.4, 16 x 2 13.6, 8 x 4 14.6; 300 x 128 3.1, 2.6, 8 x 2 3.0; fp32 131072 x 128 33.8, 16
+// x 2 21.2.
 template <typename T>
 hipError_t launch_norm_of(const LayerNormArgs& args, hipStream_t stream) {
   const int64_t groups = (args.cols + Group16<T>::N - 1) / Group16<T>::N;
@@ -419,8 +421,8 @@ __global__ __launch_bounds__(kLongThreads) void layer_norm_backward_long_kernel(
   }
 }
 
-// The rows of partial sums, in a fixed order: 64 columns to a workgroup, sixteen bytes to a thread, 64 rows at a time.  (What lies between a
-// half's end and the next quad is read and not used.)
+// The rows of partial sums, in a fixed order: 64 columns to a workgroup, sixteen bytes to a thread, 64 rows at a time.  (What lies between
+// a half's end and the next quad is read and not used.)
 constexpr int kJoinThreads = 1024, kJoinCols = 64;
 __global__ __launch_bounds__(kJoinThreads) void layer_norm_join_kernel(const float* in, int rows, int64_t first, int64_t cols,
                                                                        float* dweight, float* dbias) {
@@ -456,16 +458,17 @@ __global__ __launch_bounds__(kJoinThreads) void layer_norm_join_kernel(const flo
 }
 
 // Threads of a row, groups of sixteen bytes of each, and workgroups: what the CUs hold at a time, so that a workgroup's rows
-// share one row of partial sums.  Narrow rows are a wave's, four to a workgroup, without a barrier, or eight or sixteen lanes'.  us, the first launch alone: 16384 x 5120 bf16
-// with dsum (640 groups) 1024 x 1 (threads x groups) 155, 512 x 2 158, 128 x 5 145, 256 x 3 133, and in 256, 512, 768, 1024 workgroups > 160, 133,
-// 154, 140; 2999 x 1111 fp32 (278) 512 x 1 12.2, 256 x 2 10.8, 64 x 5 11.0, with half the rows of partial sums; 8192 x 768 bf16 (96) 256 x 1 17.2, 128 x 1 in
-// 2048 13.1, 64 x 2 in 512 13.7; 8192 x 4096 (512) 1024 x 1 71, 256 x 2 50.5, 512 x 1 49.9; 30000 x 256 (32) 128 x 1 28, 64 x 1 in 1024 17.4; 1000 x 8192
-// 512 x 2 in 256, 512 16.8, 21.4; 8192 x 1536 64 x 3 20.4, 256 x 1 in 512, 768, 1024 23.5, 20.1, 19.8.
-// With the next row on its way 1024 threads have too few registers for two groups of bf16: 2048 x 12288 (1536) 1024 x 2 98, 512 x 3 44; 2048 x 16384
-// (2048), without the next row, 1024 x 2 114, 512 x 4 67 (with it 132).  Wider rows are fp32's only: 1024 x 8832 (2208) read twice (the long kernel) 63,
-// 512 x 5 27.4, 1024 x 3 32.3; 1024 x 12288 of fp32 85, 512 x 6 65, 1024 x 3 46; 1024 x 16384 108, 512 x 8 78, 1024 x 4 89.
-// Rows of a head's width, without dsum, 64 x 1 in 1024, 16 x 1 in 512, 1024, 8 x 1 in 512, 1024: 262144 x 64 100, 36.2, 26.8, 19.4, 18.1 (5.2 TB/s),
-// 32768 x 64 16.4, 7.0, 6.3, 5.0, 5.3; 65536 x 100 47, 20.9, 15.1, 8 x 2 14.5, 17.1; 65536 x 256 30.3, 16 x 2 19.2, 21.1.
+// share one row of partial sums.  Narrow rows are a wave's, four to a workgroup, without a barrier, or eight or sixteen lanes'.  us, the
+// first launch alone: 16384 x 5120 bf16 with dsum (640 groups) 1024 x 1 (threads x groups) 155, 512 x 2 158, 128 x 5 145, 256 x 3 133, and
+// in 256, 512, 768, 1024 workgroups > 160, 133, 154, 140; 2999 x 1111 fp32 (278) 512 x 1 12.2, 256 x 2 10.8, 64 x 5 11.0, with half the
+// rows of partial sums; 8192 x 768 bf16 (96) 256 x 1 17.2, 128 x 1 in 2048 13.1, 64 x 2 in 512 13.7; 8192 x 4096 (512) 1024 x 1 71, 256 x
+// 2 50.5, 512 x 1 49.9; 30000 x 256 (32) 128 x 1 28, 64 x 1 in 1024 17.4; 1000 x 8192 512 x 2 in 256, 512 16.8, 21.4; 8192 x 1536 64 x 3
+// 20.4, 256 x 1 in 512, 768, 1024 23.5, 20.1, 19.8. With the next row on its way 1024 threads have too few registers for two groups of
+// bf16: 2048 x 12288 (1536) 1024 x 2 98, 512 x 3 44; 2048 x 16384
+// (2048), without the next row, 1024 x 2 114, 512 x 4 67 (with it 132).  Wider rows are fp32's only: 1024 x 8832 (2208) read twice (the
+// long kernel) 63, 512 x 5 27.4, 1024 x 3 32.3; 1024 x 12288 of fp32 85, 512 x 6 65, 1024 x 3 46; 1024 x 16384 108, 512 x 8 78, 1024 x 4
+// 89. Rows of a head's width, without dsum, 64 x 1 in 1024, 16 x 1 in 512, 1024, 8 x 1 in 512, 1024: 262144 x 64 100, 36.2, 26.8, 19.4,
+// 18.1 (5.2 TB/s), 32768 x 64 16.4, 7.0, 6.3, 5.0, 5.3; 65536 x 100 47, 20.9, 15.1, 8 x 2 14.5, 17.1; 65536 x 256 30.3, 16 x 2 19.2, 21.1.
 struct BackwardShape {
   int threads, groups, workgroups;
 };

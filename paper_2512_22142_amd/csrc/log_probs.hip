@@ -12,8 +12,9 @@
 // value or a lower column, so no two are equal.  The k-th largest of the keys of groups of threads is a bound that at least k elements
 // reach, and only the strips of the few threads that reach it hold such: those are read again, and their elements ranked.
 //
-// Bound by memory, one read of the logits (the gradient: one read and one write): 8192 x 32000 bf16 with entropy 100 us (5.2 TB/s), the gradient
-// 180 (5.8), the one behind the other 275-281 (the second finds a part of the logits in the Infinity Cache); 3001 x 50257 fp32 with five tokens 109
+// Bound by memory, one read of the logits (the gradient: one read and one write): 8192 x 32000 bf16 with entropy 100 us (5.2 TB/s), the
+// gradient 180 (5.8), the one behind the other 275-281 (the second finds a part of the logits in the Infinity Cache); 3001 x 50257 fp32
+// with five tokens 109
 // (5.5 TB/s).  One row of 32000 with twenty tokens 10.7, of them 3 a launch, 4 the row, the rest the order.
 #include <hip/hip_runtime.h>
 
@@ -408,8 +409,9 @@ hipError_t launch_rows(const LogProbArgs& args, hipStream_t stream) {
 // 8192 x 8192 27, 27, 29, 65, 146, 8192 x 32000 98, 103, 100, 117, 182, 1 x 8192 5.5, 4.8, 5.0, 6.2, 7.6, 1 x 32000 15, 10, 7.5, 7.3, 8.5,
 // 256 x 32000 15, 10, 8.4, 8.9, 10; with twenty tokens 16384 x 4096 (five) 44, 50, 95, 217, 632, 1100 x 32000 45, 31, 29, 32, 64,
 // 3001 x 50257 fp32 200, 175, 143, 124, 135, 1 x 8192 12.8, 8.9, 7.8, 9.7, 12.1, 1 x 32000 31, 18, 12.9, 11.7, 13.4.
-// Short rows take fewer groups together, since what is not there costs as much as what is: 64 threads, four and as here (one up to 64 groups, two up to
-// 128), 16384 x 1024 bf16 15.3, 9.7 (with eight tokens 36.9, 27.2), 16384 x 512 13.6, 7.2 (34.0, 24.0), 65536 x 128 43, 23.8 (123, 93).
+// Short rows take fewer groups together, since what is not there costs as much as what is: 64 threads, four and as here (one up to 64
+// groups, two up to 128), 16384 x 1024 bf16 15.3, 9.7 (with eight tokens 36.9, 27.2), 16384 x 512 13.6, 7.2 (34.0, 24.0), 65536 x 128 43,
+// 23.8 (123, 93).
 template <typename T>
 hipError_t launch_of(const LogProbArgs& args, hipStream_t stream) {
   const int64_t groups = (args.chunk + Group16<T>::N - 1) / Group16<T>::N;
