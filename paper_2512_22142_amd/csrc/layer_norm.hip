@@ -12,7 +12,7 @@
 //
 // Bound by memory: every row is read once and kept in registers between its statistics, the scaling and the rounding.  A copy of
 // 512 MB runs at 5.4 TB/s here.  bf16 with a residual, the sum stored: 8192 x 768 11.0 us (4.6 TB/s), 4096 x 4096 22.0 (from the caches),
-// 16384 x 5120 129 (5.2), into e4m3 118 (5.0); 1 x 4096 into e4m3 5.6, a launch; gradient with dsum and both launches 16384 x 5120 135 us
+// 16384 x 5120 129 (5.2), into e4m3 118 (5.0); 1 x 4096 into e4m3 3.9, a launch; gradient with dsum and both launches 16384 x 5120 135 us
 // (5.0 TB/s), fp32 2999 x 1111 14.5 (2.8).
 #include <hip/hip_runtime.h>
 
@@ -222,11 +222,12 @@ hipError_t launch_norm_fit(const LayerNormArgs& args, int64_t v, hipStream_t str
   return launch_norm<T, NT, V>(args, stream);
 }
 
-// Which threads share a row: a wave where it holds a narrow one and there are many, as few more as hold a wider one, many for few rows,
-// whose latency counts.  us, threads x groups, bf16 with a residual: 8192 x 768 64 x 2 11.9, 128 x 1 12.1, 256 x 1 17.2; 16384 x 5120 into
+// Which threads share a row: as few lanes or waves as hold it in one or a few groups each; for few rows, whose latency counts, in
+// one group each up to 512 threads (more waves wait longer for each other at each sum).  us, threads x groups, bf16 with a residual: 8192 x 768 64 x 2 11.9, 128 x 1 12.1, 256 x 1 17.2; 16384 x 5120 into
 // 8 bits 64 x 10 192, 128 x 5 125, 256 x 3 118, 512 x 2 137, 1024 x 1 185, into bf16 154, 134, 129, 125, 149; 4096 x 4096 128 x 4 23.0,
-// 256 x 2 21.9, 1024 x 1 33; 20000 x 1000 fp32 64 x 4 65, 256 x 1 58; 200 x 9000 256 x 5 7.1, 1024 x 2 6.6; 1 x 768 64 x 2 5.6, 1024 x 1
-// 4.3.  Rows of a head's width, without a residual, 64 x 1, 16 x 1, 8 x 1: 262144 x 64 86, 22.2, 14.0 (4.8 TB/s), 16 x 64 3.0, 2.8, 2.4;
+// 256 x 2 21.9, 1024 x 1 33; 20000 x 1000 fp32 64 x 4 65, 256 x 1 58; one row, 128 x 1, 256 x 1, 512 x 1, 1024 x 1: 1024 columns 2.8, 3.3, 3.4, 4.3, into
+// 8 bits 3.3, 3.9, 4.2, 5.4; 256 x 2, 512 x 1, 1024 x 1: 4096 3.3, 3.1, 4.1, into 8 bits 4.0, 3.9, 5.4; 512 x 2, 1024 x 1: 8192 3.7, 4.0,
+// 250 of them 5.1, 5.5; 512 x 4, 1024 x 2: 16384 5.3, 5.2, into 8 bits 6.4, 6.7.  Rows of a head's width, without a residual, 64 x 1, 16 x 1, 8 x 1: 262144 x 64 86, 22.2, 14.0 (4.8 TB/s), 16 x 64 3.0, 2.8, 2.4;
 // 131072 x 128 43, 13.6, 8 x 2 13.4; 65536 x 256 24.4, 16 x 2 13.6, 8 x 4 14.6; 300 x 128 3.1, 2.6, 8 x 2 3.0; fp32 131072 x 128 33.8, 16
 // x 2 21.2.
 template <typename T>
@@ -237,8 +238,12 @@ hipError_t launch_norm_of(const LayerNormArgs& args, hipStream_t stream) {
   if (groups <= 32) return launch_norm<T, 16, 2>(args, stream);
   if (groups <= 64) return launch_norm<T, 64, 1>(args, stream);
   if (groups <= 3 * 64 && args.rows > 1024) return launch_norm_fit<T, 64, 3>(args, (groups + 63) / 64, stream);
+  if (groups <= 128 && args.rows <= 1024) return launch_norm<T, 128, 1>(args, stream);
   if (groups <= 8 * 256 && args.rows > 256) return launch_norm_fit<T, 256, 8>(args, (groups + 255) / 256, stream);
-  if (groups <= 4 * 1024) return launch_norm_fit<T, 1024, 4>(args, (groups + 1023) / 1024, stream);
+  if (groups <= 256) return launch_norm<T, 256, 1>(args, stream);
+  if (groups <= 4 * 512) return launch_norm_fit<T, 512, 4>(args, (groups + 511) / 512, stream);
+  if (groups <= 3 * 1024) return launch_norm<T, 1024, 3>(args, stream);
+  if (groups <= 4 * 1024) return launch_norm<T, 1024, 4>(args, stream);
   const dim3 g(static_cast<uint32_t>(args.rows)), b(kLongThreads);
   if (args.scales) hipLaunchKernelGGL((layer_norm_long_kernel<T, true>), g, b, 0, stream, args);
   else hipLaunchKernelGGL((layer_norm_long_kernel<T, false>), g, b, 0, stream, args);

@@ -154,6 +154,17 @@ def test_8_bit_operands_with_a_split_inner_dimension(M, N, K, out):
         check(M, N, K, E4M3, out, **kw)
 
 
+@pytest.mark.parametrize("M,N,K,splits", [(46, 1280, 4800, 3), (17, 2560, 5120, 4), (130, 200, 2048, 4), (40, 2048, 2304, 2), (200, 11008, 4096, 2),
+                                          (450, 4096, 8192, 4), (17, 2816, 1024, 1), (300, 4096, 2048, 1)])
+@pytest.mark.parametrize("transB", [0, 1])
+def test_splits_of_the_inner_dimension(M, N, K, splits, transB):
+    plan = cleave.plan_gated(M, N, K, BF16)
+    assert cleave.gated_workspace(plan, whole=True) == (splits * 2 * M * N if splits > 1 else 0)
+    check(M, N, K, transB=transB, keep=True)
+    check(M, N, K, transB=transB, act="gelu_tanh", bias=True, out=F32, merged=True)
+    check(M, N, K, transB=transB, act="relu", pad=3, shift=1)
+
+
 FEW = [(1, 11008, 256), (1, 64, 64), (2, 1, 16), (16, 1000, 512), (5, 4096, 4096), (3, 300, 4096), (16, 77, 8192), (7, 9000, 48)]
 
 

@@ -14,7 +14,7 @@ SPARE = 70                         # sevens behind every output
 # every number of groups that a thread holds, whole and ragged; rows for waves of their own, few and many
 SIZES = [(1, 1), (3, 64), (2, 511), (5, 512), (6, 513), (4, 1001), (2, 2048), (3, 2056), (7, 4096), (2, 5120), (2, 8200),
          (3, 16384), (1, 16392), (2, 32768), (1, 40000), (1500, 100), (1500, 768), (1100, 1111), (1030, 2048), (300, 3000), (300, 5120),
-         (260, 9000), (260, 16384)]
+         (260, 9000), (260, 16384), (3, 700), (1000, 1000), (2, 1600), (9, 6000), (256, 9000), (2, 20000), (2, 11111)]
 
 
 def matrix(rows, cols, dtype, seed, pad=0, shift=0, std=1.0, mean=0.0):
