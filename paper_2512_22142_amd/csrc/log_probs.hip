@@ -425,6 +425,57 @@ hipError_t launch_of(const LogProbArgs& args, hipStream_t stream) {
 
 // ---- gradient ------------------------------------------------------------------
 
+// Far rows.  p = e^(l - lse) is as good as the fp32 lse, which holds the less of log s the further it lies from zero: of a row masked by -1e9
+// nothing.  From |lse| = kNear on, where it leaves p good to 2^-16, m and s are taken again from the row and p = e^(a (x - m) - log s).  All
+// rows near, all far, us: 8192 x 32000 bf16 187, 373, fp32 386, 634; 16384 x 1024 bf16 16.1, 19.6; 1 x 32000 bf16 4.2, 14.6.
+constexpr float kNear = 256.0f;
+
+// The gradient of such a row by NT threads, one workgroup's or a wave's.  A thread has the same groups in both passes, so that dx may lie over
+// x.  give(log p, column): the gradient.
+template <typename T, int NT, typename Give>
+__device__ __forceinline__ void backward_far(const LogProbBackwardArgs& args, int64_t row, int t, Give give) {
+  typedef Group16<T> G;
+  constexpr int N = G::N, NW = RowGroup<NT>::kWaves;
+  __shared__ float slots[2][NW];
+  const T* x = static_cast<const T*>(args.logits) + row * args.ld;
+  T* dx = static_cast<T*>(args.dlogits) + row * args.ldd;
+  const int cols = static_cast<int>(args.cols);
+  const auto walk = [&](auto visit) {   // visit(values, column of the first, how many there are)
+#pragma unroll 1
+    for (int at = t * N; at < cols; at += NT * N) {
+      float v[N];
+      G::unpack(G::read(x + at, cols - at), v);
+      visit(v, at, cols - at);
+    }
+  };
+  const auto larger = [](float a, float b) { return __builtin_fmaxf(a, b); };
+  const auto power = [&](float d) { return __builtin_amdgcn_exp2f(kLog2e * (args.scale * d)); };
+  float own = -kInf, s = 0.0f;
+  walk([&](float (&v)[N], int, int left) {
+    float most = v[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) {
+      if (e >= left) v[e] = -kInf;
+      most = larger(most, v[e]);
+    }
+    if (most > own) {
+      s *= power(own - most);
+      own = most;
+    }
+    const float from = own > -kInf ? own : 0.0f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) s += power(v[e] - from);
+  });
+  const float m = join_waves<NW>(wave_join(own, larger), slots[0], larger);
+  if (own != m) s *= power(own - m);   // (an infinite one stays: its sum is NaN)
+  const float log_s = __builtin_logf(group_total<NT>(s, slots[1]));
+  walk([&](float (&v)[N], int at, int left) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = give(args.scale * (v[e] - m) - log_s, at + e);
+    G::store(dx + at, left, v);
+  });
+}
+
 // A thread takes U groups of sixteen bytes of a row, a workgroup of NT threads a part of one (a wave a short row of its own, four
 // to a workgroup).  STREAM: non-temporal stores.  An output that the Infinity Cache cannot hold pushes the logits out of it, and the
 // next launch waits for its write-backs; a smaller one is read from there next.  8192 x 32000 bf16 behind log_probs, both, us: plain 310,
@@ -462,6 +513,13 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void log_probs_backward_ker
     h = args.entropy[row];
     dh = args.dentropy[row];
   }
+  const auto share = [&](float logp) { return -__builtin_amdgcn_exp2f(kLog2e * logp) * (d + dh * (floored(logp) + h)); };
+  if (__builtin_fabsf(given) >= kNear && !none) {   // (the same for all threads of a row)
+    // one of the row's workgroups, chosen so that those of many rows lie on all XCDs (always the first: on every parts-th)
+    if (part == static_cast<int>((blockIdx.x / static_cast<uint32_t>(args.parts)) / 4 % static_cast<uint32_t>(args.parts)))
+      backward_far<T, NT>(args, row, t, [&](float logp, int j) { return args.scale * (share(logp) + (j == id ? d : 0.0f)); });
+    return;
+  }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int at = first + (u * NT + t) * N;
@@ -469,10 +527,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void log_probs_backward_ker
     float v[N];
     G::unpack(raw[u], v);
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float logp = __builtin_fmaf(args.scale, v[e], -lse), p = __builtin_amdgcn_exp2f(kLog2e * logp);
-      v[e] = -p * (d + dh * (floored(logp) + h));
-    }
+    for (int e = 0; e < N; ++e) v[e] = share(__builtin_fmaf(args.scale, v[e], -lse));
     if (id >= at && id < at + N && !none) {
 #pragma unroll
       for (int e = 0; e < N; ++e) v[e] += at + e == id ? d : 0.0f;
