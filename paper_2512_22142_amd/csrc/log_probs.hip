@@ -429,9 +429,12 @@ hipError_t launch_of(const LogProbArgs& args, hipStream_t stream) {
 // nothing.  From |lse| = kNear on, where it leaves p good to 2^-16, m and s are taken again from the row and p = e^(a (x - m) - log s).  All
 // rows near, all far, us: 8192 x 32000 bf16 187, 373, fp32 386, 634; 16384 x 1024 bf16 16.1, 19.6; 1 x 32000 bf16 4.2, 14.6.
 constexpr float kNear = 256.0f;
+// Whose logits all lie below this has no token left: they are masked, by minus infinity or by the type's lowest value.  (Such rows are far at
+// any scale from kLeastScale on; below it all are taken as far.)
+constexpr float kMasked = -1e30f, kLeastScale = 0x1p-80f;
 
 // The gradient of such a row by NT threads, one workgroup's or a wave's.  A thread has the same groups in both passes, so that dx may lie over
-// x.  give(log p, column): the gradient.
+// x.  give(log p, column, whether the row has tokens left): the gradient.
 template <typename T, int NT, typename Give>
 __device__ __forceinline__ void backward_far(const LogProbBackwardArgs& args, int64_t row, int t, Give give) {
   typedef Group16<T> G;
@@ -471,7 +474,7 @@ __device__ __forceinline__ void backward_far(const LogProbBackwardArgs& args, in
   const float log_s = __builtin_logf(group_total<NT>(s, slots[1]));
   walk([&](float (&v)[N], int at, int left) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = give(args.scale * (v[e] - m) - log_s, at + e);
+    for (int e = 0; e < N; ++e) v[e] = give(args.scale * (v[e] - m) - log_s, at + e, !(m < kMasked));
     G::store(dx + at, left, v);
   });
 }
@@ -499,10 +502,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void log_probs_backward_ker
     const int at = first + (u * NT + t) * N;
     raw[u] = G::read(x + at, max(cols - at, 0));
   }
-  const float given = args.lse[row];
-  // Nothing left but masked tokens, by minus infinity or by the type's lowest value (of which lse holds no sum): none has any of it.
-  const bool none = given < -1e30f;
-  const float lse = none ? kInf : given;
+  const float lse = args.lse[row];
   float d = 0.0f, dh = 0.0f, h = 0.0f;
   int64_t id = -1;
   if (args.ids) {
@@ -514,10 +514,13 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void log_probs_backward_ker
     dh = args.dentropy[row];
   }
   const auto share = [&](float logp) { return -__builtin_amdgcn_exp2f(kLog2e * logp) * (d + dh * (floored(logp) + h)); };
-  if (__builtin_fabsf(given) >= kNear && !none) {   // (the same for all threads of a row)
+  if (__builtin_fabsf(lse) >= args.near) {   // (the same for all threads of a row)
     // one of the row's workgroups, chosen so that those of many rows lie on all XCDs (always the first: on every parts-th)
     if (part == static_cast<int>((blockIdx.x / static_cast<uint32_t>(args.parts)) / 4 % static_cast<uint32_t>(args.parts)))
-      backward_far<T, NT>(args, row, t, [&](float logp, int j) { return args.scale * (share(logp) + (j == id ? d : 0.0f)); });
+      backward_far<T, NT>(args, row, t, [&](float logp, int j, bool left) {
+        if (!left) return id >= cols ? __builtin_nanf("") : 0.0f;
+        return args.scale * (share(logp) + (j == id ? d : 0.0f));
+      });
     return;
   }
 #pragma unroll
@@ -528,7 +531,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void log_probs_backward_ker
     G::unpack(raw[u], v);
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = share(__builtin_fmaf(args.scale, v[e], -lse));
-    if (id >= at && id < at + N && !none) {
+    if (id >= at && id < at + N) {
 #pragma unroll
       for (int e = 0; e < N; ++e) v[e] += at + e == id ? d : 0.0f;
     }
@@ -587,6 +590,7 @@ hipError_t launch_backward(const LogProbBackwardArgs& args, bool stream_out, hip
     LogProbBackwardArgs some = args;
     some.rows = end - row;
     some.parts = static_cast<int>(parts);
+    some.near = args.scale < kLeastScale ? 0.0f : kNear;
     some.logits = static_cast<const T*>(args.logits) + row * args.ld;
     some.dlogits = static_cast<T*>(args.dlogits) + row * args.ldd;
     some.lse += row;

@@ -242,7 +242,7 @@ extern "C" int cleave_log_probs_backward(int64_t rows, int64_t cols, const void*
     return CLEAVE_EINVAL;
   if (!in_place(dlogits, ldd, dtype, logits, ld, dtype, rows)) return CLEAVE_EINVAL;
   if (rows == 0) return CLEAVE_OK;
-  const cleave::LogProbBackwardArgs args{logits, ids, lse, dlogp, entropy, dentropy, dlogits, rows, cols, ld, ldd, scale, 0};
+  const cleave::LogProbBackwardArgs args{logits, ids, lse, dlogp, entropy, dentropy, dlogits, rows, cols, ld, ldd, scale, 0, 0.0f};
   CLEAVE_HIP(cleave::launch_log_probs_backward(args, dtype, static_cast<hipStream_t>(hip_stream)));
   return CLEAVE_OK;
 }

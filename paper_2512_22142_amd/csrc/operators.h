@@ -125,7 +125,8 @@ struct LogProbBackwardArgs {
   void* dlogits;
   int64_t rows, cols, ld, ldd;
   float scale;
-  int parts;               // workgroups of a row (filled in at the launch)
+  int parts;               // workgroups of a row, and the |lse| that far rows begin at (filled in at the launch)
+  float near;
 };
 hipError_t launch_log_probs_backward(const LogProbBackwardArgs& args, int dtype, hipStream_t stream);
 
