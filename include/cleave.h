@@ -592,11 +592,10 @@ int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, int64_t ld,
  *   dlogits_j = scale (dlogp (1[j = id] - p_j) - dentropy p_j (log p_j + entropy))
  * ids and dlogp (rows floats; a row without a token gets none of it), entropy and dentropy: each pair or neither, one of the two
  * at least.  p is good to 2^-16 of itself or better; where |lse| is 256 or more it is taken from the row alone (which is read again,
- * by one workgroup), and lse only says so.  Rows whose logits are all below -1e30 (nothing but
- * masked tokens, by minus infinity or by the type's lowest value; cleave_log_probs still gives the latter even probabilities) get zeros, as
- * masked tokens do.  A row whose id is beyond it is NaN.  dlogits: rows x cols of
- * dtype; may be logits, with its leading dimension.  (Cross-entropy averaged over n tokens:
- * dlogp = -1 / n.)  CLEAVE_EINVAL as above. */
+ * by one workgroup), and lse only says so.  Masked tokens get zeros, however large the given gradients (as long as these are finite), and
+ * so do rows whose logits are all below -1e30 (nothing but masked tokens, by minus infinity or by the type's lowest value; of the
+ * latter cleave_log_probs still gives even probabilities).  A row whose id is beyond it is NaN.  dlogits: rows x cols of dtype; may
+ * be logits, with its leading dimension.  (Cross-entropy averaged over n tokens: dlogp = -1 / n.)  CLEAVE_EINVAL as above. */
 int cleave_log_probs_backward(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype,
                               float scale, const int64_t* ids, const float* lse, const float* dlogp,
                               const float* entropy, const float* dentropy, void* dlogits, int64_t ldd,

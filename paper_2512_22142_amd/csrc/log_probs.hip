@@ -427,11 +427,12 @@ hipError_t launch_of(const LogProbArgs& args, hipStream_t stream) {
 
 // Far rows.  p = e^(l - lse) is as good as the fp32 lse, which holds the less of log s the further it lies from zero: of a row masked by -1e9
 // nothing.  From |lse| = kNear on, where it leaves p good to 2^-16, m and s are taken again from the row and p = e^(a (x - m) - log s).  All
-// rows near, all far, us: 8192 x 32000 bf16 187, 373, fp32 386, 634; 16384 x 1024 bf16 16.1, 19.6; 1 x 32000 bf16 4.2, 14.6.
+// rows near, all far, us: 8192 x 32000 bf16 187, 378, fp32 386, 635; 16384 x 1024 bf16 16.2, 20.0; 1 x 32000 bf16 4.2, 16.1.
 constexpr float kNear = 256.0f;
 // Whose logits all lie below this has no token left: they are masked, by minus infinity or by the type's lowest value.  (Such rows are far at
 // any scale from kLeastScale on; below it all are taken as far.)
 constexpr float kMasked = -1e30f, kLeastScale = 0x1p-80f;
+constexpr float kLargest = 0x1p100f;
 
 // The gradient of such a row by NT threads, one workgroup's or a wave's.  A thread has the same groups in both passes, so that dx may lie over
 // x.  give(log p, column, whether the row has tokens left): the gradient.
@@ -513,13 +514,14 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void log_probs_backward_ker
     h = args.entropy[row];
     dh = args.dentropy[row];
   }
-  const auto share = [&](float logp) { return -__builtin_amdgcn_exp2f(kLog2e * logp) * (d + dh * (floored(logp) + h)); };
-  if (__builtin_fabsf(lse) >= args.near) {   // (the same for all threads of a row)
+  // (the same for all threads of a row; beyond kLargest the sum that p multiplies may be infinite, and NaN times a masked token's p)
+  if (__builtin_fabsf(lse) >= args.near || __builtin_fabsf(dh) >= kLargest || __builtin_fabsf(d) >= kLargest) {
     // one of the row's workgroups, chosen so that those of many rows lie on all XCDs (always the first: on every parts-th)
     if (part == static_cast<int>((blockIdx.x / static_cast<uint32_t>(args.parts)) / 4 % static_cast<uint32_t>(args.parts)))
       backward_far<T, NT>(args, row, t, [&](float logp, int j, bool left) {
         if (!left) return id >= cols ? __builtin_nanf("") : 0.0f;
-        return args.scale * (share(logp) + (j == id ? d : 0.0f));
+        const float p = __builtin_amdgcn_exp2f(kLog2e * logp);
+        return args.scale * ((j == id ? d : 0.0f) - (p * d + dh * (p * (floored(logp) + h))));
       });
     return;
   }
@@ -530,7 +532,10 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void log_probs_backward_ker
     float v[N];
     G::unpack(raw[u], v);
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = share(__builtin_fmaf(args.scale, v[e], -lse));
+    for (int e = 0; e < N; ++e) {
+      const float logp = __builtin_fmaf(args.scale, v[e], -lse), p = __builtin_amdgcn_exp2f(kLog2e * logp);
+      v[e] = -p * (d + dh * (floored(logp) + h));
+    }
     if (id >= at && id < at + N) {
 #pragma unroll
       for (int e = 0; e < N; ++e) v[e] += at + e == id ? d : 0.0f;
