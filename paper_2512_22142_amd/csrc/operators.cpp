@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <limits>
 
 #include "kernels.h"
@@ -40,6 +41,16 @@ struct Matrices {
 // thread.  (Rows of another pitch or type would lie over rows that others have yet to read.)
 bool in_place(const void* out, int64_t ldo, int out_dtype, const void* in, int64_t ldi, int dtype, int64_t rows) {
   return !out || out != in || rows == 0 || (out_dtype == dtype && (ldo == ldi || rows == 1));
+}
+
+// Whether none of `outs` is another one of them, or one of `ins`.  (Null: not there.)
+typedef std::initializer_list<const void*> Places;
+bool apart(Places outs, Places ins) {
+  for (const void* const* a = outs.begin(); a != outs.end(); ++a) {
+    if (!*a) continue;
+    if (std::find(a + 1, outs.end(), *a) != outs.end() || std::find(ins.begin(), ins.end(), *a) != ins.end()) return false;
+  }
+  return true;
 }
 
 bool float_dtype(int dtype) { return dtype == CLEAVE_F32 || dtype == CLEAVE_BF16; }
@@ -122,7 +133,7 @@ extern "C" int cleave_layer_norm(int64_t rows, int64_t cols, const void* x, int6
   if (!m.ok) return CLEAVE_EINVAL;
   if (!in_place(y, ldy, y_dtype, x, ldx, dtype, rows) || !in_place(y, ldy, y_dtype, residual, ldr, dtype, rows) ||
       !in_place(sum_out, lds, dtype, x, ldx, dtype, rows) || !in_place(sum_out, lds, dtype, residual, ldr, dtype, rows) ||
-      (rows > 0 && y == sum_out) || (rows > 0 && mean && mean == inv_std))
+      (rows > 0 && !(apart({y, sum_out, scales, mean, inv_std}, {weight, bias}) && apart({scales, mean, inv_std}, {x, residual}))))
     return CLEAVE_EINVAL;
   if (rows == 0) return CLEAVE_OK;
   const cleave::LayerNormArgs args{x,   residual, weight, bias, y,   scales, sum_out, mean,
@@ -152,9 +163,10 @@ extern "C" int cleave_layer_norm_backward(int64_t rows, int64_t cols, const void
   m.add_vector(dweight);
   m.add_vector(dbias, true);
   m.add_vector(workspace);
-  if (!m.ok || dweight == dbias) return CLEAVE_EINVAL;
+  if (!m.ok || !apart({dweight, dbias, workspace}, {})) return CLEAVE_EINVAL;
   if (!in_place(dx, lddx, dtype, dy, lddy, dtype, rows) || !in_place(dx, lddx, dtype, h, ldh, dtype, rows) ||
-      !in_place(dx, lddx, dtype, dsum, ldds, dtype, rows))
+      !in_place(dx, lddx, dtype, dsum, ldds, dtype, rows) ||
+      (rows > 0 && !(apart({dx, dweight, dbias}, {}) && apart({dx, workspace}, {weight, mean, inv_std}) && apart({workspace}, {dy, h, dsum}))))
     return CLEAVE_EINVAL;
   const cleave::LayerNormBackwardArgs args{dy, h,       dsum,  weight, mean, inv_std, dx,   workspace,
                                            dweight, dbias, rows,   cols, lddy,    ldh, ldds, lddx};

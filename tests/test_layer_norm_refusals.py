@@ -51,3 +51,20 @@ def test_workspace():
     assert workspace(-1, 8) == EINVAL and workspace(8, 0) == EINVAL and workspace(2 ** 31, 8) == EINVAL and workspace(8, 2 ** 31) == EINVAL
     for rows, cols in ((0, 8), (1, 1), (5000, 4096), (2 ** 31 - 1, 2 ** 31 - 1)):
         assert workspace(rows, cols) >= 2 * cols and workspace(rows, cols) % 8 == 0
+
+
+@pytest.mark.parametrize("change", [
+    dict(mean=9 * P), dict(inv=9 * P), dict(mean=3 * P), dict(inv=4 * P), dict(scales=3 * P), dict(scales=4 * P), dict(scales=5 * P),
+    dict(scales=6 * P), dict(mean=5 * P), dict(mean=6 * P), dict(inv=P), dict(mean=2 * P), dict(y=3 * P), dict(h=4 * P)])
+def test_rows_statistics_in_another_ones_place(change):
+    """Scales, mean and inv_std are written row by row, while other rows are read and written."""
+    eight = {**NORM, "y_dtype": E4M3, "scales": 9 * P, **change}
+    assert call(norm, eight) == OK       # no rows
+    assert call(norm, eight, rows=5) == EINVAL
+
+
+@pytest.mark.parametrize("change", [
+    dict(dw=10 * P), dict(db=10 * P), dict(dx=10 * P), dict(dx=8 * P), dict(dx=9 * P), dict(dx=4 * P), dict(dx=5 * P), dict(dx=6 * P),
+    dict(ws=P), dict(ws=2 * P), dict(ws=3 * P), dict(ws=4 * P), dict(ws=5 * P), dict(ws=6 * P)])
+def test_gradients_in_another_ones_place(change):
+    assert call(backward, BACKWARD, **change) == EINVAL
