@@ -468,7 +468,7 @@ int cleave_layer_norm_backward(int64_t rows, int64_t cols, const void* dy, int64
 
 /* dbias = sum over rows of dy (the gradient of a bias that every row got).
  * workspace: cleave_bias_grad_workspace(rows, cols) floats, of this call alone while
- * it runs. */
+ * it runs.  CLEAVE_EINVAL as above. */
 int64_t cleave_bias_grad_workspace(int64_t rows, int64_t cols);
 int cleave_bias_grad(int64_t rows, int64_t cols, const void* dy, int64_t lddy, int dtype,
                      float* dbias, float* workspace, void* hip_stream);

@@ -74,7 +74,7 @@ extern "C" int cleave_rms_norm(int64_t rows, int64_t cols, const void* x, int64_
   if (!m.ok) return CLEAVE_EINVAL;
   if (!in_place(y, ldy, y_dtype, x, ldx, dtype, rows) || !in_place(y, ldy, y_dtype, residual, ldr, dtype, rows) ||
       !in_place(sum_out, lds, dtype, x, ldx, dtype, rows) || !in_place(sum_out, lds, dtype, residual, ldr, dtype, rows) ||
-      (rows > 0 && y == sum_out))
+      (rows > 0 && !(apart({y, sum_out, scales, inv_rms}, {weight}) && apart({scales, inv_rms}, {x, residual}))))
     return CLEAVE_EINVAL;
   if (rows == 0) return CLEAVE_OK;
   const cleave::NormArgs args{x, residual, weight, y, scales, sum_out, inv_rms, rows, cols, ldx, ldr, ldy, lds, eps};
@@ -100,9 +100,10 @@ extern "C" int cleave_rms_norm_backward(int64_t rows, int64_t cols, const void* 
   m.add_vector(inv_rms);
   m.add_vector(dweight);
   m.add_vector(workspace);
-  if (!m.ok) return CLEAVE_EINVAL;
+  if (!m.ok || dweight == workspace) return CLEAVE_EINVAL;
   if (!in_place(dx, lddx, dtype, dy, lddy, dtype, rows) || !in_place(dx, lddx, dtype, h, ldh, dtype, rows) ||
-      !in_place(dx, lddx, dtype, dsum, ldds, dtype, rows))
+      !in_place(dx, lddx, dtype, dsum, ldds, dtype, rows) ||
+      (rows > 0 && !(apart({dx, dweight}, {}) && apart({dx, workspace}, {weight, inv_rms}) && apart({workspace}, {dy, h, dsum}))))
     return CLEAVE_EINVAL;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const int partial_rows = cleave::rms_norm_partial_rows(rows, cols);
@@ -188,6 +189,10 @@ extern "C" int cleave_bias_grad(int64_t rows, int64_t cols, const void* dy, int6
   m.add_vector(workspace);
   if (!m.ok) return CLEAVE_EINVAL;
   const cleave::ColumnSumArgs args{dy, lddy, rows, cols, dbias, workspace, cleave::column_sum_chunks(rows, cols)};
+  // (one chunk of fp32 leaves a column's sum after its last read, and uses no workspace)
+  const bool joined = args.chunks > 1;
+  if ((joined && !apart({dbias, workspace}, {rows > 0 ? dy : nullptr})) || (rows > 0 && dy == dbias && dtype == CLEAVE_BF16))
+    return CLEAVE_EINVAL;
   CLEAVE_HIP(cleave::launch_column_sum(args, dtype, static_cast<hipStream_t>(hip_stream)));
   return CLEAVE_OK;
 }
