@@ -581,7 +581,7 @@ int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_grad_args* ar
  * NULL).  Logits of minus infinity are masked tokens: they have no probability.  A row of nothing else has lse and log
  * probabilities of minus infinity and entropy 0.  A row with a NaN or plus infinity is NaN; a NaN's place in its order is that of
  * minus infinity (beside a signaling one the order is open).  workspace: cleave_log_probs_workspace(rows, cols, n_top) floats (may be NULL
- * if that is 0), of this call alone while it runs.  No two outputs in one place.  CLEAVE_EINVAL as above, and more than 2^30 columns;
+ * if that is 0), of this call alone while it runs.  Outputs and workspace overlap nothing else.  CLEAVE_EINVAL as above, and more than 2^30 columns;
  * CLEAVE_ELIMIT: n_top > 32. */
 int64_t cleave_log_probs_workspace(int64_t rows, int64_t cols, int64_t n_top);
 int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype, float scale,

@@ -228,13 +228,11 @@ extern "C" int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, 
   if (!m.ok || cols > kMostTokens || !aligned(ids, 8) || !aligned(top_ids, 8)) return CLEAVE_EINVAL;
   if ((ids != nullptr) != (logp != nullptr) || n_top < 0 || n_top > cols) return CLEAVE_EINVAL;
   if (n_top > cleave::kMostTop) return CLEAVE_ELIMIT;
-  if ((n_top > 0) != (top_ids != nullptr) || (n_top > 0) != (top_logp != nullptr) || (ids && ids == top_ids)) return CLEAVE_EINVAL;
-  if ((logp && (logp == lse || logp == entropy || logp == top_logp)) || (lse && (lse == entropy || lse == top_logp)) ||
-      (entropy && entropy == top_logp))
-    return CLEAVE_EINVAL;
+  if ((n_top > 0) != (top_ids != nullptr) || (n_top > 0) != (top_logp != nullptr)) return CLEAVE_EINVAL;
+  if (!apart({logp, lse, entropy, top_ids, top_logp}, {ids, rows > 0 ? logits : nullptr})) return CLEAVE_EINVAL;
   if (rows == 0) return CLEAVE_OK;
   int parts = cleave::log_probs_parts(rows, cols, n_top);
-  if (parts > 1 && !workspace) return CLEAVE_EINVAL;
+  if (parts > 1 && (!workspace || !apart({workspace}, {logits, ids, logp, lse, entropy, top_ids, top_logp}))) return CLEAVE_EINVAL;
   const int64_t chunk = log_probs_chunk(cols, parts);
   parts = static_cast<int>((cols + chunk - 1) / chunk);   // (rounding may leave the last ones empty)
   const cleave::LogProbArgs args{logits, ids, logp, lse, entropy, top_ids, top_logp, workspace, rows, cols, ld, scale,
@@ -257,7 +255,9 @@ extern "C" int cleave_log_probs_backward(int64_t rows, int64_t cols, const void*
   if (!m.ok || cols > kMostTokens || !aligned(ids, 8)) return CLEAVE_EINVAL;
   if ((ids != nullptr) != (dlogp != nullptr) || (entropy != nullptr) != (dentropy != nullptr) || (!ids && !entropy))
     return CLEAVE_EINVAL;
-  if (!in_place(dlogits, ldd, dtype, logits, ld, dtype, rows)) return CLEAVE_EINVAL;
+  if (!in_place(dlogits, ldd, dtype, logits, ld, dtype, rows) ||
+      (rows > 0 && !apart({dlogits}, {ids, lse, dlogp, entropy, dentropy})))
+    return CLEAVE_EINVAL;
   if (rows == 0) return CLEAVE_OK;
   const cleave::LogProbBackwardArgs args{logits, ids, lse, dlogp, entropy, dentropy, dlogits, rows, cols, ld, ldd, scale, 0, 0.0f};
   CLEAVE_HIP(cleave::launch_log_probs_backward(args, dtype, static_cast<hipStream_t>(hip_stream)));

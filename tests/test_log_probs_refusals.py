@@ -52,3 +52,21 @@ def test_backward(change):
 
 def test_in_place_with_another_stride():
     assert call(backward, BACKWARD, rows=5, dx=P, ldd=104) == EINVAL
+
+
+@pytest.mark.parametrize("change", [
+    dict(logp=P), dict(lse=P), dict(ent=P), dict(tl=P), dict(top=P), dict(logp=2 * P), dict(lse=2 * P), dict(ent=2 * P), dict(tl=2 * P),
+    dict(lse=6 * P), dict(ent=6 * P), dict(logp=6 * P), dict(tl=6 * P)])
+def test_outputs_in_an_inputs_or_another_ones_place(change):
+    assert call(log_probs, CALL, rows=5, **change) == EINVAL
+
+
+@pytest.mark.parametrize("change", [dict(ws=n * P) for n in range(1, 8)])
+def test_a_workspace_in_another_ones_place(change):
+    """Where rows are taken in parts, every row's records are read while other rows' outputs are written."""
+    assert call(log_probs, CALL, rows=2, cols=250000, ld=250000, **change) == EINVAL
+
+
+@pytest.mark.parametrize("change", [dict(dx=n * P) for n in (2, 3, 4, 5, 6)])
+def test_a_gradient_in_an_inputs_place(change):
+    assert call(backward, BACKWARD, rows=5, **change) == EINVAL
