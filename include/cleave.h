@@ -524,8 +524,8 @@ int cleave_linear(cleave_plan* plan, const cleave_linear_args* args, void* hip_s
  * alone while it runs.  whole = 1 serves bf16 calls of which A, B_gate and B_up lie on 16-byte boundaries, K, lda and ldb are
  * multiples of 8, N too with transB = 0, and lda and ldb are below 2^21; whole = 0 serves all.  (8-bit operands: either.)
  * Few rows (M <= 16) read the weights as fast as memory gives them.  Bits, upload, streams: as for cleave_linear.
- * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, an output in another one's or in an operand's place,
- * partials missing, a plan of another kind or type. */
+ * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, an output or the workspace in another one's or an input's
+ * place, partials missing, a plan of another kind or type. */
 typedef struct {
   const void* A;
   const void* B_gate;
@@ -555,7 +555,7 @@ int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* args, void* 
  * gate and dup may be up, with its leading dimension.  dtype: F32 or BF16.  plan: cleave_plan_linear's for M, N, K and dtype.
  * partials: cleave_gated_grad_workspace(plan, whole) floats, whole as above.  The gradients of A and of the two weights are
  * products of dgate and dup (cleave_linear; one each where both lie side by side in one matrix, as the weights then do).
- * CLEAVE_EINVAL as above, or an output in another one's place. */
+ * CLEAVE_EINVAL as above, or an output or the workspace in another one's place. */
 typedef struct {
   const void* A;
   const void* B;

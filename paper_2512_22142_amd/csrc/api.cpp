@@ -1622,9 +1622,8 @@ extern "C" int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* a
   if (!aligned(a->A, eb) || !aligned(a->B_gate, eb) || !aligned(a->B_up, eb) || !aligned(a->C, ob) || !aligned(a->gate, ob) ||
       !aligned(a->up, ob) || !floats_aligned(vectors, 6))
     return CLEAVE_EINVAL;
-  if (a->C == a->gate || a->C == a->up || (a->gate && a->gate == a->up)) return CLEAVE_EINVAL;   // outputs in one place
-  for (const void* out : {static_cast<const void*>(a->C), static_cast<const void*>(a->gate), static_cast<const void*>(a->up)})
-    if (out && (out == a->A || out == a->B_gate || out == a->B_up)) return CLEAVE_EINVAL;
+  if (!cleave::apart({a->C, a->gate, a->up}, {a->A, a->B_gate, a->B_up, a->bias_gate, a->bias_up, a->scale_a, a->scale_gate, a->scale_up}))
+    return CLEAVE_EINVAL;
   if (e4m3 && (!a->transB || !aligned(a->A, 16) || !aligned(a->B_gate, 16) || !aligned(a->B_up, 16) || a->lda % 16 || a->ldb % 16 ||
                a->lda >= int64_t{1} << 22 || a->ldb >= int64_t{1} << 22))
     return CLEAVE_EINVAL;
@@ -1646,7 +1645,10 @@ extern "C" int cleave_linear_gated(cleave_plan* plan, const cleave_gated_args* a
   const bool whole = e4m3 || (a->dtype == CLEAVE_BF16 && K % 8 == 0 && (a->transB || N % 8 == 0) && whole_operand(a->A, a->lda) &&
                               whole_operand(a->B_gate, a->ldb) && whole_operand(a->B_up, a->ldb));
   const bool fused = plan->fused && (few ? whole && (a->transB || gated_few_direct(N, K) == kFewAlways) : whole || packs(M, N, K));
-  if (!(fused && whole) && (!few || splits > 1) && !a->partials) return CLEAVE_EINVAL;
+  if (!(fused && whole) && (!few || splits > 1) &&
+      (!a->partials || !cleave::apart({a->partials}, {a->A, a->B_gate, a->B_up, a->C, a->gate, a->up, a->bias_gate, a->bias_up, a->scale_a,
+                                                      a->scale_gate, a->scale_up})))
+    return CLEAVE_EINVAL;
   if (fused) {
     AssembleTarget to;
     to.C = a->C;
@@ -1746,7 +1748,8 @@ extern "C" int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_gr
   const bool whole = a->dtype == CLEAVE_BF16 && K % 8 == 0 && (a->transB || N % 8 == 0) && whole_operand(a->A, a->lda) &&
                      whole_operand(a->B, a->ldb);
   const bool fused = !few && splits == 1 && !plan->for_fp32 && (whole || packs_grad(M, N, K));
-  if (!(fused && whole) && !a->partials) return CLEAVE_EINVAL;
+  if (!(fused && whole) && (!a->partials || !cleave::apart({a->partials}, {a->A, a->B, a->gate, a->up, a->dgate, a->dup})))
+    return CLEAVE_EINVAL;
   int rc = ensure_uploaded(plan);
   if (rc == CLEAVE_OK) rc = ensure_gated_ready(plan->device);
   if (rc != CLEAVE_OK) return rc;

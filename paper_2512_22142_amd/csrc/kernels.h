@@ -3,7 +3,9 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
+#include <initializer_list>
 
 #include "plan_internal.h"
 
@@ -11,6 +13,16 @@ namespace cleave {
 
 // Keeps `e` for cleave_last_hip_error; returns CLEAVE_EHIP.
 int record_hip_error(hipError_t e);
+
+// Whether none of `outs` is another one of them, or one of `ins`.  (Null: not there.)
+typedef std::initializer_list<const void*> Places;
+inline bool apart(Places outs, Places ins) {
+  for (const void* const* a = outs.begin(); a != outs.end(); ++a) {
+    if (!*a) continue;
+    if (std::find(a + 1, outs.end(), *a) != outs.end() || std::find(ins.begin(), ins.end(), *a) != ins.end()) return false;
+  }
+  return true;
+}
 
 // Most members a grouped launch (one table entry per member) can have.
 constexpr int kMaxGroup = 8;

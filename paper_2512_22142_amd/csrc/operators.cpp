@@ -7,7 +7,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <initializer_list>
 #include <limits>
 
 #include "kernels.h"
@@ -43,15 +42,7 @@ bool in_place(const void* out, int64_t ldo, int out_dtype, const void* in, int64
   return !out || out != in || rows == 0 || (out_dtype == dtype && (ldo == ldi || rows == 1));
 }
 
-// Whether none of `outs` is another one of them, or one of `ins`.  (Null: not there.)
-typedef std::initializer_list<const void*> Places;
-bool apart(Places outs, Places ins) {
-  for (const void* const* a = outs.begin(); a != outs.end(); ++a) {
-    if (!*a) continue;
-    if (std::find(a + 1, outs.end(), *a) != outs.end() || std::find(ins.begin(), ins.end(), *a) != ins.end()) return false;
-  }
-  return true;
-}
+using cleave::apart;
 
 bool float_dtype(int dtype) { return dtype == CLEAVE_F32 || dtype == CLEAVE_BF16; }
 

@@ -158,3 +158,43 @@ def test_other_calls_of_a_gated_plan_of_8_bit_operands():
     assert execute(plan, None, 0, 2, lists, 512, 0, lists, 512, 1, BF16, P, None) == EINVAL
     assert reduce(plan, P, 2, lists, 200, F32, None) == EINVAL
     lib.cleave_plan_destroy(plan)
+
+
+@pytest.mark.parametrize("M,N,K,dtype", [(300, 200, 512, F32), (2, 256, 8192, BF16), (300, 200, 513, BF16), (900, 200, 513, BF16)])
+@pytest.mark.parametrize("change", [dict(partials=n * P) for n in range(1, 9)])
+def test_a_workspace_in_another_ones_place(M, N, K, dtype, change):
+    """Through partial blocks, few rows' sums, operands laid out again."""
+    plan = gated_plan(M, N, K, dtype)
+    a = Args(A=P, B_gate=2 * P, B_up=3 * P, C=4 * P, gate=5 * P, up=6 * P, bias_gate=7 * P, bias_up=8 * P, partials=9 * P, lda=K, ldb=K,
+             ldc=N, ld_gate=N, ld_up=N, transB=1, dtype=dtype, out_dtype=BF16, act=3)
+    for name, value in change.items():
+        setattr(a, name, value)
+    assert gated(plan, ctypes.byref(a), None) == EINVAL
+    lib.cleave_plan_destroy(plan)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("change", [{out: n * P} for out in ("C", "gate", "up") for n in (7, 8, 10, 11, 12)])
+def test_outputs_in_a_vectors_place(dtype, change):
+    plan = gated_plan(300, 200, 512, dtype)
+    a = Args(A=P, B_gate=2 * P, B_up=3 * P, C=4 * P, gate=5 * P, up=6 * P, bias_gate=7 * P, bias_up=8 * P, lda=512, ldb=512, ldc=200,
+             ld_gate=200, ld_up=200, transB=1, dtype=dtype, out_dtype=BF16, act=3)
+    if dtype == E4M3:
+        a.scale_a, a.scale_gate, a.scale_up = 10 * P, 11 * P, 12 * P
+    for name, value in change.items():
+        setattr(a, name, value)
+    if dtype == E4M3 or list(change.values())[0] < 10 * P:
+        assert gated(plan, ctypes.byref(a), None) == EINVAL
+    lib.cleave_plan_destroy(plan)
+
+
+@pytest.mark.parametrize("M,K,dtype", [(300, 512, F32), (4, 512, BF16), (300, 513, BF16), (900, 513, BF16)])
+@pytest.mark.parametrize("change", [dict(partials=n * P) for n in range(1, 7)])
+def test_a_gradients_workspace_in_another_ones_place(M, K, dtype, change):
+    plan = made(M, 200, K, dtype)
+    a = GradArgs(A=P, B=2 * P, gate=3 * P, up=4 * P, dgate=5 * P, dup=6 * P, partials=7 * P, lda=K, ldb=K, ld_gate=200, ld_up=200,
+                 ld_dgate=200, ld_dup=200, transB=1, dtype=dtype, out_dtype=BF16, act=3)
+    for name, value in change.items():
+        setattr(a, name, value)
+    assert grad(plan, ctypes.byref(a), None) == EINVAL
+    lib.cleave_plan_destroy(plan)
