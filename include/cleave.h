@@ -494,7 +494,8 @@ int cleave_bias_grad(int64_t rows, int64_t cols, const void* dy, int64_t lddy, i
  * arguments' values, sizes and alignment.  Asynchronous; the plan's tables are uploaded by the first call or
  * cleave_plan_upload, after which nothing is allocated.
  * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, act_grad with a
- * bias or (unless act is NONE) without preact, a batched plan, partials missing, a plan of another type. */
+ * bias or (unless act is NONE) without preact, a batched plan, partials missing, a plan of another type, an output or the workspace
+ * in another one's or an input's place (but as above). */
 typedef struct {
   const void* A;
   const void* B;

@@ -1337,7 +1337,10 @@ extern "C" int cleave_linear(cleave_plan* plan, const cleave_linear_args* a, voi
     return CLEAVE_EINVAL;
   const int64_t splits = plan->uniform_splits;
   const bool joined = splits != 1;
-  if (joined && !a->partials) return CLEAVE_EINVAL;
+  const void* const z = a->act_grad ? nullptr : a->preact;   // an output
+  if (joined && (!a->partials || !cleave::apart({a->partials}, {a->A, a->B, a->C, a->preact, a->residual, a->bias, a->scale_a, a->scale_b})))
+    return CLEAVE_EINVAL;
+  if (!cleave::apart({a->C, z}, {a->A, a->B, a->bias, a->scale_a, a->scale_b})) return CLEAVE_EINVAL;
 
   cleave::LinearArgs epi{};
   epi.bias = a->bias;
