@@ -573,7 +573,7 @@ typedef struct {
 int64_t cleave_gated_grad_workspace(const cleave_plan* plan, int whole);
 int cleave_linear_gated_grad(cleave_plan* plan, const cleave_gated_grad_args* args, void* hip_stream);
 
-/* Log probabilities of given tokens: with l = scale * logits (rows x cols, F32 or BF16; scale > 0, the inverse of a temperature)
+/* Log probabilities of given tokens: with l = scale * logits (rows x cols, F32 or BF16; scale in (0, 2^127], the inverse of a temperature)
  * and, per row, p = e^(l - lse),
  *   lse = log sum e^l;   logp = l[id] - lse;   entropy = -sum p log p
  * and the n_top most likely tokens in descending order (the lower id where logits are equal) with their log probabilities.

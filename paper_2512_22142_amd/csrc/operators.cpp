@@ -192,6 +192,8 @@ namespace {
 
 // (columns are counted in 32 bits beyond a row's end)
 constexpr int64_t kMostTokens = int64_t{1} << 30;
+// (exponents are taken of scale / log 2 times a distance, which may be zero)
+constexpr float kMostScale = 0x1p127f;
 
 // Columns of a part of a row: whole lines of sixteen bytes for every group of threads.
 int64_t log_probs_chunk(int64_t cols, int parts) { return ((cols + parts - 1) / parts + 511) / 512 * 512; }
@@ -208,7 +210,7 @@ extern "C" int64_t cleave_log_probs_workspace(int64_t rows, int64_t cols, int64_
 extern "C" int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype, float scale,
                                 const int64_t* ids, float* logp, float* lse, float* entropy, int64_t n_top, int64_t* top_ids,
                                 float* top_logp, float* workspace, void* hip_stream) {
-  if (!float_dtype(dtype) || !(scale > 0.0f) || std::isinf(scale)) return CLEAVE_EINVAL;
+  if (!float_dtype(dtype) || !(scale > 0.0f && scale <= kMostScale)) return CLEAVE_EINVAL;
   Matrices m(rows, cols);
   m.add(logits, ld, dtype);
   m.add_vector(logp, true);
@@ -235,7 +237,7 @@ extern "C" int cleave_log_probs(int64_t rows, int64_t cols, const void* logits, 
 extern "C" int cleave_log_probs_backward(int64_t rows, int64_t cols, const void* logits, int64_t ld, int dtype, float scale,
                                          const int64_t* ids, const float* lse, const float* dlogp, const float* entropy,
                                          const float* dentropy, void* dlogits, int64_t ldd, void* hip_stream) {
-  if (!float_dtype(dtype) || !(scale > 0.0f) || std::isinf(scale)) return CLEAVE_EINVAL;
+  if (!float_dtype(dtype) || !(scale > 0.0f && scale <= kMostScale)) return CLEAVE_EINVAL;
   Matrices m(rows, cols);
   m.add(logits, ld, dtype);
   m.add(dlogits, ldd, dtype);

@@ -70,3 +70,11 @@ def test_a_workspace_in_another_ones_place(change):
 @pytest.mark.parametrize("change", [dict(dx=n * P) for n in (2, 3, 4, 5, 6)])
 def test_a_gradient_in_an_inputs_place(change):
     assert call(backward, BACKWARD, rows=5, **change) == EINVAL
+
+
+def test_a_scale_whose_product_with_log_2_of_e_overflows():
+    """(times a distance of zero, that of the largest logit, it would be NaN)"""
+    for call_of, base in ((log_probs, CALL), (backward, BACKWARD)):
+        assert call(call_of, base, scale=2.0 ** 127) == OK
+        for scale in (2.0 ** 127 * (1 + 2.0 ** -23), 2.4e38, 3.4e38):
+            assert call(call_of, base, scale=scale) == EINVAL
