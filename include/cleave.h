@@ -524,7 +524,9 @@ int cleave_linear(cleave_plan* plan, const cleave_linear_args* args, void* hip_s
  * CLEAVE_E4M3, K a multiple of 16).  partials: cleave_gated_workspace(plan, whole) floats (may be NULL if that is 0), of this call
  * alone while it runs.  whole = 1 serves bf16 calls of which A, B_gate and B_up lie on 16-byte boundaries, K, lda and ldb are
  * multiples of 8, N too with transB = 0, and lda and ldb are below 2^21; whole = 0 serves all.  (8-bit operands: either.)
- * Few rows (M <= 16) read the weights as fast as memory gives them.  Bits, upload, streams: as for cleave_linear.
+ * Few rows (M <= 16) read the weights once, at two thirds and more of memory's rate from some 10000 columns on, at less with fewer columns or
+ * 8-bit weights; weights whose rows are not whole sixteen bytes (an odd K, stored N x K) take two to three times as long.  Bits, upload,
+ * streams: as for cleave_linear.
  * CLEAVE_EINVAL: NULL or misaligned pointer, short leading dimension, bad enum, an output or the workspace in another one's or an input's
  * place, partials missing, a plan of another kind or type. */
 typedef struct {

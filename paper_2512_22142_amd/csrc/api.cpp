@@ -815,12 +815,13 @@ int execute_impl(cleave_plan* plan, const int64_t* task_ids, int64_t n_ids, cons
   const int e = 16 / eb;
   // (The epilogue's stores take any number of columns, and its kernels read A along K.)
   // (Who asks for a gated product has seen to that.)
-  const bool direct = gated || (dtype == CLEAVE_BF16 && (plan->all_n_mult8 || (linear && transB)) && !(linear && transA) && (transA ? plan->all_m_mult8 : plan->all_k_mult8) &&
-                      (!transB || plan->all_k_mult8) &&
-                      lda % e == 0 && ldb % e == 0 && aligned(A, 16) && aligned(B, 16) &&
-                      // in-tile byte offsets are kept in 32 bits
-                      lda * eb < (int64_t{1} << 22) && ldb * eb < (int64_t{1} << 22) &&
-                      offsets_multiple_of(bl.a, bl.shape, e) && offsets_multiple_of(bl.b, bl.shape, e));
+  const bool direct =
+      gated || (dtype == CLEAVE_BF16 && (plan->all_n_mult8 || (linear && transB)) && !(linear && transA) &&
+                (transA ? plan->all_m_mult8 : plan->all_k_mult8) && (!transB || plan->all_k_mult8) && lda % e == 0 && ldb % e == 0 &&
+                aligned(A, 16) && aligned(B, 16) &&
+                // in-tile byte offsets are kept in 32 bits
+                lda * eb < (int64_t{1} << 22) && ldb * eb < (int64_t{1} << 22) &&
+                offsets_multiple_of(bl.a, bl.shape, e) && offsets_multiple_of(bl.b, bl.shape, e));
   // 8-bit operands have no general kernel, and partial blocks leave theirs in whole eights of columns (cleave_linear
   // refuses what would come here otherwise, and cleave_plan_linear does not plan it).
   if (plan->pairs && (!direct || (!asm_to.C && !plan->all_n_mult8))) return CLEAVE_EINVAL;
@@ -1414,15 +1415,18 @@ bool whole_operand(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 
 
 // bf16 operands that are not whole are laid out again, in the workspace, in rows of whole sixteen bytes, zeros behind their ends (one pass
 // over what is not whole), for the direct kernel, where there are rows enough that the way through the general kernel
-// and fp32 partial blocks takes longer.  us, general / laid out, weights stored K x N:
-//   gated, K x N = 4096 x 11007, 512, 800, 1024, 1999, 4096 rows 146 / 169, 242 / 250, 286 / 252, 564 / 371, 1058 / 641; 1000 x 2500, 800, 1999, 4096
-// rows 30 / 30, 45.5 / 42.5, 78 / 70; 2048 x 4100, 800, 1200, 2048 rows 49 / 48, 68 / 73, 112 / 79.  An odd K costs the general kernel
-// more: 4097 x 11008, 200, 400, 800 rows 107 / 91, 151 / 102, 260 / 202 (stored N x K 135 / 147, 192 / 171, 308 / 271), 1001 x 2500, 200,
-// 400, 800 rows 18.9 / 21.4, 24.3 / 23.0, 32.3 / 30.0.
-//   gradient, 4097 x 11008, 200, 400, 800, 2048 rows 60 / 51, 102 / 71, 150 / 150, 299 / 234 (N x K 74 / 78, 125 / 109, 183 / 171, 347 / 262), 2049 x
-// 4096, 200, 400, 800 rows 20.5 / 14.9, 29.0 / 24.8, 37.9 / 31.3.  Rows of the output that are not whole cost the direct kernel's stores
-// more than the join's: 4096 x 11007, 800, 1024, 1999, 4096 rows 149 / 199, 159 / 178, 299 / 293, 572 / 440, 2048 x 4100, 1200, 2048, 4096
-// rows 49 / 49, 71 / 73, 126 / 91, 2048 x 2500 33 / 40, 49 / 49, 77 / 84, 1000 x 2500, 4096 rows 56 / 71.
+// and fp32 partial blocks takes longer.  us, general / laid out, weights of K x N stored so where nothing else is said:
+//   gated, whole K  4096 x 11007: 512, 800, 1024, 1999, 4096 rows 146 / 169, 242 / 250, 286 / 252, 564 / 371, 1058 / 641
+//                   1000 x 2500: 800, 1999, 4096 rows 30 / 30, 45.5 / 42.5, 78 / 70
+//                   2048 x 4100: 800, 1200, 2048 rows 49 / 48, 68 / 73, 112 / 79
+//   gated, odd K    4097 x 11008: 200, 400, 800 rows 107 / 91, 151 / 102, 260 / 202 (stored N x K 135 / 147, 192 / 171, 308 / 271)
+//                   1001 x 2500: 18.9 / 21.4, 24.3 / 23.0, 32.3 / 30.0
+//   gradient, odd K 4097 x 11008: 200, 400, 800, 2048 rows 60 / 51, 102 / 71, 150 / 150, 299 / 234 (N x K 74 / 78, 125 / 109, 183 / 171, 347 / 262)
+//                   2049 x 4096: 200, 400, 800 rows 20.5 / 14.9, 29.0 / 24.8, 37.9 / 31.3
+//   gradient, odd N (the output's rows cost the direct kernel's stores more than the join's)
+//                   4096 x 11007: 800, 1024, 1999, 4096 rows 149 / 199, 159 / 178, 299 / 293, 572 / 440
+//                   2048 x 4100: 1200, 2048, 4096 rows 49 / 49, 71 / 73, 126 / 91; 2048 x 2500: 33 / 40, 49 / 49, 77 / 84
+//                   1000 x 2500: 4096 rows 56 / 71
 int64_t eights(int64_t n) { return (n + 7) / 8 * 8; }
 bool packs(int64_t M, int64_t N, int64_t K) {
   return M >= (K % 8 != 0 ? 384 : 768) && eights(N) <= kMostPitch && eights(K) <= kMostPitch;
@@ -1476,10 +1480,14 @@ hipError_t pack_operands(Operands& o, int weights, int64_t M, int64_t N, int64_t
 
 // Splits of K for few rows: a workgroup has 64 columns of both weights, so up to 128 of them leave CUs without one; where a
 // row of K has 2 KB or more they are split, to one per CU, and joined by a second launch.  (`k` elements of `bytes`: pairs of e4m3.)  One
-// row, bf16, weights from memory, us, 1, 2, 4, 8 splits: 4096 x 4096 26, 21, 18.7, 19.5, 11008 x 4096 58, 47, 38.3, 39.8, 2048 x 5632 21,
-// 16.1, 17.1, 15.6, 8192 x 8192 76, 51.6, 53.7, 54.7; as they are 4096 x 11008 36.1, 40, 36.9, 38.5, 5120 x 13824 54.4, 61, 62, 58.0, 1024
-// x 12000 13.9, 17.8, 18.0, 19, 768 x 2048 7.1, 9.3, 9.2, 10.  From the caches, one / as here (4 to 7): 1024 x 64 6.9 / 6.6, 1024 x 4096
-// 8.8 / 9.3 (stored N x K 10.9 / 9.3), 1408 x 1062 10.9 / 9.4, 2016 x 2048 13.4 / 10.3.
+// row, bf16, K x N, us:
+//   weights from memory, 1, 2, 4, 8 splits
+//     split           4096 x 4096 26, 21, 18.7, 19.5; 11008 x 4096 58, 47, 38.3, 39.8; 2048 x 5632 21, 16.1, 17.1, 15.6;
+//                     8192 x 8192 76, 51.6, 53.7, 54.7
+//     not split       4096 x 11008 36.1, 40, 36.9, 38.5; 5120 x 13824 54.4, 61, 62, 58.0; 1024 x 12000 13.9, 17.8, 18.0, 19;
+//                     768 x 2048 7.1, 9.3, 9.2, 10
+//   weights from the caches, one / as here (4 to 7)
+//                     1024 x 64 6.9 / 6.6; 1024 x 4096 8.8 / 9.3 (stored N x K 10.9 / 9.3); 1408 x 1062 10.9 / 9.4; 2016 x 2048 13.4 / 10.3
 int64_t gated_few_splits(int64_t N, int64_t k, int64_t bytes) {
   constexpr int64_t kCUs = 256;
   const int64_t groups = (N + 63) / 64;
@@ -1491,15 +1499,20 @@ int64_t gated_few_splits(int64_t N, int64_t k, int64_t bytes) {
 
 // Splits of K for more rows, `k` in elements of two bytes.  Few items of 128 x 128: what takes least by the time of a K step (up to 64
 // items run as a part a CU, up to 128 as two, up to 256 as one item; K x N's half tiles of 32 columns are half lines, which only whole
-// products have) and of the join
-// (5 us, and both products' partial blocks written and read at 4.5 TB/s).  Otherwise as many as fill the CUs with large tiles.  bf16,
-// weights from memory, us, K x N / N x K, unsplit; 2; 4 splits: 17 rows, 2560 x 5120 (columns x K) 52 / 25; 34 / 27; 19 / 19, 4096 x 11008
-// 91 / 51; 61 / 53; 48 / 40, 5632 x 2048 34 / 18; 17 / 17; 19 / 19, 2816 x 1024 8.5 / 7.0; 10.6 / 10.6; 10.8 / 10.2; 128 rows, 4096 x 4096
-// 39 / 23; 32 / 27; 28 / 27, 2048 x 2048 15.6 / 11.4; 12.3 / 12.6; 14.9 / 14.1; 256 rows, 2048 x 5632 50 / 30; 38 / 34; 27 / 26, 4096 x
-// 2048 27 / 20; 22 / 22; 27 / 25; 1289 rows, 192 x 2880 15.1 / 12.3 and in 4 17.2 / 17.9; large tiles: 256 rows, 11008 x 4096 83 / 78; 67
-// / 67; 90 / 87, 512 rows, 4096 x 11008 118 / 109; 120 / 119; 96 / 92, 8192 x 4096 86 / 77; 73 / 77; 94 / 94, 5632 x 4096 63 / 62; 67 /
-// 66; 83 / 81, 1159 rows, 1920 x 9920 134 / 131; 152 / 178. e4m3, 17 rows, 1024 x 4096 14.8; 12.0; 9.3, 2048 x 5632 18.8; 14.1; 13.3, 4096
-// x 4096 15.7; 16.3; 18.2; 256 rows, 2048 x 2048 10.5; 15.8; 20.3.
+// products have) and of the join (5 us, and both products' partial blocks written and read at 4.5 TB/s).  Otherwise as many as fill the CUs
+// with large tiles.  bf16, weights from memory, columns x K, us, stored K x N / N x K, unsplit; 2; 4 splits:
+//   17 rows      2560 x 5120 52 / 25; 34 / 27; 19 / 19, 4096 x 11008 91 / 51; 61 / 53; 48 / 40, 5632 x 2048 34 / 18; 17 / 17; 19 / 19,
+//                2816 x 1024 8.5 / 7.0; 10.6 / 10.6; 10.8 / 10.2
+//   128 rows     4096 x 4096 39 / 23; 32 / 27; 28 / 27, 2048 x 2048 15.6 / 11.4; 12.3 / 12.6; 14.9 / 14.1
+//   256 rows     2048 x 5632 50 / 30; 38 / 34; 27 / 26, 4096 x 2048 27 / 20; 22 / 22; 27 / 25
+//   1289 rows    192 x 2880 15.1 / 12.3; not measured; 17.2 / 17.9
+//   large tiles  256 rows, 11008 x 4096 83 / 78; 67 / 67; 90 / 87; 512 rows, 4096 x 11008 118 / 109; 120 / 119; 96 / 92, 8192 x 4096 86 / 77;
+//                73 / 77; 94 / 94, 5632 x 4096 63 / 62; 67 / 66; 83 / 81; 1159 rows, 1920 x 9920 134 / 131; 152 / 178
+//   e4m3         17 rows, 1024 x 4096 14.8; 12.0; 9.3, 2048 x 5632 18.8; 14.1; 13.3, 4096 x 4096 15.7; 16.3; 18.2; 256 rows, 2048 x 2048
+//                10.5; 15.8; 20.3
+// Not split, and not measured split: 129 to 255 items (of up to 128 rows more than 8192 columns, of up to 256 more than 4096: unsplit they
+// take 1.3 to 3.0 times what their bytes do), and 33 and more of e4m3 (whose 0.25 us a K step are less than unsplit calls take, 0.34 with
+// the launch).
 int64_t gated_splits(int64_t M, int64_t N, int64_t k, bool pairs) {
   constexpr int64_t kCUs = 256;
   const int64_t items = ((M + 127) / 128) * ((2 * N + 127) / 128), large = ((M + 255) / 256) * ((2 * N + 255) / 256);
@@ -1527,11 +1540,17 @@ int64_t gated_splits(int64_t M, int64_t N, int64_t k, bool pairs) {
 }
 
 // Few rows of whole bf16 operands that the direct kernel takes in less time, though its tiles are mostly empty: short K, whose loads it
-// has on their way sooner, where every part has a CU; and long rows of K stored N x K, of which it reads whole lines, where every CU has
-// an item and few have two.  us, weights from memory, few rows / direct, K x N and N x K, one row (16): 768 x 768 7.0, 8.7 (8.1, 10.2) /
-// 6.3, 6.2 (6.4, 6.2), 4096 x 1024 9.3, 9.4 (10.5, 10.3) / 8.5, 7.1 (8.9, 7.2), 4096 x 256 5.0, 5.2 (5.7, 6.0) / 5.2, 5.1 (5.3, 5.1), 5632
-// x 1024 10.2, 10.9 / 14.5, 9.5, 2816 x 2048 10.9, 11.8 / 12.8, 11.0; 11008 x 8192 80, 86 (84, 97) / 74, 70 (77, 69), 11008 x 4096 43, 48
-// (44, 50) / 40, 43 (41, 43), 8192 x 8192 60, 65 / 111, 67, 16384 x 4096 57, 57 / 54, 64.
+// has on their way sooner, where every part has a CU; and long rows of K stored N x K, of which it reads whole lines, where 129 to 192 CUs
+// have an item each.  us, weights from memory, N x K sizes, few rows / direct:
+//   short K, stored K x N and N x K, one row (16)
+//     taken      768 x 768 7.0, 8.7 (8.1, 10.2) / 6.3, 6.2 (6.4, 6.2); 4096 x 1024 9.3, 9.4 (10.5, 10.3) / 8.5, 7.1 (8.9, 7.2);
+//                4096 x 256 5.0, 5.2 (5.7, 6.0) / 5.2, 5.1 (5.3, 5.1)
+//     not taken  5632 x 1024 10.2, 10.9 / 14.5, 9.5; 2816 x 2048 10.9, 11.8 / 12.8, 11.0
+//   long rows, stored N x K, one row (16)
+//     taken      8448 x 4096 42.9 (48.9) / 35.8 (35.1); 10240 x 4096 48.1 (50.4) / 39.4 (40.0); 12288 x 4096 51.6 (52.2) / 46.2 (46.2);
+//                8448 x 8192 88.2 (95.5) / 66.4 (66.8); 11008 x 8192 93.9 (99.4) / 75.5 (76.8); 12288 x 8192 97.3 (102.4) / 76.2 (76.7)
+//     not taken  8192 x 8192 65 / 67; 16384 x 4096 57 / 64; (13824 x 4096 50.4 (53.5) / 46.4 (45.9) and, stored K x N, 11008 x 4096 43 (44)
+//                / 40 (41), 11008 x 8192 80 (84) / 74 (77) would gain; 8192 x 8192 so 60 / 111)
 enum FewDirect { kFewNever, kFewByColumn, kFewAlways };   // ByColumn: stored N x K
 FewDirect gated_few_direct(int64_t N, int64_t K) {
   constexpr int64_t kCUs = 256;

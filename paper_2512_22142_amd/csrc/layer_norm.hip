@@ -11,9 +11,10 @@
 //   dx = i (g - mean(g) - xhat mean(g xhat)) + dsum;   dw = sum over rows of dy xhat;   db = sum over rows of dy
 //
 // Bound by memory: every row is read once and kept in registers between its statistics, the scaling and the rounding.  A copy of
-// 512 MB runs at 5.4 TB/s here.  bf16 with a residual, the sum stored: 8192 x 768 11.0 us (4.6 TB/s), 4096 x 4096 22.0 (from the caches),
-// 16384 x 5120 129 (5.2), into e4m3 118 (5.0); 1 x 4096 into e4m3 3.9, a launch; gradient with dsum and both launches 16384 x 5120 135 us
-// (5.0 TB/s), fp32 2999 x 1111 14.5 (2.8).
+// 512 MB runs at 5.4 TB/s here.  us:
+//   bf16 with a residual, the sum stored  8192 x 768 11.0 (4.6 TB/s); 4096 x 4096 22.0 (from the caches); 16384 x 5120 129 (5.2), into
+//                                         e4m3 118 (5.0); 1 x 4096 into e4m3 3.9, a launch
+//   gradient, both launches               16384 x 5120 bf16 with dsum 135-137 (4.9-5.0 TB/s); 2999 x 1111 fp32 14.5 (2.8)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -30,17 +31,18 @@ namespace {
 
 // A row's group from column `at` on.  ENDING: rows of bf16 that are not in whole groups, few of them to a thread.  The branches of a last
 // group's elements wait one after the other there, so wide loads that end with the row are put in place instead (fp32's do not wait, and
-// threads with many groups have no registers for it).  us, branches / wide loads: 8313 x 789 16.8 / 14.5, its gradient 28.7 / 19.4, 1689 x
-// 2596 12.2 / 9.8, 22.0 / 16.7, 7353 x 9235's gradient (512 x 3) 192 / 169; with whole groups 8192 x 768 11.0 / 11.7; 512 x 4, 4566 x
-// 13859's 168 / 227; fp32 2999 x 1111's 14.5 / 19.
+// threads with many groups have no registers for it).  us, branches / wide loads:
+//   forward    8313 x 789 16.8 / 14.5, 1689 x 2596 12.2 / 9.8, whole groups 8192 x 768 11.0 / 11.7
+//   gradient   8313 x 789 28.7 / 19.4, 1689 x 2596 22.0 / 16.7, 7353 x 9235 (512 x 3) 192 / 169
+//   not taken  gradient of 512 x 4, 4566 x 13859 168 / 227; fp32 2999 x 1111 14.5 / 19
 template <bool ENDING, typename T>
 __device__ __forceinline__ Raw16 read_group(const T* row, int at, int cols) {
   if constexpr (ENDING) return read_ending(row + at, cols - at);
   else return Group16<T>::read(row + at, cols - at);
 }
-template <typename T, bool ENDING>
+template <bool ENDING>
 __device__ __forceinline__ Raw16 settle_group(Raw16 w, int at, int cols) {
-  return ENDING ? settle<T>(w, cols - at) : w;
+  return ENDING ? settle(w, cols - at) : w;
 }
 bool takes_ending(int64_t cols) { return cols % 8 != 0 && cols > 8; }
 
@@ -78,12 +80,12 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_kernel(Laye
   }
   float h[V][N];
 #pragma unroll
-  for (int j = 0; j < V; ++j) G::unpack(settle_group<T, ENDING>(x_raw[j], at(j), cols), h[j]);
+  for (int j = 0; j < V; ++j) G::unpack(settle_group<ENDING>(x_raw[j], at(j), cols), h[j]);
   if (args.residual) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       float add[N];
-      G::unpack(settle_group<T, ENDING>(r_raw[j], at(j), cols), add);
+      G::unpack(settle_group<ENDING>(r_raw[j], at(j), cols), add);
 #pragma unroll
       for (int e = 0; e < N; ++e) h[j][e] += add[e];
     }
@@ -222,14 +224,22 @@ hipError_t launch_norm_fit(const LayerNormArgs& args, int64_t v, hipStream_t str
   return launch_norm<T, NT, V>(args, stream);
 }
 
-// Which threads share a row: as few lanes or waves as hold it in one or a few groups each; for few rows, whose latency counts, in
-// one group each up to 512 threads (more waves wait longer for each other at each sum).  us, threads x groups, bf16 with a residual: 8192 x 768 64 x 2 11.9, 128 x 1 12.1, 256 x 1 17.2; 16384 x 5120 into
-// 8 bits 64 x 10 192, 128 x 5 125, 256 x 3 118, 512 x 2 137, 1024 x 1 185, into bf16 154, 134, 129, 125, 149; 4096 x 4096 128 x 4 23.0,
-// 256 x 2 21.9, 1024 x 1 33; 20000 x 1000 fp32 64 x 4 65, 256 x 1 58; one row, 128 x 1, 256 x 1, 512 x 1, 1024 x 1: 1024 columns 2.8, 3.3, 3.4, 4.3, into
-// 8 bits 3.3, 3.9, 4.2, 5.4; 256 x 2, 512 x 1, 1024 x 1: 4096 3.3, 3.1, 4.1, into 8 bits 4.0, 3.9, 5.4; 512 x 2, 1024 x 1: 8192 3.7, 4.0,
-// 250 of them 5.1, 5.5; 512 x 4, 1024 x 2: 16384 5.3, 5.2, into 8 bits 6.4, 6.7.  Rows of a head's width, without a residual, 64 x 1, 16 x 1, 8 x 1: 262144 x 64 86, 22.2, 14.0 (4.8 TB/s), 16 x 64 3.0, 2.8, 2.4;
-// 131072 x 128 43, 13.6, 8 x 2 13.4; 65536 x 256 24.4, 16 x 2 13.6, 8 x 4 14.6; 300 x 128 3.1, 2.6, 8 x 2 3.0; fp32 131072 x 128 33.8, 16
-// x 2 21.2.
+// Which threads share a row: as few lanes or waves as hold it in one or a few groups each; for few rows, whose latency counts, in one
+// group each up to 512 threads (more waves wait longer for each other at each sum).  us, threads x groups of each, bf16 with a residual where
+// nothing else is said:
+//   a head's width, no residual   262144 x 64: 64 x 1 86, 16 x 1 22.2, 8 x 1 14.0 (4.8 TB/s); 16 x 64: 3.0, 2.8, 2.4
+//                                 131072 x 128: 64 x 1 43, 16 x 1 13.6, 8 x 2 13.4; 300 x 128: 3.1, 2.6, 3.0
+//                                 131072 x 128 fp32: 64 x 1 33.8, 16 x 2 21.2
+//                                 65536 x 256: 64 x 1 24.4, 16 x 2 13.6, 8 x 4 14.6
+//   many rows, up to 192 groups   8192 x 768: 64 x 2 11.9, 128 x 1 12.1, 256 x 1 17.2
+//   many rows, up to 2048         4096 x 4096: 128 x 4 23.0, 256 x 2 21.9, 1024 x 1 33
+//                                 16384 x 5120: 64 x 10 154, 128 x 5 134, 256 x 3 129, 512 x 2 125, 1024 x 1 149
+//                                 the same into 8 bits: 192, 125, 118, 137, 185
+//                                 20000 x 1000 fp32: 64 x 4 65, 256 x 1 58
+//   one row                       1024 columns: 128 x 1 2.8, 256 x 1 3.3, 512 x 1 3.4, 1024 x 1 4.3; into 8 bits 3.3, 3.9, 4.2, 5.4
+//                                 4096: 256 x 2 3.3, 512 x 1 3.1, 1024 x 1 4.1; into 8 bits 4.0, 3.9, 5.4
+//                                 8192: 512 x 2 3.7, 1024 x 1 4.0 (250 rows 5.1, 5.5)
+//                                 16384: 512 x 4 5.3, 1024 x 2 5.2; into 8 bits 6.4, 6.7
 template <typename T>
 hipError_t launch_norm_of(const LayerNormArgs& args, hipStream_t stream) {
   const int64_t groups = (args.cols + Group16<T>::N - 1) / Group16<T>::N;
@@ -308,8 +318,8 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
     float g[V][N], xhat[V][N];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      G::unpack(settle_group<T, ENDING>(cur.dy[j], at(j), cols), g[j]);
-      G::unpack(settle_group<T, ENDING>(cur.h[j], at(j), cols), xhat[j]);
+      G::unpack(settle_group<ENDING>(cur.dy[j], at(j), cols), g[j]);
+      G::unpack(settle_group<ENDING>(cur.h[j], at(j), cols), xhat[j]);
     }
     float sum = 0.0f, dot = 0.0f;
 #pragma unroll
@@ -331,7 +341,7 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void layer_norm_backward_ke
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       float add[N] = {};
-      if (args.dsum) G::unpack(settle_group<T, ENDING>(cur.add[j], at(j), cols), add);
+      if (args.dsum) G::unpack(settle_group<ENDING>(cur.add[j], at(j), cols), add);
 #pragma unroll
       for (int e = 0; e < N; ++e) g[j][e] = (g[j][e] - sum - xhat[j][e] * dot) * cur.inv + add[e];
       G::store(dx + at(j), cols - at(j), g[j]);
@@ -462,18 +472,25 @@ __global__ __launch_bounds__(kJoinThreads) void layer_norm_join_kernel(const flo
   else if (dbias && c >= half && c < half + cols) dbias[c - half] = total;
 }
 
-// Threads of a row, groups of sixteen bytes of each, and workgroups: what the CUs hold at a time, so that a workgroup's rows
-// share one row of partial sums.  Narrow rows are a wave's, four to a workgroup, without a barrier, or eight or sixteen lanes'.  us, the
-// first launch alone: 16384 x 5120 bf16 with dsum (640 groups) 1024 x 1 (threads x groups) 155, 512 x 2 158, 128 x 5 145, 256 x 3 133, and
-// in 256, 512, 768, 1024 workgroups > 160, 133, 154, 140; 2999 x 1111 fp32 (278) 512 x 1 12.2, 256 x 2 10.8, 64 x 5 11.0, with half the
-// rows of partial sums; 8192 x 768 bf16 (96) 256 x 1 17.2, 128 x 1 in 2048 13.1, 64 x 2 in 512 13.7; 8192 x 4096 (512) 1024 x 1 71, 256 x
-// 2 50.5, 512 x 1 49.9; 30000 x 256 (32) 128 x 1 28, 64 x 1 in 1024 17.4; 1000 x 8192 512 x 2 in 256, 512 16.8, 21.4; 8192 x 1536 64 x 3
-// 20.4, 256 x 1 in 512, 768, 1024 23.5, 20.1, 19.8. With the next row on its way 1024 threads have too few registers for two groups of
-// bf16: 2048 x 12288 (1536) 1024 x 2 98, 512 x 3 44; 2048 x 16384
-// (2048), without the next row, 1024 x 2 114, 512 x 4 67 (with it 132).  Wider rows are fp32's only: 1024 x 8832 (2208) read twice (the
-// long kernel) 63, 512 x 5 27.4, 1024 x 3 32.3; 1024 x 12288 of fp32 85, 512 x 6 65, 1024 x 3 46; 1024 x 16384 108, 512 x 8 78, 1024 x 4
-// 89. Rows of a head's width, without dsum, 64 x 1 in 1024, 16 x 1 in 512, 1024, 8 x 1 in 512, 1024: 262144 x 64 100, 36.2, 26.8, 19.4,
-// 18.1 (5.2 TB/s), 32768 x 64 16.4, 7.0, 6.3, 5.0, 5.3; 65536 x 100 47, 20.9, 15.1, 8 x 2 14.5, 17.1; 65536 x 256 30.3, 16 x 2 19.2, 21.1.
+// Threads of a row, groups of sixteen bytes of each, and workgroups: what the CUs hold at a time, so that a workgroup's rows share
+// one row of partial sums.  Narrow rows are a wave's, four to a workgroup, without a barrier, or eight or sixteen lanes'.  us, the first launch
+// alone, threads x groups of each (in so many workgroups), groups of a row in brackets, bf16 where nothing else is said:
+//   a head's width, no dsum  262144 x 64 [8]: 64 x 1 (1024) 100, 16 x 1 (512, 1024) 36.2, 26.8, 8 x 1 (512, 1024) 19.4 (5.2 TB/s), 18.1
+//                            32768 x 64 [8]: the same 16.4, 7.0, 6.3, 5.0, 5.3
+//                            65536 x 100 [13]: 64 x 1 47, 16 x 1 20.9, 15.1, 8 x 2 14.5, 17.1
+//                            65536 x 256 [32]: 64 x 1 30.3, 16 x 2 (512, 1024) 19.2, 21.1; 30000 x 256: 128 x 1 28, 64 x 1 17.4
+//   a wave                   8192 x 768 [96]: 256 x 1 17.2, 128 x 1 (2048) 13.1, 64 x 2 (512) 13.7
+//                            2999 x 1111 fp32 [278]: 512 x 1 12.2, 256 x 2 10.8, 64 x 5 11.0 with half the rows of partial sums
+//   one workgroup            8192 x 1536 [192]: 64 x 3 20.4, 256 x 1 (512, 768, 1024) 23.5, 20.1, 19.8
+//                            8192 x 4096 [512]: 1024 x 1 71, 256 x 2 50.5, 512 x 1 49.9
+//                            16384 x 5120 with dsum [640]: 1024 x 1 155, 512 x 2 158, 128 x 5 145, 256 x 3 (256, 512, 768, 1024) 160, 133, 154, 140
+//                            1000 x 8192 [1024]: 512 x 2 (256, 512) 16.8, 21.4
+//   with the next row on its way 1024 threads have too few registers for two groups of bf16
+//                            2048 x 12288 [1536]: 1024 x 2 98, 512 x 3 44
+//                            2048 x 16384 [2048], without the next row: 1024 x 2 114, 512 x 4 67 (with it 132)
+//   wider, fp32 only         1024 x 8832 [2208]: read twice (the long kernel) 63, 512 x 5 27.4, 1024 x 3 32.3
+//                            1024 x 12288: read twice 85, 512 x 6 65, 1024 x 3 46
+//                            1024 x 16384 [4096]: read twice 108, 512 x 8 78, 1024 x 4 89
 struct BackwardShape {
   int threads, groups, workgroups;
 };

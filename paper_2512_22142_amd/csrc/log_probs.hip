@@ -6,16 +6,17 @@
 //   s = sum e^d,  w = sum e^d d     (m -> m': with f = e^(a (m - m')), s' = f s, w' = f (w + a (m - m') s))
 // so lse = a m + log s and H = log s - w / s.  An x of minus infinity counts nothing (0 times minus infinity is 0 here).
 //
-// Gradient:  dx_j = a (dlogp (1[j = id] - p_j) - dH p_j (log p_j + H)).
+// Gradient:  dx_j = a (dlogp (1[j = id] - p_j) - dH p_j (log p_j + H)), p from lse where fp32 holds that well enough, else from the row.
 //
 // The most likely tokens: every thread also keeps its strip's first largest value.  Value and column make a 64-bit key, larger for a larger
 // value or a lower column, so no two are equal.  The k-th largest of the keys of groups of threads is a bound that at least k elements
 // reach, and only the strips of the few threads that reach it hold such: those are read again, and their elements ranked.
 //
-// Bound by memory, one read of the logits (the gradient: one read and one write): 8192 x 32000 bf16 with entropy 100 us (5.2 TB/s), the
-// gradient 180 (5.8), the one behind the other 275-281 (the second finds a part of the logits in the Infinity Cache); 3001 x 50257 fp32
-// with five tokens 109
-// (5.5 TB/s).  One row of 32000 with twenty tokens 10.7, of them 3 a launch, 4 the row, the rest the order.
+// Bound by memory, one read of the logits (the gradient: one read and one write), us:
+//   8192 x 32000 bf16 with entropy 100-104 (5.2 TB/s), the gradient 180-188 (5.6-5.8), the one behind the other 275-284 (the second finds
+//   a part of the logits in the Infinity Cache)
+//   3001 x 50257 fp32 with five tokens 109 (5.5 TB/s)
+//   1 x 32000 with twenty tokens 10.7, of them 3 a launch, 4 the row, the rest the order
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -405,13 +406,14 @@ hipError_t launch_rows(const LogProbArgs& args, hipStream_t stream) {
 }
 
 // Threads of a row.  Rows that fill the chip take few, whose sums are joined without a barrier (one wave) or a short one; few
-// rows take more, whose latency counts.  us, 64, 128, 256, 512, 1024 threads, bf16 with entropy: 16384 x 1024 19, 33, 55, 106, 239,
-// 8192 x 8192 27, 27, 29, 65, 146, 8192 x 32000 98, 103, 100, 117, 182, 1 x 8192 5.5, 4.8, 5.0, 6.2, 7.6, 1 x 32000 15, 10, 7.5, 7.3, 8.5,
-// 256 x 32000 15, 10, 8.4, 8.9, 10; with twenty tokens 16384 x 4096 (five) 44, 50, 95, 217, 632, 1100 x 32000 45, 31, 29, 32, 64,
-// 3001 x 50257 fp32 200, 175, 143, 124, 135, 1 x 8192 12.8, 8.9, 7.8, 9.7, 12.1, 1 x 32000 31, 18, 12.9, 11.7, 13.4.
-// Short rows take fewer groups together, since what is not there costs as much as what is: 64 threads, four and as here (one up to 64
-// groups, two up to 128), 16384 x 1024 bf16 15.3, 9.7 (with eight tokens 36.9, 27.2), 16384 x 512 13.6, 7.2 (34.0, 24.0), 65536 x 128 43,
-// 23.8 (123, 93).
+// rows take more, whose latency counts.  us, 64, 128, 256, 512, 1024 threads:
+//   bf16 with entropy   16384 x 1024 19, 33, 55, 106, 239; 8192 x 8192 27, 27, 29, 65, 146; 8192 x 32000 98, 103, 100, 117, 182
+//                       1 x 8192 5.5, 4.8, 5.0, 6.2, 7.6; 1 x 32000 15, 10, 7.5, 7.3, 8.5; 256 x 32000 15, 10, 8.4, 8.9, 10
+//   with twenty tokens  16384 x 4096 (five) 44, 50, 95, 217, 632; 1100 x 32000 45, 31, 29, 32, 64; 3001 x 50257 fp32 200, 175, 143, 124, 135
+//                       1 x 8192 12.8, 8.9, 7.8, 9.7, 12.1; 1 x 32000 31, 18, 12.9, 11.7, 13.4
+// Short rows take fewer groups together, since what is not there costs as much as what is: one up to 64 groups, two up to 128.  bf16, 64
+// threads, four groups and as here (with eight tokens):
+//                       16384 x 1024 15.3, 9.7 (36.9, 27.2); 16384 x 512 13.6, 7.2 (34.0, 24.0); 65536 x 128 43, 23.8 (123, 93)
 template <typename T>
 hipError_t launch_of(const LogProbArgs& args, hipStream_t stream) {
   const int64_t groups = (args.chunk + Group16<T>::N - 1) / Group16<T>::N;
@@ -552,10 +554,11 @@ __global__ __launch_bounds__(RowGroup<NT>::kThreads) void log_probs_backward_ker
 // A launch has fewer than 2^32 threads.
 constexpr int64_t kLaunchWorkgroups = int64_t{1} << 21;
 
-// Parts of a row: one, but for few long rows, whose parts a second launch joins.  us, 1, 2, 4, 8, 16 parts, bf16 with entropy: 1 x 65536
-// 8.4, 7.9, 7.2, 7.8, 9.8, 1 x 131072 12.7, 10.0, 8.7, 7.7, 8.7, 16 x 262144 21.8, 15.0, 10.9, 9.4, 9.7, 64 x 131072 13.3, 11.2, 9.0, 9.5,
-// 11.6; with twenty tokens, which every part ranks, 1 x 65536 12.8, 13.5, 12.9, 14.9, 22.5, 1 x 131072 18.8, 16.5, 14.9, 15.4, 20.8,
-// 16 x 262144 30.6, 23.5, 18.3, 17.7, 23.5, 64 x 131072 19.7, 17.3, 16.7, 18.7, 25.6.
+// Parts of a row: one, but for few long rows, whose parts a second launch joins.  us, 1, 2, 4, 8, 16 parts, bf16:
+//   with entropy                               1 x 65536 8.4, 7.9, 7.2, 7.8, 9.8; 1 x 131072 12.7, 10.0, 8.7, 7.7, 8.7
+//                                              16 x 262144 21.8, 15.0, 10.9, 9.4, 9.7; 64 x 131072 13.3, 11.2, 9.0, 9.5, 11.6
+//   with twenty tokens, which every part ranks 1 x 65536 12.8, 13.5, 12.9, 14.9, 22.5; 1 x 131072 18.8, 16.5, 14.9, 15.4, 20.8
+//                                              16 x 262144 30.6, 23.5, 18.3, 17.7, 23.5; 64 x 131072 19.7, 17.3, 16.7, 18.7, 25.6
 int log_probs_parts(int64_t rows, int64_t cols, int64_t n_top) {
   if (rows > 64 || cols < 65536) return 1;
   return n_top > 0 || rows > 16 ? 4 : static_cast<int>(std::min<int64_t>(cols / 16384, kMostParts));

@@ -97,21 +97,19 @@ struct Group16<Bf16> {
   }
 };
 
-// Groups of a row of N elements and more, without a branch: a last group that is not whole is read so that it ends with the row, what lies behind
-// the row as that one; settle() then moves what there is of it to the front, zeros behind.
-template <typename T>
-__device__ __forceinline__ Raw16 read_ending(const T* p, int left) {
-  typedef Group16<T> G;
+// Groups of a row of eight bf16 and more, without a branch: a last group that is not whole is read so that it ends with the row, what lies
+// behind the row as that one; settle() then moves what there is of it to the front, zeros behind.
+__device__ __forceinline__ Raw16 read_ending(const Bf16* p, int left) {
+  typedef Group16<Bf16> G;
   return G::read(p + min(left - G::N, 0), G::N);
 }
-template <typename T>
 __device__ __forceinline__ Raw16 settle(Raw16 w, int left) {
-  constexpr int N = Group16<T>::N, W = N / 4;   // elements to a word
+  constexpr int N = Group16<Bf16>::N;
   if (left >= N) return w;
   const int off = N - max(left, 0);
-  if (W == 2 && off % 2 != 0) w = Raw16{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
-  if (off / W & 1) w = Raw16{w[1], w[2], w[3], 0};
-  if (off / W & 2) w = Raw16{w[2], w[3], 0, 0};
+  if (off % 2 != 0) w = Raw16{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+  if (off / 2 & 1) w = Raw16{w[1], w[2], w[3], 0};
+  if (off / 2 & 2) w = Raw16{w[2], w[3], 0, 0};
   if (off == N) w = Raw16{};
   return w;
 }
