@@ -13,7 +13,7 @@
 // reach, and only the strips of the few threads that reach it hold such: those are read again, and their elements ranked.
 //
 // Bound by memory, one read of the logits (the gradient: one read and one write), us:
-//   8192 x 32000 bf16 with entropy 100-104 (5.2 TB/s), the gradient 180-188 (5.6-5.8), the one behind the other 275-284 (the second finds
+//   8192 x 32000 bf16 with entropy 100-104 (5.2 TB/s), the gradient 178-190 (5.5-5.9), the one behind the other 275-284 (the second finds
 //   a part of the logits in the Infinity Cache)
 //   3001 x 50257 fp32 with five tokens 109 (5.5 TB/s)
 //   1 x 32000 with twenty tokens 10.7, of them 3 a launch, 4 the row, the rest the order
