@@ -6,7 +6,7 @@
 // in fp32, each output rounded once.  sa, sg, su: scales of A's rows and of the weights' columns (8-bit operands).
 //
 // Bound by the products in front of them: neither sum is stored and read again, and A is read once.  4096 rows, both weights 4096 x 11008,
-// bf16, us: K x N 591-606 (1.22 to 1.25 PFLOP/s; 8192^3 of the library: 1.22 to 1.24), e4m3 572-587; the gradient's product 4096 x 11008 x 4096
+// bf16, us: K x N 591-606 (1.22 to 1.25 PFLOP/s; 8192^3 of the library: 1.22 to 1.24), e4m3 572-590; the gradient's product 4096 x 11008 x 4096
 // K x N 337, N x K 368 (1.0 PFLOP/s, with 360 MB of zg, zu, dgate and dup on the way).
 #pragma once
 
